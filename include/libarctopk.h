@@ -308,6 +308,211 @@ int64_t arc_payload_elems(const arc_ctx *ctx);
 arc_status arc_projection(uint64_t seed, int64_t t, int64_t n, int32_t r,
                           float *V);
 
+/* ---- The two ends of a training step ---- */
+
+/*
+ * Log probabilities of given tokens, with entropy and top alternatives, and
+ * their gradient: what a language model's step starts from (its gradients are
+ * what arc_step compresses), what perplexity is measured with, and what a
+ * decoder reports for each generated token.
+ *
+ * For a row x[0..V) of logits, z_j = scale * x_j and a given token y:
+ *   lse  = log sum_j exp(z_j)           p_j = exp(z_j - lse)
+ *   logp = z_y - lse                    H   = -sum_j p_j (z_j - lse)
+ * and, for upstream gradients dl, dh, dz of logp, H and lse,
+ *   dx_j = scale * (dl ([j = y] - p_j) + dz p_j - dh p_j (z_j - lse + H)).
+ * The top alternatives are the `top` tokens of largest logit, in that order,
+ * ties to the lower token, each with z - lse.
+ *
+ * Masked tokens have the logit -infinity: p = 0, and nothing of them enters a
+ * sum.  A row with nothing else has lse = logp = -infinity, H = 0, alternatives
+ * 0, 1, ... at -infinity and no gradient.  A row that holds a NaN or +infinity
+ * has no distribution: NaN everywhere, and alternatives -1.  A negative y
+ * stands for a row without a token: logp = 0, and dl is taken as 0.  y >= V
+ * gives logp = NaN and a gradient without its [j = y].  A row whose dl, dh and
+ * dz are all 0 has the gradient 0, whatever its logits.
+ *
+ * Logits and their gradient are binary32 or bfloat16, everything else is
+ * binary32; sums are held in binary32 and their order is fixed, so that a call
+ * repeats its bits.
+ */
+typedef struct arc_tokens arc_tokens;
+
+/* Most alternatives of one row. */
+#define ARC_MAX_TOP 32
+
+/*
+ *   vocab     V, logits of one row, 1 .. 2^31 - 1
+ *   max_rows  most rows of one call, 1 .. 2^31 - 1
+ *   dtype     arc_dtype of the logits and of their gradient
+ *   top       alternatives of each row, 0 .. min(V, ARC_MAX_TOP)
+ *   scale     what logits are multiplied with (1 / temperature), finite, > 0
+ */
+typedef struct {
+  int64_t vocab;
+  int64_t max_rows;
+  int32_t dtype;
+  int32_t top;
+  float scale;
+  int32_t reserved; /* must be 0 */
+} arc_tokens_config;
+
+/* Validate cfg, allocate the workspace on the current HIP device and bind the
+ * context to `hip_stream`, as arc_create does.  On failure *out is NULL. */
+arc_status arc_tokens_create(const arc_tokens_config *cfg, void *hip_stream, arc_tokens **out);
+
+/*
+ * Score `rows` rows (0 .. max_rows).  Device pointers:
+ *   logits    row i is elements [i*stride, i*stride + V), stride >= V; any
+ *             element alignment (16-byte aligned rows are fastest)
+ *   targets   [rows] int64 given tokens; may be NULL where logp is
+ *   logp, entropy, lse   [rows] binary32; each may be NULL
+ *   top_ids, top_logp    [rows][top] int32 and binary32; both or neither NULL
+ * Outputs must not overlap one another or the inputs.
+ */
+arc_status arc_tokens_score(arc_tokens *ctx, int64_t rows, const void *logits, int64_t stride,
+                            const int64_t *targets, float *logp, float *entropy, float *lse,
+                            int32_t *top_ids, float *top_logp);
+
+/*
+ * The gradient of scored rows.  lse and entropy are arc_tokens_score's of the
+ * same logits (entropy may be NULL where d_entropy is); d_logp, d_entropy and
+ * d_lse are the upstream gradients [rows], each NULL for zeros (targets may be
+ * NULL where d_logp is).  grad has rows of `grad_stride` >= V elements; it may
+ * be the logits themselves (the same pointer and stride) and must not overlap
+ * anything otherwise.
+ */
+arc_status arc_tokens_grad(arc_tokens *ctx, int64_t rows, const void *logits, int64_t stride,
+                           const int64_t *targets, const float *lse, const float *entropy,
+                           const float *d_logp, const float *d_entropy, const float *d_lse,
+                           void *grad, int64_t grad_stride);
+
+/*
+ * Both, where the upstream gradients are known beforehand (a mean negative
+ * log-likelihood has d_logp = -1 / tokens): arc_tokens_score's logp, entropy
+ * and lse (each may be NULL) and arc_tokens_grad's grad in one call.
+ */
+arc_status arc_tokens_loss(arc_tokens *ctx, int64_t rows, const void *logits, int64_t stride,
+                           const int64_t *targets, const float *d_logp, const float *d_entropy,
+                           const float *d_lse, float *logp, float *entropy, float *lse,
+                           void *grad, int64_t grad_stride);
+
+/* Waits for the context's stream; NULL is accepted. */
+arc_status arc_tokens_destroy(arc_tokens *ctx);
+
+/*
+ * AdamW over many tensors at once, and the norms of their gradients.
+ *
+ * For every element of a tensor, with g' = factor * g, T = t + 1, c1 = 1 -
+ * beta1^T, c2 = 1 - beta2^T (binary64, rounded once), lr' = lr * lr_scale:
+ *   m <- beta1 m + (1 - beta1) g'        v <- beta2 v + (1 - beta2) g'^2
+ *   x <- (1 - lr' weight_decay) x - (lr' / c1) (m / (sqrt(v) / sqrt(c2) + eps))
+ * in binary32, every product and sum of m and v rounded by itself.
+ *
+ * States.  All tensors' states lie in one array of arc_optim_state_elems
+ * elements; tensor i's begin at arc_optim_state_offset(i), a multiple of
+ * ARC_STATE_BLOCK, and elements between a tensor's end and the next one's
+ * begin are 0.  ARC_STATE_F32 holds m and v.  ARC_STATE_F8 holds m and sqrt(v)
+ * in 8 bits (OCP e4m3) times a binary32 scale for each block of
+ * ARC_STATE_BLOCK elements: a power of two, 2^(e-7) for a largest magnitude
+ * in [2^e, 2^(e+1)) (at least 2^-126).  sqrt(v), because its values span half
+ * the exponents that v's do.  Powers of two, because the values a block can
+ * hold then stay the same from step to step, and stochastic rounding, because
+ * one step moves a state by less than half the distance of two such values:
+ * rounded to the nearest, v would stay where its first step put it.  A
+ * magnitude is rounded up with the chance of what is cut off, decided by a
+ * hash of (seed, t, element) alone (the same bits on every run); a v above 0
+ * never becomes 0.  Non-finite gradients give NaN states.
+ *
+ * Parameters in bfloat16 are rounded to the nearest even, or with `stochastic`
+ * by the same hash (an update below half of the distance between two values
+ * is otherwise lost).
+ */
+typedef struct arc_optim arc_optim;
+
+#define ARC_STATE_BLOCK 128
+
+typedef enum { ARC_STATE_F32 = 0, ARC_STATE_F8 = 1 } arc_state;
+
+typedef struct {
+  int64_t count;        /* elements, >= 0                                     */
+  int32_t param_dtype;  /* arc_dtype of the parameters                        */
+  int32_t grad_dtype;   /* arc_dtype of the gradients                         */
+  float weight_decay;   /* >= 0, finite                                       */
+  float lr_scale;       /* >= 0, finite                                       */
+} arc_optim_tensor;
+
+/*
+ *   tensors, num_tensors  1 .. 2^20 tensors, host array, copied; at most 2^42
+ *                         elements in all
+ *   state                 arc_state
+ *   stochastic            1: bfloat16 parameters are rounded stochastically
+ *   seed                  of every stochastic rounding
+ */
+typedef struct {
+  const arc_optim_tensor *tensors;
+  int32_t num_tensors;
+  int32_t state;
+  int32_t stochastic;
+  int32_t reserved; /* must be 0 */
+  uint64_t seed;
+} arc_optim_config;
+
+typedef struct {
+  float lr;           /* finite */
+  float beta1, beta2; /* in [0, 1) */
+  float eps;          /* > 0, finite */
+} arc_adamw_config;
+
+/* Validate cfg, allocate the tables and the norms' workspace on the current
+ * HIP device and bind the context to `hip_stream`, as arc_create does.  On
+ * failure *out is NULL. */
+arc_status arc_optim_create(const arc_optim_config *cfg, void *hip_stream, arc_optim **out);
+
+/* Elements of each state array; -1 for NULL.  The scales have one for each
+ * ARC_STATE_BLOCK of them. */
+int64_t arc_optim_state_elems(const arc_optim *ctx);
+
+/* Where tensor i's states begin; -1 for NULL or an i that is none. */
+int64_t arc_optim_state_offset(const arc_optim *ctx, int32_t i);
+
+/*
+ * Norms of the gradients: grads is a host array of num_tensors device pointers
+ * (any element alignment; those of tensors without elements are not looked
+ * at), read before the call returns.
+ *   norms  [num_tensors] binary32, scale * ||g_i||; may be NULL
+ *   total  [2] binary32: norm = scale * the 2-norm of all gradients, and
+ *          factor = scale * min(1, max_norm / norm), for arc_optim_adamw.  A
+ *          norm that is not finite gives the factor NaN.
+ * scale >= 0 (1 / N for gradients summed over N workers); max_norm > 0, or
+ * infinity for no clipping.  Squares are summed in binary64 in a fixed order.
+ */
+arc_status arc_optim_norm(arc_optim *ctx, const void *const *grads, float scale, float max_norm,
+                          float *norms, float *total);
+
+/*
+ * One AdamW step t >= 0 of all tensors.  Host arrays of num_tensors device
+ * pointers, read before the call returns; any element alignment:
+ *   params  updated      grads   read
+ *   copies  NULL, or bfloat16 copies [count] of the updated parameters, each
+ *           of which may be NULL
+ * and device pointers:
+ *   factor  one binary32 that gradients are multiplied with (total + 1 of
+ *           arc_optim_norm); NULL for 1.  A factor that is not finite leaves
+ *           parameters, copies and states as they are.
+ *   m, v    [state_elems] binary32, or 8 bits each with m_scale, v_scale
+ *           [state_elems / ARC_STATE_BLOCK] (NULL for ARC_STATE_F32); start at
+ *           0; 16-byte aligned
+ * No two of these may overlap (checked for the states only).
+ */
+arc_status arc_optim_adamw(arc_optim *ctx, const arc_adamw_config *ac, int64_t t,
+                           void *const *params, const void *const *grads, void *const *copies,
+                           const float *factor, void *m, void *v, float *m_scale,
+                           float *v_scale);
+
+/* Waits for the context's stream; NULL is accepted. */
+arc_status arc_optim_destroy(arc_optim *ctx);
+
 /* Static string naming a status code. */
 const char *arc_status_str(arc_status s);
 

@@ -15,7 +15,12 @@ from ._lib import (  # noqa: F401
     arc_last_error, arc_model_config, arc_model_step, arc_num_rows, arc_payload_elems,
     arc_projection, arc_selected_rows, arc_set_projection, arc_status_str, arc_step,
     arc_step_static, ARC_STATIC_SCRATCH_BYTES, arc_tensor,
-    arc_timing_enable, arc_timing_read, make_config, make_model_config)
+    arc_timing_enable, arc_timing_read, make_config, make_model_config,
+    ARC_MAX_TOP, ARC_STATE_BLOCK, ARC_STATE_F32, ARC_STATE_F8, arc_adamw_config,
+    arc_optim_adamw, arc_optim_config, arc_optim_create, arc_optim_destroy, arc_optim_norm,
+    arc_optim_state_elems, arc_optim_state_offset, arc_optim_tensor, arc_tokens_config,
+    arc_tokens_create, arc_tokens_destroy, arc_tokens_grad, arc_tokens_loss, arc_tokens_score,
+    make_optim_config, make_tokens_config)
 
 
 class Compressor:
@@ -96,3 +101,12 @@ class Compressor:
             self.close()
         except Exception:
             pass
+
+
+def __getattr__(name):
+    # The classes that need torch are imported on their first use, so that the
+    # binding alone still works without it.
+    if name in ("TokenLogProbs", "AdamW"):
+        from . import train
+        return getattr(train, name)
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -34,6 +34,9 @@ ARC_DTYPE_F32, ARC_DTYPE_BF16 = 0, 1
 ARC_MAX_R = 32
 ARC_STATIC_SCRATCH_BYTES = 64 * 1024 * 1024
 ARC_NUM_STAGES = 5
+ARC_MAX_TOP = 32
+ARC_STATE_F32, ARC_STATE_F8 = 0, 1
+ARC_STATE_BLOCK = 128
 STAGE_NAMES = ("sketch", "reduce", "select", "gather_update", "step")
 
 
@@ -84,6 +87,67 @@ class arc_model_config(ctypes.Structure):
     ]
 
 
+class arc_tokens_config(ctypes.Structure):
+    _fields_ = [
+        ("vocab", ctypes.c_int64),
+        ("max_rows", ctypes.c_int64),
+        ("dtype", ctypes.c_int32),
+        ("top", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("reserved", ctypes.c_int32),
+    ]
+
+
+class arc_optim_tensor(ctypes.Structure):
+    _fields_ = [
+        ("count", ctypes.c_int64),
+        ("param_dtype", ctypes.c_int32),
+        ("grad_dtype", ctypes.c_int32),
+        ("weight_decay", ctypes.c_float),
+        ("lr_scale", ctypes.c_float),
+    ]
+
+
+class arc_optim_config(ctypes.Structure):
+    _fields_ = [
+        ("tensors", ctypes.POINTER(arc_optim_tensor)),
+        ("num_tensors", ctypes.c_int32),
+        ("state", ctypes.c_int32),
+        ("stochastic", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("seed", ctypes.c_uint64),
+    ]
+
+
+class arc_adamw_config(ctypes.Structure):
+    _fields_ = [
+        ("lr", ctypes.c_float),
+        ("beta1", ctypes.c_float),
+        ("beta2", ctypes.c_float),
+        ("eps", ctypes.c_float),
+    ]
+
+
+def make_tokens_config(*, vocab, max_rows, dtype=ARC_DTYPE_BF16, top=0, scale=1.0,
+                       reserved=0) -> arc_tokens_config:
+    return arc_tokens_config(vocab, max_rows, dtype, top, scale, reserved)
+
+
+def make_optim_config(*, counts, param_dtypes, grad_dtypes, weight_decays, lr_scales,
+                      state=ARC_STATE_F32, stochastic=0, seed=0, reserved=0):
+    """Build an ``arc_optim_config`` from one value of each list per tensor.
+    Returns (config, keepalive), as make_config does."""
+    num = len(counts)
+    if not all(len(x) == num for x in (param_dtypes, grad_dtypes, weight_decays, lr_scales)):
+        raise ValueError("one dtype, weight decay and learning rate scale for each tensor")
+    arr = (arc_optim_tensor * num)(*[
+        arc_optim_tensor(*x) for x in zip(counts, param_dtypes, grad_dtypes, weight_decays,
+                                          lr_scales)])
+    cfg = arc_optim_config(ctypes.cast(arr, ctypes.POINTER(arc_optim_tensor)), num, state,
+                           int(stochastic), reserved, seed & (2**64 - 1))
+    return cfg, arr
+
+
 def make_model_config(optimizer="sgd", *, lr, dense_steps=0, momentum=0.0, beta1=0.9,
                       beta2=0.999, eps=1e-8, weight_decay=0.0) -> arc_model_config:
     kind = OPTIMIZERS[optimizer] if isinstance(optimizer, str) else int(optimizer)
@@ -105,6 +169,21 @@ _SIGS = {
     "arc_payload_elems": (ctypes.c_int64, [_vp]),
     "arc_projection": (_st, [ctypes.c_uint64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32,
                              _vp]),
+    "arc_tokens_create": (_st, [ctypes.POINTER(arc_tokens_config), _vp, ctypes.POINTER(_vp)]),
+    "arc_tokens_score": (_st, [_vp, ctypes.c_int64, _vp, ctypes.c_int64, _vp, _vp, _vp, _vp, _vp,
+                               _vp]),
+    "arc_tokens_grad": (_st, [_vp, ctypes.c_int64, _vp, ctypes.c_int64, _vp, _vp, _vp, _vp, _vp,
+                              _vp, _vp, ctypes.c_int64]),
+    "arc_tokens_loss": (_st, [_vp, ctypes.c_int64, _vp, ctypes.c_int64, _vp, _vp, _vp, _vp, _vp,
+                              _vp, _vp, _vp, ctypes.c_int64]),
+    "arc_tokens_destroy": (_st, [_vp]),
+    "arc_optim_create": (_st, [ctypes.POINTER(arc_optim_config), _vp, ctypes.POINTER(_vp)]),
+    "arc_optim_state_elems": (ctypes.c_int64, [_vp]),
+    "arc_optim_state_offset": (ctypes.c_int64, [_vp, ctypes.c_int32]),
+    "arc_optim_norm": (_st, [_vp, _vp, ctypes.c_float, ctypes.c_float, _vp, _vp]),
+    "arc_optim_adamw": (_st, [_vp, ctypes.POINTER(arc_adamw_config), ctypes.c_int64, _vp, _vp,
+                              _vp, _vp, _vp, _vp, _vp, _vp]),
+    "arc_optim_destroy": (_st, [_vp]),
     "arc_status_str": (ctypes.c_char_p, [_st]),
     "arc_last_error": (ctypes.c_char_p, []),
     "arc_describe": (_st, [_vp, ctypes.c_char_p, ctypes.c_int64]),
@@ -226,6 +305,74 @@ def arc_payload_elems(ctx) -> int:
 def arc_projection(seed: int, t: int, n: int, r: int, out_V) -> None:
     """V_t of width n for a shared seed into host memory (numpy [n, r] f32)."""
     _check(_lib.arc_projection(seed & (2**64 - 1), t, n, r, _addr(out_V)), "arc_projection")
+
+
+def arc_tokens_create(cfg: arc_tokens_config, hip_stream=None) -> int:
+    """Returns the context handle; ``hip_stream`` as for arc_create."""
+    out = _vp()
+    _check(_lib.arc_tokens_create(ctypes.byref(cfg), getattr(hip_stream, "cuda_stream", hip_stream),
+                                  ctypes.byref(out)), "arc_tokens_create")
+    return out.value
+
+
+def arc_tokens_score(ctx, rows, logits, stride, targets, logp, entropy, lse, top_ids,
+                     top_logp) -> None:
+    _check(_lib.arc_tokens_score(ctx, rows, _addr(logits), stride, _addr(targets), _addr(logp),
+                                 _addr(entropy), _addr(lse), _addr(top_ids), _addr(top_logp)),
+           "arc_tokens_score")
+
+
+def arc_tokens_grad(ctx, rows, logits, stride, targets, lse, entropy, d_logp, d_entropy, d_lse,
+                    grad, grad_stride) -> None:
+    _check(_lib.arc_tokens_grad(ctx, rows, _addr(logits), stride, _addr(targets), _addr(lse),
+                                _addr(entropy), _addr(d_logp), _addr(d_entropy), _addr(d_lse),
+                                _addr(grad), grad_stride), "arc_tokens_grad")
+
+
+def arc_tokens_loss(ctx, rows, logits, stride, targets, d_logp, d_entropy, d_lse, logp, entropy,
+                    lse, grad, grad_stride) -> None:
+    _check(_lib.arc_tokens_loss(ctx, rows, _addr(logits), stride, _addr(targets), _addr(d_logp),
+                                _addr(d_entropy), _addr(d_lse), _addr(logp), _addr(entropy),
+                                _addr(lse), _addr(grad), grad_stride), "arc_tokens_loss")
+
+
+def arc_tokens_destroy(ctx) -> None:
+    _check(_lib.arc_tokens_destroy(ctx), "arc_tokens_destroy")
+
+
+def arc_optim_create(cfg: arc_optim_config, hip_stream=None) -> int:
+    """Returns the context handle; ``hip_stream`` as for arc_create."""
+    out = _vp()
+    _check(_lib.arc_optim_create(ctypes.byref(cfg), getattr(hip_stream, "cuda_stream", hip_stream),
+                                 ctypes.byref(out)), "arc_optim_create")
+    return out.value
+
+
+def arc_optim_state_elems(ctx) -> int:
+    return int(_lib.arc_optim_state_elems(ctx))
+
+
+def arc_optim_state_offset(ctx, i: int) -> int:
+    return int(_lib.arc_optim_state_offset(ctx, i))
+
+
+def arc_optim_norm(ctx, grads, scale: float, max_norm: float, norms, total) -> None:
+    """grads: a host array (ctypes) of one device pointer for each tensor."""
+    _check(_lib.arc_optim_norm(ctx, grads, scale, max_norm, _addr(norms), _addr(total)),
+           "arc_optim_norm")
+
+
+def arc_optim_adamw(ctx, ac: arc_adamw_config, t: int, params, grads, copies, factor, m, v,
+                    m_scale, v_scale) -> None:
+    """params, grads and copies: host arrays (ctypes) of device pointers; copies
+    may be None."""
+    _check(_lib.arc_optim_adamw(ctx, ctypes.byref(ac), t, params, grads, copies, _addr(factor),
+                                _addr(m), _addr(v), _addr(m_scale), _addr(v_scale)),
+           "arc_optim_adamw")
+
+
+def arc_optim_destroy(ctx) -> None:
+    _check(_lib.arc_optim_destroy(ctx), "arc_optim_destroy")
 
 
 def arc_status_str(status: int) -> str:

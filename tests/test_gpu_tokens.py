@@ -1,0 +1,418 @@
+"""Token log probabilities and their gradient against the formulas in 64 bits:
+sizes from one token up, odd row lengths, strides and alignments, ties, masked
+tokens and rows, non-finite logits, and the gradient against differences."""
+import math
+
+import pytest
+import torch
+
+import paper_2510_26709_amd as arc
+
+pytestmark = pytest.mark.gpu
+
+EPS = 2.0 ** -24  # half a unit in the last place of binary32, relative
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def dtype_of(word):
+    return torch.bfloat16 if word == "bf16" else torch.float32
+
+
+def place(x, dtype, pad=0, shift=0):
+    """x on the GPU in rows V + pad apart, `shift` elements into their memory."""
+    T, V = x.shape
+    buf = torch.full((shift + T * (V + pad),), float("nan"), dtype=dtype_of(dtype), device="cuda")
+    view = buf[shift:].view(T, V + pad)[:, :V]
+    view.copy_(x)
+    return view
+
+
+def formulas(x, y, scale, top):
+    """Everything in 64 bits on the CPU, from logits as they are stored."""
+    x = x.double().cpu()
+    y = y.cpu()
+    T, V = x.shape
+    z = x * scale
+    bad = torch.isnan(x).any(1) | (x == math.inf).any(1)
+    empty = (x == -math.inf).all(1)
+    most = torch.where(empty, 0.0, z.amax(1))[:, None]  # (z - most) - log total: exact far out
+    log_total = torch.logsumexp(z - most, 1)
+    lse = torch.where(bad, math.nan, most[:, 0] + log_total)
+    logq = torch.where(bad[:, None], math.nan, (z - most) - log_total[:, None])
+    logq[empty] = -math.inf
+    q = torch.exp(logq)
+    H = -torch.where(q > 0, q * logq, 0.0).sum(1)
+    H = torch.where(bad, math.nan, H)
+    logp = logq[torch.arange(T), y.clamp(0, V - 1)]
+    logp = torch.where(y >= V, math.nan, logp)
+    logp = torch.where(y < 0, 0.0, logp)
+    order = torch.sort(torch.where(bad[:, None], 0.0, x), dim=1, descending=True,
+                       stable=True).indices[:, :top]
+    near = logq.gather(1, order)
+    near[bad] = math.nan
+    order[bad] = -1
+    return {"logp": logp, "entropy": H, "lse": lse, "top_ids": order, "top_logp": near,
+            "logq": logq, "q": q, "empty": empty, "bad": bad}
+
+
+def slack(x, scale):
+    """Absolute error [T] of logp (and of lse, beside its own rounding): relative
+    errors of each exponent's argument (a difference and a product, of at most
+    110 in magnitude where the exponential is not 0; a product before it, for a
+    scale that is not 1), and of a sum whose longest chain is at most V / 256
+    terms and sixteen joins."""
+    z = x.double().cpu() * scale
+    z = torch.where(torch.isfinite(z), z, -math.inf)
+    most = z.amax(1, keepdim=True)
+    live = torch.where(z >= most - 110, z, most)
+    most = torch.where(most == -math.inf, 0.0, most)
+    live = torch.where(live == -math.inf, 0.0, live)
+    product = live.abs().amax(1) if scale != 1.0 else 0.0
+    return EPS * (8 * (most - live).amax(1) + 4 * product + x.shape[1] / 256 + 64)
+
+
+def lse_slack(x, scale, lse):
+    return slack(x, scale) + 4 * EPS * lse.abs().nan_to_num(posinf=0.0)
+
+
+def near(name, got, want, tol):
+    got, want = got.double().cpu(), want.double()
+    same = (got == want) | (torch.isnan(got) & torch.isnan(want))
+    off = torch.where(same, 0.0, (got - want).abs())
+    worst = float(off.nan_to_num(nan=math.inf).max()) if off.numel() else 0.0
+    tol = torch.as_tensor(tol, dtype=torch.float64)
+    ok = same | (off <= tol)
+    assert bool(ok.all()), f"{name}: off by {worst:.3e}, allowed {float(tol.max()):.3e}"
+
+
+def check_score(x, y, scale, top, dtype, **kw):
+    h = arc.TokenLogProbs(V=x.shape[1], rows=max(1, x.shape[0]), dtype=dtype, top=top,
+                          scale=scale)
+    got = h.score(x, y)
+    again = h.score(x, y)
+    torch.cuda.synchronize()
+    for a, b in zip(got, again):
+        assert torch.equal(a.view(torch.int32), b.view(torch.int32)), "a call repeats its bits"
+    want = formulas(x, y, scale, top)
+    tol = slack(x, scale)
+    near("lse", got.lse, want["lse"], lse_slack(x, scale, want["lse"]))
+    near("logp", got.logp, want["logp"], tol + 4 * EPS * want["logp"].abs().nan_to_num(posinf=0.0))
+    near("entropy", got.entropy, want["entropy"], tol * (2 + 2 * math.log(x.shape[1] + 1)))
+    assert torch.equal(got.top_ids.cpu().long(), want["top_ids"]), "alternatives"
+    near("top_logp", got.top_logp, want["top_logp"],
+         tol[:, None] + 4 * EPS * want["top_logp"].abs().nan_to_num(posinf=0.0))
+    h.close()
+    return got, want
+
+
+def check_grad(x, y, scale, dtype, want, got, ups, grad, name):
+    """ups: (dl, dh, dz), each a device tensor or None."""
+    T, V = x.shape
+    zero = torch.zeros(T, dtype=torch.float64)
+    dl, dh, dz = (zero if u is None else u.double().cpu() for u in ups)
+    yc = y.cpu()
+    dl = torch.where(yc < 0, 0.0, dl)
+    q, logq, H = want["q"], want["logq"], want["entropy"]
+    safe = torch.where(q > 0, logq, 0.0)
+    g = q * (dz - dl)[:, None] - dh[:, None] * q * (safe + H[:, None])
+    inside = (yc >= 0) & (yc < V)
+    g[torch.arange(T)[inside], yc[inside]] += dl[inside]
+    g *= scale
+    none = ((dl == 0) & (dh == 0) & (dz == 0)) | want["empty"]
+    g[none] = 0.0
+    # p carries the error of lse in its exponent; logq + H that of both
+    tol = lse_slack(x, scale, want["lse"])[:, None]
+    rel = 4 * tol + 8 * EPS + 8 * EPS * safe.abs().nan_to_num()
+    size = (dl.abs() + dz.abs() + dh.abs() * (H.abs().nan_to_num() + 2))[:, None] + \
+        dh.abs()[:, None] * safe.abs().nan_to_num()
+    bound = scale * q.nan_to_num() * size * rel + scale * dl.abs()[:, None] * 4 * EPS
+    bound += scale * dh.abs()[:, None] * q.nan_to_num() * tol * (4 + 2 * math.log(V + 1))
+    if dtype == "bf16":
+        bound = bound + (g.abs().nan_to_num() + bound) * 2.0 ** -8
+    near(name, grad, g, bound + 1e-37)
+
+
+def check_all(x, y, scale, dtype, top=0, seed=0):
+    got, want = check_score(x, y, scale, top, dtype)
+    T, V = x.shape
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    up = [torch.randn(T, device="cuda", generator=gen) for _ in range(3)]
+    up[0][::5] = 0.0
+    up[1][::5] = 0.0
+    up[2][::5] = 0.0
+    h = arc.TokenLogProbs(V=V, rows=T, dtype=dtype, scale=scale)
+    for ups in ((up[0], None, None), (up[0], up[1], up[2]), (None, up[1], None)):
+        grad = h.grad(x, y, got.lse, got.entropy, *ups)
+        check_grad(x, y, scale, dtype, want, got, ups, grad, "grad")
+        loss = h.loss(x, y, *ups)
+        check_grad(x, y, scale, dtype, want, got, ups, loss.grad, "loss.grad")
+        tol = slack(x, scale)
+        near("loss.lse", loss.lse, want["lse"], lse_slack(x, scale, want["lse"]))
+        near("loss.logp", loss.logp, want["logp"],
+             tol + 4 * EPS * want["logp"].abs().nan_to_num(posinf=0.0))
+        near("loss.entropy", loss.entropy, want["entropy"], tol * (2 + 2 * math.log(V + 1)))
+    h.close()
+
+
+def tokens(T, V, seed):
+    y = torch.randint(0, V, (T,), generator=torch.Generator().manual_seed(seed))
+    if T > 2:
+        y[2] = -1
+    if T > 4:
+        y[4] = V + 3
+    return y.cuda()
+
+
+SHAPES = [(1, 1), (1, 2), (3, 7), (5, 8), (2, 9), (7, 63), (5, 64), (4, 255), (4, 1000),
+          (6, 4096), (6, 4097), (3, 8193), (9, 32000), (7, 50257), (3, 131_077), (1, 200_003)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,V", SHAPES)
+def test_sizes(T, V, dtype):
+    gen = torch.Generator().manual_seed(T * 1000 + V)
+    x = place(torch.randn(T, V, generator=gen) * 3, dtype)
+    check_all(x, tokens(T, V, 1), 1.0, dtype, top=min(V, 20), seed=V)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pad,shift", [(0, 1), (1, 0), (3, 5), (47, 0), (64, 8), (0, 4)])
+@pytest.mark.parametrize("V", [33, 1001, 5000])
+def test_strides_and_alignment(V, pad, shift, dtype):
+    gen = torch.Generator().manual_seed(V + pad)
+    x = place(torch.randn(11, V, generator=gen) * 2, dtype, pad, shift)
+    check_all(x, tokens(11, V, 2), 0.7, dtype, top=5)
+
+
+def kind(word, T, V, gen):
+    x = torch.randn(T, V, generator=gen)
+    j = torch.arange(V, dtype=torch.float32)
+    if word == "ties":
+        return torch.randint(0, 3, (T, V), generator=gen).float()
+    if word == "equal":
+        return torch.full((T, V), 1.5)
+    if word == "zeros of both signs":
+        return torch.where(x > 0, 0.0, -0.0)
+    if word == "peaked":
+        x[:, V // 2] += 200.0
+        return x
+    if word == "large":
+        return x * 3e3
+    if word == "far below":
+        return x - 1e4
+    if word == "ascending":
+        return (j / V * 8 - 4).expand(T, V).clone()
+    if word == "descending":
+        return (4 - j / V * 8).expand(T, V).clone()
+    if word.startswith("every "):  # the largest lie a fixed distance apart
+        step = int(word.split()[1])
+        return torch.where(j.long() % step == 3, x.abs() + 5, x)
+    if word.startswith("run of "):  # the largest lie next to one another
+        n = int(word.split()[2])
+        x[:, V // 3:V // 3 + n] += 20.0
+        return x
+    raise ValueError(word)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("word", ["ties", "equal", "zeros of both signs", "peaked", "large",
+                                  "far below", "ascending", "descending", "every 64",
+                                  "every 1024", "every 2048", "every 4096", "every 8192",
+                                  "every 16384", "run of 100", "run of 3000"])
+@pytest.mark.parametrize("V", [777, 50257, 140_000])
+def test_values(V, word, dtype):
+    gen = torch.Generator().manual_seed(V)
+    x = place(kind(word, 3, V, gen), dtype)
+    y = tokens(3, V, 3)
+    check_score(x, y, 1.0, min(V, 32), dtype)
+    check_score(x, y, 1.0, 1, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [40, 3001, 50257])
+def test_masked_and_non_finite(V, dtype):
+    gen = torch.Generator().manual_seed(V)
+    x = torch.randn(12, V, generator=gen)
+    inf, nan = math.inf, math.nan
+    x[0, V // 2:] = -inf             # half masked
+    x[1] = -inf                      # nothing left
+    x[2, 1:] = -inf                  # one token left
+    x[3, 5] = nan
+    x[4, 7] = inf
+    x[5, 3], x[5, 9] = inf, -inf
+    x[6, 1], x[6, 2] = nan, inf
+    x[7] = nan
+    x[8, ::2] = -inf
+    x[9, :-1] = -inf                 # the last one left
+    lowest = torch.finfo(torch.bfloat16).min
+    x[10, V // 3:] = lowest          # masked with the type's lowest value
+    x[11] = lowest
+    y = torch.tensor([1, 0, 0, 1, 7, 2, -1, 3, 2, V - 1, 0, 4]).cuda()
+    x = place(x, dtype)
+    for top in (0, 8, 32):
+        check_score(x, y, 1.0, top, dtype)
+    check_all(x[:10], y[:10], 0.5, dtype, top=8)
+
+
+def test_alternatives_of_a_masked_row_are_the_first_tokens():
+    x = place(torch.full((1, 100), -math.inf), "f32")
+    h = arc.TokenLogProbs(V=100, rows=1, dtype="f32", top=4)
+    got = h.score(x, torch.tensor([5]).cuda())
+    assert got.top_ids.tolist() == [[0, 1, 2, 3]]
+    assert got.logp.item() == got.lse.item() == -math.inf and got.entropy.item() == 0.0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_without_upstream_gradient_are_zero_whatever_they_hold(dtype):
+    x = place(torch.full((2, 50), math.nan), dtype)
+    h = arc.TokenLogProbs(V=50, rows=2, dtype=dtype)
+    y = torch.tensor([-1, 3]).cuda()
+    up = torch.tensor([5.0, 0.0]).cuda()   # the first row has no token
+    assert bool((h.loss(x, y, up).grad == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,V,pad", [(3, 1000, 0), (300, 50257, 3), (5, 131_072, 0)])
+def test_gradient_in_place_of_the_logits(T, V, pad, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    x = place(torch.randn(T, V, generator=gen, device="cuda"), dtype, pad)
+    y = tokens(T, V, 4)
+    up = torch.randn(T, generator=gen, device="cuda")
+    h = arc.TokenLogProbs(V=V, rows=T, dtype=dtype)
+    s = h.score(x, y)
+    want = h.grad(x, y, s.lse, None, up)
+    for call in ("grad", "loss"):
+        z = place(x.clone(), dtype, pad)
+        got = (h.grad(z, y, s.lse, None, up, out=z) if call == "grad" else
+               h.loss(z, y, up, out=z).grad)
+        assert got.data_ptr() == z.data_ptr()
+        if call == "grad":
+            assert torch.equal(got, want)
+        else:
+            near("loss in place", got, want.double().cpu(),
+                 float(want.double().abs().max()) * (2.0 ** -7 if dtype == "bf16" else 1e-5))
+
+
+def test_gradient_against_differences():
+    T, V, step = 4, 37, 2.0 ** -5
+    gen = torch.Generator().manual_seed(3)
+    x = torch.randn(T, V, generator=gen)
+    y = torch.tensor([0, 36, 5, 17]).cuda()
+    h = arc.TokenLogProbs(V=V, rows=T, dtype="f32", scale=1.3)
+    wide = arc.TokenLogProbs(V=V, rows=T * V, dtype="f32", scale=1.3)
+    s = h.score(x.cuda(), y)
+    one = torch.ones(T, device="cuda")
+    for k, ups in ((0, (one, None, None)), (1, (None, one, None)), (2, (None, None, one))):
+        grad = h.grad(x.cuda(), y, s.lse, s.entropy, *ups).cpu()
+        bump = step * torch.eye(V)
+        up = wide.score((x[:, None, :] + bump).reshape(-1, V).cuda(), y.repeat_interleave(V))[k]
+        down = wide.score((x[:, None, :] - bump).reshape(-1, V).cuda(), y.repeat_interleave(V))[k]
+        slope = ((up - down) / (2 * step)).view(T, V).cpu()
+        # third derivatives times step^2 / 6 (at most 6 scale^3 for these
+        # functions, more for the entropy), and 2e-6 of either value over the step
+        bound = (20 if k == 1 else 6) * 1.3 ** 3 * step ** 2 / 6 + 4e-6 / step
+        assert float((slope - grad).abs().max()) < bound
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_offsets_beyond_32_bits(dtype):
+    V, stride = 50_001, 60_000
+    T = (1 << 32) // stride // (1 if dtype == "bf16" else 2) + 50
+    buf = torch.zeros(T, stride, dtype=dtype_of(dtype), device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    rows = [0, T // 2, T - 2, T - 1]
+    for r in rows:
+        buf[r] = torch.randn(stride, generator=gen, device="cuda")
+    y = torch.randint(0, V, (T,), generator=gen, device="cuda")
+    x = buf[:, :V]
+    h = arc.TokenLogProbs(V=V, rows=T, dtype=dtype, top=3)
+    got = h.score(x, y)
+    kept = x[rows].clone()
+    want = formulas(kept, y[rows], 1.0, 3)
+    near("logp", got.logp[rows], want["logp"], slack(kept, 1.0) + 64 * EPS)
+    assert torch.equal(got.top_ids[rows].cpu().long(), want["top_ids"])
+    up = torch.ones(T, device="cuda")
+    loss = h.loss(x, y, up, out=x)
+    check_grad(kept, y[rows], 1.0, dtype, want, got, (up[rows], None, None), loss.grad[rows],
+               "grad")
+
+
+def test_no_rows():
+    h = arc.TokenLogProbs(V=10, rows=4, dtype="f32", top=2)
+    x = torch.empty(0, 10, device="cuda")
+    y = torch.empty(0, dtype=torch.int64, device="cuda")
+    assert h.score(x, y).top_ids.shape == (0, 2)
+    assert h.loss(x, y, torch.empty(0, device="cuda")).grad.shape == (0, 10)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_any_of_the_outputs(dtype):
+    T, V = 5, 9000
+    x = place(torch.randn(T, V, generator=torch.Generator().manual_seed(2)), dtype)
+    y = tokens(T, V, 5)
+    h = arc.TokenLogProbs(V=V, rows=T, dtype=dtype, top=3)
+    all_ = h.score(x, y)
+    lse, ent = torch.full((2, T), math.nan, device="cuda")
+    arc.arc_tokens_score(h.ctx, T, x, x.stride(0), None, None, None, lse, None, None)
+    arc.arc_tokens_score(h.ctx, T, x, x.stride(0), None, None, ent, None, None, None)
+    assert torch.equal(lse, all_.lse)
+    assert torch.equal(ent, all_.entropy)
+    ids = torch.empty(T, 3, dtype=torch.int32, device="cuda")
+    near_ = torch.empty(T, 3, device="cuda")
+    arc.arc_tokens_score(h.ctx, T, x, x.stride(0), None, None, None, None, ids, near_)
+    assert torch.equal(ids, all_.top_ids) and torch.equal(near_, all_.top_logp)
+
+
+def test_another_stream_and_replays_of_a_graph():
+    T, V = 6, 50257
+    stream = torch.cuda.Stream()
+    x = place(torch.randn(T, V, generator=torch.Generator().manual_seed(2)), "bf16")
+    y = tokens(T, V, 5)
+    up = torch.full((T,), -0.5, device="cuda")
+    want = arc.TokenLogProbs(V=V, rows=T, top=7).score(x, y)
+    torch.cuda.synchronize()
+    h = arc.TokenLogProbs(V=V, rows=T, top=7, stream=stream)
+    got = h.score(x, y)  # outputs belong to that stream
+    stream.synchronize()
+    assert torch.equal(got.top_ids, want.top_ids) and torch.equal(got.lse, want.lse)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        s = h.score(x, y)
+        g = h.loss(x, y, up)
+    for k in range(4):
+        x.copy_(place(torch.randn(T, V, generator=torch.Generator().manual_seed(10 + k)), "bf16"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        e = arc.TokenLogProbs(V=V, rows=T, top=7)
+        eager, loss = e.score(x, y), e.loss(x, y, up)
+        for a, b in zip(tuple(s) + tuple(g), tuple(eager) + tuple(loss)):
+            assert torch.equal(a.nan_to_num(), b.nan_to_num()), k
+
+
+def test_refusals():
+    h = arc.TokenLogProbs(V=16, rows=4, dtype="f32", top=2)
+    x = torch.zeros(4, 16, device="cuda")
+    y = torch.zeros(4, dtype=torch.int64, device="cuda")
+    out = h.score(x, y)
+    for bad in (x.bfloat16(), x[:, :8], x.t(), x[0], x.cpu()):
+        with pytest.raises(ValueError):
+            h.score(bad, y)
+    for bad in (y.int(), y[:3], y.cpu()):
+        with pytest.raises(ValueError):
+            h.score(x, bad)
+    with pytest.raises(arc.ArcError):
+        h.score(torch.zeros(5, 16, device="cuda"), torch.zeros(5, dtype=torch.int64,
+                                                               device="cuda"))
+    with pytest.raises(arc.ArcError):  # d_entropy needs entropy
+        h.grad(x, y, out.lse, None, None, out.lse)
+    with pytest.raises(arc.ArcError):  # overlapping rows of logits and gradient
+        buf = torch.zeros(5 * 16, device="cuda")
+        h.grad(buf[:64].view(4, 16), y, out.lse, None, out.lse, out=buf[16:].view(4, 16))
+    with pytest.raises(arc.ArcError):
+        arc.arc_tokens_score(h.ctx, 4, x, 16, y, out.lse, out.lse, None, None, None)
