@@ -148,6 +148,38 @@ __device__ __forceinline__ uint32_t wave_sum(uint32_t v) {
   return v;
 }
 
+// Lane permutations within a row of 16 lanes that together reduce it: after
+// combining with each in turn, every lane of the row holds the whole.
+constexpr int kDppXor1 = 0xB1, kDppXor2 = 0x4E, kDppHalfMirror = 0x141, kDppMirror = 0x140;
+
+template <int kCtrl>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kCtrl, 0xF, 0xF, false);
+}
+template <int kCtrl>
+__device__ __forceinline__ float dpp(float v) {
+  return __uint_as_float(dpp<kCtrl>(__float_as_uint(v)));
+}
+template <int kCtrl>
+__device__ __forceinline__ uint64_t dpp(uint64_t v) {
+  return ((uint64_t)dpp<kCtrl>((uint32_t)(v >> 32)) << 32) | dpp<kCtrl>((uint32_t)v);
+}
+
+// op over runs of kLanes lanes (4, 8, 16) or the wave (64), on every lane of
+// them, in an order that is fixed.
+template <int kLanes, typename T, typename Op>
+__device__ __forceinline__ T lanes_reduce(T v, const Op& op) {
+  v = op(v, dpp<kDppXor1>(v));
+  v = op(v, dpp<kDppXor2>(v));
+  if constexpr (kLanes >= 8) v = op(v, dpp<kDppHalfMirror>(v));
+  if constexpr (kLanes >= 16) v = op(v, dpp<kDppMirror>(v));
+  if constexpr (kLanes >= 64) {
+    v = op(v, (T)__shfl_xor(v, 16));
+    v = op(v, (T)__shfl_xor(v, 32));
+  }
+  return v;
+}
+
 inline unsigned blocks_for(int64_t work, int threads) {
   return (unsigned)((work + threads - 1) / threads);
 }

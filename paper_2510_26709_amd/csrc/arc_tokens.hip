@@ -10,11 +10,39 @@
 namespace arc {
 namespace {
 
-constexpr int kThreads = 1024;
-constexpr int kWaves = kThreads / kWave;
+constexpr int kMaxTop = 32;           // ARC_MAX_TOP
+constexpr int64_t kSplitRows = 1024;  // calls of more rows give each a workgroup
+constexpr int64_t kSplitParts = 4096;
+constexpr int64_t kRowsPerLaunch = 1 << 20;  // threads of a launch stay below 2^32
+constexpr int kScoreThreads = 512;
+
+// ---------------------------------------------------------------------------
+// A row is read in chunks of 16 bytes a lane, from its first whole word on (a
+// row of bfloat16 may begin between words: its 16-byte loads would then reach
+// 5.5 TB/s instead of 6.5), and single elements at its ends.
+// ---------------------------------------------------------------------------
+template <bool BF16>
+constexpr int kChunk = BF16 ? 8 : 4;
+
+struct __attribute__((packed, aligned(4))) Words16 {
+  uint32_t w[4];
+};
 
 template <bool BF16>
-__device__ __forceinline__ float logit(const void* row, int64_t j) {
+__device__ __forceinline__ void unpack(const Words16& r, float (&x)[kChunk<BF16>]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if constexpr (BF16) {
+      x[2 * k] = bf16_lo(r.w[k]);
+      x[2 * k + 1] = bf16_hi(r.w[k]);
+    } else {
+      x[k] = __uint_as_float(r.w[k]);
+    }
+  }
+}
+
+template <bool BF16>
+__device__ __forceinline__ float element(const void* row, int64_t j) {
   if constexpr (BF16)
     return __uint_as_float((uint32_t) static_cast<const uint16_t*>(row)[j] << 16);
   return static_cast<const float*>(row)[j];
@@ -25,98 +53,425 @@ __device__ __forceinline__ const void* row_at(const void* base, int64_t element)
   return static_cast<const char*>(base) + element * (BF16 ? 2 : 4);
 }
 
-// Softmax statistics of part of a row relative to its largest value `most`:
-// total = sum exp(z - most), spread = sum exp(z - most) (z - most).
+// Where a row's chunks lie: `head` single elements (0 or 1), `chunks` chunks,
+// `tail` single elements.
+template <bool BF16>
+struct RowShape {
+  int32_t head, chunks, tail;
+  __device__ RowShape(const void* row, int32_t V) {
+    head = BF16 ? (int32_t)((reinterpret_cast<uintptr_t>(row) >> 1) & 1) : 0;
+    chunks = (V - head) / kChunk<BF16>;
+    tail = (V - head) % kChunk<BF16>;
+  }
+  // Single element e of head + tail.
+  __device__ int32_t edge(int32_t e, int32_t V) const { return e < head ? e : V - tail + (e - head); }
+  __device__ const Words16* body(const void* row) const {
+    return reinterpret_cast<const Words16*>(row_at<BF16>(row, head));
+  }
+};
+
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
+
+// Softmax statistics of part of a row relative to its largest logit `most`, in
+// powers of two: total = sum 2^t and spread = sum 2^t t for t = (x - most) c, c
+// = scale log2(e).  The difference is taken first: it is exact where it
+// matters, however large the logits are.
 struct Stats {
   float most, total, spread;
 };
 
-__device__ __forceinline__ Stats join(Stats a, Stats b) {
-  const float most = fmaxf(a.most, b.most);
-  if (most == -INFINITY)  // nothing, or NaN, on both sides
-    return {most, a.total + b.total, a.spread + b.spread};
-  const float da = a.most - most, db = b.most - most;
-  const float ea = expf(da), eb = expf(db);
-  // a side without weight adds nothing, however far away (0 * infinity); NaN
-  // goes by way of the total
-  const float sa = ea > 0.f ? ea * (a.spread + da * a.total) : 0.f;
-  const float sb = eb > 0.f ? eb * (b.spread + db * b.total) : 0.f;
-  return {most, ea * a.total + eb * b.total, sa + sb};
+__device__ __forceinline__ float exponent(float x, float most, float c) { return (x - most) * c; }
+
+// t below this adds nothing to a spread, and 0 * infinity would.
+constexpr float kFarBelow = -200.f;
+
+// The statistics relative to `most` instead (not below their own, -infinity
+// only with theirs).
+__device__ __forceinline__ Stats moved(Stats s, float most, float c) {
+  if (s.most == -INFINITY) return {most, s.total, 0.f};  // total: 0, or a NaN to keep
+  const float t = exponent(s.most, most, c);
+  const float e = __builtin_amdgcn_exp2f(t);
+  return {most, e * s.total, e * (s.spread + fmaxf(t, kFarBelow) * s.total)};
 }
 
 // A larger key is a larger logit, or the same logit of a lower token.
-__device__ __forceinline__ uint64_t rank_key(float x, int64_t j) {
+__device__ __forceinline__ uint64_t rank_key(float x, int32_t j) {
   const uint32_t b = __float_as_uint(x + 0.0f);
   const uint32_t up = b ^ ((b >> 31) ? 0xFFFFFFFFu : 0x80000000u);
   return ((uint64_t)up << 32) | (0xFFFFFFFFu - (uint32_t)j);
 }
+__device__ __forceinline__ int32_t key_token(uint64_t key) {
+  return (int32_t)(0xFFFFFFFFu - (uint32_t)key);
+}
+__device__ __forceinline__ float key_logit(uint64_t key) {
+  const uint32_t up = (uint32_t)(key >> 32);
+  return __uint_as_float(up ^ ((up >> 31) ? 0x80000000u : 0xFFFFFFFFu));
+}
 
-template <bool BF16>
-__global__ void __launch_bounds__(kThreads)
-token_score_kernel(TokenArgs a, TokenScores out) {
-  __shared__ Stats part[kWaves];
-  __shared__ uint64_t best[kWaves];
-  const int64_t i = blockIdx.x, V = a.vocab;
-  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-  const void* row = row_at<BF16>(a.logits, i * a.stride);
-  Stats s{-INFINITY, 0.f, 0.f};
-  for (int64_t j = threadIdx.x; j < V; j += kThreads) {
-    const float z = logit<BF16>(row, j) * a.scale;
-    if (z == -INFINITY) continue;
-    s = join(s, {z, z != z ? z : 1.f, 0.f});
-  }
+struct MaxF {
+  __device__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+struct SumF {
+  __device__ float operator()(float a, float b) const { return a + b; }
+};
+struct MaxKey {
+  __device__ uint64_t operator()(uint64_t a, uint64_t b) const { return a > b ? a : b; }
+};
+
+// What a workgroup found out about its piece of a row, for the workgroup that
+// joins the pieces.
+struct TokenPart {
+  float most, total, spread, pad;
+  uint64_t top[kMaxTop];  // keys in falling order, 0 where the piece has no more
+};
+
+// Parts are written through to where every compute unit sees them and read
+// from there.  A fence for the whole device writes back all that its XCD's
+// cache holds instead, of every workgroup: 1024 of them took 250 us.
+template <typename T>
+__device__ __forceinline__ void share_store(T* p, T v) {
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <typename T>
+__device__ __forceinline__ T share_load(const T* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Alternatives.  Every thread knows the largest logit of its own chunks and
+// the first chunk that holds it; the threads' order by (that logit, that
+// chunk) is an order of disjoint runs of tokens, so the top k elements lie in
+// the chunks of the first k threads of it.  The threads form 64 groups, a
+// bound `tau` is the k-th largest of the groups' first threads, and only the
+// threads from tau on have their chunks read once more (from the cache), by
+// the whole workgroup.  A row of noise has about k log(64 / (64 - k)) such
+// threads.  What reaches tau there, some dozens, is ordered by counting.
+constexpr int kCandidates = 2048;
+struct TopShared {
+  uint64_t group[64];
+  uint64_t tau;
+  int32_t threads, found;
+  uint64_t found_keys[kCandidates];
+};
+
+template <bool BF16, int W>
+struct Scorer {
+  static constexpr int C = kChunk<BF16>;
+  static constexpr int U = 4;  // chunks of a thread in flight
+  static constexpr int kWaves = W / kWave;
+  static constexpr int kLanes = W / 64;  // of a group
+
+  // Statistics of chunks [first, end) of the row, a thread's share, with the
+  // token at which its largest logit's chunk (or single element) begins; the
+  // single elements are the last piece's.
+  static __device__ __forceinline__ Stats share(const Words16* body, int32_t head, int32_t first,
+                                                int32_t end, float c, int32_t* at) {
+    Stats s{-INFINITY, 0.f, 0.f};
+    int32_t best = first + (int)threadIdx.x < end ? head + (first + (int)threadIdx.x) * C
+                                                  : INT32_MAX;
+    for (int32_t k = first + threadIdx.x; k < end; k += W * U) {
+      Words16 raw[U];
 #pragma unroll
-  for (int off = 1; off < kWave; off <<= 1)
-    s = join(s, {__shfl_xor(s.most, off), __shfl_xor(s.total, off), __shfl_xor(s.spread, off)});
-  if (lane == 0) part[wave] = s;
-  __syncthreads();
-  s = part[0];
-  for (int w = 1; w < kWaves; ++w) s = join(s, part[w]);
-  const bool empty = s.total == 0.f;
-  const float log_total = logf(s.total);
-  const float lse = empty ? -INFINITY : s.most + log_total;
+      for (int u = 0; u < U; ++u) {
+        const uint32_t low = BF16 ? 0xFF80FF80u : 0xFF800000u;  // -infinity
+        raw[u] = Words16{{low, low, low, low}};
+        if (k + u * W < end) raw[u] = body[k + u * W];
+      }
+      float x[U][C];
+      float most = s.most;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        unpack<BF16>(raw[u], x[u]);
+        float m = x[u][0];
+#pragma unroll
+        for (int q = 1; q < C; ++q) m = fmaxf(m, x[u][q]);
+        if (m > most) {
+          most = m;
+          best = head + (k + u * W) * C;
+        }
+      }
+      // with nothing above -infinity so far, distances are taken from 0
+      const float from = most == -INFINITY ? 0.f : most;
+      s = moved(s, from, c);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int q = 0; q < C; ++q) {
+          const float t = exponent(x[u][q], from, c);
+          const float e = __builtin_amdgcn_exp2f(t);
+          s.total += e;
+          s.spread = fmaf(e, fmaxf(t, kFarBelow), s.spread);
+        }
+      s.most = most;
+    }
+    *at = best;
+    return s;
+  }
+
+  static __device__ __forceinline__ void add_edge(float x, int32_t j, float c, Stats* s,
+                                                  int32_t* at) {
+    if (*at == INT32_MAX || x > s->most || (x == s->most && j < *at)) *at = j;
+    const float most = fmaxf(s->most, x);
+    const float from = most == -INFINITY ? 0.f : most;
+    *s = moved(*s, from, c);
+    const float t = exponent(x, from, c), e = __builtin_amdgcn_exp2f(t);
+    s->total += e;
+    s->spread = fmaf(e, fmaxf(t, kFarBelow), s->spread);
+    s->most = most;
+  }
+
+  // Over the workgroup, on every thread.
+  static __device__ __forceinline__ float all_max(float v, float* part) {
+    v = lanes_reduce<64>(v, MaxF());
+    if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = v;
+    __syncthreads();
+    v = part[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) v = fmaxf(v, part[w]);
+    return v;
+  }
+
+  // The keys found are ordered by counting, and the first k written.
+  template <typename Write>
+  static __device__ __forceinline__ void order(const TopShared& sh, int32_t n, int32_t k,
+                                               const Write& write) {
+    for (int32_t i = threadIdx.x; i < n; i += W) {
+      const uint64_t key = sh.found_keys[i];
+      int32_t rank = 0;
+      for (int32_t q = 0; q < n; ++q) rank += sh.found_keys[q] > key;
+      if (rank < k) write(rank, key);
+    }
+  }
+};
+
+// Writes a row's results; `order` holds its keys.
+struct RowResult {
+  float most, scale, log_total;
+  bool empty, none;
+  __device__ float logp(float x) const {
+    return none ? NAN : empty ? -INFINITY : (x - most) * scale - log_total;
+  }
+};
+
+__device__ __forceinline__ RowResult finish_row(const TokenArgs& a, const TokenScores& out,
+                                                int64_t i, const Stats& s, int64_t y, float xy) {
+  RowResult r;
+  r.most = s.most;
+  r.scale = a.scale;
+  r.empty = s.total == 0.f;
+  r.log_total = logf(s.total);
+  const float lse = r.empty ? -INFINITY : s.most * a.scale + r.log_total;
+  r.none = lse != lse;
   if (threadIdx.x == 0) {
     if (out.lse) out.lse[i] = lse;
-    if (out.entropy) out.entropy[i] = empty ? 0.f : log_total - s.spread / s.total;
-    if (out.logp) {
-      const int64_t y = a.targets[i];
-      float lp = 0.f;
-      if (y >= V)
-        lp = NAN;
-      else if (y >= 0)
-        lp = empty ? -INFINITY : (logit<BF16>(row, y) * a.scale - s.most) - log_total;
-      out.logp[i] = lp;
+    if (out.entropy) out.entropy[i] = r.empty ? 0.f : r.log_total - s.spread * kLn2 / s.total;
+    if (out.logp) out.logp[i] = y < 0 ? 0.f : y >= a.vocab ? NAN : r.logp(xy);
+  }
+  return r;
+}
+
+template <bool BF16, int W>
+__global__ void __launch_bounds__(W)
+token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_chunks,
+                   TokenPart* __restrict__ parts, uint32_t* __restrict__ arrived) {
+  using S = Scorer<BF16, W>;
+  __shared__ float part_most[S::kWaves];
+  __shared__ float part_sum[2][S::kWaves];
+  __shared__ float given;
+  __shared__ int32_t last;
+  __shared__ TopShared sh;
+  const int64_t i = pieces == 1 ? blockIdx.x : blockIdx.x / pieces;
+  const int32_t piece = pieces == 1 ? 0 : blockIdx.x % pieces;
+  const int32_t V = (int32_t)a.vocab, k = out.top_ids ? a.top : 0;
+  const float c = a.scale * kLog2e;
+  const void* row = row_at<BF16>(a.logits, i * a.stride);
+  const RowShape<BF16> shape(row, V);
+  const Words16* body = shape.body(row);
+  const int32_t first = piece * piece_chunks;
+  const int32_t end = min(shape.chunks, first + piece_chunks);
+  const bool edges = piece == pieces - 1;
+  const int64_t y = out.logp ? a.targets[i] : -1;
+  if (threadIdx.x == W - 1) given = y >= 0 && y < V ? element<BF16>(row, y) : 0.f;
+
+  int32_t at;
+  Stats s = S::share(body, shape.head, first, end, c, &at);
+  if (edges && (int)threadIdx.x < shape.head + shape.tail) {
+    const int32_t j = shape.edge(threadIdx.x, V);
+    S::add_edge(element<BF16>(row, j), j, c, &s, &at);
+  }
+  const uint64_t mine = at == INT32_MAX ? 0 : rank_key(s.most, at);
+  if (k) {
+    const uint64_t g = lanes_reduce<S::kLanes>(mine, MaxKey());
+    if (threadIdx.x % S::kLanes == 0) sh.group[threadIdx.x / S::kLanes] = g;
+    if (threadIdx.x == 0) {
+      sh.tau = 0;
+      sh.threads = sh.found = 0;
     }
   }
-  if (!out.top_ids) return;
-  const bool none = lse != lse;
-  uint64_t last = ~0ull;
-  for (int k = 0; k < a.top; ++k) {
-    uint64_t key = 0;
-    if (!none)
-      for (int64_t j = threadIdx.x; j < V; j += kThreads) {
-        const uint64_t q = rank_key(logit<BF16>(row, j), j);
-        if (q < last && q > key) key = q;
-      }
+  const float most = S::all_max(s.most, part_most);
+  s = moved(s, most == -INFINITY ? 0.f : most, c);
+  s.total = lanes_reduce<64>(s.total, SumF());
+  s.spread = lanes_reduce<64>(s.spread, SumF());
+  if (threadIdx.x % kWave == 0) {
+    part_sum[0][threadIdx.x / kWave] = s.total;
+    part_sum[1][threadIdx.x / kWave] = s.spread;
+  }
+  if (k) {  // the group whose rank is k - 1 sets the bound
+    const uint64_t key = sh.group[threadIdx.x / S::kLanes];
+    uint32_t rank = 0;
 #pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-      const uint64_t q = __shfl_xor((unsigned long long)key, off);
-      key = q > key ? q : key;
+    for (int q = 0; q < 64 / S::kLanes; ++q)
+      rank += sh.group[q * S::kLanes + threadIdx.x % S::kLanes] > key;
+    rank = lanes_reduce<S::kLanes>(rank, [](uint32_t p, uint32_t q) { return p + q; });
+    if (rank == (uint32_t)(k - 1) && threadIdx.x % S::kLanes == 0 && key != 0)
+      sh.tau = key - (S::C - 1);  // a run's largest element may be its last
+  }
+  __syncthreads();
+  s = {most, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < S::kWaves; ++w) {
+    s.total += part_sum[0][w];
+    s.spread += part_sum[1][w];
+  }
+  bool overflow = false;
+  if (k) {
+    const uint64_t tau = sh.tau;
+    __shared__ int32_t list[W];
+    if (mine != 0 && mine >= tau) list[atomicAdd(&sh.threads, 1)] = threadIdx.x;
+    __syncthreads();
+    const int32_t threads = sh.threads;
+    const int32_t each = (end - first + W - 1) / W;  // chunks of a thread, at most
+    const auto found = [&](float x, int32_t j) {
+      const uint64_t key = rank_key(x, j);
+      if (key >= tau) {
+        const int32_t n = atomicAdd(&sh.found, 1);
+        if (n < kCandidates) sh.found_keys[n] = key;
+      }
+    };
+    for (int32_t q = threadIdx.x; q < threads * each; q += W) {
+      const int32_t chunk = first + list[q / each] + (q % each) * W;
+      if (chunk >= end) continue;
+      float x[S::C];
+      unpack<BF16>(body[chunk], x);
+#pragma unroll
+      for (int e = 0; e < S::C; ++e) found(x[e], shape.head + chunk * S::C + e);
+    }
+    if (edges && (int)threadIdx.x < shape.head + shape.tail) {
+      const int32_t j = shape.edge(threadIdx.x, V);
+      found(element<BF16>(row, j), j);
     }
     __syncthreads();
-    if (lane == 0) best[wave] = key;
-    __syncthreads();
-    key = best[0];
-    for (int w = 1; w < kWaves; ++w) key = best[w] > key ? best[w] : key;
-    last = key;
-    if (threadIdx.x == 0) {
-      const int64_t j = 0xFFFFFFFFu - (uint32_t)key;
-      out.top_ids[i * a.top + k] = none ? -1 : (int32_t)j;
-      out.top_logp[i * a.top + k] =
-          none ? NAN : empty ? -INFINITY : (logit<BF16>(row, j) * a.scale - s.most) - log_total;
+    overflow = sh.found > kCandidates;
+  }
+  const int32_t n = k ? sh.found : 0;
+
+  // Too many for the list (the largest logits sit in few threads' chunks): the
+  // row's keys one after the other, each the largest below the one before.
+  const auto one_by_one = [&](const auto& write) {
+    uint64_t before = ~0ull;
+    for (int32_t r = 0; r < k; ++r) {
+      uint64_t key = 0;
+      const auto look = [&](float x, int32_t j) {
+        const uint64_t q = rank_key(x, j);
+        if (q < before && q > key) key = q;
+      };
+      for (int32_t q = first + threadIdx.x; q < end; q += W) {
+        float x[S::C];
+        unpack<BF16>(body[q], x);
+#pragma unroll
+        for (int e = 0; e < S::C; ++e) look(x[e], shape.head + q * S::C + e);
+      }
+      if (edges && (int)threadIdx.x < shape.head + shape.tail) {
+        const int32_t j = shape.edge(threadIdx.x, V);
+        look(element<BF16>(row, j), j);
+      }
+      key = lanes_reduce<64>(key, MaxKey());
+      __syncthreads();
+      if (threadIdx.x % kWave == 0) sh.group[threadIdx.x / kWave] = key;
+      __syncthreads();
+      key = sh.group[0];
+      for (int w = 1; w < S::kWaves; ++w) key = MaxKey()(key, sh.group[w]);
+      if (threadIdx.x == 0) write(r, key);
+      before = key;
     }
+  };
+
+  if (pieces == 1) {
+    const RowResult r = finish_row(a, out, i, s, y, given);
+    if (!k) return;
+    const auto write = [&](int32_t rank, uint64_t key) {
+      out.top_ids[i * k + rank] = r.none ? -1 : key_token(key);
+      out.top_logp[i * k + rank] = r.logp(key_logit(key));
+    };
+    if (r.none) {
+      if ((int)threadIdx.x < k) write(threadIdx.x, 0);
+    } else if (overflow) {
+      one_by_one(write);
+    } else {
+      S::order(sh, n, k, write);
+    }
+    return;
+  }
+
+  TokenPart* part = parts + blockIdx.x;
+  if (threadIdx.x == 0) {
+    share_store(&part->most, s.most);
+    share_store(&part->total, s.total);
+    share_store(&part->spread, s.spread);
+  }
+  if (k) {
+    const auto write = [&](int32_t rank, uint64_t key) { share_store(&part->top[rank], key); };
+    if (overflow) {
+      one_by_one(write);
+    } else {
+      if ((int)threadIdx.x >= n && (int)threadIdx.x < k) write(threadIdx.x, 0);
+      S::order(sh, n, k, write);
+    }
+  }
+  // The last workgroup of a row to arrive joins the pieces: every wave's part
+  // has been written before the barrier, and the count goes up behind it.
+  wave_vmem_fence();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const uint32_t before = __hip_atomic_fetch_add(&arrived[i], 1u, __ATOMIC_RELAXED,
+                                                   __HIP_MEMORY_SCOPE_AGENT);
+    last = before == (uint32_t)(pieces - 1);
+    if (last) share_store(&arrived[i], 0u);  // for the next call
+  }
+  __syncthreads();
+  if (!last) return;
+  const TokenPart* of = parts + i * pieces;
+  // A lane of each wave takes a piece (there are at most 64), in the same order.
+  const int32_t lane = threadIdx.x % kWave;
+  s = {-INFINITY, 0.f, 0.f};
+  if (lane < pieces)
+    s = {share_load(&of[lane].most), share_load(&of[lane].total), share_load(&of[lane].spread)};
+  const float pm = lanes_reduce<64>(s.most, MaxF());
+  s = moved(s, pm == -INFINITY ? 0.f : pm, c);
+  s = {pm, lanes_reduce<64>(s.total, SumF()), lanes_reduce<64>(s.spread, SumF())};
+  const RowResult r = finish_row(a, out, i, s, y, given);
+  if (!k) return;
+  // Each piece's k-th key is a bound for the row's.
+  uint64_t tau = lane < pieces ? share_load(&of[lane].top[k - 1]) : 0;
+  tau = lanes_reduce<64>(tau, MaxKey());
+  if (threadIdx.x == 0) sh.found = 0;
+  __syncthreads();
+  for (int32_t q = threadIdx.x; q < pieces * k; q += W) {
+    const uint64_t key = share_load(&of[q / k].top[q % k]);
+    if (key != 0 && key >= tau) sh.found_keys[atomicAdd(&sh.found, 1)] = key;
+  }
+  __syncthreads();
+  const auto write = [&](int32_t rank, uint64_t key) {
+    out.top_ids[i * k + rank] = r.none ? -1 : key_token(key);
+    out.top_logp[i * k + rank] = r.logp(key_logit(key));
+  };
+  if (r.none) {
+    if ((int)threadIdx.x < k) write(threadIdx.x, 0);
+  } else {
+    S::order(sh, sh.found, k, write);
   }
 }
+
+constexpr int kThreads = 1024;
 
 template <bool BF16>
 __global__ void __launch_bounds__(kThreads)
@@ -133,7 +488,7 @@ token_grad_kernel(TokenArgs a, TokenGrad g) {
   for (int64_t j = threadIdx.x; j < V; j += kThreads) {
     float d = 0.f;
     if (!zero) {
-      const float lp = logit<BF16>(row, j) * a.scale - lse;
+      const float lp = element<BF16>(row, j) * a.scale - lse;
       const float p = expf(lp);
       d = p * (dz - dl);
       if (p != 0.f) d -= dh * (p * (lp + H));
@@ -152,10 +507,50 @@ token_grad_kernel(TokenArgs a, TokenGrad g) {
 
 }  // namespace
 
-hipError_t launch_token_score(const TokenArgs& a, const TokenScores& out, hipStream_t stream) {
+size_t token_workspace_bytes(int64_t vocab, int64_t max_rows) {
+  (void)vocab;
+  const int64_t rows = max_rows < kSplitRows ? max_rows : kSplitRows;
+  return (size_t)(kSplitParts * sizeof(TokenPart) + rows * sizeof(uint32_t));
+}
+
+// Pieces of a row.
+static int32_t row_pieces(const TokenArgs& a, int32_t threads) {
+  const int64_t chunks = a.vocab / (a.bf16 ? 8 : 4);
+  if (a.rows > kSplitRows) return 1;
+  int64_t p = (chunks + threads * 2 - 1) / (threads * 2);
+  p = p < 64 ? p : 64;
+  const int64_t most = 1024 / a.rows;
+  p = p < most ? p : most;
+  p = p < kSplitParts / a.rows ? p : kSplitParts / a.rows;
+  return p < 1 ? 1 : (int32_t)p;
+}
+
+hipError_t launch_token_score(const TokenArgs& a, const TokenScores& out, void* workspace,
+                              hipStream_t stream) {
   if (a.rows <= 0) return hipSuccess;
-  hipLaunchKernelGGL(a.bf16 ? token_score_kernel<true> : token_score_kernel<false>,
-                     dim3((unsigned)a.rows), dim3(kThreads), 0, stream, a, out);
+  constexpr int W = kScoreThreads;
+  const int32_t pieces = row_pieces(a, W);
+  const int64_t chunks = a.vocab / (a.bf16 ? 8 : 4);
+  const int32_t piece_chunks = (int32_t)((chunks + pieces - 1) / pieces);
+  auto* parts = static_cast<TokenPart*>(workspace);
+  auto* arrived = reinterpret_cast<uint32_t*>(parts + kSplitParts);
+  for (int64_t lo = 0; lo < a.rows; lo += kRowsPerLaunch) {
+    TokenArgs b = a;
+    TokenScores o = out;
+    b.rows = a.rows - lo < kRowsPerLaunch ? a.rows - lo : kRowsPerLaunch;
+    b.logits = static_cast<const char*>(a.logits) + lo * a.stride * (a.bf16 ? 2 : 4);
+    if (b.targets) b.targets += lo;
+    if (o.logp) o.logp += lo;
+    if (o.entropy) o.entropy += lo;
+    if (o.lse) o.lse += lo;
+    if (o.top_ids) {
+      o.top_ids += lo * a.top;
+      o.top_logp += lo * a.top;
+    }
+    hipLaunchKernelGGL(a.bf16 ? (token_score_kernel<true, W>) : (token_score_kernel<false, W>),
+                       dim3((unsigned)(b.rows * pieces)), dim3(W), 0, stream, b, o, pieces,
+                       piece_chunks, parts, arrived);
+  }
   return hipGetLastError();
 }
 

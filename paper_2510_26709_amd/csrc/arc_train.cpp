@@ -19,6 +19,12 @@ struct arc_tokens {
   float scale = 1.f;
   hipStream_t stream = nullptr;
   int device = 0;
+  void* workspace = nullptr;
+
+  void release() {
+    (void)hipStreamSynchronize(stream);
+    if (workspace) (void)hipFree(workspace);
+  }
 };
 
 struct arc_optim {
@@ -295,10 +301,19 @@ arc_status arc_tokens_create(const arc_tokens_config* cfg, void* hip_stream, arc
   c->top = cfg->top;
   c->scale = cfg->scale;
   c->stream = static_cast<hipStream_t>(hip_stream);
-  const hipError_t e = hipGetDevice(&c->device);
+  const size_t bytes = arc::token_workspace_bytes(c->vocab, c->max_rows);
+  hipError_t e = hipGetDevice(&c->device);
+  if (e == hipSuccess) {
+    e = hipMalloc(&c->workspace, bytes);
+    if (e != hipSuccess) c->workspace = nullptr;
+  }
+  if (e == hipSuccess) e = hipMemset(c->workspace, 0, bytes);
+  if (e == hipSuccess) e = hipDeviceSynchronize();
   if (e != hipSuccess) {
+    (void)hipGetLastError();
+    c->release();
     delete c;
-    return arc::fail_hip(e, "hipGetDevice");
+    return arc::fail_hip(e, "token workspace");
   }
   *out = c;
   return ARC_OK;
@@ -312,7 +327,8 @@ arc_status arc_tokens_score(arc_tokens* c, int64_t rows, const void* logits, int
   const arc::TokenScores out{logp, entropy, lse, top_ids, top_logp};
   if ((st = check_score(c, rows, logits, stride, targets, out)) != ARC_OK) return st;
   const OnDevice here(c->device);
-  ARC_HIP(arc::launch_token_score(token_args(c, rows, logits, stride, targets), out, c->stream),
+  ARC_HIP(arc::launch_token_score(token_args(c, rows, logits, stride, targets), out,
+                                  c->workspace, c->stream),
           "token score launch");
   return ARC_OK;
 }
@@ -353,14 +369,14 @@ arc_status arc_tokens_loss(arc_tokens* c, int64_t rows, const void* logits, int6
     return fail(ARC_ERR_INVALID, "lse and entropy are needed");
   const OnDevice here(c->device);
   const arc::TokenArgs a = token_args(c, rows, logits, stride, targets);
-  ARC_HIP(arc::launch_token_score(a, out, c->stream), "token score launch");
+  ARC_HIP(arc::launch_token_score(a, out, c->workspace, c->stream), "token score launch");
   ARC_HIP(arc::launch_token_grad(a, g, c->stream), "token gradient launch");
   return ARC_OK;
 }
 
 arc_status arc_tokens_destroy(arc_tokens* c) {
   if (c == nullptr) return ARC_OK;
-  (void)hipStreamSynchronize(c->stream);
+  c->release();
   delete c;
   return ARC_OK;
 }

@@ -32,7 +32,11 @@ struct TokenGrad {
   int64_t stride = 0;
 };
 
-hipError_t launch_token_score(const TokenArgs& a, const TokenScores& out, hipStream_t stream);
+// Bytes that launch_token_score's workspace needs, zeroed before its first use;
+// it leaves the part that has to be zero so.
+size_t token_workspace_bytes(int64_t vocab, int64_t max_rows);
+hipError_t launch_token_score(const TokenArgs& a, const TokenScores& out, void* workspace,
+                              hipStream_t stream);
 hipError_t launch_token_grad(const TokenArgs& a, const TokenGrad& g, hipStream_t stream);
 
 // ---------------------------------------------------------------- optimizer

@@ -47,8 +47,9 @@ class _Bound:
         return x
 
     def _empty(self, *shape, dtype=torch.float32):
-        # memory of the stream that writes it
-        if torch.cuda.current_stream(self.device) == self.stream:
+        # memory of the stream that writes it (the raw handles compare in 0.1
+        # us, stream objects in 2)
+        if torch._C._cuda_getCurrentRawStream(self.device.index) == self.stream.cuda_stream:
             return torch.empty(shape, dtype=dtype, device=self.device)
         with torch.cuda.stream(self.stream):
             return torch.empty(shape, dtype=dtype, device=self.device)
@@ -93,12 +94,15 @@ class TokenLogProbs(_Bound):
         """(logp, entropy, lse [T], top_ids int32 and top_logp [T, top])."""
         T, stride = self._rows(logits)
         self._each("targets", targets, T, torch.int64)
-        logp, entropy, lse = self._empty(3, T).unbind()
-        ids = self._empty(T, self.top, dtype=torch.int32)
-        near = self._empty(T, self.top)
-        arc_tokens_score(self.ctx, T, logits, stride, targets, logp, entropy, lse,
-                         ids if self.top else None, near if self.top else None)
-        return Scores(logp, entropy, lse, ids, near)
+        k = T * self.top
+        out = self._empty(3 * T + 2 * k)  # one allocation: a call of one row is mostly host time
+        at = out.data_ptr()
+        arc_tokens_score(self.ctx, T, logits.data_ptr(), stride, targets.data_ptr(), at,
+                         at + 4 * T, at + 8 * T, at + 12 * T if k else None,
+                         at + 12 * T + 4 * k if k else None)
+        logp, entropy, lse, ids, near = out.split_with_sizes((T, T, T, k, k))
+        return Scores(logp, entropy, lse, ids.view(torch.int32).view(T, self.top),
+                      near.view(T, self.top))
 
     def grad(self, logits, targets, lse, entropy=None, d_logp=None, d_entropy=None, d_lse=None,
              out=None):
@@ -119,11 +123,12 @@ class TokenLogProbs(_Bound):
         T, stride = self._rows(logits)
         out, out_stride = self._out(out, T)
         each = self._each
-        logp, entropy, lse = self._empty(3, T).unbind()
+        row = self._empty(3 * T)
+        at = row.data_ptr()
         arc_tokens_loss(self.ctx, T, logits, stride, each("targets", targets, T, torch.int64),
                         each("d_logp", d_logp, T), each("d_entropy", d_entropy, T),
-                        each("d_lse", d_lse, T), logp, entropy, lse, out, out_stride)
-        return Loss(logp, entropy, lse, out)
+                        each("d_lse", d_lse, T), at, at + 4 * T, at + 8 * T, out, out_stride)
+        return Loss(*row.split(T) if T else (row,) * 3, out)
 
     def _out(self, out, T):
         if out is None:
@@ -198,7 +203,7 @@ class AdamW(_Bound):
         """Fills the host table of device pointers of this call."""
         table = self._table[key]
         if isinstance(x, torch.Tensor):  # flat
-            if len(set(dtypes)) > 1:
+            if dtypes.count(dtypes[0]) != len(dtypes):
                 raise ValueError(f"{key}: one flat tensor holds one dtype")
             self._check(key, x, dtypes[0], self._flat)
             np.multiply(self._starts, np.uint64(x.element_size()), out=table)
@@ -217,10 +222,12 @@ class AdamW(_Bound):
         """(total [2], norms [num]): scale * the norm of all gradients and the
         factor for ``step`` that also clips it to max_norm, and scale * the norm
         of each tensor's."""
-        total, norms = self._empty(2), self._empty(len(self.sizes))
+        num = len(self.sizes)
+        out = self._empty(2 + num)
+        at = out.data_ptr()
         arc_optim_norm(self.ctx, self._pointers("grad", grads, self._grad), scale, max_norm,
-                       norms, total)
-        return Norms(total, norms)
+                       at + 8, at)
+        return Norms(*out.split_with_sizes((2, num)))
 
     def step(self, t, params, grads, *, lr, beta1=0.9, beta2=0.999, eps=1e-8, factor=None,
              copies=None):
