@@ -41,6 +41,12 @@ __device__ __forceinline__ void unpack(const Words16& r, float (&x)[kChunk<BF16>
   }
 }
 
+// Words that the compiler has to keep as they are: it would hold on to what it
+// unpacked from them otherwise, twice the registers.
+__device__ __forceinline__ void keep_packed(Words16& r) {
+  asm volatile("" : "+v"(r.w[0]), "+v"(r.w[1]), "+v"(r.w[2]), "+v"(r.w[3]));
+}
+
 template <bool BF16>
 __device__ __forceinline__ float element(const void* row, int64_t j) {
   if constexpr (BF16)
@@ -471,37 +477,221 @@ token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_c
   }
 }
 
-constexpr int kThreads = 1024;
+// ---------------------------------------------------------------------------
+// Gradients.  With lp = log p of an element, dx = p (A + B lp) for the row's
+// A = scale (dz - dl - dh H) and B = -scale dh, and scale dl more at the token.
+// ---------------------------------------------------------------------------
+struct GradRow {
+  float A, B, given;
+  int32_t y;  // -1: none
+  bool zero;
+};
 
-template <bool BF16>
-__global__ void __launch_bounds__(kThreads)
-token_grad_kernel(TokenArgs a, TokenGrad g) {
-  const int64_t i = blockIdx.x, V = a.vocab;
-  const void* row = row_at<BF16>(a.logits, i * a.stride);
-  void* to = const_cast<void*>(row_at<BF16>(g.grad, i * g.stride));
-  const int64_t y = a.targets && g.d_logp ? a.targets[i] : -1;
-  const float dl = g.d_logp && y >= 0 ? g.d_logp[i] : 0.f;
+__device__ __forceinline__ GradRow grad_row(const TokenArgs& a, const TokenGrad& g, int64_t i,
+                                            float H, bool empty) {
+  const int64_t y = g.d_logp ? a.targets[i] : -1;
+  const float dl = y >= 0 ? g.d_logp[i] : 0.f;
   const float dh = g.d_entropy ? g.d_entropy[i] : 0.f;
   const float dz = g.d_lse ? g.d_lse[i] : 0.f;
-  const float lse = g.lse[i], H = g.d_entropy ? g.entropy[i] : 0.f;
-  const bool zero = (dl == 0.f && dh == 0.f && dz == 0.f) || lse == -INFINITY;
-  for (int64_t j = threadIdx.x; j < V; j += kThreads) {
-    float d = 0.f;
-    if (!zero) {
-      const float lp = element<BF16>(row, j) * a.scale - lse;
-      const float p = expf(lp);
-      d = p * (dz - dl);
-      if (p != 0.f) d -= dh * (p * (lp + H));
-      if (j == y) d += dl;
-      d *= a.scale;
+  GradRow r;
+  r.A = a.scale * (dz - dl - (dh != 0.f ? dh * H : 0.f));
+  r.B = -a.scale * dh;
+  r.given = a.scale * dl;
+  r.y = y < a.vocab ? (int32_t)y : -1;
+  r.zero = (dl == 0.f && dh == 0.f && dz == 0.f) || empty;
+  return r;
+}
+
+// Natural logarithms of p below this have p = 0, and 0 * infinity is none.
+constexpr float kNoWeight = -150.f;
+
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+  uint32_t w;
+  asm("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(w) : "v"(lo), "v"(hi));
+  return w;
+}
+
+// 16 bytes at any element alignment: the rows of a gradient need not lie as
+// those of the logits do.
+struct __attribute__((packed, aligned(2))) Halves16 {
+  uint32_t w[4];
+};
+
+template <bool BF16>
+__device__ __forceinline__ void store_chunk(void* row, int32_t j, const float (&d)[kChunk<BF16>]) {
+  if constexpr (BF16) {
+    Halves16 h;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) h.w[k] = bf16_pair(d[2 * k], d[2 * k + 1]);
+    *reinterpret_cast<Halves16*>(static_cast<uint16_t*>(row) + j) = h;
+  } else {
+    Words16 w;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w.w[k] = __float_as_uint(d[k]);
+    *reinterpret_cast<Words16*>(static_cast<float*>(row) + j) = w;
+  }
+}
+
+template <bool BF16>
+__device__ __forceinline__ void store_element(void* row, int32_t j, float d) {
+  if constexpr (BF16)
+    static_cast<uint16_t*>(row)[j] = (uint16_t)bf16_pair(d, d);
+  else
+    static_cast<float*>(row)[j] = d;
+}
+
+constexpr int kGradThreads = 256;
+constexpr int kGradChunks = 4;  // of a thread, in flight
+
+// One workgroup for each run of kGradThreads * kGradChunks chunks of a row.
+template <bool BF16>
+__global__ void __launch_bounds__(kGradThreads)
+token_grad_kernel(TokenArgs a, TokenGrad g, int32_t tiles) {
+  constexpr int C = kChunk<BF16>;
+  const int64_t i = blockIdx.x / tiles;
+  const int32_t tile = blockIdx.x % tiles, V = (int32_t)a.vocab;
+  const void* row = row_at<BF16>(a.logits, i * a.stride);
+  void* to = const_cast<void*>(row_at<BF16>(g.grad, i * g.stride));
+  const RowShape<BF16> shape(row, V);
+  const Words16* body = shape.body(row);
+  const float lse = g.lse[i];
+  const GradRow r = grad_row(a, g, i, g.d_entropy ? g.entropy[i] : 0.f, lse == -INFINITY);
+  const auto one = [&](float x) {
+    const float lp = fmaf(x, a.scale, -lse);
+    const float p = __builtin_amdgcn_exp2f(lp * kLog2e);
+    return r.zero ? 0.f : p * fmaf(r.B, fmaxf(lp, kNoWeight), r.A);
+  };
+  Words16 raw[kGradChunks];
+  const int32_t k0 = tile * (kGradThreads * kGradChunks) + threadIdx.x;
+#pragma unroll
+  for (int u = 0; u < kGradChunks; ++u) {
+    raw[u] = Words16{{0, 0, 0, 0}};
+    if (k0 + u * kGradThreads < shape.chunks && !r.zero) raw[u] = body[k0 + u * kGradThreads];
+  }
+#pragma unroll
+  for (int u = 0; u < kGradChunks; ++u) {
+    const int32_t k = k0 + u * kGradThreads;
+    if (k >= shape.chunks) break;
+    const int32_t j = shape.head + k * C;
+    float x[C];
+    unpack<BF16>(raw[u], x);
+#pragma unroll
+    for (int q = 0; q < C; ++q) x[q] = one(x[q]);
+    if (r.y >= j && r.y < j + C && !r.zero) {
+#pragma unroll
+      for (int q = 0; q < C; ++q)
+        if (r.y == j + q) x[q] += r.given;
     }
-    if constexpr (BF16) {
-      const uint32_t b = __float_as_uint(d);
-      static_cast<uint16_t*>(to)[j] =
-          d != d ? 0x7FC0 : (uint16_t)((b + 0x7FFFu + ((b >> 16) & 1u)) >> 16);
-    } else {
-      static_cast<float*>(to)[j] = d;
+    store_chunk<BF16>(to, j, x);
+  }
+  if (tile == tiles - 1 && (int)threadIdx.x < shape.head + shape.tail) {
+    const int32_t j = shape.edge(threadIdx.x, V);
+    float d = r.zero ? 0.f : one(element<BF16>(row, j));
+    if (j == r.y && !r.zero) d += r.given;
+    store_element<BF16>(to, j, d);
+  }
+}
+
+// Scores and gradient in one pass: a workgroup holds a whole row, N chunks a
+// thread, in its registers as it lies in memory.
+template <bool BF16, int W, int N>
+__global__ void __launch_bounds__(W, N <= 8 ? 8 : 4)
+token_loss_kernel(TokenArgs a, TokenScores out, TokenGrad g) {
+  using S = Scorer<BF16, W>;
+  constexpr int C = S::C;
+  __shared__ float part_most[S::kWaves];
+  __shared__ float part_sum[2][S::kWaves];
+  const int64_t i = blockIdx.x;
+  const int32_t V = (int32_t)a.vocab;
+  const float c = a.scale * kLog2e;
+  const void* row = row_at<BF16>(a.logits, i * a.stride);
+  void* to = const_cast<void*>(row_at<BF16>(g.grad, i * g.stride));
+  const RowShape<BF16> shape(row, V);
+  const Words16* body = shape.body(row);
+  constexpr uint32_t low = BF16 ? 0xFF80FF80u : 0xFF800000u;  // -infinity
+  Words16 raw[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    raw[n] = Words16{{low, low, low, low}};
+    const int32_t k = n * W + threadIdx.x;
+    if (k < shape.chunks) raw[n] = body[k];
+  }
+  const bool edge = (int)threadIdx.x < shape.head + shape.tail;
+  const int32_t edge_j = edge ? shape.edge(threadIdx.x, V) : 0;
+  const float edge_x = edge ? element<BF16>(row, edge_j) : -INFINITY;
+  const int64_t y = a.targets ? a.targets[i] : -1;
+  const float given = y >= 0 && y < V ? element<BF16>(row, y) : 0.f;
+  float most = edge_x;
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    float x[C];
+    unpack<BF16>(raw[n], x);
+#pragma unroll
+    for (int q = 0; q < C; ++q) most = fmaxf(most, x[q]);
+  }
+  most = S::all_max(most, part_most);
+  const float from = most == -INFINITY ? 0.f : most;
+  Stats s{most, 0.f, 0.f};
+  const auto add = [&](float x) {
+    const float t = exponent(x, from, c);
+    const float e = __builtin_amdgcn_exp2f(t);
+    s.total += e;
+    s.spread = fmaf(e, fmaxf(t, kFarBelow), s.spread);
+  };
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    float x[C];
+    if constexpr (BF16) keep_packed(raw[n]);
+    unpack<BF16>(raw[n], x);
+#pragma unroll
+    for (int q = 0; q < C; ++q) add(x[q]);
+  }
+  add(edge_x);
+  s.total = lanes_reduce<64>(s.total, SumF());
+  s.spread = lanes_reduce<64>(s.spread, SumF());
+  if (threadIdx.x % kWave == 0) {
+    part_sum[0][threadIdx.x / kWave] = s.total;
+    part_sum[1][threadIdx.x / kWave] = s.spread;
+  }
+  __syncthreads();
+  s.total = s.spread = 0.f;
+#pragma unroll
+  for (int w = 0; w < S::kWaves; ++w) {
+    s.total += part_sum[0][w];
+    s.spread += part_sum[1][w];
+  }
+  const RowResult res = finish_row(a, out, i, s, y, given);
+  const float H = res.empty ? 0.f : res.log_total - s.spread * kLn2 / s.total;
+  const GradRow r = grad_row(a, g, i, H, res.empty);
+  const float log2_total = res.log_total * kLog2e;
+  const float B = r.B * kLn2;  // of logarithms to the base 2
+  const auto one = [&](float x) {
+    const float t = exponent(x, from, c) - log2_total;
+    const float p = __builtin_amdgcn_exp2f(t);
+    return r.zero ? 0.f : p * fmaf(B, fmaxf(t, kFarBelow), r.A);
+  };
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int32_t k = n * W + threadIdx.x;
+    if (k < shape.chunks) {
+      const int32_t j = shape.head + k * C;
+      float x[C];
+      if constexpr (BF16) keep_packed(raw[n]);
+      unpack<BF16>(raw[n], x);
+#pragma unroll
+      for (int q = 0; q < C; ++q) x[q] = one(x[q]);
+      if (r.y >= j && r.y < j + C && !r.zero) {
+#pragma unroll
+        for (int q = 0; q < C; ++q)
+          if (r.y == j + q) x[q] += r.given;
+      }
+      store_chunk<BF16>(to, j, x);
     }
+  }
+  if (edge) {
+    float d = one(edge_x);
+    if (edge_j == r.y && !r.zero) d += r.given;
+    store_element<BF16>(to, edge_j, d);
   }
 }
 
@@ -525,6 +715,31 @@ static int32_t row_pieces(const TokenArgs& a, int32_t threads) {
   return p < 1 ? 1 : (int32_t)p;
 }
 
+// Calls launch(args, outputs, gradient) for runs of at most kRowsPerLaunch rows.
+template <typename Launch>
+static void each_rows(const TokenArgs& a, const TokenScores& out, const TokenGrad& g,
+                      int64_t most, const Launch& launch) {
+  const int64_t bytes = a.bf16 ? 2 : 4;
+  for (int64_t lo = 0; lo < a.rows; lo += most) {
+    TokenArgs b = a;
+    TokenScores o = out;
+    TokenGrad h = g;
+    b.rows = a.rows - lo < most ? a.rows - lo : most;
+    b.logits = static_cast<const char*>(a.logits) + lo * a.stride * bytes;
+    if (b.targets) b.targets += lo;
+    for (float** p : {&o.logp, &o.entropy, &o.lse})
+      if (*p) *p += lo;
+    if (o.top_ids) {
+      o.top_ids += lo * a.top;
+      o.top_logp += lo * a.top;
+    }
+    for (const float** p : {&h.lse, &h.entropy, &h.d_logp, &h.d_entropy, &h.d_lse})
+      if (*p) *p += lo;
+    h.grad = static_cast<char*>(g.grad) + lo * g.stride * bytes;
+    launch(b, o, h);
+  }
+}
+
 hipError_t launch_token_score(const TokenArgs& a, const TokenScores& out, void* workspace,
                               hipStream_t stream) {
   if (a.rows <= 0) return hipSuccess;
@@ -534,31 +749,58 @@ hipError_t launch_token_score(const TokenArgs& a, const TokenScores& out, void* 
   const int32_t piece_chunks = (int32_t)((chunks + pieces - 1) / pieces);
   auto* parts = static_cast<TokenPart*>(workspace);
   auto* arrived = reinterpret_cast<uint32_t*>(parts + kSplitParts);
-  for (int64_t lo = 0; lo < a.rows; lo += kRowsPerLaunch) {
-    TokenArgs b = a;
-    TokenScores o = out;
-    b.rows = a.rows - lo < kRowsPerLaunch ? a.rows - lo : kRowsPerLaunch;
-    b.logits = static_cast<const char*>(a.logits) + lo * a.stride * (a.bf16 ? 2 : 4);
-    if (b.targets) b.targets += lo;
-    if (o.logp) o.logp += lo;
-    if (o.entropy) o.entropy += lo;
-    if (o.lse) o.lse += lo;
-    if (o.top_ids) {
-      o.top_ids += lo * a.top;
-      o.top_logp += lo * a.top;
-    }
+  each_rows(a, out, {}, kRowsPerLaunch, [&](const TokenArgs& b, const TokenScores& o,
+                                            const TokenGrad&) {
     hipLaunchKernelGGL(a.bf16 ? (token_score_kernel<true, W>) : (token_score_kernel<false, W>),
                        dim3((unsigned)(b.rows * pieces)), dim3(W), 0, stream, b, o, pieces,
                        piece_chunks, parts, arrived);
-  }
+  });
   return hipGetLastError();
 }
 
 hipError_t launch_token_grad(const TokenArgs& a, const TokenGrad& g, hipStream_t stream) {
   if (a.rows <= 0) return hipSuccess;
-  hipLaunchKernelGGL(a.bf16 ? token_grad_kernel<true> : token_grad_kernel<false>,
-                     dim3((unsigned)a.rows), dim3(kThreads), 0, stream, a, g);
+  const int64_t chunks = a.vocab / (a.bf16 ? 8 : 4);
+  const int32_t tiles = (int32_t)((chunks + kGradThreads * kGradChunks - 1) /
+                                  (kGradThreads * kGradChunks));
+  const int32_t least_one = tiles > 0 ? tiles : 1;
+  const int64_t most = (int64_t{1} << 23) / least_one > 0 ? (int64_t{1} << 23) / least_one : 1;
+  each_rows(a, {}, g, most, [&](const TokenArgs& b, const TokenScores&, const TokenGrad& h) {
+    hipLaunchKernelGGL(a.bf16 ? token_grad_kernel<true> : token_grad_kernel<false>,
+                       dim3((unsigned)(b.rows * least_one)), dim3(kGradThreads), 0, stream, b, h,
+                       least_one);
+  });
   return hipGetLastError();
+}
+
+bool launch_token_loss(const TokenArgs& a, const TokenScores& out, const TokenGrad& g,
+                       hipStream_t stream, hipError_t* e) {
+  *e = hipSuccess;
+  if (a.rows <= 0) return true;
+  const int64_t chunks = a.vocab / (a.bf16 ? 8 : 4);
+  bool found = true;
+  each_rows(a, out, g, kRowsPerLaunch, [&](const TokenArgs& b, const TokenScores& o,
+                                           const TokenGrad& h) {
+#define ARC_LOSS(WW, NN)                                                                        \
+  if (chunks <= (WW) * (NN)) {                                                                  \
+    hipLaunchKernelGGL(a.bf16 ? (token_loss_kernel<true, WW, NN>)                               \
+                              : (token_loss_kernel<false, WW, NN>),                             \
+                       dim3((unsigned)b.rows), dim3(WW), 0, stream, b, o, h);                   \
+  } else
+    ARC_LOSS(256, 1)
+    ARC_LOSS(256, 4)
+    ARC_LOSS(512, 4)
+    ARC_LOSS(512, 8)
+    ARC_LOSS(1024, 6)
+    ARC_LOSS(1024, 7)
+    ARC_LOSS(1024, 8)
+    ARC_LOSS(1024, 13)
+    ARC_LOSS(1024, 16)
+    found = false;
+#undef ARC_LOSS
+  });
+  *e = hipGetLastError();
+  return found;
 }
 
 }  // namespace arc

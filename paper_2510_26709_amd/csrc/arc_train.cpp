@@ -365,10 +365,15 @@ arc_status arc_tokens_loss(arc_tokens* c, int64_t rows, const void* logits, int6
                   {{d_logp, rows * 4}, {d_entropy, rows * 4}, {d_lse, rows * 4},
                    {grad, row_bytes(c, rows, grad_stride)}}))
     return fail(ARC_ERR_INVALID, "outputs must not overlap one another or the inputs");
-  if (rows > 0 && (lse == nullptr || entropy == nullptr))
-    return fail(ARC_ERR_INVALID, "lse and entropy are needed");
   const OnDevice here(c->device);
   const arc::TokenArgs a = token_args(c, rows, logits, stride, targets);
+  hipError_t e;
+  if (arc::launch_token_loss(a, out, g, c->stream, &e)) {
+    ARC_HIP(e, "token loss launch");
+    return ARC_OK;
+  }
+  if (lse == nullptr || entropy == nullptr)
+    return fail(ARC_ERR_INVALID, "lse and entropy are needed");
   ARC_HIP(arc::launch_token_score(a, out, c->workspace, c->stream), "token score launch");
   ARC_HIP(arc::launch_token_grad(a, g, c->stream), "token gradient launch");
   return ARC_OK;

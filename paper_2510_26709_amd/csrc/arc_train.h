@@ -37,6 +37,10 @@ struct TokenGrad {
 size_t token_workspace_bytes(int64_t vocab, int64_t max_rows);
 hipError_t launch_token_score(const TokenArgs& a, const TokenScores& out, void* workspace,
                               hipStream_t stream);
+// Both in one pass, where a workgroup can hold a row (false: it cannot, and
+// nothing was launched); g's lse and entropy are not read.
+bool launch_token_loss(const TokenArgs& a, const TokenScores& out, const TokenGrad& g,
+                       hipStream_t stream, hipError_t* e);
 hipError_t launch_token_grad(const TokenArgs& a, const TokenGrad& g, hipStream_t stream);
 
 // ---------------------------------------------------------------- optimizer
