@@ -165,12 +165,12 @@ __device__ __forceinline__ uint64_t dpp(uint64_t v) {
   return ((uint64_t)dpp<kCtrl>((uint32_t)(v >> 32)) << 32) | dpp<kCtrl>((uint32_t)v);
 }
 
-// op over runs of kLanes lanes (4, 8, 16) or the wave (64), on every lane of
+// op over runs of kLanes lanes (1, 2, 4, 8, 16) or the wave (64), on every lane of
 // them, in an order that is fixed.
 template <int kLanes, typename T, typename Op>
 __device__ __forceinline__ T lanes_reduce(T v, const Op& op) {
-  v = op(v, dpp<kDppXor1>(v));
-  v = op(v, dpp<kDppXor2>(v));
+  if constexpr (kLanes >= 2) v = op(v, dpp<kDppXor1>(v));
+  if constexpr (kLanes >= 4) v = op(v, dpp<kDppXor2>(v));
   if constexpr (kLanes >= 8) v = op(v, dpp<kDppHalfMirror>(v));
   if constexpr (kLanes >= 16) v = op(v, dpp<kDppMirror>(v));
   if constexpr (kLanes >= 64) {

@@ -4,6 +4,9 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+#include <type_traits>
+
 #include "arc_device.h"
 #include "arc_train.h"
 
@@ -14,7 +17,10 @@ constexpr int kMaxTop = 32;           // ARC_MAX_TOP
 constexpr int64_t kSplitRows = 1024;  // calls of more rows give each a workgroup
 constexpr int64_t kSplitParts = 4096;
 constexpr int64_t kRowsPerLaunch = 1 << 20;  // threads of a launch stay below 2^32
-constexpr int kScoreThreads = 512;
+constexpr int kSplitThreads = 512;
+// Chunks of a row up to which workgroups of 64, 256 and 512 threads take it
+// (above: 1024), without and with alternatives.
+constexpr int64_t kRowChunks[2][3] = {{700, 3000, 7000}, {1500, 3500, 12520}};
 
 // ---------------------------------------------------------------------------
 // A row is read in chunks of 16 bytes a lane, from its first whole word on (a
@@ -27,6 +33,14 @@ constexpr int kChunk = BF16 ? 8 : 4;
 struct __attribute__((packed, aligned(4))) Words16 {
   uint32_t w[4];
 };
+
+typedef uint32_t loose_u32x4_t __attribute__((ext_vector_type(4), aligned(2)));
+
+// Of what is read once.
+__device__ __forceinline__ Words16 stream_load16(const Words16* p) {
+  const u32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const loose_u32x4_t*>(p));
+  return Words16{{v.x, v.y, v.z, v.w}};
+}
 
 template <bool BF16>
 __device__ __forceinline__ void unpack(const Words16& r, float (&x)[kChunk<BF16>]) {
@@ -78,40 +92,48 @@ struct RowShape {
 
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 
-// Softmax statistics of part of a row relative to its largest logit `most`, in
-// powers of two: total = sum 2^t and spread = sum 2^t t for t = (x - most) c, c
-// = scale log2(e).  The difference is taken first: it is exact where it
-// matters, however large the logits are.
+// Softmax statistics of part of a row whose largest logit is `most`, in powers
+// of two: total = sum 2^t, spread = sum 2^t t for t = c x - R, c = scale
+// log2(e).  R is c most rounded, and t one fma: R need not be the exact
+// product, as what it lacks (`rest`, exactly known) is the same for all of the
+// part, and is made up for where parts are joined.
+//
+// Far from zero (|R| >= 2^31) neighbouring logits are 2^8 apart in t and more,
+// so that only those equal to `most` count: they are taken as 0 and all others
+// as -infinity, with R = 0 (far_logit()).
 struct Stats {
   float most, total, spread;
 };
 
-__device__ __forceinline__ float exponent(float x, float most, float c) { return (x - most) * c; }
+struct Reference {
+  float R, rest;
+  bool far;
+};
+
+__device__ __forceinline__ Reference reference(float most, float c) {
+  const float p = most == -INFINITY ? 0.f : most * c;  // nothing above -infinity: from 0
+  if (!(fabsf(p) < 0x1p31f)) return {0.f, 0.f, true};
+  return {p, most == -INFINITY ? 0.f : fmaf(most, c, -p), false};
+}
+
+// NaN stays NaN, and an infinite `most` becomes one.
+__device__ __forceinline__ float far_logit(float x, float most) {
+  return x < most ? -INFINITY : x - most;
+}
+
+__device__ __forceinline__ float exponent(float x, float most, const Reference& r, float c) {
+  return r.far ? (x - most) * c : fmaf(x, c, -r.R);
+}
 
 // t below this adds nothing to a spread, and 0 * infinity would.
-constexpr float kFarBelow = -200.f;
+constexpr float kFarBelow = -300.f;
 
-// The statistics relative to `most` instead (not below their own, -infinity
-// only with theirs).
-__device__ __forceinline__ Stats moved(Stats s, float most, float c) {
+// s relative to `most` (not below s.most) instead.
+__device__ __forceinline__ Stats moved(const Stats& s, float most, const Reference& to, float c) {
   if (s.most == -INFINITY) return {most, s.total, 0.f};  // total: 0, or a NaN to keep
-  const float t = exponent(s.most, most, c);
+  const float t = (s.most - most) * c - reference(s.most, c).rest + to.rest;
   const float e = __builtin_amdgcn_exp2f(t);
   return {most, e * s.total, e * (s.spread + fmaxf(t, kFarBelow) * s.total)};
-}
-
-// A larger key is a larger logit, or the same logit of a lower token.
-__device__ __forceinline__ uint64_t rank_key(float x, int32_t j) {
-  const uint32_t b = __float_as_uint(x + 0.0f);
-  const uint32_t up = b ^ ((b >> 31) ? 0xFFFFFFFFu : 0x80000000u);
-  return ((uint64_t)up << 32) | (0xFFFFFFFFu - (uint32_t)j);
-}
-__device__ __forceinline__ int32_t key_token(uint64_t key) {
-  return (int32_t)(0xFFFFFFFFu - (uint32_t)key);
-}
-__device__ __forceinline__ float key_logit(uint64_t key) {
-  const uint32_t up = (uint32_t)(key >> 32);
-  return __uint_as_float(up ^ ((up >> 31) ? 0x80000000u : 0xFFFFFFFFu));
 }
 
 struct MaxF {
@@ -143,21 +165,62 @@ __device__ __forceinline__ T share_load(const T* p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// Alternatives.  Every thread knows the largest logit of its own chunks and
-// the first chunk that holds it; the threads' order by (that logit, that
-// chunk) is an order of disjoint runs of tokens, so the top k elements lie in
-// the chunks of the first k threads of it.  The threads form 64 groups, a
-// bound `tau` is the k-th largest of the groups' first threads, and only the
-// threads from tau on have their chunks read once more (from the cache), by
-// the whole workgroup.  A row of noise has about k log(64 / (64 - k)) such
-// threads.  What reaches tau there, some dozens, is ordered by counting.
-constexpr int kCandidates = 2048;
+// Alternatives.  Every thread keeps the largest logit of each run of its chunks
+// (at most kRuns runs).  The threads form 64 groups, and the k-th largest of
+// the groups' largest logits is a bound `tau` that at least k elements reach.
+// Only runs whose largest one reaches it are read once more (from the cache),
+// by the whole workgroup; in a row of noise they are about 64 log(64 / (64 -
+// k)).  What reaches tau there, some dozens, is ordered by counting.
+template <int W>
+constexpr int kRuns = W == 64 ? 4 : 8;
+template <int W>
+constexpr int kListed = W == 64 ? 256 : 512;
+template <int W>
+constexpr int kCandidates = W == 64 ? 256 : 512;
+template <int W>
 struct TopShared {
-  uint64_t group[64];
-  uint64_t tau;
-  int32_t threads, found;
-  uint64_t found_keys[kCandidates];
+  float group[64];
+  float run_most[kRuns<W>][W];
+  int32_t listed, found;
+  int32_t list[kListed<W>];
+  uint64_t best[16];
+  uint64_t found_keys[kCandidates<W>];  // 0 behind the last
 };
+
+// The order of logits as unsigned words, and back.
+__device__ __forceinline__ uint32_t order_word(float x) {
+  const uint32_t b = __float_as_uint(x + 0.0f);
+  return b ^ ((b >> 31) ? 0xFFFFFFFFu : 0x80000000u);
+}
+__device__ __forceinline__ float word_logit(uint32_t w) {
+  return __uint_as_float(w ^ ((w >> 31) ? 0x80000000u : 0xFFFFFFFFu));
+}
+
+// A larger key is a larger logit, or the same logit of a lower token.
+__device__ __forceinline__ uint64_t rank_key(float x, int32_t j) {
+  return ((uint64_t)order_word(x) << 32) | (0xFFFFFFFFu - (uint32_t)j);
+}
+__device__ __forceinline__ int32_t key_token(uint64_t key) {
+  return (int32_t)(0xFFFFFFFFu - (uint32_t)key);
+}
+__device__ __forceinline__ float key_logit(uint64_t key) {
+  return word_logit((uint32_t)(key >> 32));
+}
+
+// A bound that at least k of the wave's 64 values reach, and k + 3 at most
+// where that can be: bits of the k-th largest from the top, counting.
+__device__ __forceinline__ float kth_bound(float v, int32_t k) {
+  const uint32_t key = order_word(v);
+  uint32_t bound = 0;
+#pragma unroll 1
+  for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
+    const int32_t n = __popcll(__ballot(key >= (bound | bit)));
+    if (n >= k) bound |= bit;
+    if (n >= k && n <= k + 3) break;
+  }
+  const uint32_t nothing = 0x007FFFFFu;  // -infinity's
+  return bound <= nothing ? -INFINITY : word_logit(bound);
+}
 
 template <bool BF16, int W>
 struct Scorer {
@@ -166,63 +229,83 @@ struct Scorer {
   static constexpr int kWaves = W / kWave;
   static constexpr int kLanes = W / 64;  // of a group
 
-  // Statistics of chunks [first, end) of the row, a thread's share, with the
-  // token at which its largest logit's chunk (or single element) begins; the
-  // single elements are the last piece's.
-  static __device__ __forceinline__ Stats share(const Words16* body, int32_t head, int32_t first,
-                                                int32_t end, float c, int32_t* at) {
+  // Statistics of a thread's share of chunks [first, end); with TOP, the largest
+  // logit of each run of `run_batches` batches of U chunks, and their number
+  // (chunks may then be read again, and should stay in the cache).
+  template <bool TOP>
+  static __device__ __forceinline__ Stats share(const Words16* body, int32_t first, int32_t end,
+                                                float c, int32_t run_batches,
+                                                float (*run_most)[W], int32_t* runs) {
     Stats s{-INFINITY, 0.f, 0.f};
-    int32_t best = first + (int)threadIdx.x < end ? head + (first + (int)threadIdx.x) * C
-                                                  : INT32_MAX;
-    for (int32_t k = first + threadIdx.x; k < end; k += W * U) {
+    float run = -INFINITY;
+    int32_t batch = 0, done = 0;
+    // ALL: every thread has all U chunks.  The others, at the end, would cost
+    // as much arithmetic as chunks that are there, if they were not left out.
+    const auto take = [&](int32_t k, auto all) {
+      constexpr bool ALL = decltype(all)::value;
       Words16 raw[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const uint32_t low = BF16 ? 0xFF80FF80u : 0xFF800000u;  // -infinity
-        raw[u] = Words16{{low, low, low, low}};
-        if (k + u * W < end) raw[u] = body[k + u * W];
+        if (!ALL) raw[u] = Words16{{low, low, low, low}};
+        if (ALL || k + u * W < end)
+          raw[u] = TOP ? body[k + u * W] : stream_load16(body + k + u * W);
       }
       float x[U][C];
-      float most = s.most;
+      float here = -INFINITY;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         unpack<BF16>(raw[u], x[u]);
-        float m = x[u][0];
 #pragma unroll
-        for (int q = 1; q < C; ++q) m = fmaxf(m, x[u][q]);
-        if (m > most) {
-          most = m;
-          best = head + (k + u * W) * C;
+        for (int q = 0; q < C; ++q) here = fmaxf(here, x[u][q]);
+      }
+      if constexpr (TOP) {
+        run = fmaxf(run, here);
+        if (++batch == run_batches) {
+          run_most[done++][threadIdx.x] = run;
+          run = -INFINITY;
+          batch = 0;
         }
       }
-      // with nothing above -infinity so far, distances are taken from 0
-      const float from = most == -INFINITY ? 0.f : most;
-      s = moved(s, from, c);
+      const float most = fmaxf(s.most, here);
+      const Reference ref = reference(most, c);
+      s = moved(s, most, ref, c);
+      if (ref.far) {
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int q = 0; q < C; ++q) x[u][q] = far_logit(x[u][q], most);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (!ALL && k + u * W >= end) break;
 #pragma unroll
         for (int q = 0; q < C; ++q) {
-          const float t = exponent(x[u][q], from, c);
+          const float t = fmaf(x[u][q], c, -ref.R);
           const float e = __builtin_amdgcn_exp2f(t);
           s.total += e;
           s.spread = fmaf(e, fmaxf(t, kFarBelow), s.spread);
         }
-      s.most = most;
+      }
+    };
+    int32_t k = first + threadIdx.x;
+    const int32_t whole = (end - first) / (W * U);
+    for (int32_t q = 0; q < whole; ++q, k += W * U) take(k, std::true_type());
+    if (k < end) take(k, std::false_type());
+    if constexpr (TOP) {
+      if (batch > 0) run_most[done++][threadIdx.x] = run;
+      *runs = done;
     }
-    *at = best;
     return s;
   }
 
-  static __device__ __forceinline__ void add_edge(float x, int32_t j, float c, Stats* s,
-                                                  int32_t* at) {
-    if (*at == INT32_MAX || x > s->most || (x == s->most && j < *at)) *at = j;
+  static __device__ __forceinline__ void add_edge(float x, float c, Stats* s) {
     const float most = fmaxf(s->most, x);
-    const float from = most == -INFINITY ? 0.f : most;
-    *s = moved(*s, from, c);
-    const float t = exponent(x, from, c), e = __builtin_amdgcn_exp2f(t);
+    const Reference ref = reference(most, c);
+    *s = moved(*s, most, ref, c);
+    const float t = exponent(x, most, ref, c), e = __builtin_amdgcn_exp2f(t);
     s->total += e;
     s->spread = fmaf(e, fmaxf(t, kFarBelow), s->spread);
-    s->most = most;
   }
 
   // Over the workgroup, on every thread.
@@ -238,23 +321,30 @@ struct Scorer {
 
   // The keys found are ordered by counting, and the first k written.
   template <typename Write>
-  static __device__ __forceinline__ void order(const TopShared& sh, int32_t n, int32_t k,
+  static __device__ __forceinline__ void order(const TopShared<W>& sh, int32_t n, int32_t k,
                                                const Write& write) {
     for (int32_t i = threadIdx.x; i < n; i += W) {
       const uint64_t key = sh.found_keys[i];
       int32_t rank = 0;
-      for (int32_t q = 0; q < n; ++q) rank += sh.found_keys[q] > key;
+      for (int32_t q = 0; q < n; q += 8) {  // eight reads at a time; behind the n keys are 0s
+#pragma unroll
+        for (int u = 0; u < 8; ++u) rank += sh.found_keys[q + u] > key;
+      }
       if (rank < k) write(rank, key);
     }
   }
 };
 
-// Writes a row's results; `order` holds its keys.
+// A row's results from its statistics.
 struct RowResult {
-  float most, scale, log_total;
+  float most, scale, c, log_total;
+  Reference ref;
   bool empty, none;
   __device__ float logp(float x) const {
-    return none ? NAN : empty ? -INFINITY : (x - most) * scale - log_total;
+    const float t = exponent(x, most, ref, c);
+    // the lowest values' t can be beyond the type where their z is not
+    const float z = t > -0x1p31f ? t * kLn2 : (x - most) * scale;
+    return none ? NAN : empty ? -INFINITY : z - log_total;
   }
 };
 
@@ -263,9 +353,11 @@ __device__ __forceinline__ RowResult finish_row(const TokenArgs& a, const TokenS
   RowResult r;
   r.most = s.most;
   r.scale = a.scale;
+  r.c = a.scale * kLog2e;
+  r.ref = reference(s.most, r.c);
   r.empty = s.total == 0.f;
   r.log_total = logf(s.total);
-  const float lse = r.empty ? -INFINITY : s.most * a.scale + r.log_total;
+  const float lse = r.empty ? -INFINITY : s.most * a.scale + (r.log_total - r.ref.rest * kLn2);
   r.none = lse != lse;
   if (threadIdx.x == 0) {
     if (out.lse) out.lse[i] = lse;
@@ -275,8 +367,8 @@ __device__ __forceinline__ RowResult finish_row(const TokenArgs& a, const TokenS
   return r;
 }
 
-template <bool BF16, int W>
-__global__ void __launch_bounds__(W)
+template <bool BF16, int W, bool TOP>
+__global__ void __launch_bounds__(W, 8)
 token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_chunks,
                    TokenPart* __restrict__ parts, uint32_t* __restrict__ arrived) {
   using S = Scorer<BF16, W>;
@@ -284,52 +376,52 @@ token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_c
   __shared__ float part_sum[2][S::kWaves];
   __shared__ float given;
   __shared__ int32_t last;
-  __shared__ TopShared sh;
+  __shared__ TopShared<W> sh;
   const int64_t i = pieces == 1 ? blockIdx.x : blockIdx.x / pieces;
   const int32_t piece = pieces == 1 ? 0 : blockIdx.x % pieces;
-  const int32_t V = (int32_t)a.vocab, k = out.top_ids ? a.top : 0;
+  const int32_t V = (int32_t)a.vocab, k = TOP ? a.top : 0;
   const float c = a.scale * kLog2e;
   const void* row = row_at<BF16>(a.logits, i * a.stride);
   const RowShape<BF16> shape(row, V);
   const Words16* body = shape.body(row);
   const int32_t first = piece * piece_chunks;
   const int32_t end = min(shape.chunks, first + piece_chunks);
-  const bool edges = piece == pieces - 1;
+  const bool edges = piece == pieces - 1;  // single elements are the last piece's
   const int64_t y = out.logp ? a.targets[i] : -1;
   if (threadIdx.x == W - 1) given = y >= 0 && y < V ? element<BF16>(row, y) : 0.f;
 
-  int32_t at;
-  Stats s = S::share(body, shape.head, first, end, c, &at);
-  if (edges && (int)threadIdx.x < shape.head + shape.tail) {
-    const int32_t j = shape.edge(threadIdx.x, V);
-    S::add_edge(element<BF16>(row, j), j, c, &s, &at);
-  }
-  const uint64_t mine = at == INT32_MAX ? 0 : rank_key(s.most, at);
-  if (k) {
-    const uint64_t g = lanes_reduce<S::kLanes>(mine, MaxKey());
+  // Batches of a run, so that a thread has kRuns at most.
+  constexpr int32_t kMost = kRuns<W> * W * S::U;
+  const int32_t run_batches = max(1, (end - first + kMost - 1) / kMost);
+  int32_t runs = 0;
+  Stats s = S::template share<TOP>(body, first, end, c, run_batches,
+                                   sh.run_most, &runs);
+  if (edges && (int)threadIdx.x < shape.head + shape.tail)
+    S::add_edge(element<BF16>(row, shape.edge(threadIdx.x, V)), c, &s);
+  if constexpr (TOP) {
+    const float g = lanes_reduce<S::kLanes>(s.most, MaxF());
     if (threadIdx.x % S::kLanes == 0) sh.group[threadIdx.x / S::kLanes] = g;
-    if (threadIdx.x == 0) {
-      sh.tau = 0;
-      sh.threads = sh.found = 0;
-    }
+    if (threadIdx.x == 0) sh.listed = sh.found = 0;
+#pragma unroll
+    for (int q = 0; q < kCandidates<W>; q += W)
+      if (q + (int)threadIdx.x < kCandidates<W>) sh.found_keys[q + threadIdx.x] = 0;
   }
   const float most = S::all_max(s.most, part_most);
-  s = moved(s, most == -INFINITY ? 0.f : most, c);
+  s = moved(s, most, reference(most, c), c);
   s.total = lanes_reduce<64>(s.total, SumF());
   s.spread = lanes_reduce<64>(s.spread, SumF());
   if (threadIdx.x % kWave == 0) {
     part_sum[0][threadIdx.x / kWave] = s.total;
     part_sum[1][threadIdx.x / kWave] = s.spread;
   }
-  if (k) {  // the group whose rank is k - 1 sets the bound
-    const uint64_t key = sh.group[threadIdx.x / S::kLanes];
-    uint32_t rank = 0;
-#pragma unroll
-    for (int q = 0; q < 64 / S::kLanes; ++q)
-      rank += sh.group[q * S::kLanes + threadIdx.x % S::kLanes] > key;
-    rank = lanes_reduce<S::kLanes>(rank, [](uint32_t p, uint32_t q) { return p + q; });
-    if (rank == (uint32_t)(k - 1) && threadIdx.x % S::kLanes == 0 && key != 0)
-      sh.tau = key - (S::C - 1);  // a run's largest element may be its last
+  float tau = 0.f;
+  if constexpr (TOP) {
+    tau = kth_bound(sh.group[threadIdx.x % kWave], k);
+    for (int32_t r = 0; r < runs; ++r)
+      if (sh.run_most[r][threadIdx.x] >= tau) {
+        const int32_t n = atomicAdd(&sh.listed, 1);
+        if (n < kListed<W>) sh.list[n] = r * W + threadIdx.x;
+      }
   }
   __syncthreads();
   s = {most, 0.f, 0.f};
@@ -338,23 +430,18 @@ token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_c
     s.total += part_sum[0][w];
     s.spread += part_sum[1][w];
   }
-  bool overflow = false;
-  if (k) {
-    const uint64_t tau = sh.tau;
-    __shared__ int32_t list[W];
-    if (mine != 0 && mine >= tau) list[atomicAdd(&sh.threads, 1)] = threadIdx.x;
-    __syncthreads();
-    const int32_t threads = sh.threads;
-    const int32_t each = (end - first + W - 1) / W;  // chunks of a thread, at most
+  if constexpr (TOP) {
+    const int32_t each = run_batches * S::U;  // chunks of a run, at most
+    const int32_t items = sh.listed <= kListed<W> ? sh.listed * each : 0;
     const auto found = [&](float x, int32_t j) {
-      const uint64_t key = rank_key(x, j);
-      if (key >= tau) {
+      if (x >= tau) {
         const int32_t n = atomicAdd(&sh.found, 1);
-        if (n < kCandidates) sh.found_keys[n] = key;
+        if (n < kCandidates<W>) sh.found_keys[n] = rank_key(x, j);
       }
     };
-    for (int32_t q = threadIdx.x; q < threads * each; q += W) {
-      const int32_t chunk = first + list[q / each] + (q % each) * W;
+    for (int32_t q = threadIdx.x; q < items; q += W) {
+      const int32_t of = sh.list[q / each], r = of / W;
+      const int32_t chunk = first + of % W + (r * each + q % each) * W;
       if (chunk >= end) continue;
       float x[S::C];
       unpack<BF16>(body[chunk], x);
@@ -366,11 +453,12 @@ token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_c
       found(element<BF16>(row, j), j);
     }
     __syncthreads();
-    overflow = sh.found > kCandidates;
   }
-  const int32_t n = k ? sh.found : 0;
+  const int32_t n = TOP ? sh.found : 0;
+  const bool overflow = TOP && (n > kCandidates<W> || sh.listed > kListed<W>);
 
-  // Too many for the list (the largest logits sit in few threads' chunks): the
+  // Too many for the list (many equal ones, or the largest sit in few threads'
+  // chunks): the
   // row's keys one after the other, each the largest below the one before.
   const auto one_by_one = [&](const auto& write) {
     uint64_t before = ~0ull;
@@ -392,10 +480,10 @@ token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_c
       }
       key = lanes_reduce<64>(key, MaxKey());
       __syncthreads();
-      if (threadIdx.x % kWave == 0) sh.group[threadIdx.x / kWave] = key;
+      if (threadIdx.x % kWave == 0) sh.best[threadIdx.x / kWave] = key;
       __syncthreads();
-      key = sh.group[0];
-      for (int w = 1; w < S::kWaves; ++w) key = MaxKey()(key, sh.group[w]);
+      key = sh.best[0];
+      for (int w = 1; w < S::kWaves; ++w) key = MaxKey()(key, sh.best[w]);
       if (threadIdx.x == 0) write(r, key);
       before = key;
     }
@@ -452,18 +540,19 @@ token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_c
   if (lane < pieces)
     s = {share_load(&of[lane].most), share_load(&of[lane].total), share_load(&of[lane].spread)};
   const float pm = lanes_reduce<64>(s.most, MaxF());
-  s = moved(s, pm == -INFINITY ? 0.f : pm, c);
+  s = moved(s, pm, reference(pm, c), c);
   s = {pm, lanes_reduce<64>(s.total, SumF()), lanes_reduce<64>(s.spread, SumF())};
   const RowResult r = finish_row(a, out, i, s, y, given);
   if (!k) return;
   // Each piece's k-th key is a bound for the row's.
-  uint64_t tau = lane < pieces ? share_load(&of[lane].top[k - 1]) : 0;
-  tau = lanes_reduce<64>(tau, MaxKey());
+  uint64_t least = lane < pieces ? share_load(&of[lane].top[k - 1]) : 0;
+  least = lanes_reduce<64>(least, MaxKey());
   if (threadIdx.x == 0) sh.found = 0;
+  for (int q = threadIdx.x; q < kCandidates<W>; q += W) sh.found_keys[q] = 0;
   __syncthreads();
-  for (int32_t q = threadIdx.x; q < pieces * k; q += W) {
+  for (int32_t q = threadIdx.x; q < pieces * k; q += W) {  // at most kCandidates
     const uint64_t key = share_load(&of[q / k].top[q % k]);
-    if (key != 0 && key >= tau) sh.found_keys[atomicAdd(&sh.found, 1)] = key;
+    if (key != 0 && key >= least) sh.found_keys[atomicAdd(&sh.found, 1)] = key;
   }
   __syncthreads();
   const auto write = [&](int32_t rank, uint64_t key) {
@@ -497,8 +586,8 @@ __device__ __forceinline__ GradRow grad_row(const TokenArgs& a, const TokenGrad&
   r.A = a.scale * (dz - dl - (dh != 0.f ? dh * H : 0.f));
   r.B = -a.scale * dh;
   r.given = a.scale * dl;
-  r.y = y < a.vocab ? (int32_t)y : -1;
   r.zero = (dl == 0.f && dh == 0.f && dz == 0.f) || empty;
+  r.y = y < a.vocab && !r.zero ? (int32_t)y : -1;
   return r;
 }
 
@@ -511,25 +600,26 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   return w;
 }
 
-// 16 bytes at any element alignment: the rows of a gradient need not lie as
-// those of the logits do.
-struct __attribute__((packed, aligned(2))) Halves16 {
-  uint32_t w[4];
-};
+// 16 bytes at any element alignment (the rows of a gradient need not lie as
+// those of the logits do), read again by later launches at the earliest.
+__device__ __forceinline__ void stream_store16(void* p, const uint32_t (&w)[4]) {
+  const u32x4_t v = {w[0], w[1], w[2], w[3]};
+  __builtin_nontemporal_store(v, reinterpret_cast<loose_u32x4_t*>(p));
+}
+
+template <bool BF16>
+__device__ __forceinline__ Words16 pack(const float (&d)[kChunk<BF16>]) {
+  Words16 w;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    w.w[k] = BF16 ? bf16_pair(d[BF16 ? 2 * k : 0], d[BF16 ? 2 * k + 1 : 0])
+                  : __float_as_uint(d[k]);
+  return w;
+}
 
 template <bool BF16>
 __device__ __forceinline__ void store_chunk(void* row, int32_t j, const float (&d)[kChunk<BF16>]) {
-  if constexpr (BF16) {
-    Halves16 h;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) h.w[k] = bf16_pair(d[2 * k], d[2 * k + 1]);
-    *reinterpret_cast<Halves16*>(static_cast<uint16_t*>(row) + j) = h;
-  } else {
-    Words16 w;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) w.w[k] = __float_as_uint(d[k]);
-    *reinterpret_cast<Words16*>(static_cast<float*>(row) + j) = w;
-  }
+  stream_store16(static_cast<char*>(row) + (int64_t)j * (BF16 ? 2 : 4), pack<BF16>(d).w);
 }
 
 template <bool BF16>
@@ -566,7 +656,7 @@ token_grad_kernel(TokenArgs a, TokenGrad g, int32_t tiles) {
 #pragma unroll
   for (int u = 0; u < kGradChunks; ++u) {
     raw[u] = Words16{{0, 0, 0, 0}};
-    if (k0 + u * kGradThreads < shape.chunks && !r.zero) raw[u] = body[k0 + u * kGradThreads];
+    if (k0 + u * kGradThreads < shape.chunks && !r.zero) raw[u] = stream_load16(body + k0 + u * kGradThreads);
   }
 #pragma unroll
   for (int u = 0; u < kGradChunks; ++u) {
@@ -577,7 +667,7 @@ token_grad_kernel(TokenArgs a, TokenGrad g, int32_t tiles) {
     unpack<BF16>(raw[u], x);
 #pragma unroll
     for (int q = 0; q < C; ++q) x[q] = one(x[q]);
-    if (r.y >= j && r.y < j + C && !r.zero) {
+    if (r.y >= j && r.y < j + C) {
 #pragma unroll
       for (int q = 0; q < C; ++q)
         if (r.y == j + q) x[q] += r.given;
@@ -587,7 +677,7 @@ token_grad_kernel(TokenArgs a, TokenGrad g, int32_t tiles) {
   if (tile == tiles - 1 && (int)threadIdx.x < shape.head + shape.tail) {
     const int32_t j = shape.edge(threadIdx.x, V);
     float d = r.zero ? 0.f : one(element<BF16>(row, j));
-    if (j == r.y && !r.zero) d += r.given;
+    if (j == r.y) d += r.given;
     store_element<BF16>(to, j, d);
   }
 }
@@ -614,14 +704,14 @@ token_loss_kernel(TokenArgs a, TokenScores out, TokenGrad g) {
   for (int n = 0; n < N; ++n) {
     raw[n] = Words16{{low, low, low, low}};
     const int32_t k = n * W + threadIdx.x;
-    if (k < shape.chunks) raw[n] = body[k];
+    if (k < shape.chunks) raw[n] = stream_load16(body + k);
   }
   const bool edge = (int)threadIdx.x < shape.head + shape.tail;
   const int32_t edge_j = edge ? shape.edge(threadIdx.x, V) : 0;
-  const float edge_x = edge ? element<BF16>(row, edge_j) : -INFINITY;
+  const float edge_logit = edge ? element<BF16>(row, edge_j) : -INFINITY;
   const int64_t y = a.targets ? a.targets[i] : -1;
   const float given = y >= 0 && y < V ? element<BF16>(row, y) : 0.f;
-  float most = edge_x;
+  float most = edge_logit;
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     float x[C];
@@ -630,21 +720,36 @@ token_loss_kernel(TokenArgs a, TokenScores out, TokenGrad g) {
     for (int q = 0; q < C; ++q) most = fmaxf(most, x[q]);
   }
   most = S::all_max(most, part_most);
-  const float from = most == -INFINITY ? 0.f : most;
+  const Reference ref = reference(most, c);
+  float edge_x = edge_logit;
+  if (ref.far) {  // the whole row alike
+    edge_x = far_logit(edge_x, most);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      keep_packed(raw[n]);
+      float x[C];
+      unpack<BF16>(raw[n], x);
+#pragma unroll
+      for (int q = 0; q < C; ++q) x[q] = far_logit(x[q], most);
+      raw[n] = pack<BF16>(x);
+    }
+  }
   Stats s{most, 0.f, 0.f};
   const auto add = [&](float x) {
-    const float t = exponent(x, from, c);
+    const float t = fmaf(x, c, -ref.R);
     const float e = __builtin_amdgcn_exp2f(t);
     s.total += e;
     s.spread = fmaf(e, fmaxf(t, kFarBelow), s.spread);
   };
 #pragma unroll
   for (int n = 0; n < N; ++n) {
+    if (n * W + (int)threadIdx.x >= shape.chunks) break;
     float x[C];
     if constexpr (BF16) keep_packed(raw[n]);
     unpack<BF16>(raw[n], x);
 #pragma unroll
     for (int q = 0; q < C; ++q) add(x[q]);
+    __builtin_amdgcn_sched_barrier(0);  // one chunk's values at a time in registers
   }
   add(edge_x);
   s.total = lanes_reduce<64>(s.total, SumF());
@@ -663,35 +768,44 @@ token_loss_kernel(TokenArgs a, TokenScores out, TokenGrad g) {
   const RowResult res = finish_row(a, out, i, s, y, given);
   const float H = res.empty ? 0.f : res.log_total - s.spread * kLn2 / s.total;
   const GradRow r = grad_row(a, g, i, H, res.empty);
-  const float log2_total = res.log_total * kLog2e;
+  const float shift = ref.R + res.log_total * kLog2e;
   const float B = r.B * kLn2;  // of logarithms to the base 2
-  const auto one = [&](float x) {
-    const float t = exponent(x, from, c) - log2_total;
-    const float p = __builtin_amdgcn_exp2f(t);
-    return r.zero ? 0.f : p * fmaf(B, fmaxf(t, kFarBelow), r.A);
-  };
+  // A row's gradient is zero, or p A, or p (A + B t): 1, 9.5 or 11.5 operations an
+  // element beside the unpacking, and the row's whole workgroup does one of them.
+  const auto emit = [&](const auto& one) {
+    int32_t thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));  // chunk numbers are made anew, not kept in registers
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const int32_t k = n * W + threadIdx.x;
-    if (k < shape.chunks) {
-      const int32_t j = shape.head + k * C;
-      float x[C];
-      if constexpr (BF16) keep_packed(raw[n]);
-      unpack<BF16>(raw[n], x);
+    for (int n = 0; n < N; ++n) {
+      const int32_t k = n * W + thread;
+      if (k < shape.chunks) {
+        const int32_t j = shape.head + k * C;
+        float x[C];
+        if constexpr (BF16) keep_packed(raw[n]);
+        unpack<BF16>(raw[n], x);
 #pragma unroll
-      for (int q = 0; q < C; ++q) x[q] = one(x[q]);
-      if (r.y >= j && r.y < j + C && !r.zero) {
+        for (int q = 0; q < C; ++q) x[q] = one(x[q]);
+        if (r.y >= j && r.y < j + C) {
 #pragma unroll
-        for (int q = 0; q < C; ++q)
-          if (r.y == j + q) x[q] += r.given;
+          for (int q = 0; q < C; ++q)
+            if (r.y == j + q) x[q] += r.given;
+        }
+        store_chunk<BF16>(to, j, x);
       }
-      store_chunk<BF16>(to, j, x);
+      __builtin_amdgcn_sched_barrier(0);
     }
-  }
-  if (edge) {
-    float d = one(edge_x);
-    if (edge_j == r.y && !r.zero) d += r.given;
-    store_element<BF16>(to, edge_j, d);
+    if (edge) store_element<BF16>(to, edge_j, one(edge_x) + (edge_j == r.y ? r.given : 0.f));
+  };
+  const auto log2_p = [&](float x) { return fmaf(x, c, -shift); };
+  if (r.zero) {
+    emit([](float) { return 0.f; });
+  } else if (B == 0.f) {
+    emit([&](float x) { return __builtin_amdgcn_exp2f(log2_p(x)) * r.A; });
+  } else {
+    emit([&](float x) {
+      const float t = log2_p(x);
+      return __builtin_amdgcn_exp2f(t) * fmaf(B, fmaxf(t, kFarBelow), r.A);
+    });
   }
 }
 
@@ -703,16 +817,13 @@ size_t token_workspace_bytes(int64_t vocab, int64_t max_rows) {
   return (size_t)(kSplitParts * sizeof(TokenPart) + rows * sizeof(uint32_t));
 }
 
-// Pieces of a row.
-static int32_t row_pieces(const TokenArgs& a, int32_t threads) {
-  const int64_t chunks = a.vocab / (a.bf16 ? 8 : 4);
-  if (a.rows > kSplitRows) return 1;
-  int64_t p = (chunks + threads * 2 - 1) / (threads * 2);
-  p = p < 64 ? p : 64;
-  const int64_t most = 1024 / a.rows;
-  p = p < most ? p : most;
-  p = p < kSplitParts / a.rows ? p : kSplitParts / a.rows;
-  return p < 1 ? 1 : (int32_t)p;
+// Pieces of a row of that many chunks, for few rows.
+static int32_t row_pieces(int64_t rows, int64_t chunks, int32_t top) {
+  if (rows > kSplitRows) return 1;
+  int64_t p = (chunks + kSplitThreads * 4 - 1) / (kSplitThreads * 4);  // a batch a thread
+  p = std::min<int64_t>({p, 64, 1024 / rows, kSplitParts / rows});
+  if (top > 0) p = std::min<int64_t>(p, kCandidates<kSplitThreads> / top);
+  return static_cast<int32_t>(std::max<int64_t>(p, 1));
 }
 
 // Calls launch(args, outputs, gradient) for runs of at most kRowsPerLaunch rows.
@@ -740,20 +851,38 @@ static void each_rows(const TokenArgs& a, const TokenScores& out, const TokenGra
   }
 }
 
+template <int W>
+static void launch_score(const TokenArgs& a, const TokenScores& o, int32_t pieces, int64_t chunks,
+                         void* workspace, hipStream_t stream) {
+  const auto piece_chunks = static_cast<int32_t>((chunks + pieces - 1) / pieces);
+  auto* parts = static_cast<TokenPart*>(workspace);
+  auto* arrived = reinterpret_cast<uint32_t*>(parts + kSplitParts);
+  const auto kernel =
+      o.top_ids && a.top > 0
+          ? (a.bf16 ? token_score_kernel<true, W, true> : token_score_kernel<false, W, true>)
+          : (a.bf16 ? token_score_kernel<true, W, false> : token_score_kernel<false, W, false>);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(a.rows * pieces)), dim3(W), 0, stream, a, o, pieces,
+                     piece_chunks, parts, arrived);
+}
+
 hipError_t launch_token_score(const TokenArgs& a, const TokenScores& out, void* workspace,
                               hipStream_t stream) {
   if (a.rows <= 0) return hipSuccess;
-  constexpr int W = kScoreThreads;
-  const int32_t pieces = row_pieces(a, W);
   const int64_t chunks = a.vocab / (a.bf16 ? 8 : 4);
-  const int32_t piece_chunks = (int32_t)((chunks + pieces - 1) / pieces);
-  auto* parts = static_cast<TokenPart*>(workspace);
-  auto* arrived = reinterpret_cast<uint32_t*>(parts + kSplitParts);
+  const int32_t pieces = row_pieces(a.rows, chunks, out.top_ids ? a.top : 0);
   each_rows(a, out, {}, kRowsPerLaunch, [&](const TokenArgs& b, const TokenScores& o,
                                             const TokenGrad&) {
-    hipLaunchKernelGGL(a.bf16 ? (token_score_kernel<true, W>) : (token_score_kernel<false, W>),
-                       dim3((unsigned)(b.rows * pieces)), dim3(W), 0, stream, b, o, pieces,
-                       piece_chunks, parts, arrived);
+    const int64_t* most = kRowChunks[o.top_ids && a.top > 0];
+    if (pieces > 1)
+      launch_score<kSplitThreads>(b, o, pieces, chunks, workspace, stream);
+    else if (chunks <= most[0])
+      launch_score<64>(b, o, 1, chunks, workspace, stream);
+    else if (chunks <= most[1])
+      launch_score<256>(b, o, 1, chunks, workspace, stream);
+    else if (chunks <= most[2])
+      launch_score<512>(b, o, 1, chunks, workspace, stream);
+    else
+      launch_score<1024>(b, o, 1, chunks, workspace, stream);
   });
   return hipGetLastError();
 }
@@ -787,15 +916,12 @@ bool launch_token_loss(const TokenArgs& a, const TokenScores& out, const TokenGr
                               : (token_loss_kernel<false, WW, NN>),                             \
                        dim3((unsigned)b.rows), dim3(WW), 0, stream, b, o, h);                   \
   } else
-    ARC_LOSS(256, 1)
-    ARC_LOSS(256, 4)
-    ARC_LOSS(512, 4)
+    ARC_LOSS(64, 8)
+    ARC_LOSS(256, 5)
     ARC_LOSS(512, 8)
-    ARC_LOSS(1024, 6)
-    ARC_LOSS(1024, 7)
     ARC_LOSS(1024, 8)
-    ARC_LOSS(1024, 13)
-    ARC_LOSS(1024, 16)
+    ARC_LOSS(512, 24)
+    ARC_LOSS(1024, 24)
     found = false;
 #undef ARC_LOSS
   });
