@@ -16,11 +16,13 @@ namespace {
 constexpr int kMaxTop = 32;           // ARC_MAX_TOP
 constexpr int64_t kSplitRows = 1024;  // calls of more rows give each a workgroup
 constexpr int64_t kSplitParts = 4096;
+constexpr int64_t kMostPieces = 16;   // their alternatives fit the joining workgroup's list
 constexpr int64_t kRowsPerLaunch = 1 << 20;  // threads of a launch stay below 2^32
 constexpr int kSplitThreads = 512;
 // Chunks of a row up to which workgroups of 64, 256 and 512 threads take it
-// (above: 1024), without and with alternatives.
-constexpr int64_t kRowChunks[2][3] = {{700, 3000, 7000}, {1500, 3500, 12520}};
+// (above: 1024).  The same with and without alternatives, so that a row's sums
+// have the same bits.
+constexpr int64_t kRow64 = 1200, kRow256 = 3300, kRow512 = 12520;
 
 // ---------------------------------------------------------------------------
 // A row is read in chunks of 16 bytes a lane, from its first whole word on (a
@@ -534,7 +536,7 @@ token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_c
   __syncthreads();
   if (!last) return;
   const TokenPart* of = parts + i * pieces;
-  // A lane of each wave takes a piece (there are at most 64), in the same order.
+  // A lane of each wave takes a piece (there are fewer), in the same order.
   const int32_t lane = threadIdx.x % kWave;
   s = {-INFINITY, 0.f, 0.f};
   if (lane < pieces)
@@ -550,7 +552,8 @@ token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_c
   if (threadIdx.x == 0) sh.found = 0;
   for (int q = threadIdx.x; q < kCandidates<W>; q += W) sh.found_keys[q] = 0;
   __syncthreads();
-  for (int32_t q = threadIdx.x; q < pieces * k; q += W) {  // at most kCandidates
+  static_assert(kMostPieces * kMaxTop <= kCandidates<kSplitThreads>, "room for all");
+  for (int32_t q = threadIdx.x; q < pieces * k; q += W) {
     const uint64_t key = share_load(&of[q / k].top[q % k]);
     if (key != 0 && key >= least) sh.found_keys[atomicAdd(&sh.found, 1)] = key;
   }
@@ -818,11 +821,10 @@ size_t token_workspace_bytes(int64_t vocab, int64_t max_rows) {
 }
 
 // Pieces of a row of that many chunks, for few rows.
-static int32_t row_pieces(int64_t rows, int64_t chunks, int32_t top) {
+static int32_t row_pieces(int64_t rows, int64_t chunks) {
   if (rows > kSplitRows) return 1;
   int64_t p = (chunks + kSplitThreads * 4 - 1) / (kSplitThreads * 4);  // a batch a thread
-  p = std::min<int64_t>({p, 64, 1024 / rows, kSplitParts / rows});
-  if (top > 0) p = std::min<int64_t>(p, kCandidates<kSplitThreads> / top);
+  p = std::min<int64_t>({p, kMostPieces, 1024 / rows, kSplitParts / rows});
   return static_cast<int32_t>(std::max<int64_t>(p, 1));
 }
 
@@ -869,17 +871,16 @@ hipError_t launch_token_score(const TokenArgs& a, const TokenScores& out, void* 
                               hipStream_t stream) {
   if (a.rows <= 0) return hipSuccess;
   const int64_t chunks = a.vocab / (a.bf16 ? 8 : 4);
-  const int32_t pieces = row_pieces(a.rows, chunks, out.top_ids ? a.top : 0);
+  const int32_t pieces = row_pieces(a.rows, chunks);
   each_rows(a, out, {}, kRowsPerLaunch, [&](const TokenArgs& b, const TokenScores& o,
                                             const TokenGrad&) {
-    const int64_t* most = kRowChunks[o.top_ids && a.top > 0];
     if (pieces > 1)
       launch_score<kSplitThreads>(b, o, pieces, chunks, workspace, stream);
-    else if (chunks <= most[0])
+    else if (chunks <= kRow64)
       launch_score<64>(b, o, 1, chunks, workspace, stream);
-    else if (chunks <= most[1])
+    else if (chunks <= kRow256)
       launch_score<256>(b, o, 1, chunks, workspace, stream);
-    else if (chunks <= most[2])
+    else if (chunks <= kRow512)
       launch_score<512>(b, o, 1, chunks, workspace, stream);
     else
       launch_score<1024>(b, o, 1, chunks, workspace, stream);
