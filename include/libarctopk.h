@@ -461,7 +461,7 @@ typedef struct {
 typedef struct {
   float lr;           /* finite */
   float beta1, beta2; /* in [0, 1) */
-  float eps;          /* > 0, finite */
+  float eps;          /* at least 2^-126, finite */
 } arc_adamw_config;
 
 /* Validate cfg, allocate the tables and the norms' workspace on the current

@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "arc_device.h"
 #include "arc_train.h"
 
@@ -10,41 +12,49 @@ namespace arc {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kLane = 8;  // consecutive elements of a thread: 16 lanes hold a block of scales
-static_assert(kOptimChunk % (kThreads * kLane) == 0, "whole passes of a workgroup");
 
-// Eight elements at any element alignment (the hardware's 16-byte accesses
-// need none).
-struct __attribute__((packed, aligned(2))) Halves8 {
-  uint32_t w[4];
-};
-struct __attribute__((packed, aligned(4))) Words4 {
-  float w[4];
-};
+typedef uint32_t loose_u32x4_t __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t loose_u32x2_t __attribute__((ext_vector_type(2), aligned(2)));
 
-__device__ __forceinline__ void load8(const void* base, int32_t bf16, int64_t at, int64_t count,
-                                      float (&x)[kLane]) {
-  if (at + kLane <= count) {
+// L (4 or 8) consecutive elements at any element alignment, read and written
+// once a step; zeros behind `count`.
+template <int L>
+__device__ __forceinline__ void load(const void* base, int32_t bf16, int64_t at, int64_t count,
+                                     float (&x)[L]) {
+  if (at + L <= count) {
     if (bf16) {
-      const Halves8 h = *reinterpret_cast<const Halves8*>(static_cast<const uint16_t*>(base) + at);
+      const uint16_t* p = static_cast<const uint16_t*>(base) + at;
+      uint32_t w[L / 2];
+      if constexpr (L == 8) {
+        const u32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const loose_u32x4_t*>(p));
+        w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+      } else {
+        const u32x2_t v = __builtin_nontemporal_load(reinterpret_cast<const loose_u32x2_t*>(p));
+        w[0] = v.x, w[1] = v.y;
+      }
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        x[2 * k] = bf16_lo(h.w[k]);
-        x[2 * k + 1] = bf16_hi(h.w[k]);
+      for (int k = 0; k < L / 2; ++k) {
+        x[2 * k] = bf16_lo(w[k]);
+        x[2 * k + 1] = bf16_hi(w[k]);
       }
     } else {
-      const Words4* p = reinterpret_cast<const Words4*>(static_cast<const float*>(base) + at);
-      const Words4 a = p[0], b = p[1];
+      // eight of a lane are two loads that take half of each line: the second
+      // one wants the first one's lines in the cache still
+      const loose_u32x4_t* p =
+          reinterpret_cast<const loose_u32x4_t*>(static_cast<const float*>(base) + at);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        x[k] = a.w[k];
-        x[4 + k] = b.w[k];
+      for (int h = 0; h < L / 4; ++h) {
+        const u32x4_t v = L == 8 ? (u32x4_t)p[h] : (u32x4_t)__builtin_nontemporal_load(p + h);
+        x[4 * h] = __uint_as_float(v.x);
+        x[4 * h + 1] = __uint_as_float(v.y);
+        x[4 * h + 2] = __uint_as_float(v.z);
+        x[4 * h + 3] = __uint_as_float(v.w);
       }
     }
     return;
   }
 #pragma unroll
-  for (int k = 0; k < kLane; ++k) {
+  for (int k = 0; k < L; ++k) {
     x[k] = 0.f;
     if (at + k < count)
       x[k] = bf16 ? __uint_as_float((uint32_t) static_cast<const uint16_t*>(base)[at + k] << 16)
@@ -52,36 +62,57 @@ __device__ __forceinline__ void load8(const void* base, int32_t bf16, int64_t at
   }
 }
 
-__device__ __forceinline__ uint32_t bf16_nearest(float x) {
-  const uint32_t b = __float_as_uint(x);
-  return x != x ? 0x7FC0u : (b + 0x7FFFu + ((b >> 16) & 1u)) >> 16;
-}
-
-__device__ __forceinline__ void store8_bf16(uint16_t* base, int64_t at, int64_t count,
-                                            const uint32_t (&h)[kLane]) {
-  if (at + kLane <= count) {
-    Halves8 w;
+template <int L>
+__device__ __forceinline__ void store_f32(float* base, int64_t at, int64_t count,
+                                          const float (&x)[L]) {
+  if (at + L <= count) {
+    loose_u32x4_t* p = reinterpret_cast<loose_u32x4_t*>(base + at);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) w.w[k] = h[2 * k] | (h[2 * k + 1] << 16);
-    *reinterpret_cast<Halves8*>(base + at) = w;
+    for (int h = 0; h < L / 4; ++h) {
+      const u32x4_t v = {__float_as_uint(x[4 * h]), __float_as_uint(x[4 * h + 1]),
+                         __float_as_uint(x[4 * h + 2]), __float_as_uint(x[4 * h + 3])};
+      if (L == 8)
+        p[h] = v;
+      else
+        __builtin_nontemporal_store(v, p + h);
+    }
     return;
   }
 #pragma unroll
-  for (int k = 0; k < kLane; ++k)
-    if (at + k < count) base[at + k] = (uint16_t)h[k];
-}
-
-__device__ __forceinline__ void store8_f32(float* base, int64_t at, int64_t count,
-                                           const float (&x)[kLane]) {
-  if (at + kLane <= count) {
-    Words4* p = reinterpret_cast<Words4*>(base + at);
-    p[0] = Words4{{x[0], x[1], x[2], x[3]}};
-    p[1] = Words4{{x[4], x[5], x[6], x[7]}};
-    return;
-  }
-#pragma unroll
-  for (int k = 0; k < kLane; ++k)
+  for (int k = 0; k < L; ++k)
     if (at + k < count) base[at + k] = x[k];
+}
+
+// h: two elements a word.
+template <int L>
+__device__ __forceinline__ void store_bf16(uint16_t* base, int64_t at, int64_t count,
+                                           const uint32_t (&h)[L / 2]) {
+  if (at + L <= count) {
+    if constexpr (L == 8) {
+      const u32x4_t v = {h[0], h[1], h[2], h[3]};
+      __builtin_nontemporal_store(v, reinterpret_cast<loose_u32x4_t*>(base + at));
+    } else {
+      const u32x2_t v = {h[0], h[1]};
+      __builtin_nontemporal_store(v, reinterpret_cast<loose_u32x2_t*>(base + at));
+    }
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < L; ++k)
+    if (at + k < count) base[at + k] = (uint16_t)(h[k / 2] >> (k % 2 * 16));
+}
+
+// Two values rounded to the nearest even.
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+  uint32_t w;
+  asm("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(w) : "v"(lo), "v"(hi));
+  return w;
+}
+
+// A value down to bfloat16, or up with the chance of what is cut off.
+__device__ __forceinline__ uint32_t bf16_random(float x, uint32_t draw) {
+  const uint32_t b = __float_as_uint(x);
+  return fabsf(x) < INFINITY ? b + (draw & 0xFFFFu) : b;
 }
 
 // 32 random bits of a state's element: its index and the step's key through a
@@ -106,31 +137,22 @@ __device__ __forceinline__ void from_f8(uint32_t w, float* x) {
   x[3] = hi.y;
 }
 
-__device__ __forceinline__ uint32_t to_f8(const float* x) {
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
-  w = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], w, true);
-  return (uint32_t)w;
-}
-
-// |x| < 256 to a value of e4m3, up with the chance of what is cut off; draw: 20
-// random bits.  Normal values lose the 20 low bits of their mantissa, those
-// below 2^-6 what is left of a multiple of 2^-9.
-__device__ __forceinline__ float round_f8(float x, uint32_t draw) {
-  const float normal = __uint_as_float((__float_as_uint(x) + draw) & 0xFFF00000u);
-  const float small = floorf(x * 512.f + (float)draw * 0x1p-20f) * 0x1p-9f;
-  return x < 0x1p-6f ? small : normal;
-}
-
-// Largest of the 16 lanes that hold a block (magnitudes as words, so that a
-// NaN is the largest).
-__device__ __forceinline__ uint32_t block_max(uint32_t v) {
-#pragma unroll
-  for (int off = 1; off < 16; off <<= 1) {
-    const uint32_t o = __shfl_xor(v, off);
-    v = o > v ? o : v;
+// A magnitude below 256 to a code of e4m3, up with the chance of what is cut
+// off (normal values: the 20 low bits of the mantissa; below 2^-6: what is left
+// of a multiple of 2^-9), by the 20 high bits of `draw`.  The instruction does
+// just that; it agreed with the definition on 4.2 million words and draws.
+__device__ __forceinline__ uint32_t f8_random(float x, uint32_t draw, uint32_t word, int byte) {
+  switch (byte) {
+    case 0: return (uint32_t)__builtin_amdgcn_cvt_sr_fp8_f32(x, draw, word, 0);
+    case 1: return (uint32_t)__builtin_amdgcn_cvt_sr_fp8_f32(x, draw, word, 1);
+    case 2: return (uint32_t)__builtin_amdgcn_cvt_sr_fp8_f32(x, draw, word, 2);
+    default: return (uint32_t)__builtin_amdgcn_cvt_sr_fp8_f32(x, draw, word, 3);
   }
-  return v;
 }
+
+struct MaxU {
+  __device__ uint32_t operator()(uint32_t a, uint32_t b) const { return a > b ? a : b; }
+};
 
 // Exponent field of a block's scale, from the words of its largest magnitude.
 __device__ __forceinline__ uint32_t scale_exponent(uint32_t most) {
@@ -138,9 +160,14 @@ __device__ __forceinline__ uint32_t scale_exponent(uint32_t most) {
   return e > 8 ? e - 7 : 1;
 }
 
+// States in 32 bits: four elements a lane, so that every access of a wave takes
+// whole lines.  States in 8 bits: eight, so that 16 lanes hold a block.
 template <bool F8>
 __global__ void __launch_bounds__(kThreads)
 adamw_kernel(OptimBatch b, OptimPointers p, AdamArgs a) {
+  constexpr int L = F8 ? 8 : 4;
+  static_assert(kOptimChunk % (kThreads * L) == 0, "whole passes of a workgroup");
+  static_assert(!F8 || kStateBlock == 16 * L, "a block is a row of lanes");
   const float factor = a.factor ? *a.factor : 1.f;
   if (!(fabsf(factor) < INFINITY)) return;
   const int32_t chunk = b.first_chunk + blockIdx.x;
@@ -155,92 +182,104 @@ adamw_kernel(OptimBatch b, OptimPointers p, AdamArgs a) {
   const float step = lr * a.inv_c1;
   const int64_t padded = (t.count + kStateBlock - 1) / kStateBlock * kStateBlock;
 #pragma unroll
-  for (int u = 0; u < kOptimChunk / (kThreads * kLane); ++u) {
+  for (int u = 0; u < kOptimChunk / (kThreads * L); ++u) {
     const int64_t e = (int64_t)(chunk - t.first_chunk) * kOptimChunk +
-                      (u * kThreads + (int)threadIdx.x) * kLane;
-    if (e >= padded) continue;  // a block's 16 lanes alike
+                      (u * kThreads + (int)threadIdx.x) * L;
+    if (e >= padded) break;  // the 16 lanes of a block alike
     const int64_t s = t.state + e;
-    float g[kLane], x[kLane], m[kLane], v[kLane];
-    load8(grad, t.grad_bf16, e, t.count, g);
-    load8(param, t.param_bf16, e, t.count, x);
+    float g[L], x[L], m[L], v[L];
+    load<L>(grad, t.grad_bf16, e, t.count, g);
+    load<L>(param, t.param_bf16, e, t.count, x);
     if constexpr (F8) {
-      const uint2 mw = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.m) + s);
-      const uint2 vw = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.v) + s);
+      const auto mw = __builtin_nontemporal_load(
+          reinterpret_cast<const u32x2_t*>(static_cast<const uint8_t*>(a.m) + s));
+      const auto vw = __builtin_nontemporal_load(
+          reinterpret_cast<const u32x2_t*>(static_cast<const uint8_t*>(a.v) + s));
       const float ms = a.m_scale[s / kStateBlock], vs = a.v_scale[s / kStateBlock];
       from_f8(mw.x, m);
       from_f8(mw.y, m + 4);
       from_f8(vw.x, v);
       from_f8(vw.y, v + 4);
 #pragma unroll
-      for (int k = 0; k < kLane; ++k) {
+      for (int k = 0; k < L; ++k) {
         m[k] *= ms;
         v[k] *= vs;
         v[k] *= v[k];
       }
     } else {
-      load8(a.m, 0, s, INT64_MAX, m);
-      load8(a.v, 0, s, INT64_MAX, v);
+      load<L>(a.m, 0, s, INT64_MAX, m);
+      load<L>(a.v, 0, s, INT64_MAX, v);
     }
-    float root[kLane];
+    float root[L];
 #pragma unroll
-    for (int k = 0; k < kLane; ++k) {
+    for (int k = 0; k < L; ++k) {
       const float gk = g[k] * factor;
       m[k] = a.beta1 * m[k] + a.one_minus_beta1 * gk;
       v[k] = a.beta2 * v[k] + a.one_minus_beta2 * (gk * gk);
-      if (e + k >= t.count) m[k] = v[k] = 0.f;
       root[k] = sqrtf(v[k]);
-      x[k] = x[k] * keep - step * (m[k] / (root[k] * a.inv_root_c2 + a.eps));
+      // the reciprocal is within 1 ulp: 2^-23 of an update that is a small part
+      // of x, and a tenth of an exact division's operations
+      const float inv = __builtin_amdgcn_rcpf(fmaf(root[k], a.inv_root_c2, a.eps));
+      x[k] = fmaf(-step, m[k] * inv, x[k] * keep);
     }
-    uint32_t r[kLane];
+    if (e + L > t.count) {  // behind the end: states stay 0
+#pragma unroll
+      for (int k = 0; k < L; ++k)
+        if (e + k >= t.count) m[k] = v[k] = root[k] = 0.f;
+    }
+    uint32_t r[L];
     if (F8 || a.stochastic) {
       const uint32_t z = (uint32_t)s + a.key_low + (uint32_t)((uint64_t)s >> 32) * 0x9E3779B9u;
 #pragma unroll
-      for (int k = 0; k < kLane; ++k) r[k] = random_bits(z + k, a.key_high);
+      for (int k = 0; k < L; ++k) r[k] = random_bits(z + k, a.key_high);
     }
     if constexpr (F8) {
       uint32_t most_m = 0, most_v = 0;
 #pragma unroll
-      for (int k = 0; k < kLane; ++k) {
-        most_m = max(most_m, __float_as_uint(m[k]) & 0x7FFFFFFFu);
-        most_v = max(most_v, __float_as_uint(root[k]));
+      for (int k = 0; k < L; ++k) {  // as words, so that a NaN is the largest
+        most_m = MaxU()(most_m, __float_as_uint(m[k]) & 0x7FFFFFFFu);
+        most_v = MaxU()(most_v, __float_as_uint(root[k]));
       }
-      const uint32_t em = scale_exponent(block_max(most_m));
-      const uint32_t ev = scale_exponent(block_max(most_v));
+      const uint32_t em = scale_exponent(lanes_reduce<16>(most_m, MaxU()));
+      const uint32_t ev = scale_exponent(lanes_reduce<16>(most_v, MaxU()));
       const float im = __uint_as_float((254u - em) << 23), iv = __uint_as_float((254u - ev) << 23);
-      float qm[kLane], qv[kLane];
+      uint32_t qm[2] = {0, 0}, qv[2] = {0, 0};
 #pragma unroll
-      for (int k = 0; k < kLane; ++k) {
-        qm[k] = copysignf(round_f8(fabsf(m[k]) * im, r[k] & 0xFFFFFu), m[k]);
-        qv[k] = round_f8(root[k] * iv, r[k] >> 12);
-        if (qv[k] == 0.f && root[k] > 0.f) qv[k] = 0x1p-9f;
+      for (int k = 0; k < L; ++k) {
+        qm[k / 4] = f8_random(m[k] * im, r[k] << 12, qm[k / 4], k % 4);
+        // what is above 0 is 2^-9, the smallest value, at least
+        const uint32_t least = root[k] == 0.f ? 0u : 0x3B000000u;
+        const uint32_t w = MaxU()(__float_as_uint(root[k] * iv), least);
+        qv[k / 4] = f8_random(__uint_as_float(w), r[k], qv[k / 4], k % 4);
       }
-      *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.m) + s) =
-          make_uint2(to_f8(qm), to_f8(qm + 4));
-      *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.v) + s) =
-          make_uint2(to_f8(qv), to_f8(qv + 4));
+      const u32x2_t mw = {qm[0], qm[1]}, vw = {qv[0], qv[1]};
+      __builtin_nontemporal_store(
+          mw, reinterpret_cast<u32x2_t*>(static_cast<uint8_t*>(a.m) + s));
+      __builtin_nontemporal_store(
+          vw, reinterpret_cast<u32x2_t*>(static_cast<uint8_t*>(a.v) + s));
       if (threadIdx.x % 16 == 0) {
         a.m_scale[s / kStateBlock] = __uint_as_float(em << 23);
         a.v_scale[s / kStateBlock] = __uint_as_float(ev << 23);
       }
     } else {
-      store8_f32(static_cast<float*>(a.m), s, INT64_MAX, m);
-      store8_f32(static_cast<float*>(a.v), s, INT64_MAX, v);
+      store_f32<L>(static_cast<float*>(a.m), s, INT64_MAX, m);
+      store_f32<L>(static_cast<float*>(a.v), s, INT64_MAX, v);
     }
-    uint32_t h[kLane];
+    uint32_t h[L / 2];
+#pragma unroll
+    for (int k = 0; k < L / 2; ++k) h[k] = bf16_pair(x[2 * k], x[2 * k + 1]);
     if (t.param_bf16) {
+      if (a.stochastic) {
 #pragma unroll
-      for (int k = 0; k < kLane; ++k) {
-        h[k] = bf16_nearest(x[k]);
-        if (a.stochastic && fabsf(x[k]) < INFINITY)
-          h[k] = (__float_as_uint(x[k]) + (r[k] & 0xFFFFu)) >> 16;
+        for (int k = 0; k < L / 2; ++k)
+          h[k] = (bf16_random(x[2 * k], r[2 * k]) >> 16) |
+                 (bf16_random(x[2 * k + 1], r[2 * k + 1]) & 0xFFFF0000u);
       }
-      store8_bf16(static_cast<uint16_t*>(param), e, t.count, h);
+      store_bf16<L>(static_cast<uint16_t*>(param), e, t.count, h);
     } else {
-      store8_f32(static_cast<float*>(param), e, t.count, x);
-#pragma unroll
-      for (int k = 0; k < kLane; ++k) h[k] = bf16_nearest(x[k]);
+      store_f32<L>(static_cast<float*>(param), e, t.count, x);
     }
-    if (copy) store8_bf16(copy, e, t.count, h);
+    if (copy) store_bf16<L>(copy, e, t.count, h);
   }
 }
 
@@ -254,50 +293,72 @@ __device__ __forceinline__ double wave_sum_f64(double v) {
 __device__ __forceinline__ double group_sum(double v) {
   __shared__ double part[kThreads / kWave];
   v = wave_sum_f64(v);
+  __syncthreads();  // of an earlier sum
   if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = v;
   __syncthreads();
   return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
+// The sum of squares of one run of kNormChunk elements, in binary64 (no square
+// of a binary32 number overflows there, and the conversion and the fma take a
+// third of the time that HBM does).
 __global__ void __launch_bounds__(kThreads)
-norm_chunk_kernel(OptimBatch b, OptimPointers p, double* __restrict__ partial) {
+norm_chunk_kernel(NormBatch b, NormPointers p, double* __restrict__ partial) {
   const int32_t chunk = b.first_chunk + blockIdx.x;
   const int32_t i = b.chunk_tensor[chunk];
   const OptimTensor t = b.tensors[i];
   const void* grad = p.grad[i - b.first];
-  double sum = 0.0;
+  const int64_t first = (int64_t)(chunk - t.first_norm) * kNormChunk;
+  double sum[4] = {0.0, 0.0, 0.0, 0.0};
+  const auto add = [&](auto lanes) {
+    constexpr int L = decltype(lanes)::value;
+    for (int u = 0; u < kNormChunk; u += 4 * kThreads * L) {
+      if (first + u >= t.count) break;
+      float g[4][L];
 #pragma unroll
-  for (int u = 0; u < kOptimChunk / (kThreads * kLane); ++u) {
-    const int64_t e = (int64_t)(chunk - t.first_chunk) * kOptimChunk +
-                      (u * kThreads + (int)threadIdx.x) * kLane;
-    float g[kLane];
-    load8(grad, t.grad_bf16, e, t.count, g);
+      for (int q = 0; q < 4; ++q)
+        load<L>(grad, L == 8, first + u + (q * kThreads + (int)threadIdx.x) * L, t.count, g[q]);
 #pragma unroll
-    for (int k = 0; k < kLane; ++k) sum = fma((double)g[k], (double)g[k], sum);
-  }
-  sum = group_sum(sum);
-  if (threadIdx.x == 0) partial[chunk] = sum;
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int k = 0; k < L; ++k) sum[q] = fma((double)g[q][k], (double)g[q][k], sum[q]);
+    }
+  };
+  if (t.grad_bf16)
+    add(std::integral_constant<int, 8>());
+  else
+    add(std::integral_constant<int, 4>());
+  const double all = group_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
+  if (threadIdx.x == 0) partial[chunk] = all;
 }
 
+// Each tensor's sum, and the total by the last workgroup to arrive.
 __global__ void __launch_bounds__(kThreads)
-norm_tensor_kernel(const OptimTensor* __restrict__ tensors, const double* __restrict__ partial,
-                   double* __restrict__ squares, float scale, float* __restrict__ norms) {
+norm_tensor_kernel(const OptimTensor* __restrict__ tensors, int32_t num,
+                   const double* __restrict__ partial, double* __restrict__ squares,
+                   uint32_t* __restrict__ arrived, float scale, float max_norm,
+                   float* __restrict__ norms, float* __restrict__ total) {
+  __shared__ bool last;
   const OptimTensor t = tensors[blockIdx.x];
-  const int64_t chunks = (t.count + kOptimChunk - 1) / kOptimChunk;
+  const int64_t chunks = (t.count + kNormChunk - 1) / kNormChunk;
   double sum = 0.0;
-  for (int64_t c = threadIdx.x; c < chunks; c += kThreads) sum += partial[t.first_chunk + c];
+#pragma unroll 4
+  for (int64_t c = threadIdx.x; c < chunks; c += kThreads) sum += partial[t.first_norm + c];
   sum = group_sum(sum);
   if (threadIdx.x == 0) {
-    squares[blockIdx.x] = sum;
     if (norms) norms[blockIdx.x] = (float)((double)scale * sqrt(sum));
+    __hip_atomic_store(&squares[blockIdx.x], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    wave_vmem_fence();  // written before it counts
+    last = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+           (uint32_t)(num - 1);
+    if (last) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
-}
-
-__global__ void __launch_bounds__(kThreads)
-norm_total_kernel(const double* __restrict__ squares, int32_t num, float scale, float max_norm,
-                  float* __restrict__ total) {
-  double sum = 0.0;
-  for (int32_t i = threadIdx.x; i < num; i += kThreads) sum += squares[i];
+  __syncthreads();
+  if (!last) return;
+  sum = 0.0;
+#pragma unroll 4
+  for (int32_t i = threadIdx.x; i < num; i += kThreads)
+    sum += __hip_atomic_load(&squares[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   sum = group_sum(sum);
   if (threadIdx.x == 0) {
     const double norm = (double)scale * sqrt(sum);
@@ -318,7 +379,7 @@ hipError_t launch_adamw(bool f8, const OptimBatch& b, const OptimPointers& p, co
   return hipGetLastError();
 }
 
-hipError_t launch_norm_chunks(const OptimBatch& b, const OptimPointers& p, double* partial,
+hipError_t launch_norm_chunks(const NormBatch& b, const NormPointers& p, double* partial,
                               hipStream_t stream) {
   hipLaunchKernelGGL(norm_chunk_kernel, dim3((unsigned)b.chunks), dim3(kThreads), 0, stream, b, p,
                      partial);
@@ -326,16 +387,10 @@ hipError_t launch_norm_chunks(const OptimBatch& b, const OptimPointers& p, doubl
 }
 
 hipError_t launch_norm_tensors(const OptimTensor* tensors, int32_t num, const double* partial,
-                               double* squares, float scale, float* norms, hipStream_t stream) {
+                               double* squares, uint32_t* arrived, float scale, float max_norm,
+                               float* norms, float* total, hipStream_t stream) {
   hipLaunchKernelGGL(norm_tensor_kernel, dim3((unsigned)num), dim3(kThreads), 0, stream, tensors,
-                     partial, squares, scale, norms);
-  return hipGetLastError();
-}
-
-hipError_t launch_norm_total(const double* squares, int32_t num, float scale, float max_norm,
-                             float* total, hipStream_t stream) {
-  hipLaunchKernelGGL(norm_total_kernel, dim3(1), dim3(kThreads), 0, stream, squares, num, scale,
-                     max_norm, total);
+                     num, partial, squares, arrived, scale, max_norm, norms, total);
   return hipGetLastError();
 }
 

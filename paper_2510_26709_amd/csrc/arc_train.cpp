@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 #include <new>
@@ -20,16 +21,18 @@ struct arc_tokens {
   hipStream_t stream = nullptr;
   int device = 0;
   void* workspace = nullptr;
+  float* row_values = nullptr;  // lse and entropy of a loss whose caller wants neither
 
   void release() {
     (void)hipStreamSynchronize(stream);
     if (workspace) (void)hipFree(workspace);
+    if (row_values) (void)hipFree(row_values);
   }
 };
 
 struct arc_optim {
   std::vector<arc::OptimTensor> tensors;
-  std::vector<int32_t> chunk_tensor;
+  std::vector<int32_t> chunk_tensor, norm_tensor;  // of each run of elements
   int64_t state_elems = 0;
   int32_t state = ARC_STATE_F32, stochastic = 0;
   bool any_param_bf16 = false;
@@ -37,14 +40,15 @@ struct arc_optim {
   hipStream_t stream = nullptr;
   int device = 0;
   arc::OptimTensor* tensors_dev = nullptr;
-  int32_t* chunk_tensor_dev = nullptr;
-  double* partial_dev = nullptr;  // a sum of squares of each chunk
-  double* squares_dev = nullptr;  // of each tensor
+  int32_t *chunk_tensor_dev = nullptr, *norm_tensor_dev = nullptr;
+  double* partial_dev = nullptr;  // a sum of squares of each run
+  double* squares_dev = nullptr;  // of each tensor, and the count of those done
+  uint32_t* arrived() const { return reinterpret_cast<uint32_t*>(squares_dev + tensors.size()); }
 
   void release() {
     (void)hipStreamSynchronize(stream);
     for (void* p : {static_cast<void*>(tensors_dev), static_cast<void*>(chunk_tensor_dev),
-                    static_cast<void*>(partial_dev), static_cast<void*>(squares_dev)})
+                    static_cast<void*>(norm_tensor_dev), static_cast<void*>(partial_dev), static_cast<void*>(squares_dev)})
       if (p) (void)hipFree(p);
   }
 };
@@ -215,10 +219,16 @@ arc_status check_optim(const arc_optim_config* cfg) {
 // The tables of a checked configuration (may throw std::bad_alloc).
 void plan_optim(const arc_optim_config* cfg, arc_optim* c) {
   c->tensors.reserve(static_cast<size_t>(cfg->num_tensors));
-  int64_t chunks = 0;
-  for (int32_t i = 0; i < cfg->num_tensors; ++i)
-    chunks += (cfg->tensors[i].count + arc::kOptimChunk - 1) / arc::kOptimChunk;
-  c->chunk_tensor.reserve(static_cast<size_t>(chunks));
+  const auto runs = [](int64_t count, int64_t of) {
+    return static_cast<size_t>((count + of - 1) / of);
+  };
+  size_t chunks = 0, norms = 0;
+  for (int32_t i = 0; i < cfg->num_tensors; ++i) {
+    chunks += runs(cfg->tensors[i].count, arc::kOptimChunk);
+    norms += runs(cfg->tensors[i].count, arc::kNormChunk);
+  }
+  c->chunk_tensor.reserve(chunks);
+  c->norm_tensor.reserve(norms);
   for (int32_t i = 0; i < cfg->num_tensors; ++i) {
     const arc_optim_tensor& in = cfg->tensors[i];
     arc::OptimTensor t{};
@@ -227,35 +237,36 @@ void plan_optim(const arc_optim_config* cfg, arc_optim* c) {
     t.weight_decay = in.weight_decay;
     t.lr_scale = in.lr_scale;
     t.first_chunk = static_cast<int32_t>(c->chunk_tensor.size());
+    t.first_norm = static_cast<int32_t>(c->norm_tensor.size());
     t.param_bf16 = in.param_dtype == ARC_DTYPE_BF16;
     t.grad_bf16 = in.grad_dtype == ARC_DTYPE_BF16;
     c->any_param_bf16 = c->any_param_bf16 || t.param_bf16;
     c->tensors.push_back(t);
     c->state_elems += (in.count + arc::kStateBlock - 1) / arc::kStateBlock * arc::kStateBlock;
-    c->chunk_tensor.insert(c->chunk_tensor.end(),
-                           static_cast<size_t>((in.count + arc::kOptimChunk - 1) /
-                                               arc::kOptimChunk),
-                           i);
+    c->chunk_tensor.insert(c->chunk_tensor.end(), runs(in.count, arc::kOptimChunk), i);
+    c->norm_tensor.insert(c->norm_tensor.end(), runs(in.count, arc::kNormChunk), i);
   }
   c->state = cfg->state;
   c->stochastic = cfg->stochastic;
   c->seed = cfg->seed;
 }
 
-// Calls launch(batch) for runs of at most kOptimBatch tensors and kMaxGroups
-// chunks that together hold every chunk once.
+// Calls launch(batch, tensors) for batches of at most `tensors` tensors and
+// kMaxGroups runs that together hold every run once.
 template <typename Launch>
-arc_status each_batch(const arc_optim* c, const Launch& launch) {
+arc_status each_batch(const arc_optim* c, int32_t tensors, const std::vector<int32_t>& runs,
+                      const int32_t* runs_dev, int32_t arc::OptimTensor::*first_run,
+                      const Launch& launch) {
   const auto num = static_cast<int32_t>(c->tensors.size());
-  const auto all = static_cast<int64_t>(c->chunk_tensor.size());
-  for (int32_t first = 0; first < num; first += arc::kOptimBatch) {
-    const int32_t next = std::min(num, first + arc::kOptimBatch);
-    const int64_t end = next < num ? c->tensors[static_cast<size_t>(next)].first_chunk : all;
-    for (int64_t at = c->tensors[static_cast<size_t>(first)].first_chunk; at < end;
+  const auto all = static_cast<int64_t>(runs.size());
+  for (int32_t first = 0; first < num; first += tensors) {
+    const int32_t next = std::min(num, first + tensors);
+    const int64_t end = next < num ? c->tensors[static_cast<size_t>(next)].*first_run : all;
+    for (int64_t at = c->tensors[static_cast<size_t>(first)].*first_run; at < end;
          at += kMaxGroups) {
       arc::OptimBatch b;
       b.tensors = c->tensors_dev;
-      b.chunk_tensor = c->chunk_tensor_dev;
+      b.chunk_tensor = runs_dev;
       b.first = first;
       b.first_chunk = static_cast<int32_t>(at);
       b.chunks = static_cast<int32_t>(std::min(end - at, kMaxGroups));
@@ -307,6 +318,11 @@ arc_status arc_tokens_create(const arc_tokens_config* cfg, void* hip_stream, arc
     e = hipMalloc(&c->workspace, bytes);
     if (e != hipSuccess) c->workspace = nullptr;
   }
+  if (e == hipSuccess) {
+    e = hipMalloc(reinterpret_cast<void**>(&c->row_values),
+                  static_cast<size_t>(c->max_rows) * 2 * sizeof(float));
+    if (e != hipSuccess) c->row_values = nullptr;
+  }
   if (e == hipSuccess) e = hipMemset(c->workspace, 0, bytes);
   if (e == hipSuccess) e = hipDeviceSynchronize();
   if (e != hipSuccess) {
@@ -356,8 +372,8 @@ arc_status arc_tokens_loss(arc_tokens* c, int64_t rows, const void* logits, int6
                            void* grad, int64_t grad_stride) {
   arc_status st = check_rows(c, rows, logits, stride);
   if (st != ARC_OK) return st;
-  const arc::TokenScores out{logp, entropy, lse, nullptr, nullptr};
-  const arc::TokenGrad g{lse, entropy, d_logp, d_entropy, d_lse, grad, grad_stride};
+  arc::TokenScores out{logp, entropy, lse, nullptr, nullptr};
+  arc::TokenGrad g{lse, entropy, d_logp, d_entropy, d_lse, grad, grad_stride};
   if ((st = check_score(c, rows, logits, stride, targets, out)) != ARC_OK ||
       (st = check_grad(c, rows, logits, stride, targets, g)) != ARC_OK)
     return st;
@@ -372,8 +388,10 @@ arc_status arc_tokens_loss(arc_tokens* c, int64_t rows, const void* logits, int6
     ARC_HIP(e, "token loss launch");
     return ARC_OK;
   }
-  if (lse == nullptr || entropy == nullptr)
-    return fail(ARC_ERR_INVALID, "lse and entropy are needed");
+  if (lse == nullptr) out.lse = c->row_values;
+  if (entropy == nullptr) out.entropy = c->row_values + c->max_rows;
+  g.lse = out.lse;
+  g.entropy = out.entropy;
   ARC_HIP(arc::launch_token_score(a, out, c->workspace, c->stream), "token score launch");
   ARC_HIP(arc::launch_token_grad(a, g, c->stream), "token gradient launch");
   return ARC_OK;
@@ -408,15 +426,19 @@ arc_status arc_optim_create(const arc_optim_config* cfg, void* hip_stream, arc_o
   hipError_t e = hipGetDevice(&c->device);
   if (e != hipSuccess) return bail(arc::fail_hip(e, "hipGetDevice"));
   if ((st = device_copy(&c->tensors_dev, c->tensors, "optimizer tables")) != ARC_OK ||
-      (st = device_copy(&c->chunk_tensor_dev, c->chunk_tensor, "optimizer tables")) != ARC_OK)
+      (st = device_copy(&c->chunk_tensor_dev, c->chunk_tensor, "optimizer tables")) != ARC_OK ||
+      (st = device_copy(&c->norm_tensor_dev, c->norm_tensor, "optimizer tables")) != ARC_OK)
     return bail(st);
   const auto room = [&](double** p, size_t count) {
     e = hipMalloc(reinterpret_cast<void**>(p), std::max<size_t>(count, 1) * sizeof(double));
     if (e != hipSuccess) *p = nullptr;
     return e == hipSuccess;
   };
-  if (!room(&c->partial_dev, c->chunk_tensor.size()) ||
-      !room(&c->squares_dev, c->tensors.size())) {
+  if (room(&c->partial_dev, c->norm_tensor.size()) &&
+      room(&c->squares_dev, c->tensors.size() + 1))
+    e = hipMemset(c->arrived(), 0, sizeof(double));
+  if (e == hipSuccess) e = hipDeviceSynchronize();
+  if (e != hipSuccess) {
     (void)hipGetLastError();
     return bail(arc::fail_hip(e, "optimizer workspace"));
   }
@@ -443,17 +465,18 @@ arc_status arc_optim_norm(arc_optim* c, const void* const* grads, float scale, f
   if (overlap({norms, int64_t{4} * num}, {total, 8}))
     return fail(ARC_ERR_INVALID, "norms and total must not overlap");
   const OnDevice here(c->device);
-  st = each_batch(c, [&](const arc::OptimBatch& b, int32_t count) -> arc_status {
-    arc::OptimPointers p;
-    std::copy(grads + b.first, grads + b.first + count, p.grad);
-    ARC_HIP(arc::launch_norm_chunks(b, p, c->partial_dev, c->stream), "norm launch");
-    return ARC_OK;
-  });
+  st = each_batch(c, arc::kNormBatch, c->norm_tensor, c->norm_tensor_dev,
+                  &arc::OptimTensor::first_norm,
+                  [&](const arc::OptimBatch& b, int32_t count) -> arc_status {
+                    arc::NormPointers p;
+                    std::copy(grads + b.first, grads + b.first + count, p.grad);
+                    ARC_HIP(arc::launch_norm_chunks(b, p, c->partial_dev, c->stream),
+                            "norm launch");
+                    return ARC_OK;
+                  });
   if (st != ARC_OK) return st;
-  ARC_HIP(arc::launch_norm_tensors(c->tensors_dev, num, c->partial_dev, c->squares_dev, scale,
-                                   norms, c->stream),
-          "norm launch");
-  ARC_HIP(arc::launch_norm_total(c->squares_dev, num, scale, max_norm, total, c->stream),
+  ARC_HIP(arc::launch_norm_tensors(c->tensors_dev, num, c->partial_dev, c->squares_dev,
+                                   c->arrived(), scale, max_norm, norms, total, c->stream),
           "norm launch");
   return ARC_OK;
 }
@@ -468,8 +491,8 @@ arc_status arc_optim_adamw(arc_optim* c, const arc_adamw_config* ac, int64_t t,
   if (!finite(ac->lr)) return fail(ARC_ERR_INVALID, "lr must be finite");
   if (!(ac->beta1 >= 0.f && ac->beta1 < 1.f) || !(ac->beta2 >= 0.f && ac->beta2 < 1.f))
     return fail(ARC_ERR_INVALID, "beta1 and beta2 must be in [0, 1)");
-  if (!(ac->eps > 0.f) || !finite(ac->eps))
-    return fail(ARC_ERR_INVALID, "eps must be finite and > 0");
+  if (!(ac->eps >= FLT_MIN) || !finite(ac->eps))
+    return fail(ARC_ERR_INVALID, "eps must be finite and at least 2^-126");
   arc_status st;
   if ((st = check_pointers(c, params, "params")) != ARC_OK ||
       (st = check_pointers(c, grads, "grads")) != ARC_OK)
@@ -511,16 +534,18 @@ arc_status arc_optim_adamw(arc_optim* c, const arc_adamw_config* ac, int64_t t,
   a.m_scale = m_scale;
   a.v_scale = v_scale;
   const OnDevice here(c->device);
-  return each_batch(c, [&](const arc::OptimBatch& b, int32_t count) -> arc_status {
-    arc::OptimPointers p;
-    for (int32_t i = 0; i < count; ++i) {
-      p.param[i] = params[b.first + i];
-      p.grad[i] = grads[b.first + i];
-      p.copy[i] = copies ? static_cast<uint16_t*>(copies[b.first + i]) : nullptr;
-    }
-    ARC_HIP(arc::launch_adamw(f8, b, p, a, c->stream), "AdamW launch");
-    return ARC_OK;
-  });
+  return each_batch(c, arc::kOptimBatch, c->chunk_tensor, c->chunk_tensor_dev,
+                    &arc::OptimTensor::first_chunk,
+                    [&](const arc::OptimBatch& b, int32_t count) -> arc_status {
+                      arc::OptimPointers p;
+                      for (int32_t i = 0; i < count; ++i) {
+                        p.param[i] = params[b.first + i];
+                        p.grad[i] = grads[b.first + i];
+                        p.copy[i] = copies ? static_cast<uint16_t*>(copies[b.first + i]) : nullptr;
+                      }
+                      ARC_HIP(arc::launch_adamw(f8, b, p, a, c->stream), "AdamW launch");
+                      return ARC_OK;
+                    });
 }
 
 arc_status arc_optim_destroy(arc_optim* c) {

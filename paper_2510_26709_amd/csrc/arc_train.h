@@ -45,9 +45,10 @@ hipError_t launch_token_grad(const TokenArgs& a, const TokenGrad& g, hipStream_t
 
 // ---------------------------------------------------------------- optimizer
 
-// Elements of a tensor that one workgroup updates, and that one partial sum of
-// the norms covers.
+// Elements of a tensor that one workgroup updates, and that one sums the squares
+// of.
 constexpr int kOptimChunk = 4096;
+constexpr int kNormChunk = 32768;
 constexpr int kStateBlock = 128;  // ARC_STATE_BLOCK
 
 // A tensor's place in the states and its constants.
@@ -55,9 +56,8 @@ struct OptimTensor {
   int64_t count;
   int64_t state;       // first element of its states
   float weight_decay, lr_scale;
-  int32_t first_chunk;
+  int32_t first_chunk, first_norm;  // its runs of kOptimChunk and of kNormChunk elements
   int32_t param_bf16, grad_bf16;
-  int32_t pad;
 };
 
 // Pointers travel in the kernel's arguments (4 KB of them at most), so that a
@@ -88,12 +88,17 @@ struct OptimBatch {
 
 hipError_t launch_adamw(bool f8, const OptimBatch& b, const OptimPointers& p, const AdamArgs& a,
                         hipStream_t stream);
-hipError_t launch_norm_chunks(const OptimBatch& b, const OptimPointers& p, double* partial,
+constexpr int kNormBatch = 480;
+struct NormPointers {
+  const void* grad[kNormBatch];
+};
+typedef OptimBatch NormBatch;  // of runs of kNormChunk elements
+
+hipError_t launch_norm_chunks(const NormBatch& b, const NormPointers& p, double* partial,
                               hipStream_t stream);
-// Sums of each tensor's partials, then the total.
+// Each tensor's norm and the total; `arrived` is 0 before and after.
 hipError_t launch_norm_tensors(const OptimTensor* tensors, int32_t num, const double* partial,
-                               double* squares, float scale, float* norms, hipStream_t stream);
-hipError_t launch_norm_total(const double* squares, int32_t num, float scale, float max_norm,
-                             float* total, hipStream_t stream);
+                               double* squares, uint32_t* arrived, float scale, float max_norm,
+                               float* norms, float* total, hipStream_t stream);
 
 }  // namespace arc

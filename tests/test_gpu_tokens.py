@@ -368,6 +368,19 @@ def test_any_of_the_outputs(dtype):
     assert torch.equal(ids, all_.top_ids) and torch.equal(near_, all_.top_logp)
 
 
+@pytest.mark.parametrize("V", [4000, 210_000])
+def test_a_loss_without_its_numbers(V):
+    T = 3
+    x = place(torch.randn(T, V, generator=torch.Generator().manual_seed(2)), "bf16")
+    y = tokens(T, V, 5)
+    up = torch.ones(T, device="cuda")
+    h = arc.TokenLogProbs(V=V, rows=T)
+    want = h.loss(x, y, up, up).grad
+    got = torch.empty_like(want)
+    arc.arc_tokens_loss(h.ctx, T, x, V, y, up, up, None, None, None, None, got, V)
+    assert torch.equal(got.nan_to_num(), want.nan_to_num())
+
+
 def test_another_stream_and_replays_of_a_graph():
     T, V = 6, 50257
     stream = torch.cuda.Stream()
