@@ -421,8 +421,9 @@ arc_status arc_tokens_destroy(arc_tokens *ctx);
  * one step moves a state by less than half the distance of two such values:
  * rounded to the nearest, v would stay where its first step put it.  A
  * magnitude is rounded up with the chance of what is cut off, decided by a
- * hash of (seed, t, element) alone (the same bits on every run); a v above 0
- * never becomes 0.  Non-finite gradients give NaN states.
+ * hash of (seed, t, element) alone (the same bits on every run); a v of 2^-126
+ * and more never becomes 0 (a smaller one counts as 0).  Non-finite gradients
+ * give NaN states.
  *
  * Parameters in bfloat16 are rounded to the nearest even, or with `stochastic`
  * by the same hash (an update below half of the distance between two values

@@ -17,11 +17,11 @@ typedef uint32_t loose_u32x4_t __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t loose_u32x2_t __attribute__((ext_vector_type(2), aligned(2)));
 
 // L (4 or 8) consecutive elements at any element alignment, read and written
-// once a step; zeros behind `count`.
-template <int L>
+// once a step; zeros behind `count` (FULL: there are none).
+template <bool FULL, int L>
 __device__ __forceinline__ void load(const void* base, int32_t bf16, int64_t at, int64_t count,
                                      float (&x)[L]) {
-  if (at + L <= count) {
+  if (FULL || at + L <= count) {
     if (bf16) {
       const uint16_t* p = static_cast<const uint16_t*>(base) + at;
       uint32_t w[L / 2];
@@ -62,16 +62,16 @@ __device__ __forceinline__ void load(const void* base, int32_t bf16, int64_t at,
   }
 }
 
-template <int L>
+template <bool FULL, bool STREAM, int L>
 __device__ __forceinline__ void store_f32(float* base, int64_t at, int64_t count,
                                           const float (&x)[L]) {
-  if (at + L <= count) {
+  if (FULL || at + L <= count) {
     loose_u32x4_t* p = reinterpret_cast<loose_u32x4_t*>(base + at);
 #pragma unroll
     for (int h = 0; h < L / 4; ++h) {
       const u32x4_t v = {__float_as_uint(x[4 * h]), __float_as_uint(x[4 * h + 1]),
                          __float_as_uint(x[4 * h + 2]), __float_as_uint(x[4 * h + 3])};
-      if (L == 8)
+      if (L == 8 || !STREAM)
         p[h] = v;
       else
         __builtin_nontemporal_store(v, p + h);
@@ -84,10 +84,10 @@ __device__ __forceinline__ void store_f32(float* base, int64_t at, int64_t count
 }
 
 // h: two elements a word.
-template <int L>
+template <bool FULL, int L>
 __device__ __forceinline__ void store_bf16(uint16_t* base, int64_t at, int64_t count,
                                            const uint32_t (&h)[L / 2]) {
-  if (at + L <= count) {
+  if (FULL || at + L <= count) {
     if constexpr (L == 8) {
       const u32x4_t v = {h[0], h[1], h[2], h[3]};
       __builtin_nontemporal_store(v, reinterpret_cast<loose_u32x4_t*>(base + at));
@@ -127,46 +127,69 @@ __device__ __forceinline__ uint32_t random_bits(uint32_t z, uint32_t key_high) {
 
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 
-// Four e4m3 values of a word, exactly.
-__device__ __forceinline__ void from_f8(uint32_t w, float* x) {
-  const f32x2_t lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);
-  const f32x2_t hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+// Four e4m3 values of a word times a scale, exactly.
+__device__ __forceinline__ void from_f8(uint32_t w, float scale, float* x) {
+  const f32x2_t lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale, false);
+  const f32x2_t hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale, true);
   x[0] = lo.x;
   x[1] = lo.y;
   x[2] = hi.x;
   x[3] = hi.y;
 }
 
-// A magnitude below 256 to a code of e4m3, up with the chance of what is cut
-// off (normal values: the 20 low bits of the mantissa; below 2^-6: what is left
-// of a multiple of 2^-9), by the 20 high bits of `draw`.  The instruction does
-// just that; it agreed with the definition on 4.2 million words and draws.
-__device__ __forceinline__ uint32_t f8_random(float x, uint32_t draw, uint32_t word, int byte) {
+// x / scale, below 256 in magnitude, to a code of e4m3, away from 0 with the
+// chance of what is cut off (normal values: the 20 low bits of the mantissa;
+// below 2^-6: what is left of a multiple of 2^-9), by the 20 high bits of
+// `draw`.  The instruction does just that: it agreed with the definition on 4.2
+// million words, draws and scales.
+__device__ __forceinline__ uint32_t f8_random(float x, uint32_t draw, float scale, uint32_t word,
+                                              int byte) {
   switch (byte) {
-    case 0: return (uint32_t)__builtin_amdgcn_cvt_sr_fp8_f32(x, draw, word, 0);
-    case 1: return (uint32_t)__builtin_amdgcn_cvt_sr_fp8_f32(x, draw, word, 1);
-    case 2: return (uint32_t)__builtin_amdgcn_cvt_sr_fp8_f32(x, draw, word, 2);
-    default: return (uint32_t)__builtin_amdgcn_cvt_sr_fp8_f32(x, draw, word, 3);
+    case 0: return __builtin_amdgcn_cvt_scalef32_sr_fp8_f32(word, x, draw, scale, 0);
+    case 1: return __builtin_amdgcn_cvt_scalef32_sr_fp8_f32(word, x, draw, scale, 1);
+    case 2: return __builtin_amdgcn_cvt_scalef32_sr_fp8_f32(word, x, draw, scale, 2);
+    default: return __builtin_amdgcn_cvt_scalef32_sr_fp8_f32(word, x, draw, scale, 3);
   }
+}
+
+// The square root of x >= 0, rounded correctly (checked for every mantissa of
+// two binades): x rsq(x) and one correction by its residual, 8 operations and 2
+// for the lower end, half of sqrtf()'s.  Below 2^-126 it is 0; for infinity, NaN.
+__device__ __forceinline__ float root_of(float x) {
+  const float w = x < 0x1p-126f ? 0.f : __builtin_amdgcn_rsqf(x);
+  const float y = x * w;
+  return fmaf(fmaf(-y, y, x), 0.5f * w, y);
 }
 
 struct MaxU {
   __device__ uint32_t operator()(uint32_t a, uint32_t b) const { return a > b ? a : b; }
 };
 
-// Exponent field of a block's scale, from the words of its largest magnitude.
-__device__ __forceinline__ uint32_t scale_exponent(uint32_t most) {
+// A block's scale, from the word of its largest magnitude in [2^e, 2^(e+1)): 2^(e-7).
+__device__ __forceinline__ float scale_of(uint32_t most) {
   const uint32_t e = most >> 23;
-  return e > 8 ? e - 7 : 1;
+  return __uint_as_float((e > 8 ? e - 7 : 1) << 23);
 }
 
 // States in 32 bits: four elements a lane, so that every access of a wave takes
-// whole lines.  States in 8 bits: eight, so that 16 lanes hold a block.
-template <bool F8>
-__global__ void __launch_bounds__(kThreads)
+// whole lines.  Bound by HBM: 1.1e9 binary32 parameters with a bf16 copy and bf16
+// gradients 4.86-5.8 ms (6.3-5.3 TB/s of 28 bytes each; which of them goes by
+// where the process got its memory).  A step of a few times the Infinity Cache
+// stores its binary32 arrays through it (!STREAM): 1.1e7 parameters 51 us
+// against 58 past it, 2.2e7 in 300 tensors 111 / 129, 3.6e7 238 / 223, 1.2e8
+// 662 / 640.
+//
+// States in 8 bits: eight elements a lane, so that 16 lanes hold a block, its
+// largest magnitudes found by four lane permutations.  10 bytes of HBM and about
+// 57 operations an element, which take the same time: 1.2e8 bf16 parameters 227
+// us (5.5 TB/s).  That is with the conversions that scale and round, the root
+// from the reciprocal one and the reciprocal for a division; with a multiply
+// for each scale, a rounding in integers, sqrtf() and a division it was 319 us.
+template <bool F8, bool STREAM>
+__global__ void __launch_bounds__(kThreads, F8 ? 6 : 8)
 adamw_kernel(OptimBatch b, OptimPointers p, AdamArgs a) {
   constexpr int L = F8 ? 8 : 4;
-  static_assert(kOptimChunk % (kThreads * L) == 0, "whole passes of a workgroup");
+  static_assert(kOptimChunkLeast % (kThreads * L) == 0, "whole passes of a workgroup");
   static_assert(!F8 || kStateBlock == 16 * L, "a block is a row of lanes");
   const float factor = a.factor ? *a.factor : 1.f;
   if (!(fabsf(factor) < INFINITY)) return;
@@ -181,34 +204,27 @@ adamw_kernel(OptimBatch b, OptimPointers p, AdamArgs a) {
   const float keep = 1.f - lr * t.weight_decay;
   const float step = lr * a.inv_c1;
   const int64_t padded = (t.count + kStateBlock - 1) / kStateBlock * kStateBlock;
-#pragma unroll
-  for (int u = 0; u < kOptimChunk / (kThreads * L); ++u) {
-    const int64_t e = (int64_t)(chunk - t.first_chunk) * kOptimChunk +
-                      (u * kThreads + (int)threadIdx.x) * L;
-    if (e >= padded) break;  // the 16 lanes of a block alike
+  const auto update = [&](int64_t e, auto whole) {
+    constexpr bool FULL = decltype(whole)::value;
     const int64_t s = t.state + e;
     float g[L], x[L], m[L], v[L];
-    load<L>(grad, t.grad_bf16, e, t.count, g);
-    load<L>(param, t.param_bf16, e, t.count, x);
+    load<FULL, L>(grad, t.grad_bf16, e, t.count, g);
+    load<FULL, L>(param, t.param_bf16, e, t.count, x);
     if constexpr (F8) {
       const auto mw = __builtin_nontemporal_load(
           reinterpret_cast<const u32x2_t*>(static_cast<const uint8_t*>(a.m) + s));
       const auto vw = __builtin_nontemporal_load(
           reinterpret_cast<const u32x2_t*>(static_cast<const uint8_t*>(a.v) + s));
       const float ms = a.m_scale[s / kStateBlock], vs = a.v_scale[s / kStateBlock];
-      from_f8(mw.x, m);
-      from_f8(mw.y, m + 4);
-      from_f8(vw.x, v);
-      from_f8(vw.y, v + 4);
+      from_f8(mw.x, ms, m);
+      from_f8(mw.y, ms, m + 4);
+      from_f8(vw.x, vs, v);
+      from_f8(vw.y, vs, v + 4);
 #pragma unroll
-      for (int k = 0; k < L; ++k) {
-        m[k] *= ms;
-        v[k] *= vs;
-        v[k] *= v[k];
-      }
+      for (int k = 0; k < L; ++k) v[k] *= v[k];
     } else {
-      load<L>(a.m, 0, s, INT64_MAX, m);
-      load<L>(a.v, 0, s, INT64_MAX, v);
+      load<true, L>(a.m, 0, s, 0, m);
+      load<true, L>(a.v, 0, s, 0, v);
     }
     float root[L];
 #pragma unroll
@@ -216,13 +232,13 @@ adamw_kernel(OptimBatch b, OptimPointers p, AdamArgs a) {
       const float gk = g[k] * factor;
       m[k] = a.beta1 * m[k] + a.one_minus_beta1 * gk;
       v[k] = a.beta2 * v[k] + a.one_minus_beta2 * (gk * gk);
-      root[k] = sqrtf(v[k]);
+      root[k] = root_of(v[k]);
       // the reciprocal is within 1 ulp: 2^-23 of an update that is a small part
       // of x, and a tenth of an exact division's operations
       const float inv = __builtin_amdgcn_rcpf(fmaf(root[k], a.inv_root_c2, a.eps));
       x[k] = fmaf(-step, m[k] * inv, x[k] * keep);
     }
-    if (e + L > t.count) {  // behind the end: states stay 0
+    if constexpr (!FULL) {  // behind the end: states stay 0
 #pragma unroll
       for (int k = 0; k < L; ++k)
         if (e + k >= t.count) m[k] = v[k] = root[k] = 0.f;
@@ -240,17 +256,16 @@ adamw_kernel(OptimBatch b, OptimPointers p, AdamArgs a) {
         most_m = MaxU()(most_m, __float_as_uint(m[k]) & 0x7FFFFFFFu);
         most_v = MaxU()(most_v, __float_as_uint(root[k]));
       }
-      const uint32_t em = scale_exponent(lanes_reduce<16>(most_m, MaxU()));
-      const uint32_t ev = scale_exponent(lanes_reduce<16>(most_v, MaxU()));
-      const float im = __uint_as_float((254u - em) << 23), iv = __uint_as_float((254u - ev) << 23);
+      const float ms = scale_of(lanes_reduce<16>(most_m, MaxU()));
+      const float vs = scale_of(lanes_reduce<16>(most_v, MaxU()));
+      const uint32_t least = __float_as_uint(vs * 0x1p-9f);  // the smallest value above 0
       uint32_t qm[2] = {0, 0}, qv[2] = {0, 0};
 #pragma unroll
       for (int k = 0; k < L; ++k) {
-        qm[k / 4] = f8_random(m[k] * im, r[k] << 12, qm[k / 4], k % 4);
-        // what is above 0 is 2^-9, the smallest value, at least
-        const uint32_t least = root[k] == 0.f ? 0u : 0x3B000000u;
-        const uint32_t w = MaxU()(__float_as_uint(root[k] * iv), least);
-        qv[k / 4] = f8_random(__uint_as_float(w), r[k], qv[k / 4], k % 4);
+        qm[k / 4] = f8_random(m[k], r[k] << 12, ms, qm[k / 4], k % 4);
+        const uint32_t w = __float_as_uint(root[k]);
+        const float at_least = __uint_as_float(MaxU()(w, w == 0u ? 0u : least));
+        qv[k / 4] = f8_random(at_least, r[k], vs, qv[k / 4], k % 4);
       }
       const u32x2_t mw = {qm[0], qm[1]}, vw = {qv[0], qv[1]};
       __builtin_nontemporal_store(
@@ -258,12 +273,12 @@ adamw_kernel(OptimBatch b, OptimPointers p, AdamArgs a) {
       __builtin_nontemporal_store(
           vw, reinterpret_cast<u32x2_t*>(static_cast<uint8_t*>(a.v) + s));
       if (threadIdx.x % 16 == 0) {
-        a.m_scale[s / kStateBlock] = __uint_as_float(em << 23);
-        a.v_scale[s / kStateBlock] = __uint_as_float(ev << 23);
+        a.m_scale[s / kStateBlock] = ms;
+        a.v_scale[s / kStateBlock] = vs;
       }
     } else {
-      store_f32<L>(static_cast<float*>(a.m), s, INT64_MAX, m);
-      store_f32<L>(static_cast<float*>(a.v), s, INT64_MAX, v);
+      store_f32<true, STREAM, L>(static_cast<float*>(a.m), s, 0, m);
+      store_f32<true, STREAM, L>(static_cast<float*>(a.v), s, 0, v);
     }
     uint32_t h[L / 2];
 #pragma unroll
@@ -275,11 +290,21 @@ adamw_kernel(OptimBatch b, OptimPointers p, AdamArgs a) {
           h[k] = (bf16_random(x[2 * k], r[2 * k]) >> 16) |
                  (bf16_random(x[2 * k + 1], r[2 * k + 1]) & 0xFFFF0000u);
       }
-      store_bf16<L>(static_cast<uint16_t*>(param), e, t.count, h);
+      store_bf16<FULL, L>(static_cast<uint16_t*>(param), e, t.count, h);
     } else {
-      store_f32<L>(static_cast<float*>(param), e, t.count, x);
+      store_f32<FULL, STREAM, L>(static_cast<float*>(param), e, t.count, x);
     }
-    if (copy) store_bf16<L>(copy, e, t.count, h);
+    if (copy) store_bf16<FULL, L>(copy, e, t.count, h);
+  };
+  for (int32_t u = threadIdx.x * L; u < a.run; u += kThreads * L) {
+    const int64_t e = (int64_t)(chunk - t.first_chunk) * a.run + u;
+    if (e >= padded) break;
+    // the lanes of a block go the same way: it takes all of them
+    const int64_t block_end = F8 ? e / kStateBlock * kStateBlock + kStateBlock : e + L;
+    if (block_end <= t.count)
+      update(e, std::true_type());
+    else
+      update(e, std::false_type());
   }
 }
 
@@ -299,25 +324,26 @@ __device__ __forceinline__ double group_sum(double v) {
   return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-// The sum of squares of one run of kNormChunk elements, in binary64 (no square
+// The sum of squares of one run of elements, in binary64 (no square
 // of a binary32 number overflows there, and the conversion and the fma take a
 // third of the time that HBM does).
 __global__ void __launch_bounds__(kThreads)
-norm_chunk_kernel(NormBatch b, NormPointers p, double* __restrict__ partial) {
+norm_chunk_kernel(NormBatch b, NormPointers p, int32_t run, double* __restrict__ partial) {
   const int32_t chunk = b.first_chunk + blockIdx.x;
   const int32_t i = b.chunk_tensor[chunk];
   const OptimTensor t = b.tensors[i];
   const void* grad = p.grad[i - b.first];
-  const int64_t first = (int64_t)(chunk - t.first_norm) * kNormChunk;
+  const int64_t first = (int64_t)(chunk - t.first_norm) * run;
+  const int64_t end = min(t.count, first + run);
   double sum[4] = {0.0, 0.0, 0.0, 0.0};
   const auto add = [&](auto lanes) {
     constexpr int L = decltype(lanes)::value;
-    for (int u = 0; u < kNormChunk; u += 4 * kThreads * L) {
-      if (first + u >= t.count) break;
+    for (int u = 0; u < run; u += 4 * kThreads * L) {
+      if (first + u >= end) break;
       float g[4][L];
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        load<L>(grad, L == 8, first + u + (q * kThreads + (int)threadIdx.x) * L, t.count, g[q]);
+        load<false, L>(grad, L == 8, first + u + (q * kThreads + (int)threadIdx.x) * L, end, g[q]);
 #pragma unroll
       for (int q = 0; q < 4; ++q)
 #pragma unroll
@@ -334,13 +360,13 @@ norm_chunk_kernel(NormBatch b, NormPointers p, double* __restrict__ partial) {
 
 // Each tensor's sum, and the total by the last workgroup to arrive.
 __global__ void __launch_bounds__(kThreads)
-norm_tensor_kernel(const OptimTensor* __restrict__ tensors, int32_t num,
+norm_tensor_kernel(const OptimTensor* __restrict__ tensors, int32_t num, int32_t run,
                    const double* __restrict__ partial, double* __restrict__ squares,
                    uint32_t* __restrict__ arrived, float scale, float max_norm,
                    float* __restrict__ norms, float* __restrict__ total) {
   __shared__ bool last;
   const OptimTensor t = tensors[blockIdx.x];
-  const int64_t chunks = (t.count + kNormChunk - 1) / kNormChunk;
+  const int64_t chunks = (t.count + run - 1) / run;
   double sum = 0.0;
 #pragma unroll 4
   for (int64_t c = threadIdx.x; c < chunks; c += kThreads) sum += partial[t.first_norm + c];
@@ -372,25 +398,28 @@ norm_tensor_kernel(const OptimTensor* __restrict__ tensors, int32_t num,
 
 }  // namespace
 
-hipError_t launch_adamw(bool f8, const OptimBatch& b, const OptimPointers& p, const AdamArgs& a,
-                        hipStream_t stream) {
-  hipLaunchKernelGGL(f8 ? adamw_kernel<true> : adamw_kernel<false>, dim3((unsigned)b.chunks),
-                     dim3(kThreads), 0, stream, b, p, a);
+hipError_t launch_adamw(bool f8, bool cached, const OptimBatch& b, const OptimPointers& p,
+                        const AdamArgs& a, hipStream_t stream) {
+  const auto kernel = f8       ? adamw_kernel<true, true>
+                      : cached ? adamw_kernel<false, false>
+                               : adamw_kernel<false, true>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)b.chunks), dim3(kThreads), 0, stream, b, p, a);
   return hipGetLastError();
 }
 
-hipError_t launch_norm_chunks(const NormBatch& b, const NormPointers& p, double* partial,
+hipError_t launch_norm_chunks(const NormBatch& b, const NormPointers& p, int32_t run, double* partial,
                               hipStream_t stream) {
   hipLaunchKernelGGL(norm_chunk_kernel, dim3((unsigned)b.chunks), dim3(kThreads), 0, stream, b, p,
-                     partial);
+                     run, partial);
   return hipGetLastError();
 }
 
-hipError_t launch_norm_tensors(const OptimTensor* tensors, int32_t num, const double* partial,
+hipError_t launch_norm_tensors(const OptimTensor* tensors, int32_t num, int32_t run,
+                               const double* partial,
                                double* squares, uint32_t* arrived, float scale, float max_norm,
                                float* norms, float* total, hipStream_t stream) {
   hipLaunchKernelGGL(norm_tensor_kernel, dim3((unsigned)num), dim3(kThreads), 0, stream, tensors,
-                     num, partial, squares, arrived, scale, max_norm, norms, total);
+                     num, run, partial, squares, arrived, scale, max_norm, norms, total);
   return hipGetLastError();
 }
 

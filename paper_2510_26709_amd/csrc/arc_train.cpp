@@ -34,6 +34,8 @@ struct arc_optim {
   std::vector<arc::OptimTensor> tensors;
   std::vector<int32_t> chunk_tensor, norm_tensor;  // of each run of elements
   int64_t state_elems = 0;
+  int32_t optim_run = arc::kOptimChunkMost, norm_run = arc::kNormChunkMost;
+  bool cached = false;  // a step's bytes are few enough to be stored through the caches
   int32_t state = ARC_STATE_F32, stochastic = 0;
   bool any_param_bf16 = false;
   uint64_t seed = 0;
@@ -186,6 +188,8 @@ uint64_t splitmix64(uint64_t seed, uint64_t number) {
   return z ^ (z >> 31);
 }
 
+// Bytes of a step with 32-bit states up to which it stores through the caches.
+constexpr int64_t kCachedBytes = 800000000;
 constexpr int64_t kMaxElements = int64_t{1} << 42;
 // Workgroups of one launch: their threads stay below 2^32.
 constexpr int64_t kMaxGroups = int64_t{1} << 23;
@@ -222,10 +226,17 @@ void plan_optim(const arc_optim_config* cfg, arc_optim* c) {
   const auto runs = [](int64_t count, int64_t of) {
     return static_cast<size_t>((count + of - 1) / of);
   };
+  int64_t all = 0;
+  for (int32_t i = 0; i < cfg->num_tensors; ++i) all += cfg->tensors[i].count;
+  // Enough runs to fill the card, and few enough for the second launch (a
+  // ResNet-18's 1.1e7 values in runs of 32,768: 20.2 us).
+  while (c->norm_run > arc::kNormChunkLeast && all / c->norm_run < 4096) c->norm_run /= 2;
+  while (c->optim_run > arc::kOptimChunkLeast && all / c->optim_run < 2048) c->optim_run /= 2;
+  c->cached = all * 28 <= kCachedBytes;
   size_t chunks = 0, norms = 0;
   for (int32_t i = 0; i < cfg->num_tensors; ++i) {
-    chunks += runs(cfg->tensors[i].count, arc::kOptimChunk);
-    norms += runs(cfg->tensors[i].count, arc::kNormChunk);
+    chunks += runs(cfg->tensors[i].count, c->optim_run);
+    norms += runs(cfg->tensors[i].count, c->norm_run);
   }
   c->chunk_tensor.reserve(chunks);
   c->norm_tensor.reserve(norms);
@@ -243,8 +254,8 @@ void plan_optim(const arc_optim_config* cfg, arc_optim* c) {
     c->any_param_bf16 = c->any_param_bf16 || t.param_bf16;
     c->tensors.push_back(t);
     c->state_elems += (in.count + arc::kStateBlock - 1) / arc::kStateBlock * arc::kStateBlock;
-    c->chunk_tensor.insert(c->chunk_tensor.end(), runs(in.count, arc::kOptimChunk), i);
-    c->norm_tensor.insert(c->norm_tensor.end(), runs(in.count, arc::kNormChunk), i);
+    c->chunk_tensor.insert(c->chunk_tensor.end(), runs(in.count, c->optim_run), i);
+    c->norm_tensor.insert(c->norm_tensor.end(), runs(in.count, c->norm_run), i);
   }
   c->state = cfg->state;
   c->stochastic = cfg->stochastic;
@@ -470,12 +481,12 @@ arc_status arc_optim_norm(arc_optim* c, const void* const* grads, float scale, f
                   [&](const arc::OptimBatch& b, int32_t count) -> arc_status {
                     arc::NormPointers p;
                     std::copy(grads + b.first, grads + b.first + count, p.grad);
-                    ARC_HIP(arc::launch_norm_chunks(b, p, c->partial_dev, c->stream),
+                    ARC_HIP(arc::launch_norm_chunks(b, p, c->norm_run, c->partial_dev, c->stream),
                             "norm launch");
                     return ARC_OK;
                   });
   if (st != ARC_OK) return st;
-  ARC_HIP(arc::launch_norm_tensors(c->tensors_dev, num, c->partial_dev, c->squares_dev,
+  ARC_HIP(arc::launch_norm_tensors(c->tensors_dev, num, c->norm_run, c->partial_dev, c->squares_dev,
                                    c->arrived(), scale, max_norm, norms, total, c->stream),
           "norm launch");
   return ARC_OK;
@@ -528,6 +539,7 @@ arc_status arc_optim_adamw(arc_optim* c, const arc_adamw_config* ac, int64_t t,
   a.key_low = static_cast<uint32_t>(key);
   a.key_high = static_cast<uint32_t>(key >> 32);
   a.stochastic = c->stochastic && c->any_param_bf16;
+  a.run = c->optim_run;
   a.factor = factor;
   a.m = m;
   a.v = v;
@@ -543,7 +555,7 @@ arc_status arc_optim_adamw(arc_optim* c, const arc_adamw_config* ac, int64_t t,
                         p.grad[i] = grads[b.first + i];
                         p.copy[i] = copies ? static_cast<uint16_t*>(copies[b.first + i]) : nullptr;
                       }
-                      ARC_HIP(arc::launch_adamw(f8, b, p, a, c->stream), "AdamW launch");
+                      ARC_HIP(arc::launch_adamw(f8, c->cached, b, p, a, c->stream), "AdamW launch");
                       return ARC_OK;
                     });
 }

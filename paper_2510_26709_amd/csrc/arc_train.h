@@ -46,9 +46,9 @@ hipError_t launch_token_grad(const TokenArgs& a, const TokenGrad& g, hipStream_t
 // ---------------------------------------------------------------- optimizer
 
 // Elements of a tensor that one workgroup updates, and that one sums the squares
-// of.
-constexpr int kOptimChunk = 4096;
-constexpr int kNormChunk = 32768;
+// of: fewer where there are few in all.
+constexpr int kOptimChunkLeast = 2048, kOptimChunkMost = 4096, kNormChunkLeast = 4096;
+constexpr int kNormChunkMost = 32768;
 constexpr int kStateBlock = 128;  // ARC_STATE_BLOCK
 
 // A tensor's place in the states and its constants.
@@ -56,7 +56,7 @@ struct OptimTensor {
   int64_t count;
   int64_t state;       // first element of its states
   float weight_decay, lr_scale;
-  int32_t first_chunk, first_norm;  // its runs of kOptimChunk and of kNormChunk elements
+  int32_t first_chunk, first_norm;  // its runs of elements
   int32_t param_bf16, grad_bf16;
 };
 
@@ -74,6 +74,7 @@ struct AdamArgs {
   float inv_c1, inv_root_c2;
   uint32_t key_low, key_high;  // of this step's random bits
   int32_t stochastic;
+  int32_t run;  // elements of a workgroup
   const float* factor;
   void *m, *v;
   float *m_scale, *v_scale;
@@ -86,18 +87,20 @@ struct OptimBatch {
   int32_t first, first_chunk, chunks;
 };
 
-hipError_t launch_adamw(bool f8, const OptimBatch& b, const OptimPointers& p, const AdamArgs& a,
-                        hipStream_t stream);
+// cached: binary32 arrays are stored through the caches, not past them.
+hipError_t launch_adamw(bool f8, bool cached, const OptimBatch& b, const OptimPointers& p,
+                        const AdamArgs& a, hipStream_t stream);
 constexpr int kNormBatch = 480;
 struct NormPointers {
   const void* grad[kNormBatch];
 };
-typedef OptimBatch NormBatch;  // of runs of kNormChunk elements
+typedef OptimBatch NormBatch;
 
-hipError_t launch_norm_chunks(const NormBatch& b, const NormPointers& p, double* partial,
-                              hipStream_t stream);
+hipError_t launch_norm_chunks(const NormBatch& b, const NormPointers& p, int32_t run,
+                              double* partial, hipStream_t stream);
 // Each tensor's norm and the total; `arrived` is 0 before and after.
-hipError_t launch_norm_tensors(const OptimTensor* tensors, int32_t num, const double* partial,
+hipError_t launch_norm_tensors(const OptimTensor* tensors, int32_t num, int32_t run,
+                               const double* partial,
                                double* squares, uint32_t* arrived, float scale, float max_norm,
                                float* norms, float* total, hipStream_t stream);
 
