@@ -172,12 +172,14 @@ __device__ __forceinline__ float scale_of(uint32_t most) {
 }
 
 // States in 32 bits: four elements a lane, so that every access of a wave takes
-// whole lines.  Bound by HBM: 1.1e9 binary32 parameters with a bf16 copy and bf16
-// gradients 4.86-5.8 ms (6.3-5.3 TB/s of 28 bytes each; which of them goes by
-// where the process got its memory).  A step of a few times the Infinity Cache
+// whole lines, and the loads of four passes ahead of the first update.  Bound by
+// HBM: 1.2e8 binary32 parameters 600 us, bf16 ones with 32-bit states 469 (5.8
+// TB/s; one pass at a time at twice the occupancy 643 and 525); 1.1e9 binary32
+// ones with a bf16 copy and bf16 gradients 4.7 to 5.6 ms, by where the process
+// got its memory.  A step of a few times the Infinity Cache
 // stores its binary32 arrays through it (!STREAM): 1.1e7 parameters 51 us
 // against 58 past it, 2.2e7 in 300 tensors 111 / 129, 3.6e7 238 / 223, 1.2e8
-// 662 / 640.
+// 662 / 640 (one pass at a time).
 //
 // States in 8 bits: eight elements a lane, so that 16 lanes hold a block, its
 // largest magnitudes found by four lane permutations.  10 bytes of HBM and about
@@ -186,7 +188,7 @@ __device__ __forceinline__ float scale_of(uint32_t most) {
 // from the reciprocal one and the reciprocal for a division; with a multiply
 // for each scale, a rounding in integers, sqrtf() and a division it was 319 us.
 template <bool F8, bool STREAM>
-__global__ void __launch_bounds__(kThreads, F8 ? 6 : 8)
+__global__ void __launch_bounds__(kThreads, F8 ? 6 : 4)
 adamw_kernel(OptimBatch b, OptimPointers p, AdamArgs a) {
   constexpr int L = F8 ? 8 : 4;
   static_assert(kOptimChunkLeast % (kThreads * L) == 0, "whole passes of a workgroup");
@@ -204,10 +206,10 @@ adamw_kernel(OptimBatch b, OptimPointers p, AdamArgs a) {
   const float keep = 1.f - lr * t.weight_decay;
   const float step = lr * a.inv_c1;
   const int64_t padded = (t.count + kStateBlock - 1) / kStateBlock * kStateBlock;
-  const auto update = [&](int64_t e, auto whole) {
+  const auto fetch = [&](int64_t e, auto whole, float (&g)[L], float (&x)[L], float (&m)[L],
+                         float (&v)[L]) {
     constexpr bool FULL = decltype(whole)::value;
     const int64_t s = t.state + e;
-    float g[L], x[L], m[L], v[L];
     load<FULL, L>(grad, t.grad_bf16, e, t.count, g);
     load<FULL, L>(param, t.param_bf16, e, t.count, x);
     if constexpr (F8) {
@@ -226,6 +228,11 @@ adamw_kernel(OptimBatch b, OptimPointers p, AdamArgs a) {
       load<true, L>(a.m, 0, s, 0, m);
       load<true, L>(a.v, 0, s, 0, v);
     }
+  };
+  const auto finish = [&](int64_t e, auto whole, float (&g)[L], float (&x)[L], float (&m)[L],
+                          float (&v)[L]) {
+    constexpr bool FULL = decltype(whole)::value;
+    const int64_t s = t.state + e;
     float root[L];
 #pragma unroll
     for (int k = 0; k < L; ++k) {
@@ -296,8 +303,30 @@ adamw_kernel(OptimBatch b, OptimPointers p, AdamArgs a) {
     }
     if (copy) store_bf16<FULL, L>(copy, e, t.count, h);
   };
+  const auto update = [&](int64_t e, auto whole) {
+    float g[L], x[L], m[L], v[L];
+    fetch(e, whole, g, x, m, v);
+    finish(e, whole, g, x, m, v);
+  };
+  const int64_t first = (int64_t)(chunk - t.first_chunk) * a.run;
+  if constexpr (!F8) {
+    // Whole runs: the loads of four passes ahead of the first update.
+    constexpr int U = 4;
+    if (a.run == U * kThreads * L && first + a.run <= t.count) {
+      float g[U][L], x[U][L], m[U][L], v[U][L];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        fetch(first + (u * kThreads + (int)threadIdx.x) * L, std::true_type(), g[u], x[u], m[u],
+              v[u]);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        finish(first + (u * kThreads + (int)threadIdx.x) * L, std::true_type(), g[u], x[u], m[u],
+               v[u]);
+      return;
+    }
+  }
   for (int32_t u = threadIdx.x * L; u < a.run; u += kThreads * L) {
-    const int64_t e = (int64_t)(chunk - t.first_chunk) * a.run + u;
+    const int64_t e = first + u;
     if (e >= padded) break;
     // the lanes of a block go the same way: it takes all of them
     const int64_t block_end = F8 ? e / kStateBlock * kStateBlock + kStateBlock : e + L;
