@@ -194,7 +194,11 @@ class AdamW(_Bound):
                     x = torch.zeros(n, dtype=torch.uint8 if dtype.itemsize == 1 else dtype,
                                     device=self.device).view(dtype)
             setattr(self, name, x)
-        self._starts = np.cumsum([0] + self.sizes[:-1], dtype=np.uint64) if num else None
+        self._states = [x if x is None else x.data_ptr()
+                        for x in (self.m, self.v, self.m_scale, self.v_scale)]
+        starts = np.cumsum([0] + self.sizes[:-1], dtype=np.uint64)
+        self._starts = {2: starts * np.uint64(2), 4: starts * np.uint64(4)}  # in bytes
+        self._copy = [torch.bfloat16] * num
         self._table = {k: np.zeros(num, dtype=np.uint64) for k in ("param", "grad", "copy")}
         self._args = {k: ctypes.c_void_p(v.ctypes.data) for k, v in self._table.items()}
         self._flat = sum(self.sizes)
@@ -206,8 +210,7 @@ class AdamW(_Bound):
             if dtypes.count(dtypes[0]) != len(dtypes):
                 raise ValueError(f"{key}: one flat tensor holds one dtype")
             self._check(key, x, dtypes[0], self._flat)
-            np.multiply(self._starts, np.uint64(x.element_size()), out=table)
-            table += np.uint64(x.data_ptr())
+            np.add(self._starts[dtypes[0].itemsize], np.uint64(x.data_ptr()), out=table)
         else:
             if len(x) != len(table):
                 raise ValueError(f"{key}: need {len(table)} tensors, got {len(x)}")
@@ -239,9 +242,8 @@ class AdamW(_Bound):
             self.ctx, arc_adamw_config(lr, beta1, beta2, eps), t,
             self._pointers("param", params, self._param),
             self._pointers("grad", grads, self._grad),
-            None if copies is None else self._pointers("copy", copies,
-                                                       [torch.bfloat16] * len(self.sizes)),
-            factor, self.m, self.v, self.m_scale, self.v_scale)
+            None if copies is None else self._pointers("copy", copies, self._copy),
+            factor, *self._states)
 
     def close(self):
         if getattr(self, "ctx", None):
