@@ -346,7 +346,7 @@ typedef struct arc_tokens arc_tokens;
  *   max_rows  most rows of one call, 1 .. 2^31 - 1
  *   dtype     arc_dtype of the logits and of their gradient
  *   top       alternatives of each row, 0 .. min(V, ARC_MAX_TOP)
- *   scale     what logits are multiplied with (1 / temperature), finite, > 0
+ *   scale     what logits are multiplied with (1 / temperature), 2^-64 .. 2^64
  */
 typedef struct {
   int64_t vocab;
@@ -375,7 +375,9 @@ arc_status arc_tokens_score(arc_tokens *ctx, int64_t rows, const void *logits, i
                             int32_t *top_ids, float *top_logp);
 
 /*
- * The gradient of scored rows.  lse and entropy are arc_tokens_score's of the
+ * The gradient of scored rows, with p = exp(z - lse) for the binary32 lse (off
+ * by |lse| 2^-24 of itself: logits of 10^5 and more want arc_tokens_loss, which
+ * holds the normaliser relative to the largest logit).  lse and entropy are arc_tokens_score's of the
  * same logits (entropy may be NULL where d_entropy is); d_logp, d_entropy and
  * d_lse are the upstream gradients [rows], each NULL for zeros (targets may be
  * NULL where d_logp is).  grad has rows of `grad_stride` >= V elements; it may

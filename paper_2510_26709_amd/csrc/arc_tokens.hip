@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <type_traits>
 
 #include "arc_device.h"
@@ -13,15 +14,26 @@
 namespace arc {
 namespace {
 
-constexpr int kMaxTop = 32;           // ARC_MAX_TOP
-constexpr int64_t kSplitRows = 1024;  // calls of more rows give each a workgroup
-constexpr int64_t kSplitParts = 4096;
-constexpr int64_t kMostPieces = 16;   // their alternatives fit the joining workgroup's list
+constexpr int kMaxTop = 32;                  // ARC_MAX_TOP
 constexpr int64_t kRowsPerLaunch = 1 << 20;  // threads of a launch stay below 2^32
+
+// Few rows are split into pieces of 2048 chunks, a batch of loads for each of
+// 512 threads: at most 16 of them, whose alternatives fit the joining
+// workgroup's list, and as many as fill the card.  One row of 32,000 bf16 without
+// / with 5 alternatives 4.7 / 8.0 us (pieces of 1024: 4.4 / 7.9), 24 of 50,257
+// binary32 with 20 12.1 (15.2), 100 of 50,257 bf16 with 5 11.9 (12.6).
 constexpr int kSplitThreads = 512;
+constexpr int64_t kPieceChunks = 4 * kSplitThreads, kMostPieces = 16, kSplitParts = 1024;
+
 // Chunks of a row up to which workgroups of 64, 256 and 512 threads take it
 // (above: 1024).  The same with and without alternatives, so that a row's sums
-// have the same bits.
+// have the same bits.  us at 64 / 256 / 512 / 1024 threads, without and with
+// alternatives: 30,000 rows of 4000 bf16 (500 chunks) 42 / 56 / 92 / 150 and 52 /
+// 97 / 200 / 391, 20,000 of 8000 (1000) 55 / 53 / 77 / 137 and 67 / 80 / 141 /
+// 301, 8753 of 18,560 (2320) 60 / 59 / 63 / 78 and 72 / 65 / 81 / 141, 8192 of
+// 32,000 (4000) 88 / 86 / 83 / 93 and 110 / 100 / 99 / 157, 4000 of 100,000
+// (12,500) 135 / 138 / 131 / 126 and 224 / 157 / 148 / 156, 2000 of 150,000
+// binary32 (37,500) 186 / 201 / 195 / 185 and 400 / 240 / 225 / 210.
 constexpr int64_t kRow64 = 1200, kRow256 = 3300, kRow512 = 12520;
 
 // ---------------------------------------------------------------------------
@@ -209,8 +221,9 @@ __device__ __forceinline__ float key_logit(uint64_t key) {
   return word_logit((uint32_t)(key >> 32));
 }
 
-// A bound that at least k of the wave's 64 values reach, and k + 3 at most
-// where that can be: bits of the k-th largest from the top, counting.
+// A bound that at least k of the wave's 64 values reach (or all that are above
+// -infinity), and k + 3 at most where that can be: bits of the k-th largest from
+// the top, counting.
 __device__ __forceinline__ float kth_bound(float v, int32_t k) {
   const uint32_t key = order_word(v);
   uint32_t bound = 0;
@@ -220,8 +233,8 @@ __device__ __forceinline__ float kth_bound(float v, int32_t k) {
     if (n >= k) bound |= bit;
     if (n >= k && n <= k + 3) break;
   }
-  const uint32_t nothing = 0x007FFFFFu;  // -infinity's
-  return bound <= nothing ? -INFINITY : word_logit(bound);
+  // not -infinity, which is masked, but what is next to it
+  return fmaxf(word_logit(bound < 0x00800000u ? 0x00800000u : bound), -FLT_MAX);
 }
 
 template <bool BF16, int W>
@@ -364,6 +377,10 @@ __device__ __forceinline__ RowResult finish_row(const TokenArgs& a, const TokenS
   if (threadIdx.x == 0) {
     if (out.lse) out.lse[i] = lse;
     if (out.entropy) out.entropy[i] = r.empty ? 0.f : r.log_total - s.spread * kLn2 / s.total;
+    if (out.sums) {
+      out.sums[2 * i] = s.most;
+      out.sums[2 * i + 1] = s.total;
+    }
     if (out.logp) out.logp[i] = y < 0 ? 0.f : y >= a.vocab ? NAN : r.logp(xy);
   }
   return r;
@@ -456,40 +473,99 @@ token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_c
     }
     __syncthreads();
   }
-  const int32_t n = TOP ? sh.found : 0;
-  const bool overflow = TOP && (n > kCandidates<W> || sh.listed > kListed<W>);
-
-  // Too many for the list (many equal ones, or the largest sit in few threads'
-  // chunks): the
-  // row's keys one after the other, each the largest below the one before.
-  const auto one_by_one = [&](const auto& write) {
-    uint64_t before = ~0ull;
-    for (int32_t r = 0; r < k; ++r) {
-      uint64_t key = 0;
-      const auto look = [&](float x, int32_t j) {
-        const uint64_t q = rank_key(x, j);
-        if (q < before && q > key) key = q;
-      };
-      for (int32_t q = first + threadIdx.x; q < end; q += W) {
+  int32_t n = TOP ? sh.found : 0;
+  bool one_by_one = false;
+  if constexpr (TOP) {
+    // All elements of the piece, a chunk a thread, in the order of the tokens but
+    // for the single ones.
+    const auto each_chunk = [&](int32_t from, int32_t to, const auto& look) {
+      for (int32_t q = from + threadIdx.x; q < to; q += W) {
         float x[S::C];
         unpack<BF16>(body[q], x);
 #pragma unroll
         for (int e = 0; e < S::C; ++e) look(x[e], shape.head + q * S::C + e);
       }
+    };
+    const auto each_edge = [&](const auto& look) {
       if (edges && (int)threadIdx.x < shape.head + shape.tail) {
         const int32_t j = shape.edge(threadIdx.x, V);
         look(element<BF16>(row, j), j);
       }
-      key = lanes_reduce<64>(key, MaxKey());
+    };
+    const auto add = [&](float x, int32_t j) {
+      const int32_t at = atomicAdd(&sh.found, 1);
+      if (at < kCandidates<W>) sh.found_keys[at] = rank_key(x, j);
+    };
+    if (n > kCandidates<W> || sh.listed > kListed<W>) {
+      // Too many for the lists: as a rule equal ones (a mask of the type's lowest
+      // value, logits of a head of zeros).  What is above tau, then as many of
+      // those at tau as are wanted, from the first token on.
       __syncthreads();
-      if (threadIdx.x % kWave == 0) sh.best[threadIdx.x / kWave] = key;
+      for (int q = threadIdx.x; q < kCandidates<W>; q += W) sh.found_keys[q] = 0;
+      if (threadIdx.x == 0) sh.found = 0;
       __syncthreads();
-      key = sh.best[0];
-      for (int w = 1; w < S::kWaves; ++w) key = MaxKey()(key, sh.best[w]);
-      if (threadIdx.x == 0) write(r, key);
-      before = key;
+      const auto above = [&](float x, int32_t j) {
+        if (x > tau) add(x, j);
+      };
+      each_chunk(first, end, above);
+      each_edge(above);
+      __syncthreads();
+      n = sh.found;
+      // few threads' chunks hold the largest: the keys one after the other
+      one_by_one = n > kCandidates<W> / 2;
+      if (n < k) {
+        const auto at_tau = [&](float x, int32_t j) {
+          if (x == tau) add(x, j);
+        };
+        constexpr int32_t kSome = kCandidates<W> / 2 / S::C - 1;  // with the single ones half the list
+        each_edge(at_tau);
+        for (int32_t from = first; from < end; from += kSome) {
+          each_chunk(from, min(end, from + kSome), at_tau);
+          __syncthreads();
+          n = sh.found;
+          __syncthreads();
+          if (n >= k + 8) break;  // the single ones may be behind those still to come
+        }
+        __syncthreads();
+        n = sh.found;
+      }
+    } else if (n < k) {
+      // Fewer than k that are not masked (tau is above -infinity): among the
+      // piece's first k tokens are as many masked ones as are wanted.
+      __syncthreads();
+      const auto masked = [&](float x, int32_t j) {
+        if (x == -INFINITY) add(x, j);
+      };
+      each_chunk(first, min(end, first + (k + S::C - 1) / S::C), masked);
+      each_edge(masked);
+      __syncthreads();
+      n = sh.found;
     }
-  };
+    if (one_by_one) {  // each key the largest below the one before
+      uint64_t before = ~0ull;
+      for (int32_t r = 0; r < k; ++r) {
+        uint64_t key = 0;
+        const auto look = [&](float x, int32_t j) {
+          const uint64_t q = rank_key(x, j);
+          if (q < before && q > key) key = q;
+        };
+        each_chunk(first, end, look);
+        each_edge(look);
+        key = lanes_reduce<64>(key, MaxKey());
+        __syncthreads();
+        if (threadIdx.x % kWave == 0) sh.best[threadIdx.x / kWave] = key;
+        __syncthreads();
+        key = sh.best[0];
+        for (int w = 1; w < S::kWaves; ++w) key = MaxKey()(key, sh.best[w]);
+        if (threadIdx.x == 0) sh.found_keys[r] = key;
+        before = key;
+      }
+      n = k;
+      __syncthreads();
+      if ((int)threadIdx.x >= k && threadIdx.x < 40) sh.found_keys[threadIdx.x] = 0;
+      __syncthreads();
+    }
+  }
 
   if (pieces == 1) {
     const RowResult r = finish_row(a, out, i, s, y, given);
@@ -500,8 +576,6 @@ token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_c
     };
     if (r.none) {
       if ((int)threadIdx.x < k) write(threadIdx.x, 0);
-    } else if (overflow) {
-      one_by_one(write);
     } else {
       S::order(sh, n, k, write);
     }
@@ -516,12 +590,8 @@ token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_c
   }
   if (k) {
     const auto write = [&](int32_t rank, uint64_t key) { share_store(&part->top[rank], key); };
-    if (overflow) {
-      one_by_one(write);
-    } else {
-      if ((int)threadIdx.x >= n && (int)threadIdx.x < k) write(threadIdx.x, 0);
-      S::order(sh, n, k, write);
-    }
+    if ((int)threadIdx.x >= n && (int)threadIdx.x < k) write(threadIdx.x, 0);
+    S::order(sh, n, k, write);
   }
   // The last workgroup of a row to arrive joins the pieces: every wave's part
   // has been written before the barrier, and the count goes up behind it.
@@ -636,8 +706,9 @@ __device__ __forceinline__ void store_element(void* row, int32_t j, float d) {
 constexpr int kGradThreads = 256;
 constexpr int kGradChunks = 4;  // of a thread, in flight
 
-// One workgroup for each run of kGradThreads * kGradChunks chunks of a row.
-template <bool BF16>
+// One workgroup for each run of kGradThreads * kGradChunks chunks of a row.  SUMS:
+// from the row's sums, as token_loss_kernel does.
+template <bool BF16, bool SUMS>
 __global__ void __launch_bounds__(kGradThreads)
 token_grad_kernel(TokenArgs a, TokenGrad g, int32_t tiles) {
   constexpr int C = kChunk<BF16>;
@@ -647,12 +718,21 @@ token_grad_kernel(TokenArgs a, TokenGrad g, int32_t tiles) {
   void* to = const_cast<void*>(row_at<BF16>(g.grad, i * g.stride));
   const RowShape<BF16> shape(row, V);
   const Words16* body = shape.body(row);
-  const float lse = g.lse[i];
-  const GradRow r = grad_row(a, g, i, g.d_entropy ? g.entropy[i] : 0.f, lse == -INFINITY);
+  const float most = SUMS ? g.sums[2 * i] : 0.f, total = SUMS ? g.sums[2 * i + 1] : 1.f;
+  const float lse = SUMS ? 0.f : g.lse[i];
+  const bool empty = SUMS ? total == 0.f : lse == -INFINITY;
+  const GradRow r = grad_row(a, g, i, g.d_entropy ? g.entropy[i] : 0.f, empty);
+  const float c = a.scale * kLog2e;
+  const Reference ref = reference(most, c);
+  const float B2 = r.B * kLn2 / total, A2 = r.A / total - B2 * (logf(total) * kLog2e);
   const auto one = [&](float x) {
+    if (r.zero) return 0.f;
+    if constexpr (SUMS) {
+      const float t = fmaf(ref.far ? far_logit(x, most) : x, c, -ref.R);
+      return __builtin_amdgcn_exp2f(t) * fmaf(B2, fmaxf(t, kFarBelow), A2);
+    }
     const float lp = fmaf(x, a.scale, -lse);
-    const float p = __builtin_amdgcn_exp2f(lp * kLog2e);
-    return r.zero ? 0.f : p * fmaf(r.B, fmaxf(lp, kNoWeight), r.A);
+    return __builtin_amdgcn_exp2f(lp * kLog2e) * fmaf(r.B, fmaxf(lp, kNoWeight), r.A);
   };
   Words16 raw[kGradChunks];
   const int32_t k0 = tile * (kGradThreads * kGradChunks) + threadIdx.x;
@@ -771,9 +851,11 @@ token_loss_kernel(TokenArgs a, TokenScores out, TokenGrad g) {
   const RowResult res = finish_row(a, out, i, s, y, given);
   const float H = res.empty ? 0.f : res.log_total - s.spread * kLn2 / s.total;
   const GradRow r = grad_row(a, g, i, H, res.empty);
-  const float shift = ref.R + res.log_total * kLog2e;
-  const float B = r.B * kLn2;  // of logarithms to the base 2
-  // A row's gradient is zero, or p A, or p (A + B t): 1, 9.5 or 11.5 operations an
+  // p (A + B log p) with p = 2^t / total: 2^t (A' + B' t).  (t less the logarithm
+  // of the total would be rounded as R is, however large.)
+  const float B = r.B * kLn2 / s.total;
+  const float A = r.A / s.total - B * (res.log_total * kLog2e);
+  // A row's gradient is zero, or p A, or p (A + B log p): 1, 9.5 or 11.5 operations an
   // element beside the unpacking, and the row's whole workgroup does one of them.
   const auto emit = [&](const auto& one) {
     int32_t thread = threadIdx.x;
@@ -799,33 +881,30 @@ token_loss_kernel(TokenArgs a, TokenScores out, TokenGrad g) {
     }
     if (edge) store_element<BF16>(to, edge_j, one(edge_x) + (edge_j == r.y ? r.given : 0.f));
   };
-  const auto log2_p = [&](float x) { return fmaf(x, c, -shift); };
+  const auto power = [&](float x) { return fmaf(x, c, -ref.R); };
   if (r.zero) {
     emit([](float) { return 0.f; });
-  } else if (B == 0.f) {
-    emit([&](float x) { return __builtin_amdgcn_exp2f(log2_p(x)) * r.A; });
+  } else if (r.B == 0.f) {
+    emit([&](float x) { return __builtin_amdgcn_exp2f(power(x)) * A; });
   } else {
     emit([&](float x) {
-      const float t = log2_p(x);
-      return __builtin_amdgcn_exp2f(t) * fmaf(B, fmaxf(t, kFarBelow), r.A);
+      const float t = power(x);
+      return __builtin_amdgcn_exp2f(t) * fmaf(B, fmaxf(t, kFarBelow), A);
     });
   }
 }
 
 }  // namespace
 
-size_t token_workspace_bytes(int64_t vocab, int64_t max_rows) {
-  (void)vocab;
-  const int64_t rows = max_rows < kSplitRows ? max_rows : kSplitRows;
-  return (size_t)(kSplitParts * sizeof(TokenPart) + rows * sizeof(uint32_t));
+size_t token_workspace_bytes() {
+  return (size_t)kSplitParts * (sizeof(TokenPart) + sizeof(uint32_t));
 }
 
 // Pieces of a row of that many chunks, for few rows.
 static int32_t row_pieces(int64_t rows, int64_t chunks) {
-  if (rows > kSplitRows) return 1;
-  int64_t p = (chunks + kSplitThreads * 4 - 1) / (kSplitThreads * 4);  // a batch a thread
-  p = std::min<int64_t>({p, kMostPieces, 1024 / rows, kSplitParts / rows});
-  return static_cast<int32_t>(std::max<int64_t>(p, 1));
+  const int64_t p = (chunks + kPieceChunks - 1) / kPieceChunks;
+  return static_cast<int32_t>(
+      std::max<int64_t>(std::min<int64_t>({p, kMostPieces, kSplitParts / rows}), 1));
 }
 
 // Calls launch(args, outputs, gradient) for runs of at most kRowsPerLaunch rows.
@@ -846,6 +925,8 @@ static void each_rows(const TokenArgs& a, const TokenScores& out, const TokenGra
       o.top_ids += lo * a.top;
       o.top_logp += lo * a.top;
     }
+    if (o.sums) o.sums += 2 * lo;
+    if (h.sums) h.sums += 2 * lo;
     for (const float** p : {&h.lse, &h.entropy, &h.d_logp, &h.d_entropy, &h.d_lse})
       if (*p) *p += lo;
     h.grad = static_cast<char*>(g.grad) + lo * g.stride * bytes;
@@ -896,7 +977,10 @@ hipError_t launch_token_grad(const TokenArgs& a, const TokenGrad& g, hipStream_t
   const int32_t least_one = tiles > 0 ? tiles : 1;
   const int64_t most = (int64_t{1} << 23) / least_one > 0 ? (int64_t{1} << 23) / least_one : 1;
   each_rows(a, {}, g, most, [&](const TokenArgs& b, const TokenScores&, const TokenGrad& h) {
-    hipLaunchKernelGGL(a.bf16 ? token_grad_kernel<true> : token_grad_kernel<false>,
+    hipLaunchKernelGGL(h.sums ? (a.bf16 ? token_grad_kernel<true, true>
+                                        : token_grad_kernel<false, true>)
+                              : (a.bf16 ? token_grad_kernel<true, false>
+                                        : token_grad_kernel<false, false>),
                        dim3((unsigned)(b.rows * least_one)), dim3(kGradThreads), 0, stream, b, h,
                        least_one);
   });

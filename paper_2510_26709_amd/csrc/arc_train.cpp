@@ -21,7 +21,7 @@ struct arc_tokens {
   hipStream_t stream = nullptr;
   int device = 0;
   void* workspace = nullptr;
-  float* row_values = nullptr;  // lse and entropy of a loss whose caller wants neither
+  float* row_values = nullptr;  // between a loss's two launches: sums, then entropies
 
   void release() {
     (void)hipStreamSynchronize(stream);
@@ -312,8 +312,8 @@ arc_status arc_tokens_create(const arc_tokens_config* cfg, void* hip_stream, arc
     return fail(ARC_ERR_INVALID, "dtype must be ARC_DTYPE_F32 or ARC_DTYPE_BF16");
   if (cfg->top < 0 || cfg->top > ARC_MAX_TOP || cfg->top > cfg->vocab)
     return fail(ARC_ERR_INVALID, "top must be in 0..min(vocab, ARC_MAX_TOP)");
-  if (!(cfg->scale > 0.f) || !finite(cfg->scale))
-    return fail(ARC_ERR_INVALID, "scale must be finite and > 0");
+  if (!(cfg->scale >= 0x1p-64f && cfg->scale <= 0x1p64f))
+    return fail(ARC_ERR_INVALID, "scale must be in 2^-64..2^64");
   if (cfg->reserved != 0) return fail(ARC_ERR_INVALID, "reserved must be 0");
   arc_tokens* c = new (std::nothrow) arc_tokens();
   if (c == nullptr) return fail(ARC_ERR_NOMEM, "host allocation failed");
@@ -323,7 +323,7 @@ arc_status arc_tokens_create(const arc_tokens_config* cfg, void* hip_stream, arc
   c->top = cfg->top;
   c->scale = cfg->scale;
   c->stream = static_cast<hipStream_t>(hip_stream);
-  const size_t bytes = arc::token_workspace_bytes(c->vocab, c->max_rows);
+  const size_t bytes = arc::token_workspace_bytes();
   hipError_t e = hipGetDevice(&c->device);
   if (e == hipSuccess) {
     e = hipMalloc(&c->workspace, bytes);
@@ -331,7 +331,7 @@ arc_status arc_tokens_create(const arc_tokens_config* cfg, void* hip_stream, arc
   }
   if (e == hipSuccess) {
     e = hipMalloc(reinterpret_cast<void**>(&c->row_values),
-                  static_cast<size_t>(c->max_rows) * 2 * sizeof(float));
+                  static_cast<size_t>(c->max_rows) * 3 * sizeof(float));
     if (e != hipSuccess) c->row_values = nullptr;
   }
   if (e == hipSuccess) e = hipMemset(c->workspace, 0, bytes);
@@ -399,9 +399,9 @@ arc_status arc_tokens_loss(arc_tokens* c, int64_t rows, const void* logits, int6
     ARC_HIP(e, "token loss launch");
     return ARC_OK;
   }
-  if (lse == nullptr) out.lse = c->row_values;
-  if (entropy == nullptr) out.entropy = c->row_values + c->max_rows;
-  g.lse = out.lse;
+  out.sums = c->row_values;
+  if (entropy == nullptr) out.entropy = c->row_values + 2 * c->max_rows;
+  g.sums = out.sums;
   g.entropy = out.entropy;
   ARC_HIP(arc::launch_token_score(a, out, c->workspace, c->stream), "token score launch");
   ARC_HIP(arc::launch_token_grad(a, g, c->stream), "token gradient launch");

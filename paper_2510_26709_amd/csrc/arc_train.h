@@ -23,6 +23,7 @@ struct TokenScores {
   float *logp = nullptr, *entropy = nullptr, *lse = nullptr;
   int32_t* top_ids = nullptr;
   float* top_logp = nullptr;
+  float* sums = nullptr;  // for a gradient that follows: each row's largest logit and its total
 };
 
 struct TokenGrad {
@@ -30,11 +31,12 @@ struct TokenGrad {
   const float *d_logp = nullptr, *d_entropy = nullptr, *d_lse = nullptr;
   void* grad = nullptr;
   int64_t stride = 0;
+  const float* sums = nullptr;  // TokenScores' instead of lse: not rounded at its size
 };
 
 // Bytes that launch_token_score's workspace needs, zeroed before its first use;
 // it leaves the part that has to be zero so.
-size_t token_workspace_bytes(int64_t vocab, int64_t max_rows);
+size_t token_workspace_bytes();
 hipError_t launch_token_score(const TokenArgs& a, const TokenScores& out, void* workspace,
                               hipStream_t stream);
 // Both in one pass, where a workgroup can hold a row (false: it cannot, and

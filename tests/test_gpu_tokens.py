@@ -259,6 +259,52 @@ def test_masked_and_non_finite(V, dtype):
     check_all(x[:10], y[:10], 0.5, dtype, top=8)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [40, 700, 9001, 50257, 150_001])
+@pytest.mark.parametrize("mask", ["infinity", "lowest", "zero"])
+def test_fewer_live_tokens_than_alternatives(V, mask, dtype):
+    """The alternatives that are left are masked tokens, from the first one on."""
+    gen = torch.Generator().manual_seed(V)
+    value = {"infinity": -math.inf, "lowest": torch.finfo(torch.bfloat16).min, "zero": 0.0}[mask]
+    x = torch.full((6, V), value)
+    for row, live in enumerate(([], [V - 1], [0], [0, 1, 2, V // 2], list(range(0, V, V // 13)),
+                                list(range(V - 31, V)))):
+        x[row, live] = torch.rand(len(live), generator=gen) + 1
+    y = torch.tensor([0, V - 1, 0, 2, 0, V - 1]).cuda()
+    for pad, shift in ((0, 0), (1, 1)):
+        check_score(place(x, dtype, pad, shift), y, 1.0, 32, dtype)
+        check_score(place(x, dtype, pad, shift), y, 1.0, 5, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", [1e8, 1.488e9, 3e9, 1e20, 1e37])
+@pytest.mark.parametrize("V", [3000, 100_001])
+def test_logits_far_from_zero(V, size, dtype):
+    gen = torch.Generator().manual_seed(7)
+    x = torch.randn(6, V, generator=gen)
+    x[0] = size
+    x[1] = -size
+    x[2] = size * (1 + x[2] * 1e-3)
+    x[3] = -size * (1 + x[3] * 1e-3)
+    x[4, ::3] = -size
+    x[5] = size * x[5].sign()
+    x, y = place(x, dtype), tokens(6, V, 9)
+    got, want = check_score(x, y, 1.0, 9, dtype)
+    # the loss alone: a binary32 lse does not hold what a later gradient needs here
+    up = torch.randn(6, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    loss = arc.TokenLogProbs(V=V, rows=6, dtype=dtype).loss(x, y, up)
+    g = -up.double().cpu()[:, None] * want["q"]
+    yc = y.cpu()
+    g[yc < 0] = 0.0
+    at = (yc >= 0) & (yc < V)
+    g[torch.arange(6)[at], yc[at]] += up.double().cpu()[at]
+    # p by its exponent's error (at most 110 in magnitude where p is not 0), and the type's
+    tol = up.double().abs().cpu()[:, None] * (want["q"] * EPS * (8 * 110 + 128) + 4 * EPS)
+    if dtype == "bf16":
+        tol = tol + g.abs() * 2.0 ** -8
+    near("loss.grad", loss.grad, g, tol + 1e-37)
+
+
 def test_alternatives_of_a_masked_row_are_the_first_tokens():
     x = place(torch.full((1, 100), -math.inf), "f32")
     h = arc.TokenLogProbs(V=100, rows=1, dtype="f32", top=4)
