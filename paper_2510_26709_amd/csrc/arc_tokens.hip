@@ -106,15 +106,17 @@ struct RowShape {
 
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 
-// Softmax statistics of part of a row whose largest logit is `most`, in powers
-// of two: total = sum 2^t, spread = sum 2^t t for t = c x - R, c = scale
-// log2(e).  R is c most rounded, and t one fma: R need not be the exact
-// product, as what it lacks (`rest`, exactly known) is the same for all of the
-// part, and is made up for where parts are joined.
+// Softmax statistics of part of a row relative to a logit `most`, in powers of
+// two: total = sum 2^t, spread = sum 2^t t for t = c x - R, c = scale log2(e).
+// `most` is the part's largest logit, or less by no more than 16 in t: a sum of
+// binary32 numbers does not care, and needs no scaling of what it holds
+// whenever a larger logit comes.  R is c most rounded, and t one fma: R need not
+// be the exact product, as what it lacks (`rest`, exactly known) is the same for
+// all of the part, and is made up for where parts are joined.
 //
-// Far from zero (|R| >= 2^31) neighbouring logits are 2^8 apart in t and more,
-// so that only those equal to `most` count: they are taken as 0 and all others
-// as -infinity, with R = 0 (far_logit()).
+// Far from zero (|R| >= 2^30) neighbouring logits are 2^6 apart in t and more,
+// so that only those equal to the largest count: it is `most`, they are taken as
+// 0 and all others as -infinity, with R = 0 (far_logit()).
 struct Stats {
   float most, total, spread;
 };
@@ -126,7 +128,7 @@ struct Reference {
 
 __device__ __forceinline__ Reference reference(float most, float c) {
   const float p = most == -INFINITY ? 0.f : most * c;  // nothing above -infinity: from 0
-  if (!(fabsf(p) < 0x1p31f)) return {0.f, 0.f, true};
+  if (!(fabsf(p) < 0x1p30f)) return {0.f, 0.f, true};
   return {p, most == -INFINITY ? 0.f : fmaf(most, c, -p), false};
 }
 
@@ -141,6 +143,8 @@ __device__ __forceinline__ float exponent(float x, float most, const Reference& 
 
 // t below this adds nothing to a spread, and 0 * infinity would.
 constexpr float kFarBelow = -300.f;
+
+constexpr float kMostAbove = 16.f;  // of a t
 
 // s relative to `most` (not below s.most) instead.
 __device__ __forceinline__ Stats moved(const Stats& s, float most, const Reference& to, float c) {
@@ -250,9 +254,13 @@ struct Scorer {
   template <bool TOP>
   static __device__ __forceinline__ Stats share(const Words16* body, int32_t first, int32_t end,
                                                 float c, int32_t run_batches,
-                                                float (*run_most)[W], int32_t* runs) {
+                                                float (*run_most)[W], int32_t* runs,
+                                                float* largest) {
     Stats s{-INFINITY, 0.f, 0.f};
-    float run = -INFINITY;
+    Reference ref{0.f, 0.f, false};
+    float limit = -INFINITY;  // logits up to which `most` serves
+    const float above = kMostAbove / c;
+    float run = -INFINITY, top = -INFINITY;
     int32_t batch = 0, done = 0;
     // ALL: every thread has all U chunks.  The others, at the end, would cost
     // as much arithmetic as chunks that are there, if they were not left out.
@@ -276,20 +284,23 @@ struct Scorer {
       }
       if constexpr (TOP) {
         run = fmaxf(run, here);
+        top = fmaxf(top, here);
         if (++batch == run_batches) {
           run_most[done++][threadIdx.x] = run;
           run = -INFINITY;
           batch = 0;
         }
       }
-      const float most = fmaxf(s.most, here);
-      const Reference ref = reference(most, c);
-      s = moved(s, most, ref, c);
+      if (here > limit) {
+        ref = reference(here, c);
+        s = moved(s, here, ref, c);
+        limit = ref.far ? here : here + above;
+      }
       if (ref.far) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-          for (int q = 0; q < C; ++q) x[u][q] = far_logit(x[u][q], most);
+          for (int q = 0; q < C; ++q) x[u][q] = far_logit(x[u][q], s.most);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -310,6 +321,7 @@ struct Scorer {
     if constexpr (TOP) {
       if (batch > 0) run_most[done++][threadIdx.x] = run;
       *runs = done;
+      *largest = top;
     }
     return s;
   }
@@ -413,12 +425,15 @@ token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_c
   constexpr int32_t kMost = kRuns<W> * W * S::U;
   const int32_t run_batches = max(1, (end - first + kMost - 1) / kMost);
   int32_t runs = 0;
-  Stats s = S::template share<TOP>(body, first, end, c, run_batches,
-                                   sh.run_most, &runs);
-  if (edges && (int)threadIdx.x < shape.head + shape.tail)
-    S::add_edge(element<BF16>(row, shape.edge(threadIdx.x, V)), c, &s);
+  float largest = -INFINITY;  // of the thread's logits
+  Stats s = S::template share<TOP>(body, first, end, c, run_batches, sh.run_most, &runs, &largest);
+  if (edges && (int)threadIdx.x < shape.head + shape.tail) {
+    const float x = element<BF16>(row, shape.edge(threadIdx.x, V));
+    S::add_edge(x, c, &s);
+    largest = fmaxf(largest, x);
+  }
   if constexpr (TOP) {
-    const float g = lanes_reduce<S::kLanes>(s.most, MaxF());
+    const float g = lanes_reduce<S::kLanes>(largest, MaxF());
     if (threadIdx.x % S::kLanes == 0) sh.group[threadIdx.x / S::kLanes] = g;
     if (threadIdx.x == 0) sh.listed = sh.found = 0;
 #pragma unroll
@@ -450,8 +465,8 @@ token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_c
     s.spread += part_sum[1][w];
   }
   if constexpr (TOP) {
-    const int32_t each = run_batches * S::U;  // chunks of a run, at most
-    const int32_t items = sh.listed <= kListed<W> ? sh.listed * each : 0;
+    const int32_t of_run = run_batches * S::U;  // chunks of a run, at most
+    const int32_t items = sh.listed <= kListed<W> ? sh.listed * of_run : 0;
     const auto found = [&](float x, int32_t j) {
       if (x >= tau) {
         const int32_t n = atomicAdd(&sh.found, 1);
@@ -459,8 +474,8 @@ token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_c
       }
     };
     for (int32_t q = threadIdx.x; q < items; q += W) {
-      const int32_t of = sh.list[q / each], r = of / W;
-      const int32_t chunk = first + of % W + (r * each + q % each) * W;
+      const int32_t of = sh.list[q / of_run], r = of / W;
+      const int32_t chunk = first + of % W + (r * of_run + q % of_run) * W;
       if (chunk >= end) continue;
       float x[S::C];
       unpack<BF16>(body[chunk], x);
@@ -476,15 +491,12 @@ token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_c
   int32_t n = TOP ? sh.found : 0;
   bool one_by_one = false;
   if constexpr (TOP) {
-    // All elements of the piece, a chunk a thread, in the order of the tokens but
-    // for the single ones.
-    const auto each_chunk = [&](int32_t from, int32_t to, const auto& look) {
-      for (int32_t q = from + threadIdx.x; q < to; q += W) {
-        float x[S::C];
-        unpack<BF16>(body[q], x);
-#pragma unroll
-        for (int e = 0; e < S::C; ++e) look(x[e], shape.head + q * S::C + e);
-      }
+    // Tokens of the piece but for the single elements, in order; one at a time,
+    // so that this rare way leaves the common one its registers.
+    const int32_t begin = shape.head + first * S::C, stop = shape.head + end * S::C;
+    const auto each = [&](int32_t from, int32_t to, const auto& look) {
+#pragma unroll 1
+      for (int32_t j = from + threadIdx.x; j < to; j += W) look(element<BF16>(row, j), j);
     };
     const auto each_edge = [&](const auto& look) {
       if (edges && (int)threadIdx.x < shape.head + shape.tail) {
@@ -507,7 +519,7 @@ token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_c
       const auto above = [&](float x, int32_t j) {
         if (x > tau) add(x, j);
       };
-      each_chunk(first, end, above);
+      each(begin, stop, above);
       each_edge(above);
       __syncthreads();
       n = sh.found;
@@ -517,10 +529,10 @@ token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_c
         const auto at_tau = [&](float x, int32_t j) {
           if (x == tau) add(x, j);
         };
-        constexpr int32_t kSome = kCandidates<W> / 2 / S::C - 1;  // with the single ones half the list
+        constexpr int32_t kSome = kCandidates<W> / 2 - 8;  // half the list, with the single ones
         each_edge(at_tau);
-        for (int32_t from = first; from < end; from += kSome) {
-          each_chunk(from, min(end, from + kSome), at_tau);
+        for (int32_t from = begin; from < stop; from += kSome) {
+          each(from, min(stop, from + kSome), at_tau);
           __syncthreads();
           n = sh.found;
           __syncthreads();
@@ -536,7 +548,7 @@ token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_c
       const auto masked = [&](float x, int32_t j) {
         if (x == -INFINITY) add(x, j);
       };
-      each_chunk(first, min(end, first + (k + S::C - 1) / S::C), masked);
+      each(begin, min(stop, begin + k), masked);
       each_edge(masked);
       __syncthreads();
       n = sh.found;
@@ -549,7 +561,7 @@ token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_c
           const uint64_t q = rank_key(x, j);
           if (q < before && q > key) key = q;
         };
-        each_chunk(first, end, look);
+        each(begin, stop, look);
         each_edge(look);
         key = lanes_reduce<64>(key, MaxKey());
         __syncthreads();
