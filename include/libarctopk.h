@@ -377,12 +377,12 @@ arc_status arc_tokens_score(arc_tokens *ctx, int64_t rows, const void *logits, i
 /*
  * The gradient of scored rows, with p = exp(z - lse) for the binary32 lse (off
  * by |lse| 2^-24 of itself: logits of 10^5 and more want arc_tokens_loss, which
- * holds the normaliser relative to the largest logit).  lse and entropy are arc_tokens_score's of the
- * same logits (entropy may be NULL where d_entropy is); d_logp, d_entropy and
- * d_lse are the upstream gradients [rows], each NULL for zeros (targets may be
- * NULL where d_logp is).  grad has rows of `grad_stride` >= V elements; it may
- * be the logits themselves (the same pointer and stride) and must not overlap
- * anything otherwise.
+ * holds the normaliser relative to the largest logit).  lse and entropy are
+ * arc_tokens_score's of the same logits (entropy may be NULL where d_entropy
+ * is); d_logp, d_entropy and d_lse are the upstream gradients [rows], each NULL
+ * for zeros (targets may be NULL where d_logp is).  grad has rows of
+ * `grad_stride` >= V elements; it may be the logits themselves (the same
+ * pointer and stride) and must not overlap anything otherwise.
  */
 arc_status arc_tokens_grad(arc_tokens *ctx, int64_t rows, const void *logits, int64_t stride,
                            const int64_t *targets, const float *lse, const float *entropy,

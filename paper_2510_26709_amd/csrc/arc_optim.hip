@@ -175,18 +175,19 @@ __device__ __forceinline__ float scale_of(uint32_t most) {
 // whole lines, and the loads of four passes ahead of the first update.  Bound by
 // HBM: 1.2e8 binary32 parameters 600 us, bf16 ones with 32-bit states 469 (5.8
 // TB/s; one pass at a time at twice the occupancy 643 and 525); 1.1e9 binary32
-// ones with a bf16 copy and bf16 gradients 4.7 to 5.6 ms, by where the process
-// got its memory.  A step of a few times the Infinity Cache
+// ones with a bf16 copy and bf16 gradients 4.8 to 5.6 ms, by where the process
+// got its memory (6.4 to 5.5 TB/s).  A step of a few times the Infinity Cache
 // stores its binary32 arrays through it (!STREAM): 1.1e7 parameters 51 us
 // against 58 past it, 2.2e7 in 300 tensors 111 / 129, 3.6e7 238 / 223, 1.2e8
 // 662 / 640 (one pass at a time).
 //
 // States in 8 bits: eight elements a lane, so that 16 lanes hold a block, its
-// largest magnitudes found by four lane permutations.  10 bytes of HBM and about
-// 57 operations an element, which take the same time: 1.2e8 bf16 parameters 227
-// us (5.5 TB/s).  That is with the conversions that scale and round, the root
-// from the reciprocal one and the reciprocal for a division; with a multiply
-// for each scale, a rounding in integers, sqrtf() and a division it was 319 us.
+// largest magnitudes found by four lane permutations.  10 bytes of HBM and 53
+// instructions an element, which take the same time: 1.2e8 bf16 parameters 222
+// to 229 us (5.7 to 5.5 TB/s).  That is with the conversions that scale and round,
+// the root from the reciprocal one and the reciprocal for a division; with a
+// multiply for each scale, a rounding in integers, sqrtf() and a division it was
+// 319 us.
 template <bool F8, bool STREAM>
 __global__ void __launch_bounds__(kThreads, F8 ? 6 : 4)
 adamw_kernel(OptimBatch b, OptimPointers p, AdamArgs a) {
@@ -353,9 +354,9 @@ __device__ __forceinline__ double group_sum(double v) {
   return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-// The sum of squares of one run of elements, in binary64 (no square
-// of a binary32 number overflows there, and the conversion and the fma take a
-// third of the time that HBM does).
+// The sum of squares of one run of elements, in binary64: no square of a binary32
+// number overflows there.  Bound by HBM, four loads of a thread in flight: 1.2e8
+// binary32 values 74 us (6.8 TB/s), 1.1e9 bf16 ones 313 (7.0).
 __global__ void __launch_bounds__(kThreads)
 norm_chunk_kernel(NormBatch b, NormPointers p, int32_t run, double* __restrict__ partial) {
   const int32_t chunk = b.first_chunk + blockIdx.x;

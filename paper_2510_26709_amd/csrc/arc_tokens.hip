@@ -715,11 +715,17 @@ __device__ __forceinline__ void store_element(void* row, int32_t j, float d) {
     static_cast<float*>(row)[j] = d;
 }
 
-constexpr int kGradThreads = 256;
-constexpr int kGradChunks = 4;  // of a thread, in flight
+constexpr int kGradThreads = 128;
+constexpr int kGradChunks = 2;  // of a thread, in flight
 
-// One workgroup for each run of kGradThreads * kGradChunks chunks of a row.  SUMS:
-// from the row's sums, as token_loss_kernel does.
+// dx = s (dl ([j = y] - p) + dz p - dh p (log p + H)) with p = exp(s x - lse): one
+// exponential and a product with A + B log p an element, A and B the row's.  One
+// workgroup for each run of kGradThreads * kGradChunks chunks of a row, so that
+// few rows fill the card too.  Bound by HBM: 2048 rows of 32,000 binary32 80 us
+// (6.6 TB/s; 13 instructions an element).  us with one, two and four chunks of 256
+// threads, and with two of 512 and of 128: those 81 / 82 / 87, 88 / 80; 20,000 rows
+// of 1001 bf16 24 / 25 / 25, 36 / 21; 8192 of 50,257 bf16 269 / 270 / 283, 270 /
+// 275.  SUMS: from the row's sums, as token_loss_kernel does.
 template <bool BF16, bool SUMS>
 __global__ void __launch_bounds__(kGradThreads)
 token_grad_kernel(TokenArgs a, TokenGrad g, int32_t tiles) {
@@ -751,7 +757,8 @@ token_grad_kernel(TokenArgs a, TokenGrad g, int32_t tiles) {
 #pragma unroll
   for (int u = 0; u < kGradChunks; ++u) {
     raw[u] = Words16{{0, 0, 0, 0}};
-    if (k0 + u * kGradThreads < shape.chunks && !r.zero) raw[u] = stream_load16(body + k0 + u * kGradThreads);
+    const int32_t k = k0 + u * kGradThreads;
+    if (k < shape.chunks && !r.zero) raw[u] = stream_load16(body + k);
   }
 #pragma unroll
   for (int u = 0; u < kGradChunks; ++u) {
@@ -778,7 +785,12 @@ token_grad_kernel(TokenArgs a, TokenGrad g, int32_t tiles) {
 }
 
 // Scores and gradient in one pass: a workgroup holds a whole row, N chunks a
-// thread, in its registers as it lies in memory.
+// thread, in its registers as it lies in memory, so that HBM moves each logit
+// once in and its gradient once out.  dx = 2^t (A' + B' t) from the exponent
+// relative to the row's reference, A' and B' divided by the row's sum.  8192 rows of
+// 32,000 binary32 361 us (5.8 TB/s): HBM.  4096 of 50,257 bf16 159 us (5.2 TB/s):
+// 19 instructions an element, and two workgroups a compute unit that read, add
+// and write more or less in step.
 template <bool BF16, int W, int N>
 __global__ void __launch_bounds__(W, N <= 8 ? 8 : 4)
 token_loss_kernel(TokenArgs a, TokenScores out, TokenGrad g) {
@@ -1012,6 +1024,13 @@ bool launch_token_loss(const TokenArgs& a, const TokenScores& out, const TokenGr
   bool found = true;
   each_rows(a, out, g, kRowsPerLaunch, [&](const TokenArgs& b, const TokenScores& o,
                                            const TokenGrad& h) {
+  // The smallest that holds the row.  us with a variant and with the next larger:
+  // (64, 8) 100,000 rows of 1001 bf16 112 / 214, 20,000 of 1001 binary32 31 / 44;
+  // (256, 5) 20,000 of 8000 bf16 110 / 159, 8000 of 9000 56 / 69, but 20,000 of 5000
+  // binary32 148 / 138; (512, 8) 10,000 of 16,000 bf16 123 / 159, 8192 of 32,000 186 /
+  // 201, but 10,000 of 16,000 binary32 224 / 214; (1024, 8) 4096 of 50,257 bf16 160 /
+  // 189, 8192 of 32,000 binary32 362 / 371; (512, 24) 3000 of 80,000 bf16 208 / 258,
+  // 2000 of 45,000 binary32 145 / 147.
 #define ARC_LOSS(WW, NN)                                                                        \
   if (chunks <= (WW) * (NN)) {                                                                  \
     hipLaunchKernelGGL(a.bf16 ? (token_loss_kernel<true, WW, NN>)                               \
