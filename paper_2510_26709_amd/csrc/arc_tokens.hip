@@ -722,7 +722,7 @@ constexpr int kGradChunks = 2;  // of a thread, in flight
 // exponential and a product with A + B log p an element, A and B the row's.  One
 // workgroup for each run of kGradThreads * kGradChunks chunks of a row, so that
 // few rows fill the card too.  Bound by HBM: 2048 rows of 32,000 binary32 80 us
-// (6.6 TB/s; 13 instructions an element).  us with one, two and four chunks of 256
+// (6.6 TB/s; 14 instructions an element).  us with one, two and four chunks of 256
 // threads, and with two of 512 and of 128: those 81 / 82 / 87, 88 / 80; 20,000 rows
 // of 1001 bf16 24 / 25 / 25, 36 / 21; 8192 of 50,257 bf16 269 / 270 / 283, 270 /
 // 275.  SUMS: from the row's sums, as token_loss_kernel does.
