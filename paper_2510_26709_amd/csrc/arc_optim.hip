@@ -437,8 +437,8 @@ hipError_t launch_adamw(bool f8, bool cached, const OptimBatch& b, const OptimPo
   return hipGetLastError();
 }
 
-hipError_t launch_norm_chunks(const NormBatch& b, const NormPointers& p, int32_t run, double* partial,
-                              hipStream_t stream) {
+hipError_t launch_norm_chunks(const NormBatch& b, const NormPointers& p, int32_t run,
+                              double* partial, hipStream_t stream) {
   hipLaunchKernelGGL(norm_chunk_kernel, dim3((unsigned)b.chunks), dim3(kThreads), 0, stream, b, p,
                      run, partial);
   return hipGetLastError();

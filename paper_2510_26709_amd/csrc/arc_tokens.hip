@@ -98,7 +98,9 @@ struct RowShape {
     tail = (V - head) % kChunk<BF16>;
   }
   // Single element e of head + tail.
-  __device__ int32_t edge(int32_t e, int32_t V) const { return e < head ? e : V - tail + (e - head); }
+  __device__ int32_t edge(int32_t e, int32_t V) const {
+    return e < head ? e : V - tail + (e - head);
+  }
   __device__ const Words16* body(const void* row) const {
     return reinterpret_cast<const Words16*>(row_at<BF16>(row, head));
   }

@@ -50,7 +50,8 @@ struct arc_optim {
   void release() {
     (void)hipStreamSynchronize(stream);
     for (void* p : {static_cast<void*>(tensors_dev), static_cast<void*>(chunk_tensor_dev),
-                    static_cast<void*>(norm_tensor_dev), static_cast<void*>(partial_dev), static_cast<void*>(squares_dev)})
+                    static_cast<void*>(norm_tensor_dev), static_cast<void*>(partial_dev),
+                    static_cast<void*>(squares_dev)})
       if (p) (void)hipFree(p);
   }
 };
