@@ -525,6 +525,7 @@ token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_c
       each_edge(above);
       __syncthreads();
       n = sh.found;
+      __syncthreads();  // the same n on every wave, before more is found
       // few threads' chunks hold the largest: the keys one after the other
       one_by_one = n > kCandidates<W> / 2;
       if (n < k) {
