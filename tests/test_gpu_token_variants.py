@@ -117,3 +117,30 @@ def test_rows_that_flood_the_lists_split(times, chunks, dtype):
     K = x.shape[0]
     x, y = repeated(x, tokens(K, V, chunks), times, dtype, pad=3)
     check_scores(x, y, K, 1.0, 32, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_longest_row(dtype):
+    """2^31 - 1 logits, all equal but for three: the lists flood in every piece,
+    the last of which ends where token numbers do."""
+    V = (1 << 31) - 1
+    x = torch.full((1, V), 0.25, dtype=dtype_of(dtype), device="cuda")
+    y = torch.tensor([V - 2], device="cuda")
+    for j, v in ((V - 1, 3.0), (V - 2, 2.0), (5, 1.0)):
+        x[0, j] = v
+    h = arc.TokenLogProbs(V=V, rows=1, dtype=dtype, top=8)
+    got = h.score(x, y)
+    assert got.top_ids.tolist() == [[V - 1, V - 2, 5, 0, 1, 2, 3, 4]]
+    total = (V - 3) * math.exp(0.25) + math.exp(3) + math.exp(2) + math.exp(1)
+    lse = math.log(total)
+    # a lane's chain of at most V / 8192 terms, and joins
+    tol = EPS * (V / 8192 + 64)
+    near("lse", got.lse, torch.tensor([lse], dtype=torch.float64), tol)
+    near("logp", got.logp, torch.tensor([2 - lse]), tol + 64 * EPS)
+    near("top_logp", got.top_logp, torch.tensor([[3.0, 2, 1] + [0.25] * 5]) - lse, tol + 64 * EPS)
+    grad = h.loss(x, y, torch.ones(1, device="cuda"), out=x).grad
+    p = [math.exp(v - lse) for v in (0.25, 1.0, 2.0, 3.0)]
+    want = torch.tensor([[-p[0], -p[1], 1 - p[2], -p[3], -p[0]]], dtype=torch.float64)
+    at = [0, 5, V - 2, V - 1, V - 3]
+    near("grad", grad[:, at], want, want.abs() * (tol + 64 * EPS + (dtype == "bf16") * 2.0 ** -8))
+    assert int((grad == grad[0, 0]).sum()) == V - 3
