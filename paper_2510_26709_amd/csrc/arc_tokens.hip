@@ -494,13 +494,16 @@ token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_c
   bool one_by_one = false;
   if constexpr (TOP) {
     // Tokens of the piece but for the single elements, in order; one at a time,
-    // so that this rare way leaves the common one its registers.  Unsigned: a step
-    // from the last tokens of the longest row passes 2^31.
-    const uint32_t begin = shape.head + first * S::C, stop = shape.head + end * S::C;
-    const auto each = [&](uint32_t from, uint32_t to, const auto& look) {
+    // so that this rare way leaves the common one its registers.  No step goes past
+    // the last token: the longest row's is 2^31 - 2.
+    const int32_t begin = shape.head + first * S::C, stop = shape.head + end * S::C;
+    const auto each = [&](int32_t from, int32_t to, const auto& look) {
+      if ((int32_t)threadIdx.x >= to - from) return;
 #pragma unroll 1
-      for (uint32_t j = from + threadIdx.x; j < to; j += W)
-        look(element<BF16>(row, j), (int32_t)j);
+      for (int32_t j = from + threadIdx.x;; j += W) {
+        look(element<BF16>(row, j), j);
+        if (to - j <= W) break;
+      }
     };
     const auto each_edge = [&](const auto& look) {
       if (edges && (int)threadIdx.x < shape.head + shape.tail) {
@@ -534,10 +537,11 @@ token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_c
         const auto at_tau = [&](float x, int32_t j) {
           if (x == tau) add(x, j);
         };
-        constexpr uint32_t kSome = kCandidates<W> / 2 - 8;  // half the list, with the single ones
+        constexpr int32_t kSome = kCandidates<W> / 2 - 8;  // half the list, with the single ones
         each_edge(at_tau);
-        for (uint32_t from = begin; from < stop; from += kSome) {
-          each(from, min(stop, from + kSome), at_tau);
+        for (int32_t from = begin, to; from < stop; from = to) {
+          to = from + min(kSome, stop - from);
+          each(from, to, at_tau);
           __syncthreads();
           n = sh.found;
           __syncthreads();
