@@ -409,7 +409,9 @@ arc_status arc_tokens_destroy(arc_tokens *ctx);
  * beta1^T, c2 = 1 - beta2^T (binary64, rounded once), lr' = lr * lr_scale:
  *   m <- beta1 m + (1 - beta1) g'        v <- beta2 v + (1 - beta2) g'^2
  *   x <- (1 - lr' weight_decay) x - (lr' / c1) (m / (sqrt(v) / sqrt(c2) + eps))
- * in binary32, every product and sum of m and v rounded by itself.
+ * in binary32, every product and sum of m and v rounded by itself.  So where
+ * |g'| is some 2^64 and more v is infinite, and x only decays; where it is some
+ * 2^-75 and less v is 0, and eps alone divides m.
  *
  * States.  All tensors' states lie in one array of arc_optim_state_elems
  * elements; tensor i's begin at arc_optim_state_offset(i), a multiple of
@@ -423,9 +425,11 @@ arc_status arc_tokens_destroy(arc_tokens *ctx);
  * one step moves a state by less than half the distance of two such values:
  * rounded to the nearest, v would stay where its first step put it.  A
  * magnitude is rounded up with the chance of what is cut off, decided by a
- * hash of (seed, t, element) alone (the same bits on every run); a v of 2^-126
- * and more never becomes 0 (a smaller one counts as 0).  Non-finite gradients
- * give NaN states.
+ * hash of (seed, t, element) alone (the same bits on every run); a v above 0 is
+ * never held as 0.  Non-finite gradients give NaN states, and so does an
+ * infinite v in 8 bits; a block that holds a NaN has the scale 2^121, and what
+ * its other elements held is lost with it.  (A factor that is NaN for such
+ * gradients, as arc_optim_norm's is, keeps the states from them.)
  *
  * Parameters in bfloat16 are rounded to the nearest even, or with `stochastic`
  * by the same hash (an update below half of the distance between two values

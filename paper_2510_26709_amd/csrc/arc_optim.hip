@@ -152,13 +152,18 @@ __device__ __forceinline__ uint32_t f8_random(float x, uint32_t draw, float scal
   }
 }
 
-// The square root of x >= 0, rounded correctly (checked for every mantissa of
-// two binades): x rsq(x) and one correction by its residual, 8 operations and 2
-// for the lower end, half of sqrtf()'s.  Below 2^-126 it is 0; for infinity, NaN.
+// The square root of x >= 0 (or NaN), rounded correctly (checked for every binary32
+// value): x rsq(x) and one correction by its residual, 5 operations, and 7 for the
+// ends of the range.  Below 2^-96 binary32 does not hold the residual: the root of
+// x times 2^64 then.  0 and infinity are their own roots.
 __device__ __forceinline__ float root_of(float x) {
-  const float w = x < 0x1p-126f ? 0.f : __builtin_amdgcn_rsqf(x);
-  const float y = x * w;
-  return fmaf(fmaf(-y, y, x), 0.5f * w, y);
+  const bool small = x < 0x1p-96f;
+  const float s = x * (small ? 0x1p64f : 1.f);
+  const float w = __builtin_amdgcn_rsqf(s);
+  const float y = s * w;
+  const float root = fmaf(fmaf(-y, y, s), 0.5f * w, y) * (small ? 0x1p-32f : 1.f);
+  constexpr int kZeros = 0x060, kPlusInfinity = 0x200;
+  return __builtin_amdgcn_classf(x, kZeros | kPlusInfinity) ? x : root;
 }
 
 struct MaxU {
