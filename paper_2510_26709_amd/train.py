@@ -144,8 +144,15 @@ class TokenLogProbs(_Bound):
             self.ctx = None
 
 
+def _state(name):
+    return property(lambda self: self._states[name],
+                    lambda self, x: self._take_state(name, x),
+                    doc=f"{name} of all tensors; a tensor assigned here is what later steps use.")
+
+
 class AdamW(_Bound):
-    """AdamW over tensors of the given ``sizes``, with their states.
+    """AdamW over tensors of the given ``sizes``, with their states ``m``, ``v``
+    and, in 8 bits, ``m_scale``, ``v_scale``.
 
     Parameters, gradients and copies are passed to each call, as a list of one
     tensor each or as one flat tensor that holds them in order.  ``param_dtype``
@@ -181,27 +188,42 @@ class AdamW(_Bound):
         S = arc_optim_state_elems(self.ctx)
         self.offsets = [arc_optim_state_offset(self.ctx, i) for i in range(num)]
         kind = torch.float8_e4m3fn if state == "f8" else torch.float32
-        want = {"m": (S, kind), "v": (S, kind)}
+        self._want = {"m": (kind, S), "v": (kind, S)}
         if state == "f8":
-            want.update(m_scale=(S // ARC_STATE_BLOCK, torch.float32),
-                        v_scale=(S // ARC_STATE_BLOCK, torch.float32))
-        self.m_scale = self.v_scale = None
-        for name, (n, dtype) in want.items():
-            if states is not None and name in states:
-                x = self._check(name, states[name], dtype, n)
-            else:
+            self._want.update(m_scale=(torch.float32, S // ARC_STATE_BLOCK),
+                              v_scale=(torch.float32, S // ARC_STATE_BLOCK))
+        self._states = dict.fromkeys(("m", "v", "m_scale", "v_scale"))
+        self._checked = None  # the states' addresses and lengths that were looked at last
+        for name, (dtype, n) in self._want.items():
+            x = None if states is None else states.get(name)
+            if x is None:
                 with torch.cuda.stream(self.stream):
                     x = torch.zeros(n, dtype=torch.uint8 if dtype.itemsize == 1 else dtype,
                                     device=self.device).view(dtype)
-            setattr(self, name, x)
-        self._states = [x if x is None else x.data_ptr()
-                        for x in (self.m, self.v, self.m_scale, self.v_scale)]
+            self._take_state(name, x)
         starts = np.cumsum([0] + self.sizes[:-1], dtype=np.uint64)
         self._starts = {2: starts * np.uint64(2), 4: starts * np.uint64(4)}  # in bytes
         self._copy = [torch.bfloat16] * num
         self._table = {k: np.zeros(num, dtype=np.uint64) for k in ("param", "grad", "copy")}
         self._args = {k: ctypes.c_void_p(v.ctypes.data) for k, v in self._table.items()}
         self._flat = sum(self.sizes)
+
+    m, v, m_scale, v_scale = (_state(name) for name in ("m", "v", "m_scale", "v_scale"))
+
+    def _take_state(self, name, x):
+        if name not in self._want:
+            raise ValueError(f"{name}: states in {self.state!r} have none")
+        self._states[name] = self._check(name, x, *self._want[name])
+        self._held = [x for x in self._states.values() if x is not None]
+
+    def _state_pointers(self):
+        held = self._held
+        now = [*map(torch.Tensor.data_ptr, held), *map(torch.Tensor.numel, held)]
+        if now != self._checked:  # other tensors, or another storage of the same ones
+            for name, want in self._want.items():
+                self._check(name, self._states[name], *want)
+            self._checked = now
+        return now[:4] if len(held) == 4 else (now[0], now[1], None, None)
 
     def _pointers(self, key, x, dtypes):
         """Fills the host table of device pointers of this call."""
@@ -243,7 +265,7 @@ class AdamW(_Bound):
             self._pointers("param", params, self._param),
             self._pointers("grad", grads, self._grad),
             None if copies is None else self._pointers("copy", copies, self._copy),
-            factor, *self._states)
+            factor, *self._state_pointers())
 
     def close(self):
         if getattr(self, "ctx", None):
