@@ -3,8 +3,12 @@ probabilities of given tokens, entropy, top alternatives and their gradient)
 and ``AdamW`` (gradient norms and the AdamW step over many tensors).
 
 Both own one context of the C library, bound to a torch stream: inputs must be
-ready on that stream, and outputs are.  Tensors are checked here for what the
-library cannot see in a pointer (type, device, shape, strides).
+ready on that stream, and outputs are.  Where it is not the current stream,
+making them so (an event, a synchronization) is the caller's part.  Tensors may
+be dropped after a call all the same: the allocator keeps inputs until the
+context's stream is done with them, and outputs until the stream is that was
+current at the call.  Tensors are checked here for what the library cannot see
+in a pointer (type, device, shape, strides).
 """
 from __future__ import annotations
 
@@ -46,13 +50,26 @@ class _Bound:
             raise ValueError(f"{name}: need {count} elements, got {x.numel()}")
         return x
 
+    def _elsewhere(self):
+        # (the raw handles compare in 0.1 us, stream objects in 2)
+        return torch._C._cuda_getCurrentRawStream(self.device.index) != self.stream.cuda_stream
+
     def _empty(self, *shape, dtype=torch.float32):
-        # memory of the stream that writes it (the raw handles compare in 0.1
-        # us, stream objects in 2)
-        if torch._C._cuda_getCurrentRawStream(self.device.index) == self.stream.cuda_stream:
+        # memory of the stream that writes it
+        if not self._elsewhere():
             return torch.empty(shape, dtype=dtype, device=self.device)
         with torch.cuda.stream(self.stream):
-            return torch.empty(shape, dtype=dtype, device=self.device)
+            out = torch.empty(shape, dtype=dtype, device=self.device)
+        out.record_stream(torch.cuda.current_stream(self.device))
+        return out
+
+    def _used(self, *tensors):
+        """What a call that was made reads or writes: tensors, lists of them, None."""
+        if self._elsewhere():
+            for x in tensors:
+                for y in x if isinstance(x, (list, tuple)) else (x,):
+                    if y is not None:
+                        y.record_stream(self.stream)
 
     def __del__(self):
         try:
@@ -100,6 +117,7 @@ class TokenLogProbs(_Bound):
         arc_tokens_score(self.ctx, T, logits.data_ptr(), stride, targets.data_ptr(), at,
                          at + 4 * T, at + 8 * T, at + 12 * T if k else None,
                          at + 12 * T + 4 * k if k else None)
+        self._used(logits, targets)
         logp, entropy, lse, ids, near = out.split_with_sizes((T, T, T, k, k))
         return Scores(logp, entropy, lse, ids.view(torch.int32).view(T, self.top),
                       near.view(T, self.top))
@@ -115,6 +133,7 @@ class TokenLogProbs(_Bound):
                         each("lse", lse, T), each("entropy", entropy, T),
                         each("d_logp", d_logp, T), each("d_entropy", d_entropy, T),
                         each("d_lse", d_lse, T), out, out_stride)
+        self._used(logits, targets, lse, entropy, d_logp, d_entropy, d_lse, out)
         return out
 
     def loss(self, logits, targets, d_logp=None, d_entropy=None, d_lse=None, out=None):
@@ -128,6 +147,7 @@ class TokenLogProbs(_Bound):
         arc_tokens_loss(self.ctx, T, logits, stride, each("targets", targets, T, torch.int64),
                         each("d_logp", d_logp, T), each("d_entropy", d_entropy, T),
                         each("d_lse", d_lse, T), at, at + 4 * T, at + 8 * T, out, out_stride)
+        self._used(logits, targets, d_logp, d_entropy, d_lse, out)
         return Loss(*row.split(T) if T else (row,) * 3, out)
 
     def _out(self, out, T):
@@ -215,6 +235,7 @@ class AdamW(_Bound):
             raise ValueError(f"{name}: states in {self.state!r} have none")
         self._states[name] = self._check(name, x, *self._want[name])
         self._held = [x for x in self._states.values() if x is not None]
+        x.record_stream(self.stream)
 
     def _state_pointers(self):
         held = self._held
@@ -252,20 +273,23 @@ class AdamW(_Bound):
         at = out.data_ptr()
         arc_optim_norm(self.ctx, self._pointers("grad", grads, self._grad), scale, max_norm,
                        at + 8, at)
+        self._used(grads)
         return Norms(*out.split_with_sizes((2, num)))
 
     def step(self, t, params, grads, *, lr, beta1=0.9, beta2=0.999, eps=1e-8, factor=None,
              copies=None):
         """One step t >= 0, in place.  ``factor``: norm()'s total [2], whose
         second value multiplies the gradients."""
+        at = None
         if factor is not None:
-            factor = self._check("factor", factor, torch.float32, 2).data_ptr() + 4
+            at = self._check("factor", factor, torch.float32, 2).data_ptr() + 4
         arc_optim_adamw(
             self.ctx, arc_adamw_config(lr, beta1, beta2, eps), t,
             self._pointers("param", params, self._param),
             self._pointers("grad", grads, self._grad),
             None if copies is None else self._pointers("copy", copies, self._copy),
-            factor, *self._state_pointers())
+            at, *self._state_pointers())
+        self._used(params, grads, copies, factor)
 
     def close(self):
         if getattr(self, "ctx", None):
