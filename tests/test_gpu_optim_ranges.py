@@ -120,3 +120,21 @@ def test_values_that_8_bits_do_not_hold_are_nan(value):
     assert x[7].item() == 2.0 if finite else math.isnan(x[7].item())
     assert bool(torch.isfinite(x[8:]).all())
     assert bool(torch.isfinite(opt.v[BLOCK:].float()).all()), "other blocks"
+
+
+@pytest.mark.parametrize("grads", ["f32", "bf16"])
+def test_norms_of_more_tensors_than_one_launch_takes(grads):
+    gen = torch.Generator().manual_seed(8)
+    sizes = [int(k) for k in torch.randint(0, 3000, (1301,), generator=gen)]
+    sizes[479] = sizes[480] = sizes[960] = 0
+    sizes[1300] = 100_003
+    opt = arc.AdamW(sizes, grad_dtype=grads)
+    flat = torch.randn(sum(sizes), generator=gen)
+    flat = flat.bfloat16() if grads == "bf16" else flat
+    each = torch.stack([t.double().norm() for t in torch.split(flat, sizes)])
+    total, norms = opt.norm(flat.cuda(), max_norm=1.0, scale=0.5)
+    # a binary64 sum of exact squares, rounded once
+    assert bool(((norms.cpu().double() - 0.5 * each).abs() <= 2 * EPS * each).all())
+    norm = 0.5 * float(each.norm())
+    assert abs(total[0].item() - norm) <= 2 * EPS * norm
+    assert abs(total[1].item() - 0.5 / norm) <= 4 * EPS / norm

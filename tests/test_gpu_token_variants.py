@@ -8,7 +8,7 @@ import pytest
 import torch
 
 import paper_2510_26709_amd as arc
-from test_gpu_tokens import EPS, dtype_of, formulas, kind, near, place, tokens
+from test_gpu_tokens import EPS, dtype_of, formulas, kind, near, tokens
 
 pytestmark = pytest.mark.gpu
 
@@ -117,6 +117,135 @@ def test_rows_that_flood_the_lists_split(times, chunks, dtype):
     K = x.shape[0]
     x, y = repeated(x, tokens(K, V, chunks), times, dtype, pad=3)
     check_scores(x, y, K, 1.0, 32, dtype)
+
+
+def mixed(V, gen):
+    """Rows of every sort: noise, masked, non-finite, far from zero; their targets."""
+    inf, nan = math.inf, math.nan
+    x = torch.randn(14, V, generator=gen) * 3
+    x[1, V // 2:] = -inf             # half masked
+    x[2] = -inf                      # nothing left
+    x[3, 1:] = -inf                  # one token left
+    x[4, V - 1] = nan
+    x[5, V // 3] = inf
+    x[6, ::2] = -inf
+    x[7, V // 3:] = torch.finfo(torch.bfloat16).min
+    x[8] -= 1e4
+    x[9, V // 2] += 200.0
+    x[10] = 3e9 * x[10].sign()       # far from zero: the largest alone count
+    x[11] = -1.0
+    y = torch.tensor([V - 1, 0, 0, 0, 1, 7, 1, V // 3 - 1, V // 2, V // 2, 5, 2, -1, V + 3])
+    return x, y
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("chunks", CHUNKS + [40_000])
+@pytest.mark.parametrize("top,scale", [(20, 1.0), (0, 0.7)])
+def test_scores_of_rows_unsplit(top, scale, chunks, dtype):
+    V = length(chunks, dtype)
+    x, y = mixed(V, torch.Generator().manual_seed(chunks))
+    K = x.shape[0]
+    x, y = repeated(x, y, -(-513 // K), dtype, pad=3, shift=1)
+    check_scores(x, y, K, scale, top, dtype)
+
+
+def gradient(x, y, scale, want, ups, dtype):
+    """The gradient of rows in 64 bits, and a bound of its error: p relative to the
+    row's largest logit (its error is logp's), the entropy's, and the last
+    roundings."""
+    T, V = x.shape
+    dl, dh, dz = (torch.zeros(T, dtype=torch.float64) if u is None else u.double().cpu()
+                  for u in ups)
+    y = y.cpu()
+    dl = torch.where(y < 0, 0.0, dl)
+    q, H = want["q"], want["entropy"]
+    logq = torch.where(q > 0, want["logq"], 0.0)
+    g = q * (dz - dl)[:, None] - dh[:, None] * q * (logq + H[:, None])
+    at = (y >= 0) & (y < V)
+    g[torch.arange(T)[at], y[at]] += dl[at]
+    g *= scale
+    g[((dl == 0) & (dh == 0) & (dz == 0)) | want["empty"]] = 0.0
+    tol = slack(x, scale)[:, None]
+    size = (dl.abs() + dz.abs() + dh.abs() * (H.abs().nan_to_num() + 2))[:, None] + \
+        dh.abs()[:, None] * logq.abs().nan_to_num()
+    p = q.nan_to_num()
+    bound = scale * p * size * (4 * tol + 8 * EPS + 8 * EPS * logq.abs().nan_to_num())
+    bound = bound + scale * dl.abs()[:, None] * 4 * EPS
+    bound = bound + scale * dh.abs()[:, None] * p * tol * (4 + 2 * math.log(V + 1))
+    if dtype == "bf16":
+        bound = bound + (g.abs().nan_to_num() + bound) * 2.0 ** -8
+    return g, bound + 1e-37
+
+
+# Chunks up to which a workgroup's registers hold a row, each variant's first and
+# last, and beyond them all (two launches).
+LOSS_CHUNKS = [1, 512, 513, 1280, 1281, 4096, 4097, 8192, 8193, 12_288, 12_289, 24_576, 24_577]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("chunks", LOSS_CHUNKS)
+@pytest.mark.parametrize("times", [1, 10])   # 14 rows (long ones: two launches), 140
+def test_losses(times, chunks, dtype):
+    V = chunks * (8 if dtype == "bf16" else 4) + 3
+    gen = torch.Generator().manual_seed(chunks)
+    x, y = mixed(V, gen)
+    K, scale = x.shape[0], 1.25
+    ups = torch.randn(3, K, generator=gen)
+    ups[:, 11] = 0.0
+    logits, targets = x, y
+    x, y = repeated(logits, targets, times, dtype, pad=1)
+    h = arc.TokenLogProbs(V=V, rows=x.shape[0], dtype=dtype, scale=scale)
+    want = formulas(x[:K], y[:K], scale, 0)
+    tol = slack(x[:K], scale)
+    for which in ((0,), (0, 1, 2), (1,), (0, 2)):
+        up = [ups[k].cuda().repeat(times) if k in which else None for k in range(3)]
+        loss = h.loss(x, y, *up)
+        z = repeated(logits, targets, times, dtype, pad=1)[0]
+        inside = h.loss(z, y, *up, out=z)
+        torch.cuda.synchronize()
+        assert inside.grad.data_ptr() == z.data_ptr()
+        for name in ("logp", "entropy", "lse"):
+            a, b = getattr(loss, name), getattr(inside, name)
+            assert torch.equal(a.view(torch.int32), b.view(torch.int32)), name
+            same_bits(name, a, K)
+        assert torch.equal(loss.grad.nan_to_num(nan=7.0), z.nan_to_num(nan=7.0)), "in place"
+        for lo in range(K, x.shape[0], K):
+            assert torch.equal(loss.grad[lo:lo + K].nan_to_num(nan=7.0),
+                               loss.grad[:K].nan_to_num(nan=7.0)), lo
+        large = lambda v: 4 * EPS * v.abs().nan_to_num(posinf=0.0)  # noqa: E731
+        near("logp", loss.logp[:K], want["logp"], tol + large(want["logp"]))
+        near("entropy", loss.entropy[:K], want["entropy"], tol * (2 + 2 * math.log(V + 1)))
+        near("lse", loss.lse[:K], want["lse"], tol + large(want["lse"]))
+        g, bound = gradient(x[:K], y[:K], scale, want, [None if u is None else u[:K] for u in up],
+                            dtype)
+        near("grad", loss.grad[:K], g, bound)
+    h.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [(1 << 20) + 1000, (1 << 23) + 1000])
+def test_more_rows_than_one_launch_takes(rows, dtype):
+    V, scale = 9, 1.0
+    gen = torch.Generator().manual_seed(5)
+    x = torch.randn(997, V, generator=gen) * 3
+    y = torch.randint(-1, V, (997,), generator=gen)
+    K, times = 997, -(-rows // 997)
+    ups = torch.randn(3, K, generator=gen)
+    x, y = repeated(x, y, times, dtype, pad=1)
+    if rows < 1 << 21:
+        check_scores(x, y, K, scale, 5, dtype)
+    h = arc.TokenLogProbs(V=V, rows=x.shape[0], dtype=dtype, scale=scale)
+    up = [u.cuda().repeat(times) for u in ups]
+    s = h.score(x, y)
+    want = formulas(x[:K], y[:K], scale, 0)
+    g, bound = gradient(x[:K], y[:K], scale, want, [u[:K] for u in up], dtype)
+    # (lse rounded to binary32: its own error in the exponent, of at most 16)
+    bound = bound * 2 + 16 * 8 * EPS * g.abs()
+    for grad in (h.grad(x, y, s.lse, s.entropy, *up), h.loss(x, y, *up).grad):
+        near("grad", grad[:K], g, bound)
+        assert torch.equal(grad.view(times, K, V), grad[:K].expand(times, K, V))
+    for v in (s.logp, s.entropy, s.lse):
+        assert torch.equal(v.view(times, K), v[:K].expand(times, K))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
