@@ -27,14 +27,18 @@ constexpr int64_t kPieceChunks = 4 * kSplitThreads, kMostPieces = 16, kSplitPart
 
 // Chunks of a row up to which workgroups of 64, 256 and 512 threads take it
 // (above: 1024).  The same with and without alternatives, so that a row's sums
-// have the same bits.  us at 64 / 256 / 512 / 1024 threads, without and with
-// alternatives: 30,000 rows of 4000 bf16 (500 chunks) 42 / 56 / 92 / 150 and 52 /
-// 97 / 200 / 391, 20,000 of 8000 (1000) 55 / 53 / 77 / 137 and 67 / 80 / 141 /
-// 301, 8753 of 18,560 (2320) 60 / 59 / 63 / 78 and 72 / 65 / 81 / 141, 8192 of
-// 32,000 (4000) 88 / 86 / 83 / 93 and 110 / 100 / 99 / 157, 4000 of 100,000
-// (12,500) 135 / 138 / 131 / 126 and 224 / 157 / 148 / 156, 2000 of 150,000
-// binary32 (37,500) 186 / 201 / 195 / 185 and 400 / 240 / 225 / 210.
-constexpr int64_t kRow64 = 1200, kRow256 = 3300, kRow512 = 12520;
+// have the same bits.  us at 64 / 256 / 512 / 1024 threads, 5e8 bytes of rows of
+// bf16, without and with 20 alternatives: 600 chunks 86 / 108 / 176 / 287 and 129 /
+// 199 / 423 / 796, 1200 83 / 85 / 107 / 183 and 131 / 135 / 225 / 458, 2400 82 / 80 /
+// 86 / 115 and 128 / 101 / 143 / 251, 3300 87 / 82 / 79 / 99 and 133 / 100 / 122 /
+// 196, 6000 94 / 82 / 79 / 86 and 144 / 99 / 96 / 142, 10,000 89 / 84 / 82 / 82 and
+// 140 / 103 / 96 / 115, 16,000 86 / 82 / 81 / 79 and 141 / 100 / 95 / 97, 25,000 122 /
+// 85 / 81 / 79 and 180 / 101 / 97 / 94.  From 3300 to 5500 the larger workgroup gains
+// 1 to 4% without alternatives and loses with 20 of them, 20% falling to 4% (1% with 5
+// at 4000).  Between 512 and 1024 the two kinds together are even near 16,000: 12,600
+// bf16 81 / 79 and 97 / 103, binary32 78 / 76 and 93 / 92; 17,500 83 / 81 and 96 / 100,
+// 80 / 77 and 91 / 92; 19,000 83 / 83 and 100 / 100, 80 / 78 and 96 / 93.
+constexpr int64_t kRow64 = 1200, kRow256 = 3300, kRow512 = 16000;
 
 // ---------------------------------------------------------------------------
 // A row is read in chunks of 16 bytes a lane, from its first whole word on (a
@@ -1033,13 +1037,13 @@ bool launch_token_loss(const TokenArgs& a, const TokenScores& out, const TokenGr
   bool found = true;
   each_rows(a, out, g, kRowsPerLaunch, [&](const TokenArgs& b, const TokenScores& o,
                                            const TokenGrad& h) {
-  // The smallest that holds the row.  us with a variant and with the next larger:
-  // (64, 8) 100,000 rows of 1001 bf16 112 / 214, 20,000 of 1001 binary32 31 / 44;
-  // (256, 5) 20,000 of 8000 bf16 110 / 159, 8000 of 9000 56 / 69, but 20,000 of 5000
-  // binary32 148 / 138; (512, 8) 10,000 of 16,000 bf16 123 / 159, 8192 of 32,000 186 /
-  // 201, but 10,000 of 16,000 binary32 224 / 214; (1024, 8) 4096 of 50,257 bf16 160 /
-  // 189, 8192 of 32,000 binary32 362 / 371; (512, 24) 3000 of 80,000 bf16 208 / 258,
-  // 2000 of 45,000 binary32 145 / 147.
+  // The smallest that holds the row.  us with a variant and with the next larger, 2.5e8
+  // bytes of rows, bf16 and binary32: (64, 8) 125 chunks 130 / 258 and 91 / 203, 500
+  // 101 / 112 and 93 / 87; (256, 5) 600 104 / 163 and 82 / 110, 1250 91 / 112 and 92 /
+  // 87; (512, 8) 2500 97 / 111 and 88 / 93, 4000 96 / 104 and 89 / 86; (1024, 8) 5000
+  // 100 / 120 and 86 / 87, 8190 107 / 115 and 96 / 96; (512, 24) 9000 111 / 138 and 92 /
+  // 98, 12,288 107 / 128 and 94 / 98.  Binary32 rows that just fit one of the first
+  // three would be 3 to 6% faster in the next; the rule is the same for both types.
 #define ARC_LOSS(WW, NN)                                                                        \
   if (chunks <= (WW) * (NN)) {                                                                  \
     hipLaunchKernelGGL(a.bf16 ? (token_loss_kernel<true, WW, NN>)                               \

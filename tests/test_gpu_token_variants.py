@@ -74,7 +74,7 @@ def check_scores(x, y, K, scale, top, dtype):
 
 
 # 16-byte chunks of a row, for workgroups of 64, 256, 256, 512 and 1024 threads.
-CHUNKS = [100, 1500, 2900, 5000, 13_000]
+CHUNKS = [100, 1500, 2900, 5000, 20_000]
 
 
 def length(chunks, dtype):
@@ -139,7 +139,7 @@ def mixed(V, gen):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("chunks", CHUNKS + [40_000])
+@pytest.mark.parametrize("chunks", CHUNKS + [13_000, 40_000])
 @pytest.mark.parametrize("top,scale", [(20, 1.0), (0, 0.7)])
 def test_scores_of_rows_unsplit(top, scale, chunks, dtype):
     V = length(chunks, dtype)
