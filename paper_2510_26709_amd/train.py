@@ -39,10 +39,12 @@ class _Bound:
         self.device = torch.device(device or "cuda")
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index
         self.stream = stream or torch.cuda.current_stream(self.device)
+        self._raw_stream = self.stream.cuda_stream
 
     def _check(self, name, x, dtype, count=None):
-        if x.dtype != dtype or x.device != self.device:
+        if x.dtype != dtype or x.get_device() != self._index:  # (half the time of devices)
             raise ValueError(f"{name}: need {dtype} on {self.device}, got {x.dtype} on {x.device}")
         if not x.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
@@ -52,7 +54,7 @@ class _Bound:
 
     def _elsewhere(self):
         # (the raw handles compare in 0.1 us, stream objects in 2)
-        return torch._C._cuda_getCurrentRawStream(self.device.index) != self.stream.cuda_stream
+        return torch._C._cuda_getCurrentRawStream(self._index) != self._raw_stream
 
     def _empty(self, *shape, dtype=torch.float32):
         # memory of the stream that writes it
@@ -63,13 +65,13 @@ class _Bound:
         out.record_stream(torch.cuda.current_stream(self.device))
         return out
 
-    def _used(self, *tensors):
-        """What a call that was made reads or writes: tensors, lists of them, None."""
-        if self._elsewhere():
-            for x in tensors:
-                for y in x if isinstance(x, (list, tuple)) else (x,):
-                    if y is not None:
-                        y.record_stream(self.stream)
+    def _keep(self, *tensors):
+        """What a call on another stream than the current one reads or writes:
+        tensors, lists of them, None."""
+        for x in tensors:
+            for y in x if isinstance(x, (list, tuple)) else (x,):
+                if y is not None:
+                    y.record_stream(self.stream)
 
     def __del__(self):
         try:
@@ -117,7 +119,8 @@ class TokenLogProbs(_Bound):
         arc_tokens_score(self.ctx, T, logits.data_ptr(), stride, targets.data_ptr(), at,
                          at + 4 * T, at + 8 * T, at + 12 * T if k else None,
                          at + 12 * T + 4 * k if k else None)
-        self._used(logits, targets)
+        if self._elsewhere():
+            self._keep(logits, targets)
         logp, entropy, lse, ids, near = out.split_with_sizes((T, T, T, k, k))
         return Scores(logp, entropy, lse, ids.view(torch.int32).view(T, self.top),
                       near.view(T, self.top))
@@ -133,7 +136,8 @@ class TokenLogProbs(_Bound):
                         each("lse", lse, T), each("entropy", entropy, T),
                         each("d_logp", d_logp, T), each("d_entropy", d_entropy, T),
                         each("d_lse", d_lse, T), out, out_stride)
-        self._used(logits, targets, lse, entropy, d_logp, d_entropy, d_lse, out)
+        if self._elsewhere():
+            self._keep(logits, targets, lse, entropy, d_logp, d_entropy, d_lse, out)
         return out
 
     def loss(self, logits, targets, d_logp=None, d_entropy=None, d_lse=None, out=None):
@@ -147,7 +151,8 @@ class TokenLogProbs(_Bound):
         arc_tokens_loss(self.ctx, T, logits, stride, each("targets", targets, T, torch.int64),
                         each("d_logp", d_logp, T), each("d_entropy", d_entropy, T),
                         each("d_lse", d_lse, T), at, at + 4 * T, at + 8 * T, out, out_stride)
-        self._used(logits, targets, d_logp, d_entropy, d_lse, out)
+        if self._elsewhere():
+            self._keep(logits, targets, d_logp, d_entropy, d_lse, out)
         return Loss(*row.split(T) if T else (row,) * 3, out)
 
     def _out(self, out, T):
@@ -224,6 +229,8 @@ class AdamW(_Bound):
         starts = np.cumsum([0] + self.sizes[:-1], dtype=np.uint64)
         self._starts = {2: starts * np.uint64(2), 4: starts * np.uint64(4)}  # in bytes
         self._copy = [torch.bfloat16] * num
+        self._one = {k: d[0] if len(set(d)) == 1 else None for k, d in (
+            ("param", self._param), ("grad", self._grad), ("copy", self._copy))}
         self._table = {k: np.zeros(num, dtype=np.uint64) for k in ("param", "grad", "copy")}
         self._args = {k: ctypes.c_void_p(v.ctypes.data) for k, v in self._table.items()}
         self._flat = sum(self.sizes)
@@ -250,10 +257,11 @@ class AdamW(_Bound):
         """Fills the host table of device pointers of this call."""
         table = self._table[key]
         if isinstance(x, torch.Tensor):  # flat
-            if dtypes.count(dtypes[0]) != len(dtypes):
+            dtype = self._one[key]
+            if dtype is None:
                 raise ValueError(f"{key}: one flat tensor holds one dtype")
-            self._check(key, x, dtypes[0], self._flat)
-            np.add(self._starts[dtypes[0].itemsize], np.uint64(x.data_ptr()), out=table)
+            self._check(key, x, dtype, self._flat)
+            np.add(self._starts[dtype.itemsize], x.data_ptr(), table)
         else:
             if len(x) != len(table):
                 raise ValueError(f"{key}: need {len(table)} tensors, got {len(x)}")
@@ -273,13 +281,15 @@ class AdamW(_Bound):
         at = out.data_ptr()
         arc_optim_norm(self.ctx, self._pointers("grad", grads, self._grad), scale, max_norm,
                        at + 8, at)
-        self._used(grads)
+        if self._elsewhere():
+            self._keep(grads)
         return Norms(*out.split_with_sizes((2, num)))
 
     def step(self, t, params, grads, *, lr, beta1=0.9, beta2=0.999, eps=1e-8, factor=None,
              copies=None):
         """One step t >= 0, in place.  ``factor``: norm()'s total [2], whose
-        second value multiplies the gradients."""
+        second value multiplies the gradients.  (In a captured graph every
+        replay is this step again, t, lr and random bits with it.)"""
         at = None
         if factor is not None:
             at = self._check("factor", factor, torch.float32, 2).data_ptr() + 4
@@ -289,7 +299,8 @@ class AdamW(_Bound):
             self._pointers("grad", grads, self._grad),
             None if copies is None else self._pointers("copy", copies, self._copy),
             at, *self._state_pointers())
-        self._used(params, grads, copies, factor)
+        if self._elsewhere():
+            self._keep(params, grads, copies, factor)
 
     def close(self):
         if getattr(self, "ctx", None):
