@@ -511,6 +511,10 @@ arc_status arc_optim_norm(arc_optim *ctx, const void *const *grads, float scale,
  *           [state_elems / ARC_STATE_BLOCK] (NULL for ARC_STATE_F32); start at
  *           0; 16-byte aligned
  * No two of these may overlap (checked for the states only).
+ * A call captured in a HIP graph repeats its step at every replay: t, lr and the
+ * other numbers, and with t the corrections c1 and c2 and every random bit.  A run
+ * of steps wants a call for each (stochastic rounding with the same bits again and
+ * again is biased).
  */
 arc_status arc_optim_adamw(arc_optim *ctx, const arc_adamw_config *ac, int64_t t,
                            void *const *params, const void *const *grads, void *const *copies,

@@ -117,7 +117,8 @@ __device__ __forceinline__ uint32_t bf16_random(float x, uint32_t draw) {
 
 // 32 random bits of a state's element: its index and the step's key through a
 // bijection of 32-bit words (two multiplications, three folds), with the high
-// half of the key in between.
+// half of the key in between.  Multipliers and shifts are those of least bias that
+// C. Wellons published from a search for such mixers (2018).
 __device__ __forceinline__ uint32_t random_bits(uint32_t z, uint32_t key_high) {
   z = (z ^ (z >> 16)) * 0x7FEB352Du;
   z ^= key_high;
@@ -187,12 +188,12 @@ __device__ __forceinline__ float scale_of(uint32_t most) {
 // 662 / 640 (one pass at a time).
 //
 // States in 8 bits: eight elements a lane, so that 16 lanes hold a block, its
-// largest magnitudes found by four lane permutations.  10 bytes of HBM and 53
-// instructions an element, which take the same time: 1.2e8 bf16 parameters 222
-// to 229 us (5.7 to 5.5 TB/s).  That is with the conversions that scale and round,
-// the root from the reciprocal one and the reciprocal for a division; with a
-// multiply for each scale, a rounding in integers, sqrtf() and a division it was
-// 319 us.
+// largest magnitudes found by four lane permutations.  10 bytes of HBM and 58
+// instructions an element, which take the same time: 1.2e8 bf16 parameters 225
+// to 243 us (5.6 to 5.2 TB/s).  That is with the conversions that scale and round,
+// the root from the reciprocal one (5 instructions for the ends of its range, 3 to
+// 5% of the time) and the reciprocal for a division; with a multiply for each
+// scale, a rounding in integers, sqrtf() and a division it was 319 us.
 template <bool F8, bool STREAM>
 __global__ void __launch_bounds__(kThreads, F8 ? 6 : 4)
 adamw_kernel(OptimBatch b, OptimPointers p, AdamArgs a) {

@@ -34,8 +34,8 @@ constexpr int64_t kPieceChunks = 4 * kSplitThreads, kMostPieces = 16, kSplitPart
 // 196, 6000 94 / 82 / 79 / 86 and 144 / 99 / 96 / 142, 10,000 89 / 84 / 82 / 82 and
 // 140 / 103 / 96 / 115, 16,000 86 / 82 / 81 / 79 and 141 / 100 / 95 / 97, 25,000 122 /
 // 85 / 81 / 79 and 180 / 101 / 97 / 94.  From 3300 to 5500 the larger workgroup gains
-// 1 to 4% without alternatives and loses with 20 of them, 20% falling to 4% (1% with 5
-// at 4000).  Between 512 and 1024 the two kinds together are even near 16,000: 12,600
+// 1 to 4% without alternatives and loses with 20 of them, 20% falling to 4% (with 5,
+// 8192 rows of 4000 chunks 100 / 99).  Between 512 and 1024 the two kinds together are even near 16,000: 12,600
 // bf16 81 / 79 and 97 / 103, binary32 78 / 76 and 93 / 92; 17,500 83 / 81 and 96 / 100,
 // 80 / 77 and 91 / 92; 19,000 83 / 83 and 100 / 100, 80 / 78 and 96 / 93.
 constexpr int64_t kRow64 = 1200, kRow256 = 3300, kRow512 = 16000;
