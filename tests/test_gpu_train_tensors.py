@@ -75,9 +75,9 @@ def test_states_of_another_kind_are_refused(state):
 
 
 def busy(stream):
-    """Some tenths of a second of work that touches no memory."""
+    """About a second of work that touches no memory."""
     with torch.cuda.stream(stream):
-        torch.cuda._sleep(1 << 29)
+        torch.cuda._sleep(1 << 31)
 
 
 def token_calls(h, x, y, up):
