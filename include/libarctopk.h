@@ -399,6 +399,139 @@ arc_status arc_tokens_loss(arc_tokens *ctx, int64_t rows, const void *logits, in
                            const float *d_lse, float *logp, float *entropy, float *lse,
                            void *grad, int64_t grad_stride);
 
+/*
+ * The clipped policy loss of generated tokens, with a KL term against a reference
+ * model and an entropy bonus, and its gradient.
+ *
+ * For a token y >= 0 of log probability l and entropy H (those of arc_tokens_score),
+ * old log probability o, reference log probability f, advantage A and weight
+ * w' = scale * w:
+ *   ratio = exp(l - o)                                 (1 without old_logp)
+ *   gain  = min(ratio A, max(1 - clip_low, min(ratio, 1 + clip_high)) A)
+ *           and, for A < 0 with dual != 0, not below dual A
+ *   KL    = exp(f - l) - (f - l) - 1                   (0 without ref_logp)
+ *   loss  = -gain + kl KL - entropy H
+ *   d loss / d l = -ratio A, or 0 where gain is not ratio A, + kl (1 - exp(f - l))
+ *   d loss / d H = -entropy
+ * totals are the sums over tokens of w' times loss, ratio, KL, H and [gain is not
+ * ratio A] (the token is clipped); gradients are those of the first.  A token with
+ * y < 0 has loss = ratio = KL = 0 and is in no sum; whatever its other inputs hold
+ * is not looked at.  A token with w' = 0 has its loss, ratio and KL, and adds
+ * nothing to sums and gradients, whatever they are.  Elsewhere infinities and NaN
+ * go the way of the formulas (y >= V has l = NaN; a given token that is masked has
+ * l = -infinity, ratio = 0 and, with a KL term, an infinite gradient).
+ *
+ * Terms are binary32; totals are summed in binary64 in a fixed order and rounded
+ * once.
+ */
+#define ARC_POLICY_TOTALS 5
+
+typedef struct {
+  float clip_low;  /* 0 .. 1                                              */
+  float clip_high; /* >= 0, or infinity for no upper border               */
+  float dual;      /* 0 for none, or finite and at least 1                */
+  float kl;        /* finite, >= 0                                        */
+  float entropy;   /* finite                                              */
+  float scale;     /* of all weights, finite (1 / tokens for a mean)      */
+} arc_policy_config;
+
+/*
+ * From `rows` rows of logits to their gradient: arc_tokens_score's logits, stride,
+ * targets, logp, entropy and lse (each output may be NULL) and arc_tokens_grad's
+ * grad and grad_stride, and device pointers:
+ *   old_logp, ref_logp, weights   [rows] binary32; each may be NULL (ref_logp
+ *                                 where kl is 0; NULL weights are 1)
+ *   advantages        [rows] binary32
+ *   loss, ratio, kl   [rows] binary32, not weighted; each may be NULL
+ *   totals            [ARC_POLICY_TOTALS] binary32
+ * Outputs must not overlap one another or the inputs, but grad may be the logits.
+ */
+arc_status arc_tokens_policy(arc_tokens *ctx, const arc_policy_config *cfg, int64_t rows,
+                             const void *logits, int64_t stride, const int64_t *targets,
+                             const float *old_logp, const float *ref_logp,
+                             const float *advantages, const float *weights, float *logp,
+                             float *entropy, float *lse, float *loss, float *ratio, float *kl,
+                             float *totals, void *grad, int64_t grad_stride);
+
+/*
+ * The same from log probabilities: logp and entropy [rows] (entropy may be NULL
+ * where its coefficient is 0) to d_logp and d_entropy [rows] (each may be NULL),
+ * the upstream gradients that arc_tokens_grad takes.
+ */
+arc_status arc_tokens_policy_terms(arc_tokens *ctx, const arc_policy_config *cfg, int64_t rows,
+                                   const float *logp, const float *entropy,
+                                   const int64_t *targets, const float *old_logp,
+                                   const float *ref_logp, const float *advantages,
+                                   const float *weights, float *loss, float *ratio, float *kl,
+                                   float *totals, float *d_logp, float *d_entropy);
+
+/*
+ * The loss of preferred and rejected answers by their paired log ratios, and its
+ * gradient.
+ *
+ * The rows are tokens of 2 P sequences one after the other: sequence s is rows
+ * [offsets[s], offsets[s + 1]), the P preferred ones first, and sequence P + p is
+ * what p's was preferred to.  With l and f the log probabilities of a sequence's
+ * given tokens (y >= 0) and those of a reference model (0 without ref_logp):
+ *   h_s = sum (l - f), or with `average` its mean (0 for a sequence without tokens)
+ *   reward_s = beta h_s        z = reward_p - reward_(P+p) - margin
+ *   sigmoid:  loss = -(1 - smoothing) log sigmoid(z) - smoothing log sigmoid(-z)
+ *   hinge:    loss = max(0, 1 - z)
+ *   squared:  loss = ((z - 1/2) / beta)^2
+ * totals are the sums over pairs of w' = scale * w times loss, reward_p -
+ * reward_(P+p) and [reward_p > reward_(P+p)]; gradients are those of the first.  A
+ * pair with w' = 0 has its loss and rewards and adds nothing to sums and
+ * gradients; rows without a token, before the first and behind the last sequence
+ * have the gradient 0.  Sums and pairs are in binary64, in a fixed order.
+ *
+ * offsets are on the device and not seen by the host: they have to ascend from >= 0
+ * to at most `rows`.  Others give other sums, and nothing outside the rows is read
+ * or written for them.
+ */
+#define ARC_PREFERENCE_TOTALS 3
+
+typedef enum {
+  ARC_PREFERENCE_SIGMOID = 0,
+  ARC_PREFERENCE_HINGE = 1,
+  ARC_PREFERENCE_SQUARED = 2
+} arc_preference;
+
+typedef struct {
+  int32_t kind;    /* arc_preference                                      */
+  int32_t average; /* 1: means over tokens, not sums                      */
+  float beta;      /* 2^-20 .. 2^20                                       */
+  float margin;    /* finite                                              */
+  float smoothing; /* 0 .. 1/2; 0 but for the sigmoid                     */
+  float scale;     /* of all weights, finite (1 / pairs for a mean)       */
+} arc_preference_config;
+
+/*
+ * From `rows` rows of logits to their gradient: arc_tokens_score's logits, stride,
+ * targets, logp, entropy and lse (each output may be NULL) and arc_tokens_grad's
+ * grad and grad_stride, and device pointers:
+ *   offsets    [2 pairs + 1] int64 (pairs 0 .. 2^30; may be NULL for 0)
+ *   ref_logp   [rows] binary32, may be NULL
+ *   weights    [pairs] binary32, NULL for 1
+ *   loss       [pairs] binary32, not weighted; may be NULL
+ *   rewards    [2 pairs] binary32; may be NULL
+ *   totals     [ARC_PREFERENCE_TOTALS] binary32
+ * Outputs must not overlap one another or the inputs, but grad may be the logits.
+ */
+arc_status arc_tokens_preference(arc_tokens *ctx, const arc_preference_config *cfg, int64_t rows,
+                                 const void *logits, int64_t stride, const int64_t *targets,
+                                 int64_t pairs, const int64_t *offsets, const float *ref_logp,
+                                 const float *weights, float *logp, float *entropy, float *lse,
+                                 float *loss, float *rewards, float *totals, void *grad,
+                                 int64_t grad_stride);
+
+/* The same from log probabilities: logp [rows] to d_logp [rows] (may be NULL),
+ * the upstream gradient that arc_tokens_grad takes. */
+arc_status arc_tokens_preference_terms(arc_tokens *ctx, const arc_preference_config *cfg,
+                                       int64_t rows, const float *logp, const int64_t *targets,
+                                       int64_t pairs, const int64_t *offsets,
+                                       const float *ref_logp, const float *weights, float *loss,
+                                       float *rewards, float *totals, float *d_logp);
+
 /* Waits for the context's stream; NULL is accepted. */
 arc_status arc_tokens_destroy(arc_tokens *ctx);
 

@@ -20,7 +20,11 @@ from ._lib import (  # noqa: F401
     arc_optim_adamw, arc_optim_config, arc_optim_create, arc_optim_destroy, arc_optim_norm,
     arc_optim_state_elems, arc_optim_state_offset, arc_optim_tensor, arc_tokens_config,
     arc_tokens_create, arc_tokens_destroy, arc_tokens_grad, arc_tokens_loss, arc_tokens_score,
-    make_optim_config, make_tokens_config)
+    make_optim_config, make_tokens_config,
+    ARC_POLICY_TOTALS, ARC_PREFERENCE_HINGE, ARC_PREFERENCE_SIGMOID, ARC_PREFERENCE_SQUARED,
+    ARC_PREFERENCE_TOTALS, PREFERENCES, arc_policy_config, arc_preference_config,
+    arc_tokens_policy, arc_tokens_policy_terms, arc_tokens_preference,
+    arc_tokens_preference_terms)
 
 
 class Compressor:

@@ -128,6 +128,34 @@ class arc_adamw_config(ctypes.Structure):
     ]
 
 
+class arc_policy_config(ctypes.Structure):
+    _fields_ = [
+        ("clip_low", ctypes.c_float),
+        ("clip_high", ctypes.c_float),
+        ("dual", ctypes.c_float),
+        ("kl", ctypes.c_float),
+        ("entropy", ctypes.c_float),
+        ("scale", ctypes.c_float),
+    ]
+
+
+ARC_POLICY_TOTALS, ARC_PREFERENCE_TOTALS = 5, 3
+ARC_PREFERENCE_SIGMOID, ARC_PREFERENCE_HINGE, ARC_PREFERENCE_SQUARED = 0, 1, 2
+PREFERENCES = {"sigmoid": ARC_PREFERENCE_SIGMOID, "hinge": ARC_PREFERENCE_HINGE,
+               "squared": ARC_PREFERENCE_SQUARED}
+
+
+class arc_preference_config(ctypes.Structure):
+    _fields_ = [
+        ("kind", ctypes.c_int32),
+        ("average", ctypes.c_int32),
+        ("beta", ctypes.c_float),
+        ("margin", ctypes.c_float),
+        ("smoothing", ctypes.c_float),
+        ("scale", ctypes.c_float),
+    ]
+
+
 def make_tokens_config(*, vocab, max_rows, dtype=ARC_DTYPE_BF16, top=0, scale=1.0,
                        reserved=0) -> arc_tokens_config:
     return arc_tokens_config(vocab, max_rows, dtype, top, scale, reserved)
@@ -176,6 +204,16 @@ _SIGS = {
                               _vp, _vp, ctypes.c_int64]),
     "arc_tokens_loss": (_st, [_vp, ctypes.c_int64, _vp, ctypes.c_int64, _vp, _vp, _vp, _vp, _vp,
                               _vp, _vp, _vp, ctypes.c_int64]),
+    "arc_tokens_policy": (_st, [_vp, ctypes.POINTER(arc_policy_config), ctypes.c_int64, _vp,
+                                ctypes.c_int64] + [_vp] * 13 + [ctypes.c_int64]),
+    "arc_tokens_policy_terms": (_st, [_vp, ctypes.POINTER(arc_policy_config), ctypes.c_int64]
+                                + [_vp] * 13),
+    "arc_tokens_preference": (_st, [_vp, ctypes.POINTER(arc_preference_config), ctypes.c_int64,
+                                    _vp, ctypes.c_int64, _vp, ctypes.c_int64] + [_vp] * 10
+                              + [ctypes.c_int64]),
+    "arc_tokens_preference_terms": (_st, [_vp, ctypes.POINTER(arc_preference_config),
+                                          ctypes.c_int64, _vp, _vp, ctypes.c_int64]
+                                    + [_vp] * 7),
     "arc_tokens_destroy": (_st, [_vp]),
     "arc_optim_create": (_st, [ctypes.POINTER(arc_optim_config), _vp, ctypes.POINTER(_vp)]),
     "arc_optim_state_elems": (ctypes.c_int64, [_vp]),
@@ -334,6 +372,45 @@ def arc_tokens_loss(ctx, rows, logits, stride, targets, d_logp, d_entropy, d_lse
     _check(_lib.arc_tokens_loss(ctx, rows, _addr(logits), stride, _addr(targets), _addr(d_logp),
                                 _addr(d_entropy), _addr(d_lse), _addr(logp), _addr(entropy),
                                 _addr(lse), _addr(grad), grad_stride), "arc_tokens_loss")
+
+
+def arc_tokens_policy(ctx, cfg: arc_policy_config, rows, logits, stride, targets, old_logp,
+                      ref_logp, advantages, weights, logp, entropy, lse, loss, ratio, kl, totals,
+                      grad, grad_stride) -> None:
+    _check(_lib.arc_tokens_policy(ctx, ctypes.byref(cfg), rows, _addr(logits), stride,
+                                  *map(_addr, (targets, old_logp, ref_logp, advantages, weights,
+                                               logp, entropy, lse, loss, ratio, kl, totals,
+                                               grad)), grad_stride), "arc_tokens_policy")
+
+
+def arc_tokens_policy_terms(ctx, cfg: arc_policy_config, rows, logp, entropy, targets, old_logp,
+                            ref_logp, advantages, weights, loss, ratio, kl, totals, d_logp,
+                            d_entropy) -> None:
+    _check(_lib.arc_tokens_policy_terms(ctx, ctypes.byref(cfg), rows,
+                                        *map(_addr, (logp, entropy, targets, old_logp, ref_logp,
+                                                     advantages, weights, loss, ratio, kl,
+                                                     totals, d_logp, d_entropy))),
+           "arc_tokens_policy_terms")
+
+
+def arc_tokens_preference(ctx, cfg: arc_preference_config, rows, logits, stride, targets, pairs,
+                          offsets, ref_logp, weights, logp, entropy, lse, loss, rewards, totals,
+                          grad, grad_stride) -> None:
+    _check(_lib.arc_tokens_preference(ctx, ctypes.byref(cfg), rows, _addr(logits), stride,
+                                      _addr(targets), pairs,
+                                      *map(_addr, (offsets, ref_logp, weights, logp, entropy, lse,
+                                                   loss, rewards, totals, grad)), grad_stride),
+           "arc_tokens_preference")
+
+
+def arc_tokens_preference_terms(ctx, cfg: arc_preference_config, rows, logp, targets, pairs,
+                                offsets, ref_logp, weights, loss, rewards, totals,
+                                d_logp) -> None:
+    _check(_lib.arc_tokens_preference_terms(ctx, ctypes.byref(cfg), rows, _addr(logp),
+                                            _addr(targets), pairs,
+                                            *map(_addr, (offsets, ref_logp, weights, loss,
+                                                         rewards, totals, d_logp))),
+           "arc_tokens_preference_terms")
 
 
 def arc_tokens_destroy(ctx) -> None:

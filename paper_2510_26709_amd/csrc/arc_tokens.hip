@@ -9,6 +9,8 @@
 #include <type_traits>
 
 #include "arc_device.h"
+#include "arc_objective.h"
+#include "arc_policy.h"
 #include "arc_train.h"
 
 namespace arc {
@@ -674,12 +676,8 @@ struct GradRow {
   bool zero;
 };
 
-__device__ __forceinline__ GradRow grad_row(const TokenArgs& a, const TokenGrad& g, int64_t i,
-                                            float H, bool empty) {
-  const int64_t y = g.d_logp ? a.targets[i] : -1;
-  const float dl = y >= 0 ? g.d_logp[i] : 0.f;
-  const float dh = g.d_entropy ? g.d_entropy[i] : 0.f;
-  const float dz = g.d_lse ? g.d_lse[i] : 0.f;
+__device__ __forceinline__ GradRow grad_row(const TokenArgs& a, int64_t y, float dl, float dh,
+                                            float dz, float H, bool empty) {
   GradRow r;
   r.A = a.scale * (dz - dl - (dh != 0.f ? dh * H : 0.f));
   r.B = -a.scale * dh;
@@ -687,6 +685,13 @@ __device__ __forceinline__ GradRow grad_row(const TokenArgs& a, const TokenGrad&
   r.zero = (dl == 0.f && dh == 0.f && dz == 0.f) || empty;
   r.y = y < a.vocab && !r.zero ? (int32_t)y : -1;
   return r;
+}
+
+__device__ __forceinline__ GradRow grad_row(const TokenArgs& a, const TokenGrad& g, int64_t i,
+                                            float H, bool empty) {
+  const int64_t y = g.d_logp ? a.targets[i] : -1;
+  return grad_row(a, y, y >= 0 ? g.d_logp[i] : 0.f, g.d_entropy ? g.d_entropy[i] : 0.f,
+                  g.d_lse ? g.d_lse[i] : 0.f, H, empty);
 }
 
 // Natural logarithms of p below this have p = 0, and 0 * infinity is none.
@@ -803,10 +808,11 @@ token_grad_kernel(TokenArgs a, TokenGrad g, int32_t tiles) {
 // relative to the row's reference, A' and B' divided by the row's sum.  8192 rows of
 // 32,000 binary32 361 us (5.8 TB/s): HBM.  4096 of 50,257 bf16 159 us (5.2 TB/s): two
 // workgroups a compute unit that read, add and write more or less in step (three
-// of its 19 instructions an element left out made no difference).
-template <bool BF16, int W, int N>
+// of its 19 instructions an element left out made no difference).  POLICY: the
+// upstream gradients come from the row's own logp and entropy (policy_term()).
+template <bool BF16, int W, int N, bool POLICY>
 __global__ void __launch_bounds__(W, N <= 8 ? 8 : 4)
-token_loss_kernel(TokenArgs a, TokenScores out, TokenGrad g) {
+token_loss_kernel(TokenArgs a, TokenScores out, TokenGrad g, PolicyArgs p) {
   using S = Scorer<BF16, W>;
   constexpr int C = S::C;
   __shared__ float part_most[S::kWaves];
@@ -887,7 +893,14 @@ token_loss_kernel(TokenArgs a, TokenScores out, TokenGrad g) {
   }
   const RowResult res = finish_row(a, out, i, s, y, given);
   const float H = res.empty ? 0.f : res.log_total - s.spread * kLn2 / s.total;
-  const GradRow r = grad_row(a, g, i, H, res.empty);
+  GradRow r;
+  if constexpr (POLICY) {
+    const float logp = y >= a.vocab ? NAN : res.logp(given);
+    const PolicyTerm t = policy_term(p, i, y >= 0, logp, H);
+    r = grad_row(a, y, t.d_logp, t.d_entropy, 0.f, H, res.empty);
+  } else {
+    r = grad_row(a, g, i, H, res.empty);
+  }
   // p (A + B log p) with p = 2^t / total: 2^t (A' + B' t).  (t less the logarithm
   // of the total would be rounded as R is, however large.)
   const float B = r.B * kLn2 / s.total;
@@ -1025,7 +1038,7 @@ hipError_t launch_token_grad(const TokenArgs& a, const TokenGrad& g, hipStream_t
 }
 
 bool launch_token_loss(const TokenArgs& a, const TokenScores& out, const TokenGrad& g,
-                       hipStream_t stream, hipError_t* e) {
+                       hipStream_t stream, hipError_t* e, const PolicyArgs* policy) {
   *e = hipSuccess;
   if (a.rows <= 0) return true;
   const int64_t chunks = a.vocab / (a.bf16 ? 8 : 4);
@@ -1035,6 +1048,7 @@ bool launch_token_loss(const TokenArgs& a, const TokenScores& out, const TokenGr
   // 64 of 128,256 bf16 25.6 / 16.1, 128 26.4 / 24.9, 256 32.8 / 40.3.
   if (chunks > 5000 && a.rows <= (chunks > 12288 && a.bf16 ? 128 : 32)) return false;
   bool found = true;
+  PolicyArgs p = policy ? *policy : PolicyArgs{};
   each_rows(a, out, g, kRowsPerLaunch, [&](const TokenArgs& b, const TokenScores& o,
                                            const TokenGrad& h) {
   // The smallest that holds the row.  us with a variant and with the next larger, 2.5e8
@@ -1046,9 +1060,11 @@ bool launch_token_loss(const TokenArgs& a, const TokenScores& out, const TokenGr
   // three would be 3 to 6% faster in the next; the rule is the same for both types.
 #define ARC_LOSS(WW, NN)                                                                        \
   if (chunks <= (WW) * (NN)) {                                                                  \
-    hipLaunchKernelGGL(a.bf16 ? (token_loss_kernel<true, WW, NN>)                               \
-                              : (token_loss_kernel<false, WW, NN>),                             \
-                       dim3((unsigned)b.rows), dim3(WW), 0, stream, b, o, h);                   \
+    hipLaunchKernelGGL(policy ? (a.bf16 ? (token_loss_kernel<true, WW, NN, true>)               \
+                                        : (token_loss_kernel<false, WW, NN, true>))             \
+                              : (a.bf16 ? (token_loss_kernel<true, WW, NN, false>)              \
+                                        : (token_loss_kernel<false, WW, NN, false>)),           \
+                       dim3((unsigned)b.rows), dim3(WW), 0, stream, b, o, h, p);                \
   } else
     ARC_LOSS(64, 8)
     ARC_LOSS(256, 5)
@@ -1058,6 +1074,8 @@ bool launch_token_loss(const TokenArgs& a, const TokenScores& out, const TokenGr
     ARC_LOSS(1024, 24)
     found = false;
 #undef ARC_LOSS
+    for (const float** q : {&p.old_logp, &p.ref_logp, &p.advantages, &p.weights})
+      if (*q) *q += b.rows;
   });
   *e = hipGetLastError();
   return found;

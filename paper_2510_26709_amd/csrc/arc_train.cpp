@@ -11,24 +11,9 @@
 
 #include "arc_context.h"
 #include "arc_train.h"
+#include "arc_train_host.h"
 
 static_assert(arc::kStateBlock == ARC_STATE_BLOCK, "one block size");
-
-struct arc_tokens {
-  int64_t vocab = 0, max_rows = 0;
-  int32_t bf16 = 0, top = 0;
-  float scale = 1.f;
-  hipStream_t stream = nullptr;
-  int device = 0;
-  void* workspace = nullptr;
-  float* row_values = nullptr;  // between a loss's two launches: sums, then entropies
-
-  void release() {
-    (void)hipStreamSynchronize(stream);
-    if (workspace) (void)hipFree(workspace);
-    if (row_values) (void)hipFree(row_values);
-  }
-};
 
 struct arc_optim {
   std::vector<arc::OptimTensor> tensors;
@@ -58,127 +43,17 @@ struct arc_optim {
 
 namespace {
 
+using arc::any_overlap;
+using arc::check_grad;
+using arc::check_rows;
+using arc::check_score;
+using arc::device_copy;
 using arc::fail;
-
-// Work goes to the context's device whatever the caller's current one is.
-class OnDevice {
- public:
-  explicit OnDevice(int device) {
-    if (hipGetDevice(&before_) == hipSuccess && before_ != device) {
-      changed_ = true;
-      (void)hipSetDevice(device);
-    }
-  }
-  ~OnDevice() {
-    if (changed_) (void)hipSetDevice(before_);
-  }
-  OnDevice(const OnDevice&) = delete;
-  OnDevice& operator=(const OnDevice&) = delete;
-
- private:
-  int before_ = 0;
-  bool changed_ = false;
-};
-
-struct Range {
-  const void* p;
-  int64_t bytes;
-};
-
-bool overlap(const Range& a, const Range& b) {
-  if (a.p == nullptr || b.p == nullptr || a.bytes <= 0 || b.bytes <= 0) return false;
-  const uintptr_t pa = reinterpret_cast<uintptr_t>(a.p), pb = reinterpret_cast<uintptr_t>(b.p);
-  return pa < pb + static_cast<uintptr_t>(b.bytes) && pb < pa + static_cast<uintptr_t>(a.bytes);
-}
-
-// Whether an output overlaps another one or an input.
-bool any_overlap(std::initializer_list<Range> outputs, std::initializer_list<Range> inputs) {
-  for (const Range* a = outputs.begin(); a != outputs.end(); ++a) {
-    for (const Range* b = a + 1; b != outputs.end(); ++b)
-      if (overlap(*a, *b)) return true;
-    for (const Range& b : inputs)
-      if (overlap(*a, b)) return true;
-  }
-  return false;
-}
-
-bool finite(float v) { return std::isfinite(v); }
-
-template <typename T>
-arc_status device_copy(T** to, const std::vector<T>& from, const char* what) {
-  const size_t bytes = std::max<size_t>(from.size(), 1) * sizeof(T);
-  hipError_t e = hipMalloc(reinterpret_cast<void**>(to), bytes);
-  if (e != hipSuccess) {
-    *to = nullptr;
-    (void)hipGetLastError();
-    return arc::fail_hip(e, what);
-  }
-  if (!from.empty())
-    ARC_HIP(hipMemcpy(*to, from.data(), from.size() * sizeof(T), hipMemcpyHostToDevice), what);
-  return ARC_OK;
-}
-
-// ---------------------------------------------------------------- tokens
-
-int64_t row_bytes(const arc_tokens* c, int64_t rows, int64_t stride) {
-  return rows <= 0 ? 0 : ((rows - 1) * stride + c->vocab) * (c->bf16 ? 2 : 4);
-}
-
-arc_status check_rows(const arc_tokens* c, int64_t rows, const void* logits, int64_t stride) {
-  if (c == nullptr) return fail(ARC_ERR_INVALID, "ctx is NULL");
-  if (rows < 0 || rows > c->max_rows) return fail(ARC_ERR_INVALID, "rows must be in 0..max_rows");
-  if (rows > 0 && logits == nullptr) return fail(ARC_ERR_INVALID, "logits is NULL");
-  if (stride < c->vocab) return fail(ARC_ERR_INVALID, "stride must be at least vocab");
-  if (stride > INT64_MAX / 8 / std::max<int64_t>(rows, 1))
-    return fail(ARC_ERR_INVALID, "rows * stride overflows");
-  return ARC_OK;
-}
-
-arc::TokenArgs token_args(const arc_tokens* c, int64_t rows, const void* logits, int64_t stride,
-                          const int64_t* targets) {
-  arc::TokenArgs a;
-  a.logits = logits;
-  a.targets = targets;
-  a.rows = rows;
-  a.stride = stride;
-  a.vocab = c->vocab;
-  a.scale = c->scale;
-  a.bf16 = c->bf16;
-  a.top = c->top;
-  return a;
-}
-
-arc_status check_score(const arc_tokens* c, int64_t rows, const void* logits, int64_t stride,
-                       const int64_t* targets, const arc::TokenScores& out) {
-  if (out.logp != nullptr && targets == nullptr)
-    return fail(ARC_ERR_INVALID, "logp needs targets");
-  if ((out.top_ids == nullptr) != (out.top_logp == nullptr))
-    return fail(ARC_ERR_INVALID, "top_ids and top_logp are given together");
-  const int64_t v = rows * 4, k = v * c->top;
-  if (any_overlap({{out.logp, v}, {out.entropy, v}, {out.lse, v}, {out.top_ids, k},
-                   {out.top_logp, k}},
-                  {{logits, row_bytes(c, rows, stride)}, {targets, rows * 8}}))
-    return fail(ARC_ERR_INVALID, "outputs must not overlap one another or the inputs");
-  return ARC_OK;
-}
-
-arc_status check_grad(const arc_tokens* c, int64_t rows, const void* logits, int64_t stride,
-                      const int64_t* targets, const arc::TokenGrad& g) {
-  if (rows > 0 && g.grad == nullptr) return fail(ARC_ERR_INVALID, "grad is NULL");
-  if (g.stride < c->vocab) return fail(ARC_ERR_INVALID, "grad_stride must be at least vocab");
-  if (g.stride > INT64_MAX / 8 / std::max<int64_t>(rows, 1))
-    return fail(ARC_ERR_INVALID, "rows * grad_stride overflows");
-  if (g.d_logp != nullptr && targets == nullptr)
-    return fail(ARC_ERR_INVALID, "d_logp needs targets");
-  const int64_t v = rows * 4;
-  const bool in_place = g.grad == logits && g.stride == stride;
-  if (any_overlap({{g.grad, row_bytes(c, rows, g.stride)}},
-                  {{in_place ? nullptr : logits, row_bytes(c, rows, stride)}, {targets, rows * 8},
-                   {g.lse, v}, {g.entropy, v}, {g.d_logp, v}, {g.d_entropy, v}, {g.d_lse, v}}))
-    return fail(ARC_ERR_INVALID,
-                "grad must not overlap the inputs (unless it is the logits themselves)");
-  return ARC_OK;
-}
+using arc::finite;
+using arc::OnDevice;
+using arc::overlap;
+using arc::row_bytes;
+using arc::token_args;
 
 // ---------------------------------------------------------------- optimizer
 
@@ -332,9 +207,14 @@ arc_status arc_tokens_create(const arc_tokens_config* cfg, void* hip_stream, arc
   }
   if (e == hipSuccess) {
     e = hipMalloc(reinterpret_cast<void**>(&c->row_values),
-                  static_cast<size_t>(c->max_rows) * 3 * sizeof(float));
+                  static_cast<size_t>(c->max_rows) * 6 * sizeof(float));
     if (e != hipSuccess) c->row_values = nullptr;
   }
+  if (e == hipSuccess) {
+    e = hipMalloc(reinterpret_cast<void**>(&c->scratch), sizeof(arc::ObjectiveScratch));
+    if (e != hipSuccess) c->scratch = nullptr;
+  }
+  if (e == hipSuccess) e = hipMemset(c->scratch, 0, sizeof(arc::ObjectiveScratch));
   if (e == hipSuccess) e = hipMemset(c->workspace, 0, bytes);
   if (e == hipSuccess) e = hipDeviceSynchronize();
   if (e != hipSuccess) {
@@ -401,7 +281,7 @@ arc_status arc_tokens_loss(arc_tokens* c, int64_t rows, const void* logits, int6
     return ARC_OK;
   }
   out.sums = c->row_values;
-  if (entropy == nullptr) out.entropy = c->row_values + 2 * c->max_rows;
+  if (entropy == nullptr) out.entropy = c->entropies();
   g.sums = out.sums;
   g.entropy = out.entropy;
   ARC_HIP(arc::launch_token_score(a, out, c->workspace, c->stream), "token score launch");

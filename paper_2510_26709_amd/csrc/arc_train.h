@@ -40,9 +40,11 @@ size_t token_workspace_bytes();
 hipError_t launch_token_score(const TokenArgs& a, const TokenScores& out, void* workspace,
                               hipStream_t stream);
 // Both in one pass, where a workgroup can hold a row (false: it cannot, and
-// nothing was launched); g's lse and entropy are not read.
+// nothing was launched); g's lse and entropy are not read.  With `policy` the
+// upstream gradients are the policy loss's, and g's are not read.
+struct PolicyArgs;
 bool launch_token_loss(const TokenArgs& a, const TokenScores& out, const TokenGrad& g,
-                       hipStream_t stream, hipError_t* e);
+                       hipStream_t stream, hipError_t* e, const PolicyArgs* policy = nullptr);
 hipError_t launch_token_grad(const TokenArgs& a, const TokenGrad& g, hipStream_t stream);
 
 // ---------------------------------------------------------------- optimizer

@@ -19,16 +19,22 @@ import numpy as np
 import torch
 
 from . import _lib
-from ._lib import (ARC_DTYPE_BF16, ARC_DTYPE_F32, ARC_STATE_BLOCK, ARC_STATE_F32, ARC_STATE_F8,
-                   arc_adamw_config, arc_optim_adamw, arc_optim_create, arc_optim_destroy,
+from ._lib import (ARC_DTYPE_BF16, ARC_DTYPE_F32, ARC_POLICY_TOTALS, ARC_PREFERENCE_TOTALS,
+                   ARC_STATE_BLOCK, ARC_STATE_F32, ARC_STATE_F8, PREFERENCES, arc_adamw_config, arc_optim_adamw, arc_optim_create, arc_optim_destroy,
                    arc_optim_norm, arc_optim_state_elems, arc_optim_state_offset,
-                   arc_tokens_create, arc_tokens_destroy, arc_tokens_grad, arc_tokens_loss,
+                   arc_policy_config, arc_preference_config, arc_tokens_create,
+                   arc_tokens_destroy, arc_tokens_grad, arc_tokens_loss, arc_tokens_policy,
+                   arc_tokens_policy_terms, arc_tokens_preference, arc_tokens_preference_terms,
                    arc_tokens_score, make_optim_config, make_tokens_config)
 
 _DTYPES = {"f32": (ARC_DTYPE_F32, torch.float32), "bf16": (ARC_DTYPE_BF16, torch.bfloat16)}
 
 Scores = namedtuple("Scores", "logp entropy lse top_ids top_logp")
 Loss = namedtuple("Loss", "logp entropy lse grad")
+Policy = namedtuple("Policy", "totals loss ratio kl d_logp d_entropy")
+PolicyLoss = namedtuple("PolicyLoss", "totals logp entropy lse loss ratio kl grad")
+Preference = namedtuple("Preference", "totals loss rewards d_logp")
+PreferenceLoss = namedtuple("PreferenceLoss", "totals logp entropy lse loss rewards grad")
 Norms = namedtuple("Norms", "total norms")
 
 
@@ -154,6 +160,114 @@ class TokenLogProbs(_Bound):
         if self._elsewhere():
             self._keep(logits, targets, d_logp, d_entropy, d_lse, out)
         return Loss(*row.split(T) if T else (row,) * 3, out)
+
+    def _policy_inputs(self, T, targets, advantages, old_logp, ref_logp, weights):
+        each = self._each
+        return (each("targets", targets, T, torch.int64), each("old_logp", old_logp, T),
+                each("ref_logp", ref_logp, T), each("advantages", advantages, T),
+                each("weights", weights, T))
+
+    def policy_loss(self, logits, targets, advantages, *, old_logp=None, ref_logp=None,
+                    weights=None, clip_low=0.2, clip_high=0.2, dual=0.0, kl_coef=0.0,
+                    entropy_coef=0.0, scale=1.0, out=None):
+        """The clipped policy loss with a KL term and an entropy bonus: (totals
+        [5]: loss, ratio, KL, entropy and clipped share, weighted; logp, entropy,
+        lse, loss, ratio, kl [T]; grad [T, V], of the first total).  ``weights``
+        [T] times ``scale`` is each token's part (scale = 1 / tokens for a mean);
+        without ``old_logp`` the ratio is 1.  ``out``: where to write the gradient
+        (the logits themselves allowed)."""
+        T, stride = self._rows(logits)
+        out, out_stride = self._out(out, T)
+        y, old, ref, A, w = self._policy_inputs(T, targets, advantages, old_logp, ref_logp,
+                                                weights)
+        row = self._empty(6 * T + ARC_POLICY_TOTALS)
+        at = [row.data_ptr() + 4 * k * T for k in range(7)]
+        arc_tokens_policy(self.ctx, arc_policy_config(clip_low, clip_high, dual, kl_coef,
+                                                      entropy_coef, scale),
+                          T, logits, stride, y, old, ref, A, w, *at, out, out_stride)
+        if self._elsewhere():
+            self._keep(logits, targets, old_logp, ref_logp, advantages, weights, out)
+        *rows, totals = row.split_with_sizes((T,) * 6 + (ARC_POLICY_TOTALS,))
+        return PolicyLoss(totals, *rows, out)
+
+    def policy(self, logp, targets, advantages, *, entropy=None, old_logp=None, ref_logp=None,
+               weights=None, clip_low=0.2, clip_high=0.2, dual=0.0, kl_coef=0.0,
+               entropy_coef=0.0, scale=1.0):
+        """The same from scored rows: (totals [5], loss, ratio, kl, d_logp and, where
+        entropy_coef is not 0, d_entropy [T]); d_logp and d_entropy are for ``grad``."""
+        T = targets.numel()
+        y, old, ref, A, w = self._policy_inputs(T, targets, advantages, old_logp, ref_logp,
+                                                weights)
+        self._each("logp", logp, T)
+        self._each("entropy", entropy, T)
+        n = 5 if entropy_coef else 4
+        row = self._empty(n * T + ARC_POLICY_TOTALS)
+        at = [row.data_ptr() + 4 * k * T for k in range(n + 1)]
+        loss, ratio, kl, d_logp, *d_entropy, totals = at
+        arc_tokens_policy_terms(self.ctx, arc_policy_config(clip_low, clip_high, dual, kl_coef,
+                                                            entropy_coef, scale),
+                                T, logp, entropy, y, old, ref, A, w, loss, ratio, kl, totals,
+                                d_logp, d_entropy[0] if d_entropy else None)
+        if self._elsewhere():
+            self._keep(logp, entropy, targets, old_logp, ref_logp, advantages, weights)
+        *rows, totals = row.split_with_sizes((T,) * n + (ARC_POLICY_TOTALS,))
+        return Policy(totals, *rows, *(() if entropy_coef else (None,)))
+
+    def _pairs(self, T, targets, offsets, ref_logp, weights):
+        P = (offsets.numel() - 1) // 2
+        if offsets.numel() != 2 * P + 1:
+            raise ValueError(f"offsets: need 2 * pairs + 1 elements, got {offsets.numel()}")
+        self._each("targets", targets, T, torch.int64)
+        self._each("offsets", offsets, 2 * P + 1, torch.int64)
+        self._each("ref_logp", ref_logp, T)
+        self._each("weights", weights, P)
+        return P
+
+    def preference_loss(self, logits, targets, offsets, *, ref_logp=None, weights=None,
+                        kind="sigmoid", beta=0.1, margin=0.0, smoothing=0.0, average=False,
+                        scale=1.0, out=None):
+        """The loss of preferred and rejected answers by their paired log ratios:
+        (totals [3]: loss, margin of the rewards and share of pairs whose preferred
+        answer has the larger one, weighted; logp, entropy, lse [T]; loss [P];
+        rewards [2 P]; grad [T, V], of the first total).  The rows are 2 P sequences
+        one after the other, the preferred ones first; ``offsets`` [2 P + 1] int64,
+        ascending in 0 .. T, says where they begin and end.  ``weights`` [P] times
+        ``scale`` is each pair's part.  ``out``: where to write the gradient (the
+        logits themselves allowed)."""
+        T, stride = self._rows(logits)
+        P = self._pairs(T, targets, offsets, ref_logp, weights)
+        out, out_stride = self._out(out, T)
+        row = self._empty(3 * T + 3 * P + ARC_PREFERENCE_TOTALS)
+        at = row.data_ptr()
+        arc_tokens_preference(
+            self.ctx, arc_preference_config(PREFERENCES[kind], average, beta, margin, smoothing,
+                                            scale),
+            T, logits, stride, targets, P, offsets, ref_logp, weights, at, at + 4 * T, at + 8 * T,
+            at + 12 * T, at + 4 * (3 * T + P), at + 12 * (T + P), out, out_stride)
+        if self._elsewhere():
+            self._keep(logits, targets, offsets, ref_logp, weights, out)
+        *rows, totals = row.split_with_sizes((T, T, T, P, 2 * P, ARC_PREFERENCE_TOTALS))
+        return PreferenceLoss(totals, *rows, out)
+
+    def preference(self, logp, targets, offsets, *, ref_logp=None, weights=None, kind="sigmoid",
+                   beta=0.1, margin=0.0, smoothing=0.0, average=False, scale=1.0):
+        """The same from scored rows: (totals [3], loss [P], rewards [2 P], d_logp
+        [T]); d_logp is for ``grad``."""
+        T = targets.numel()
+        P = self._pairs(T, targets, offsets, ref_logp, weights)
+        self._each("logp", logp, T)
+        row = self._empty(T + 3 * P + ARC_PREFERENCE_TOTALS)
+        at = row.data_ptr()
+        arc_tokens_preference_terms(
+            self.ctx, arc_preference_config(PREFERENCES[kind], average, beta, margin, smoothing,
+                                            scale),
+            T, logp, targets, P, offsets, ref_logp, weights, at + 4 * T, at + 4 * (T + P),
+            at + 4 * (T + 3 * P), at)
+        if self._elsewhere():
+            self._keep(logp, targets, offsets, ref_logp, weights)
+        d_logp, loss, rewards, totals = row.split_with_sizes(
+            (T, P, 2 * P, ARC_PREFERENCE_TOTALS))
+        return Preference(totals, loss, rewards, d_logp)
 
     def _out(self, out, T):
         if out is None:
