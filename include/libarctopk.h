@@ -657,6 +657,103 @@ arc_status arc_optim_adamw(arc_optim *ctx, const arc_adamw_config *ac, int64_t t
 /* Waits for the context's stream; NULL is accepted. */
 arc_status arc_optim_destroy(arc_optim *ctx);
 
+/*
+ * Orthogonalised updates of many matrices at once (the optimizer known as Muon):
+ * the momentum of each matrix is replaced by the nearest matrix of equal singular
+ * values, nearly, by a few products, and that is its step.
+ *
+ * For a matrix U of norm ||U|| (the root of the sum of its squares), X its shorter
+ * side first (U itself, or its transpose where it has more rows than columns):
+ *   X_0 = X / ||U||  (0 for a U of zeros),   and for k = 0 .. steps - 1
+ *   A = X_k X_k',   X_(k+1) = a_k X_k + (b_k A + c_k A A) X_k
+ * and O(U) is the last X, turned back.  Each step takes a singular value s to
+ * a s + b s^3 + c s^5; five with 3.4445, -4.7750, 2.0315 take all from 0.01 or so to
+ * 1 into 0.7 .. 1.2.  An optimizer step is, with g' = factor * g and lr' = lr * lr_scale,
+ *   m <- momentum m + g'        U = g' + momentum m (nesterov), or m
+ *   x <- (1 - lr' weight_decay) x - lr' O(U)
+ *
+ * X and A are held in 22 bits (two binary16 numbers each), products are summed in
+ * binary32 in a fixed order, norms in binary64, all else is binary32: O is as exact
+ * as binary32 products make it, and a call repeats its bits.  A matrix with a NaN
+ * or infinity in U gets NaN everywhere, the others none of it.
+ *
+ * Momenta lie in one array of arc_muon_state_elems binary32 elements, matrix i's from
+ * arc_muon_state_offset(i), a multiple of ARC_STATE_BLOCK, on, row after row.
+ */
+typedef struct arc_muon arc_muon;
+
+typedef struct {
+  int64_t rows, cols;   /* >= 0; the shorter 2^15 at most, the longer 2^21,
+                           2^34 elements                                     */
+  int32_t param_dtype;  /* arc_dtype of the parameters                       */
+  int32_t grad_dtype;   /* arc_dtype of the gradients                        */
+  float weight_decay;   /* >= 0, finite                                      */
+  float lr_scale;       /* finite; sqrt(max(1, rows / cols)) is usual        */
+} arc_muon_matrix;
+
+/*
+ *   matrices, num_matrices  1 .. 2^20 matrices, host array, copied; 2^42 elements at
+ *                           most in all
+ *   steps                   1 .. 64
+ *   coefficients            [steps][3] finite a, b, c, host array, copied; NULL for
+ *                           3.4445, -4.7750, 2.0315 in every step.  Singular values
+ *                           in 0 .. 1 have to stay below 2.7 before every step, and a
+ *                           + b s^2 + c s^4 below 7.7.
+ */
+typedef struct {
+  const arc_muon_matrix *matrices;
+  const float *coefficients;
+  int32_t num_matrices;
+  int32_t steps;
+  int64_t reserved; /* must be 0 */
+} arc_muon_config;
+
+typedef struct {
+  float lr;         /* finite   */
+  float momentum;   /* in [0, 1) */
+  int32_t nesterov; /* 0 or 1   */
+  int32_t reserved; /* must be 0 */
+} arc_muon_step_config;
+
+/* Validate cfg, allocate the tables and the workspace (12 bytes for each element and
+ * 8 for each of a square of the shorter side, of as many matrices as fit into 4 GiB,
+ * or of the largest) on the current HIP device and bind the context to `hip_stream`,
+ * as arc_create does.  On failure *out is NULL. */
+arc_status arc_muon_create(const arc_muon_config *cfg, void *hip_stream, arc_muon **out);
+
+/* Elements of the momenta; -1 for NULL. */
+int64_t arc_muon_state_elems(const arc_muon *ctx);
+
+/* Where matrix i's momentum begins; -1 for NULL or an i that is none. */
+int64_t arc_muon_state_offset(const arc_muon *ctx, int32_t i);
+
+/*
+ * O of each matrix: host arrays of num_matrices device pointers, read before the call
+ * returns, to matrices without gaps at any element alignment: `in` in the gradients'
+ * dtypes and `out` in the parameters'.  Those of matrices without elements are not
+ * looked at.  No two may overlap (not checked).
+ */
+arc_status arc_muon_orthogonalize(arc_muon *ctx, const void *const *in, void *const *out);
+
+/*
+ * One optimizer step.  Host arrays of num_matrices device pointers as above:
+ *   params  updated      grads   read
+ *   copies  NULL, or bfloat16 copies of the updated parameters, each of which may be
+ *           NULL
+ * and device pointers:
+ *   factor  one binary32 that gradients are multiplied with (total + 1 of
+ *           arc_optim_norm); NULL for 1.  A factor that is not finite leaves
+ *           parameters, copies and momenta as they are.
+ *   m       [state_elems] binary32, starts at 0; 16-byte aligned
+ * No two of these may overlap (checked for m and factor only).
+ */
+arc_status arc_muon_step(arc_muon *ctx, const arc_muon_step_config *sc, void *const *params,
+                         const void *const *grads, void *const *copies, const float *factor,
+                         float *m);
+
+/* Waits for the context's stream; NULL is accepted. */
+arc_status arc_muon_destroy(arc_muon *ctx);
+
 /* Static string naming a status code. */
 const char *arc_status_str(arc_status s);
 

@@ -24,7 +24,10 @@ from ._lib import (  # noqa: F401
     ARC_POLICY_TOTALS, ARC_PREFERENCE_HINGE, ARC_PREFERENCE_SIGMOID, ARC_PREFERENCE_SQUARED,
     ARC_PREFERENCE_TOTALS, PREFERENCES, arc_policy_config, arc_preference_config,
     arc_tokens_policy, arc_tokens_policy_terms, arc_tokens_preference,
-    arc_tokens_preference_terms)
+    arc_tokens_preference_terms,
+    arc_muon_config, arc_muon_create, arc_muon_destroy, arc_muon_matrix, arc_muon_orthogonalize,
+    arc_muon_state_elems, arc_muon_state_offset, arc_muon_step, arc_muon_step_config,
+    make_muon_config)
 
 
 class Compressor:
@@ -110,7 +113,7 @@ class Compressor:
 def __getattr__(name):
     # The classes that need torch are imported on their first use, so that the
     # binding alone still works without it.
-    if name in ("TokenLogProbs", "AdamW"):
+    if name in ("TokenLogProbs", "AdamW", "Muon"):
         from . import train
         return getattr(train, name)
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -156,6 +156,36 @@ class arc_preference_config(ctypes.Structure):
     ]
 
 
+class arc_muon_matrix(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int64),
+        ("cols", ctypes.c_int64),
+        ("param_dtype", ctypes.c_int32),
+        ("grad_dtype", ctypes.c_int32),
+        ("weight_decay", ctypes.c_float),
+        ("lr_scale", ctypes.c_float),
+    ]
+
+
+class arc_muon_config(ctypes.Structure):
+    _fields_ = [
+        ("matrices", ctypes.POINTER(arc_muon_matrix)),
+        ("coefficients", ctypes.POINTER(ctypes.c_float)),
+        ("num_matrices", ctypes.c_int32),
+        ("steps", ctypes.c_int32),
+        ("reserved", ctypes.c_int64),
+    ]
+
+
+class arc_muon_step_config(ctypes.Structure):
+    _fields_ = [
+        ("lr", ctypes.c_float),
+        ("momentum", ctypes.c_float),
+        ("nesterov", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+    ]
+
+
 def make_tokens_config(*, vocab, max_rows, dtype=ARC_DTYPE_BF16, top=0, scale=1.0,
                        reserved=0) -> arc_tokens_config:
     return arc_tokens_config(vocab, max_rows, dtype, top, scale, reserved)
@@ -174,6 +204,33 @@ def make_optim_config(*, counts, param_dtypes, grad_dtypes, weight_decays, lr_sc
     cfg = arc_optim_config(ctypes.cast(arr, ctypes.POINTER(arc_optim_tensor)), num, state,
                            int(stochastic), reserved, seed & (2**64 - 1))
     return cfg, arr
+
+
+def make_muon_config(*, shapes, param_dtypes, grad_dtypes, weight_decays, lr_scales, steps=5,
+                     coefficients=None, reserved=0):
+    """Build an ``arc_muon_config`` from one value of each list per matrix;
+    ``coefficients``: a, b, c of every step, or one triple for all of them.
+    Returns (config, keepalive), as make_config does."""
+    num = len(shapes)
+    if not all(len(x) == num for x in (param_dtypes, grad_dtypes, weight_decays, lr_scales)):
+        raise ValueError("one dtype, weight decay and learning rate scale for each matrix")
+    arr = (arc_muon_matrix * num)(*[
+        arc_muon_matrix(r, c, *x) for (r, c), *x in zip(shapes, param_dtypes, grad_dtypes,
+                                                       weight_decays, lr_scales)])
+    numbers = None
+    if coefficients is not None:
+        rows = list(coefficients)
+        if len(rows) == 3 and not hasattr(rows[0], "__len__"):
+            rows = [rows] * steps
+        flat = [float(v) for row in rows for v in row]
+        if len(rows) != steps or len(flat) != 3 * steps:
+            raise ValueError(f"coefficients: need three for each of {steps} steps")
+        numbers = (ctypes.c_float * len(flat))(*flat)
+    cfg = arc_muon_config(
+        ctypes.cast(arr, ctypes.POINTER(arc_muon_matrix)),
+        None if numbers is None else ctypes.cast(numbers, ctypes.POINTER(ctypes.c_float)), num,
+        steps, reserved)
+    return cfg, (arr, numbers)
 
 
 def make_model_config(optimizer="sgd", *, lr, dense_steps=0, momentum=0.0, beta1=0.9,
@@ -222,6 +279,12 @@ _SIGS = {
     "arc_optim_adamw": (_st, [_vp, ctypes.POINTER(arc_adamw_config), ctypes.c_int64, _vp, _vp,
                               _vp, _vp, _vp, _vp, _vp, _vp]),
     "arc_optim_destroy": (_st, [_vp]),
+    "arc_muon_create": (_st, [ctypes.POINTER(arc_muon_config), _vp, ctypes.POINTER(_vp)]),
+    "arc_muon_state_elems": (ctypes.c_int64, [_vp]),
+    "arc_muon_state_offset": (ctypes.c_int64, [_vp, ctypes.c_int32]),
+    "arc_muon_orthogonalize": (_st, [_vp, _vp, _vp]),
+    "arc_muon_step": (_st, [_vp, ctypes.POINTER(arc_muon_step_config), _vp, _vp, _vp, _vp, _vp]),
+    "arc_muon_destroy": (_st, [_vp]),
     "arc_status_str": (ctypes.c_char_p, [_st]),
     "arc_last_error": (ctypes.c_char_p, []),
     "arc_describe": (_st, [_vp, ctypes.c_char_p, ctypes.c_int64]),
@@ -450,6 +513,38 @@ def arc_optim_adamw(ctx, ac: arc_adamw_config, t: int, params, grads, copies, fa
 
 def arc_optim_destroy(ctx) -> None:
     _check(_lib.arc_optim_destroy(ctx), "arc_optim_destroy")
+
+
+def arc_muon_create(cfg: arc_muon_config, hip_stream=None) -> int:
+    """Returns the context handle; ``hip_stream`` as for arc_create."""
+    out = _vp()
+    _check(_lib.arc_muon_create(ctypes.byref(cfg), getattr(hip_stream, "cuda_stream", hip_stream),
+                                ctypes.byref(out)), "arc_muon_create")
+    return out.value
+
+
+def arc_muon_state_elems(ctx) -> int:
+    return int(_lib.arc_muon_state_elems(ctx))
+
+
+def arc_muon_state_offset(ctx, i: int) -> int:
+    return int(_lib.arc_muon_state_offset(ctx, i))
+
+
+def arc_muon_orthogonalize(ctx, inputs, outputs) -> None:
+    """inputs and outputs: host arrays (ctypes) of device pointers."""
+    _check(_lib.arc_muon_orthogonalize(ctx, inputs, outputs), "arc_muon_orthogonalize")
+
+
+def arc_muon_step(ctx, sc: arc_muon_step_config, params, grads, copies, factor, m) -> None:
+    """params, grads and copies: host arrays (ctypes) of device pointers; copies
+    may be None."""
+    _check(_lib.arc_muon_step(ctx, ctypes.byref(sc), params, grads, copies, _addr(factor),
+                              _addr(m)), "arc_muon_step")
+
+
+def arc_muon_destroy(ctx) -> None:
+    _check(_lib.arc_muon_destroy(ctx), "arc_muon_destroy")
 
 
 def arc_status_str(status: int) -> str:

@@ -1,0 +1,378 @@
+// Host side of the matrix optimizer: argument checks, the plan of a context (its
+// matrices in groups that share a workspace, and each group's tiles) and the
+// enqueue on its stream.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <new>
+#include <vector>
+
+#include "arc_context.h"
+#include "arc_muon.h"
+#include "arc_train_host.h"
+
+namespace arc {
+
+// Matrices that go through the launches together.
+struct MuonGroup {
+  int32_t first = 0, count = 0;
+  int64_t first_run = 0, runs = 0;
+  int64_t split = 0, splits = 0;    // their tiles in the context's list
+  int64_t half = 0, halves = 0;     // of symmetric results
+  int64_t whole = 0, wholes = 0;
+};
+
+}  // namespace arc
+
+struct arc_muon {
+  std::vector<arc::MuonMatrix> matrices;
+  std::vector<arc::MuonGroup> groups;
+  std::vector<arc::MuonTile> tiles;
+  std::vector<int32_t> run_matrix;
+  std::vector<float> coefficients;  // three a step
+  int32_t side = 128;
+  int64_t state_elems = 0, workspace_bytes = 0;
+  hipStream_t stream = nullptr;
+  int device = 0;
+  arc::MuonMatrix* matrices_dev = nullptr;
+  arc::MuonTile* tiles_dev = nullptr;
+  int32_t* run_matrix_dev = nullptr;
+  double *sums_dev = nullptr, *inverse_dev = nullptr;
+  char* workspace = nullptr;
+
+  void release() {
+    (void)hipStreamSynchronize(stream);
+    for (void* p : {static_cast<void*>(matrices_dev), static_cast<void*>(tiles_dev),
+                    static_cast<void*>(run_matrix_dev), static_cast<void*>(sums_dev),
+                    static_cast<void*>(inverse_dev), static_cast<void*>(workspace)})
+      if (p) (void)hipFree(p);
+  }
+};
+
+namespace {
+
+using arc::device_copy;
+using arc::fail;
+using arc::finite;
+using arc::OnDevice;
+using arc::overlap;
+
+constexpr int64_t kMaxShort = int64_t{1} << 15, kMaxLong = int64_t{1} << 21;
+constexpr int64_t kMaxMatrix = int64_t{1} << 34, kMaxElements = int64_t{1} << 42;
+constexpr int32_t kMaxSteps = 64;
+constexpr float kQuintic[3] = {3.4445f, -4.7750f, 2.0315f};
+// What a group's pairs may take: enough matrices to fill the card many times over.
+constexpr int64_t kGroupBytes = int64_t{4} << 30;
+
+int64_t up_to(int64_t v, int64_t of) { return (v + of - 1) / of * of; }
+
+// The largest |a + b s + c s^2| for s in [0, top].
+double largest(double a, double b, double c, double top, bool odd) {
+  // odd: of x (a + b x^2 + c x^4), x = sqrt(s), whose derivative is a + 3 b s + 5 c s^2
+  const auto at = [&](double s) {
+    const double v = a + b * s + c * s * s;
+    return std::fabs(odd ? std::sqrt(s) * v : v);
+  };
+  double most = std::max(at(0.0), at(top));
+  const double q = odd ? 5.0 * c : 0.0, h = odd ? 3.0 * b : 2.0 * c, k = odd ? a : b;
+  const auto turn = [&](double s) {
+    if (s > 0.0 && s < top) most = std::max(most, at(s));
+  };
+  if (q != 0.0) {
+    const double d = h * h - 4.0 * q * k;
+    if (d >= 0.0) {
+      turn((-h + std::sqrt(d)) / (2.0 * q));
+      turn((-h - std::sqrt(d)) / (2.0 * q));
+    }
+  } else if (h != 0.0) {
+    turn(-k / h);
+  }
+  return most;
+}
+
+// Whether no entry of X, X X' and the polynomial leaves the pairs' range: entries
+// are at most the largest singular value, which starts at 1.
+bool in_range(const std::vector<float>& coefficients) {
+  constexpr double kMost = 7.75;  // 2^13 times it is below binary16's end
+  double top = 1.001;             // rounding
+  for (size_t k = 0; k < coefficients.size(); k += 3) {
+    const double a = coefficients[k], b = coefficients[k + 1], c = coefficients[k + 2];
+    if (top * top > kMost || largest(a, b, c, top * top, false) > kMost) return false;
+    top = largest(a, b, c, top * top, true) * 1.001;
+  }
+  return true;  // the last X is not held in pairs
+}
+
+arc_status check_muon(const arc_muon_config* cfg) {
+  if (cfg == nullptr) return fail(ARC_ERR_INVALID, "cfg is NULL");
+  if (cfg->matrices == nullptr) return fail(ARC_ERR_INVALID, "matrices is NULL");
+  if (cfg->num_matrices < 1 || cfg->num_matrices > (1 << 20))
+    return fail(ARC_ERR_INVALID, "num_matrices must be in 1..2^20");
+  if (cfg->steps < 1 || cfg->steps > kMaxSteps)
+    return fail(ARC_ERR_INVALID, "steps must be in 1..64");
+  if (cfg->reserved != 0) return fail(ARC_ERR_INVALID, "reserved must be 0");
+  if (cfg->coefficients != nullptr)
+    for (int32_t k = 0; k < 3 * cfg->steps; ++k)
+      if (!finite(cfg->coefficients[k]))
+        return fail(ARC_ERR_INVALID, "coefficients must be finite");
+  int64_t left = kMaxElements;
+  for (int32_t i = 0; i < cfg->num_matrices; ++i) {
+    const arc_muon_matrix& t = cfg->matrices[i];
+    if (t.rows < 0 || t.cols < 0 || std::min(t.rows, t.cols) > kMaxShort ||
+        std::max(t.rows, t.cols) > kMaxLong || t.rows * t.cols > kMaxMatrix ||
+        t.rows * t.cols > left)
+      return fail(ARC_ERR_INVALID,
+                  "sides must be >= 0, the shorter one 2^15 at most and the longer one 2^21, "
+                  "2^34 elements a matrix and 2^42 in all");
+    left -= t.rows * t.cols;
+    for (int32_t dt : {t.param_dtype, t.grad_dtype})
+      if (dt != ARC_DTYPE_F32 && dt != ARC_DTYPE_BF16)
+        return fail(ARC_ERR_INVALID, "dtypes must be ARC_DTYPE_F32 or ARC_DTYPE_BF16");
+    if (!(t.weight_decay >= 0.f) || !finite(t.weight_decay) || !finite(t.lr_scale))
+      return fail(ARC_ERR_INVALID, "weight_decay must be >= 0 and finite, lr_scale finite");
+  }
+  return ARC_OK;
+}
+
+// Tiles of 128 where they fill the card, else of 64.
+int32_t side_of(const arc_muon_config* cfg) {
+  int64_t tiles = 0;
+  for (int32_t i = 0; i < cfg->num_matrices; ++i)
+    tiles += ((cfg->matrices[i].rows + 127) / 128) * ((cfg->matrices[i].cols + 127) / 128);
+  return tiles >= 256 ? 128 : 64;
+}
+
+// The tables of a checked configuration (may throw std::bad_alloc).
+void plan_muon(const arc_muon_config* cfg, arc_muon* c) {
+  c->side = side_of(cfg);
+  const int32_t side = c->side;
+  std::vector<arc::MuonTile> split, half, whole;
+  arc::MuonGroup g;
+  int64_t bytes = 0, runs = 0;
+  const auto finish = [&] {
+    if (g.count == 0) return;
+    const auto take = [&](std::vector<arc::MuonTile>& from, int64_t* at, int64_t* count) {
+      *at = static_cast<int64_t>(c->tiles.size());
+      *count = static_cast<int64_t>(from.size());
+      c->tiles.insert(c->tiles.end(), from.begin(), from.end());
+      from.clear();
+    };
+    take(split, &g.split, &g.splits);
+    take(half, &g.half, &g.halves);
+    take(whole, &g.whole, &g.wholes);
+    g.runs = runs - g.first_run;
+    c->groups.push_back(g);
+    c->workspace_bytes = std::max(c->workspace_bytes, bytes);
+  };
+  for (int32_t i = 0; i < cfg->num_matrices; ++i) {
+    const arc_muon_matrix& in = cfg->matrices[i];
+    arc::MuonMatrix t{};
+    const int64_t count = in.rows * in.cols;
+    t.rows = static_cast<int32_t>(in.rows);
+    t.cols = static_cast<int32_t>(in.cols);
+    t.tall = in.rows > in.cols;
+    t.m = std::min(t.rows, t.cols);
+    t.n = std::max(t.rows, t.cols);
+    t.mp = static_cast<int32_t>(up_to(t.m, side));
+    t.np = static_cast<int32_t>(count > 0 ? up_to(t.n, side) : 0);
+    t.param_bf16 = in.param_dtype == ARC_DTYPE_BF16;
+    t.grad_bf16 = in.grad_dtype == ARC_DTYPE_BF16;
+    t.weight_decay = in.weight_decay;
+    t.lr_scale = in.lr_scale;
+    t.state = c->state_elems;
+    c->state_elems += up_to(count, ARC_STATE_BLOCK);
+    const int64_t long_bytes = int64_t{4} * t.mp * t.np, short_bytes = int64_t{4} * t.mp * t.mp;
+    const int64_t need = count > 0 ? 3 * long_bytes + 2 * short_bytes : 0;
+    if (g.count == arc::kMuonBatch || (g.count > 0 && bytes + need > kGroupBytes)) {
+      finish();
+      g = arc::MuonGroup{};
+      g.first = i;
+      g.first_run = runs;
+      bytes = 0;
+    }
+    ++g.count;
+    t.first_run = runs;
+    t.runs = static_cast<int32_t>((count + arc::kMuonRun - 1) / arc::kMuonRun);
+    runs += t.runs;
+    c->run_matrix.insert(c->run_matrix.end(), static_cast<size_t>(t.runs), i);
+    t.x = bytes;
+    t.xt[0] = t.x + long_bytes;
+    t.xt[1] = t.xt[0] + long_bytes;
+    t.gram = t.xt[1] + long_bytes;
+    t.poly = t.gram + short_bytes;
+    bytes += need;
+    c->matrices.push_back(t);
+    if (count == 0) continue;
+    const int32_t s = arc::kSplitTile;
+    for (int32_t a = 0; a < t.mp / s; ++a)
+      for (int32_t b = 0; b < t.np / s; ++b) split.push_back({i, a, b});
+    for (int32_t a = 0; a < t.mp / side; ++a) {
+      for (int32_t b = 0; b <= a; ++b) half.push_back({i, a, b});
+      for (int32_t b = 0; b < t.np / side; ++b) whole.push_back({i, a, b});
+    }
+  }
+  finish();
+}
+
+arc_status check_pointers(const arc_muon* c, const void* const* p, const char* what) {
+  if (p == nullptr) return fail(ARC_ERR_INVALID, std::string(what) + " is NULL");
+  for (size_t i = 0; i < c->matrices.size(); ++i)
+    if (p[i] == nullptr && c->matrices[i].m > 0)
+      return fail(ARC_ERR_INVALID, std::string(what) + " holds a NULL");
+  return ARC_OK;
+}
+
+// One pass over all groups.
+arc_status enqueue(const arc_muon* c, arc::MuonArgs a, void* const* params,
+                   const void* const* grads, void* const* copies) {
+  a.matrices = c->matrices_dev;
+  a.workspace = c->workspace;
+  a.sums = c->sums_dev;
+  a.inverse = c->inverse_dev;
+  const OnDevice here(c->device);
+  for (const arc::MuonGroup& g : c->groups) {
+    if (g.wholes == 0) continue;
+    a.first = g.first;
+    arc::MuonPointers p;
+    for (int32_t i = 0; i < g.count; ++i) {
+      p.grad[i] = grads[g.first + i];
+      p.param[i] = params[g.first + i];
+      p.copy[i] = copies ? static_cast<uint16_t*>(copies[g.first + i]) : nullptr;
+    }
+    ARC_HIP(arc::launch_muon_momentum(a, p, c->run_matrix_dev, g.first_run, g.runs, c->stream),
+            "momentum launch");
+    ARC_HIP(arc::launch_muon_norms(a, g.count, c->stream), "norm launch");
+    ARC_HIP(arc::launch_muon_split(a, p, c->tiles_dev + g.split, g.splits, c->stream),
+            "split launch");
+    const size_t steps = c->coefficients.size() / 3;
+    for (size_t k = 0; k < steps; ++k) {
+      const float* q = &c->coefficients[3 * k];
+      const arc::MuonStep s{q[0], q[1], q[2], static_cast<int32_t>(k % 2)};
+      const arc::MuonTile *half = c->tiles_dev + g.half, *whole = c->tiles_dev + g.whole;
+      ARC_HIP(arc::launch_muon_product(arc::kMuonGram, c->side, a, nullptr, s, half, g.halves,
+                                       c->stream),
+              "product launch");
+      ARC_HIP(arc::launch_muon_product(arc::kMuonPoly, c->side, a, nullptr, s, half, g.halves,
+                                       c->stream),
+              "product launch");
+      ARC_HIP(arc::launch_muon_product(k + 1 < steps ? arc::kMuonApply : arc::kMuonLast, c->side,
+                                       a, &p, s, whole, g.wholes, c->stream),
+              "product launch");
+    }
+  }
+  return ARC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+arc_status arc_muon_create(const arc_muon_config* cfg, void* hip_stream, arc_muon** out) {
+  if (out == nullptr) return fail(ARC_ERR_INVALID, "out is NULL");
+  *out = nullptr;
+  arc_status st = check_muon(cfg);
+  if (st != ARC_OK) return st;
+  arc_muon* c = new (std::nothrow) arc_muon();
+  if (c == nullptr) return fail(ARC_ERR_NOMEM, "host allocation failed");
+  try {
+    for (int32_t k = 0; k < 3 * cfg->steps; ++k)
+      c->coefficients.push_back(cfg->coefficients ? cfg->coefficients[k] : kQuintic[k % 3]);
+    if (!in_range(c->coefficients)) {
+      delete c;
+      return fail(ARC_ERR_INVALID,
+                  "coefficients: singular values in 0..1 have to stay below 2.7, and the "
+                  "polynomials below 7.7");
+    }
+    plan_muon(cfg, c);
+  } catch (const std::exception&) {
+    delete c;
+    return fail(ARC_ERR_NOMEM, "host allocation failed");
+  }
+  c->stream = static_cast<hipStream_t>(hip_stream);
+  const auto bail = [&](arc_status s) {
+    c->release();
+    delete c;
+    return s;
+  };
+  hipError_t e = hipGetDevice(&c->device);
+  if (e != hipSuccess) return bail(arc::fail_hip(e, "hipGetDevice"));
+  if ((st = device_copy(&c->matrices_dev, c->matrices, "matrix tables")) != ARC_OK ||
+      (st = device_copy(&c->tiles_dev, c->tiles, "matrix tables")) != ARC_OK ||
+      (st = device_copy(&c->run_matrix_dev, c->run_matrix, "matrix tables")) != ARC_OK)
+    return bail(st);
+  const auto room = [&](auto** p, size_t bytes) {
+    if (e != hipSuccess) return;
+    e = hipMalloc(reinterpret_cast<void**>(p), std::max<size_t>(bytes, 16));
+    if (e != hipSuccess) *p = nullptr;
+  };
+  room(&c->sums_dev, c->run_matrix.size() * sizeof(double));
+  room(&c->inverse_dev, c->matrices.size() * sizeof(double));
+  room(&c->workspace, static_cast<size_t>(c->workspace_bytes));
+  if (e == hipSuccess) e = arc::prepare_muon_products();
+  if (e == hipSuccess) e = hipDeviceSynchronize();
+  if (e != hipSuccess) {
+    (void)hipGetLastError();
+    return bail(arc::fail_hip(e, "matrix workspace"));
+  }
+  c->tiles = {};  // on the device from here on
+  c->run_matrix = {};
+  *out = c;
+  return ARC_OK;
+}
+
+int64_t arc_muon_state_elems(const arc_muon* c) { return c ? c->state_elems : -1; }
+
+int64_t arc_muon_state_offset(const arc_muon* c, int32_t i) {
+  if (c == nullptr || i < 0 || static_cast<size_t>(i) >= c->matrices.size()) return -1;
+  return c->matrices[static_cast<size_t>(i)].state;
+}
+
+arc_status arc_muon_orthogonalize(arc_muon* c, const void* const* in, void* const* out) {
+  if (c == nullptr) return fail(ARC_ERR_INVALID, "ctx is NULL");
+  arc_status st;
+  if ((st = check_pointers(c, in, "in")) != ARC_OK ||
+      (st = check_pointers(c, out, "out")) != ARC_OK)
+    return st;
+  return enqueue(c, arc::MuonArgs{}, out, in, nullptr);
+}
+
+arc_status arc_muon_step(arc_muon* c, const arc_muon_step_config* sc, void* const* params,
+                         const void* const* grads, void* const* copies, const float* factor,
+                         float* m) {
+  if (c == nullptr) return fail(ARC_ERR_INVALID, "ctx is NULL");
+  if (sc == nullptr) return fail(ARC_ERR_INVALID, "config is NULL");
+  if (!finite(sc->lr)) return fail(ARC_ERR_INVALID, "lr must be finite");
+  if (!(sc->momentum >= 0.f && sc->momentum < 1.f))
+    return fail(ARC_ERR_INVALID, "momentum must be in [0, 1)");
+  if (sc->nesterov != 0 && sc->nesterov != 1)
+    return fail(ARC_ERR_INVALID, "nesterov must be 0 or 1");
+  if (sc->reserved != 0) return fail(ARC_ERR_INVALID, "reserved must be 0");
+  arc_status st;
+  if ((st = check_pointers(c, params, "params")) != ARC_OK ||
+      (st = check_pointers(c, grads, "grads")) != ARC_OK)
+    return st;
+  if (c->state_elems > 0 && m == nullptr) return fail(ARC_ERR_INVALID, "m is NULL");
+  if (reinterpret_cast<uintptr_t>(m) % 16)
+    return fail(ARC_ERR_INVALID, "m must be 16-byte aligned");
+  if (overlap({m, c->state_elems * 4}, {factor, 4}))
+    return fail(ARC_ERR_INVALID, "m and factor must not overlap");
+  arc::MuonArgs a{};
+  a.factor = factor;
+  a.m = m;
+  a.momentum = sc->momentum;
+  a.lr = sc->lr;
+  a.nesterov = sc->nesterov;
+  a.update = 1;
+  return enqueue(c, a, params, grads, copies);
+}
+
+arc_status arc_muon_destroy(arc_muon* c) {
+  if (c == nullptr) return ARC_OK;
+  c->release();
+  delete c;
+  return ARC_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,78 @@
+// Internal declarations of the matrix optimizer: momenta orthogonalised by
+// Newton-Schulz products (arc_muon.hip), and its host side (arc_muon.cpp).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace arc {
+
+// Binary32 numbers inside the products are pairs of binary16: hi = x 2^13 rounded,
+// lo = what hi lacks, rounded.  2^13, because no entry of a matrix here is larger
+// than 2^2.9 (the host checks the coefficients for it) and binary16 ends at 2^16.
+constexpr float kPairScale = 8192.f;
+constexpr int kPairLine = 32;  // numbers of a row whose pairs lie in one line: 32 hi, 32 lo
+
+constexpr int kMuonRun = 8192;  // elements of a matrix whose squares one workgroup sums
+constexpr int kSplitTile = 64;  // sides of what one workgroup splits into pairs
+constexpr int kMuonBatch = 160; // matrices of a launch (their pointers are arguments)
+
+// A matrix, seen from its shorter side: X is m x n, m <= n, or its transpose.
+struct MuonMatrix {
+  int64_t state;                        // first element of its momentum
+  int64_t x, xt[2], gram, poly;         // where its pairs lie in the workspace, bytes
+  int64_t first_run;                    // its runs' sums
+  int32_t rows, cols;                   // as the caller has it
+  int32_t m, n, mp, np;                 // sides, and those of the workspace
+  int32_t tall;                         // X is its transpose
+  int32_t param_bf16, grad_bf16;
+  float weight_decay, lr_scale;
+  int32_t runs;
+};
+
+// One workgroup's part of a launch.
+struct MuonTile {
+  int32_t matrix;
+  int32_t i, j;
+};
+
+struct MuonPointers {
+  const void* grad[kMuonBatch];
+  void* param[kMuonBatch];
+  uint16_t* copy[kMuonBatch];
+};
+
+struct MuonArgs {
+  const MuonMatrix* matrices;  // all of them
+  int32_t first;               // matrix of the first pointers
+  const float* factor;         // NULL: 1
+  float* m;                    // momenta; NULL: the gradients themselves are taken
+  float momentum, lr;
+  int32_t nesterov, update;    // update: parameters; otherwise they are overwritten
+  char* workspace;
+  double* sums;                // of the runs' squares
+  double* inverse;             // kPairScale / the norm, of each matrix
+};
+
+enum MuonProduct { kMuonGram, kMuonPoly, kMuonApply, kMuonLast };
+
+struct MuonStep {
+  float a, b, c;
+  int32_t from;  // which of xt holds the transpose
+};
+
+// The momenta, and the squares of what is orthogonalised.
+hipError_t launch_muon_momentum(const MuonArgs& a, const MuonPointers& p, const int32_t* run_matrix,
+                                int64_t first_run, int64_t runs, hipStream_t stream);
+hipError_t launch_muon_norms(const MuonArgs& a, int32_t count, hipStream_t stream);
+// X and its transpose in pairs, of norm 1.
+hipError_t launch_muon_split(const MuonArgs& a, const MuonPointers& p, const MuonTile* tiles,
+                             int64_t count, hipStream_t stream);
+// Products of square tiles of `side`.
+hipError_t launch_muon_product(MuonProduct what, int32_t side, const MuonArgs& a,
+                               const MuonPointers* p, const MuonStep& s, const MuonTile* tiles,
+                               int64_t count, hipStream_t stream);
+hipError_t prepare_muon_products();
+
+}  // namespace arc

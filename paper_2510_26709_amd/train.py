@@ -20,12 +20,15 @@ import torch
 
 from . import _lib
 from ._lib import (ARC_DTYPE_BF16, ARC_DTYPE_F32, ARC_POLICY_TOTALS, ARC_PREFERENCE_TOTALS,
-                   ARC_STATE_BLOCK, ARC_STATE_F32, ARC_STATE_F8, PREFERENCES, arc_adamw_config, arc_optim_adamw, arc_optim_create, arc_optim_destroy,
+                   ARC_STATE_BLOCK, ARC_STATE_F32, ARC_STATE_F8, PREFERENCES, arc_adamw_config,
+                   arc_muon_create, arc_muon_destroy, arc_muon_orthogonalize,
+                   arc_muon_state_elems, arc_muon_state_offset, arc_muon_step,
+                   arc_muon_step_config, arc_optim_adamw, arc_optim_create, arc_optim_destroy,
                    arc_optim_norm, arc_optim_state_elems, arc_optim_state_offset,
                    arc_policy_config, arc_preference_config, arc_tokens_create,
                    arc_tokens_destroy, arc_tokens_grad, arc_tokens_loss, arc_tokens_policy,
                    arc_tokens_policy_terms, arc_tokens_preference, arc_tokens_preference_terms,
-                   arc_tokens_score, make_optim_config, make_tokens_config)
+                   arc_tokens_score, make_muon_config, make_optim_config, make_tokens_config)
 
 _DTYPES = {"f32": (ARC_DTYPE_F32, torch.float32), "bf16": (ARC_DTYPE_BF16, torch.bfloat16)}
 
@@ -289,7 +292,69 @@ def _state(name):
                     doc=f"{name} of all tensors; a tensor assigned here is what later steps use.")
 
 
-class AdamW(_Bound):
+class _Optimizer(_Bound):
+    """Tensors of given sizes that each call gets, and the states kept for them."""
+
+    def _start(self, states):
+        """Takes the states of ``_want``: name -> (dtype, elements)."""
+        self._states = dict.fromkeys(self._names)
+        self._checked = None  # the states' addresses and lengths that were looked at last
+        for name, (dtype, n) in self._want.items():
+            x = None if states is None else states.get(name)
+            if x is None:
+                with torch.cuda.stream(self.stream):
+                    x = torch.zeros(n, dtype=torch.uint8 if dtype.itemsize == 1 else dtype,
+                                    device=self.device).view(dtype)
+            self._take_state(name, x)
+        num = len(self.sizes)
+        starts = np.cumsum([0] + self.sizes[:-1], dtype=np.uint64)
+        self._starts = {2: starts * np.uint64(2), 4: starts * np.uint64(4)}  # in bytes
+        self._copy = [torch.bfloat16] * num
+        self._one = {k: d[0] if len(set(d)) == 1 else None for k, d in (
+            ("param", self._param), ("grad", self._grad), ("copy", self._copy))}
+        self._table = {k: np.zeros(num, dtype=np.uint64) for k in ("param", "grad", "copy")}
+        self._args = {k: ctypes.c_void_p(v.ctypes.data) for k, v in self._table.items()}
+        self._flat = sum(self.sizes)
+
+    def _take_state(self, name, x):
+        if name not in self._want:
+            raise ValueError(f"{name}: there is no such state here")
+        self._states[name] = self._check(name, x, *self._want[name])
+        self._held = [x for x in self._states.values() if x is not None]
+        x.record_stream(self.stream)
+
+    def _state_pointers(self):
+        held = self._held
+        now = [*map(torch.Tensor.data_ptr, held), *map(torch.Tensor.numel, held)]
+        if now != self._checked:  # other tensors, or another storage of the same ones
+            for name, want in self._want.items():
+                self._check(name, self._states[name], *want)
+            self._checked = now
+        return now[:len(held)]
+
+    def _pointers(self, key, x, dtypes):
+        """Fills the host table of device pointers of this call."""
+        table = self._table[key]
+        if isinstance(x, torch.Tensor):  # flat
+            dtype = self._one[key]
+            if dtype is None:
+                raise ValueError(f"{key}: one flat tensor holds one dtype")
+            self._check(key, x, dtype, self._flat)
+            np.add(self._starts[dtype.itemsize], x.data_ptr(), table)
+        else:
+            if len(x) != len(table):
+                raise ValueError(f"{key}: need {len(table)} tensors, got {len(x)}")
+            for i, (t, n, dtype) in enumerate(zip(x, self.sizes, dtypes)):
+                if t is None and (key == "copy" or n == 0):
+                    table[i] = 0
+                elif t is None:
+                    raise ValueError(f"{key}[{i}] is missing")
+                else:
+                    table[i] = self._check(f"{key}[{i}]", t, dtype, n).data_ptr()
+        return self._args[key]
+
+
+class AdamW(_Optimizer):
     """AdamW over tensors of the given ``sizes``, with their states ``m``, ``v``
     and, in 8 bits, ``m_scale``, ``v_scale``.
 
@@ -331,60 +396,10 @@ class AdamW(_Bound):
         if state == "f8":
             self._want.update(m_scale=(torch.float32, S // ARC_STATE_BLOCK),
                               v_scale=(torch.float32, S // ARC_STATE_BLOCK))
-        self._states = dict.fromkeys(("m", "v", "m_scale", "v_scale"))
-        self._checked = None  # the states' addresses and lengths that were looked at last
-        for name, (dtype, n) in self._want.items():
-            x = None if states is None else states.get(name)
-            if x is None:
-                with torch.cuda.stream(self.stream):
-                    x = torch.zeros(n, dtype=torch.uint8 if dtype.itemsize == 1 else dtype,
-                                    device=self.device).view(dtype)
-            self._take_state(name, x)
-        starts = np.cumsum([0] + self.sizes[:-1], dtype=np.uint64)
-        self._starts = {2: starts * np.uint64(2), 4: starts * np.uint64(4)}  # in bytes
-        self._copy = [torch.bfloat16] * num
-        self._one = {k: d[0] if len(set(d)) == 1 else None for k, d in (
-            ("param", self._param), ("grad", self._grad), ("copy", self._copy))}
-        self._table = {k: np.zeros(num, dtype=np.uint64) for k in ("param", "grad", "copy")}
-        self._args = {k: ctypes.c_void_p(v.ctypes.data) for k, v in self._table.items()}
-        self._flat = sum(self.sizes)
+        self._start(states)
 
-    m, v, m_scale, v_scale = (_state(name) for name in ("m", "v", "m_scale", "v_scale"))
-
-    def _take_state(self, name, x):
-        if name not in self._want:
-            raise ValueError(f"{name}: states in {self.state!r} have none")
-        self._states[name] = self._check(name, x, *self._want[name])
-        self._held = [x for x in self._states.values() if x is not None]
-        x.record_stream(self.stream)
-
-    def _state_pointers(self):
-        held = self._held
-        now = [*map(torch.Tensor.data_ptr, held), *map(torch.Tensor.numel, held)]
-        if now != self._checked:  # other tensors, or another storage of the same ones
-            for name, want in self._want.items():
-                self._check(name, self._states[name], *want)
-            self._checked = now
-        return now[:4] if len(held) == 4 else (now[0], now[1], None, None)
-
-    def _pointers(self, key, x, dtypes):
-        """Fills the host table of device pointers of this call."""
-        table = self._table[key]
-        if isinstance(x, torch.Tensor):  # flat
-            dtype = self._one[key]
-            if dtype is None:
-                raise ValueError(f"{key}: one flat tensor holds one dtype")
-            self._check(key, x, dtype, self._flat)
-            np.add(self._starts[dtype.itemsize], x.data_ptr(), table)
-        else:
-            if len(x) != len(table):
-                raise ValueError(f"{key}: need {len(table)} tensors, got {len(x)}")
-            for i, (t, n, dtype) in enumerate(zip(x, self.sizes, dtypes)):
-                if t is None and (key == "copy" or n == 0):
-                    table[i] = 0
-                else:
-                    table[i] = self._check(f"{key}[{i}]", t, dtype, n).data_ptr()
-        return self._args[key]
+    _names = ("m", "v", "m_scale", "v_scale")
+    m, v, m_scale, v_scale = (_state(name) for name in _names)
 
     def norm(self, grads, *, max_norm=float("inf"), scale=1.0):
         """(total [2], norms [num]): scale * the norm of all gradients and the
@@ -412,11 +427,99 @@ class AdamW(_Bound):
             self._pointers("param", params, self._param),
             self._pointers("grad", grads, self._grad),
             None if copies is None else self._pointers("copy", copies, self._copy),
-            at, *self._state_pointers())
+            at, *(*self._state_pointers(), None, None)[:4])
         if self._elsewhere():
             self._keep(params, grads, copies, factor)
 
     def close(self):
         if getattr(self, "ctx", None):
             arc_optim_destroy(self.ctx)
+            self.ctx = None
+
+
+class Muon(_Optimizer):
+    """Orthogonalised updates of matrices of the given ``shapes``, with their
+    momenta ``m``.
+
+    Parameters, gradients and copies are passed to each call as ``AdamW`` takes
+    them, a list of one tensor each or one flat tensor; ``param_dtype``,
+    ``grad_dtype``, ``weight_decay`` and ``lr_scale`` are one value for all
+    matrices or a list.  A tensor of more than one dimension has a matrix's rows
+    first (a convolution's weight is [out, in * height * width]).  ``lr_scale``
+    None: sqrt(max(1, rows / cols)).
+    ``coefficients``: a, b, c of one Newton-Schulz step, or of each of ``steps``.
+    ``states``: a dict with existing momenta, used in place; else they start at
+    zero.
+    """
+
+    _names = ("m",)
+    m = _state("m")
+
+    def __init__(self, shapes, *, param_dtype="f32", grad_dtype="f32", weight_decay=0.0,
+                 lr_scale=None, steps=5, coefficients=None, states=None, device=None,
+                 stream=None):
+        self._bind(device, stream)
+        self.shapes = [(int(r), int(c)) for r, c in shapes]
+        self.sizes = [r * c for r, c in self.shapes]
+        num = len(self.shapes)
+
+        def each(v):
+            return list(v) if isinstance(v, (list, tuple)) else [v] * num
+
+        if lr_scale is None:
+            lr_scale = [max(1.0, r / max(c, 1)) ** 0.5 for r, c in self.shapes]
+        params, grads = each(param_dtype), each(grad_dtype)
+        self._param = [_DTYPES[d][1] for d in params]
+        self._grad = [_DTYPES[d][1] for d in grads]
+        cfg, keep = make_muon_config(
+            shapes=self.shapes, param_dtypes=[_DTYPES[d][0] for d in params],
+            grad_dtypes=[_DTYPES[d][0] for d in grads], weight_decays=each(weight_decay),
+            lr_scales=each(lr_scale), steps=steps, coefficients=coefficients)
+        with torch.cuda.device(self.device):
+            self.ctx = arc_muon_create(cfg, self.stream)
+        del keep
+        self.offsets = [arc_muon_state_offset(self.ctx, i) for i in range(num)]
+        self._want = {"m": (torch.float32, arc_muon_state_elems(self.ctx))}
+        self._start(states)
+
+    def _pointers(self, key, x, dtypes):
+        if not isinstance(x, torch.Tensor):
+            for i, (t, (rows, _)) in enumerate(zip(x, self.shapes)):
+                if t is not None and t.dim() != 1 and (t.dim() == 0 or t.shape[0] != rows):
+                    raise ValueError(f"{key}[{i}]: need {self.shapes[i]}, got {tuple(t.shape)}")
+        return super()._pointers(key, x, dtypes)
+
+    def orthogonalize(self, x, out=None):
+        """The orthogonalised matrices, in the parameters' dtypes: one flat tensor
+        for one, else a list.  ``out``: where to write them."""
+        if out is None:
+            if isinstance(x, torch.Tensor):
+                if self._one["param"] is None:
+                    raise ValueError("param: one flat tensor holds one dtype")
+                out = self._empty(self._flat, dtype=self._one["param"])
+            else:
+                out = [self._empty(*s, dtype=d) for s, d in zip(self.shapes, self._param)]
+        arc_muon_orthogonalize(self.ctx, self._pointers("grad", x, self._grad),
+                               self._pointers("param", out, self._param))
+        if self._elsewhere():
+            self._keep(x, out)
+        return out
+
+    def step(self, params, grads, *, lr, momentum=0.95, nesterov=True, factor=None, copies=None):
+        """One step, in place.  ``factor``: a total [2] of ``AdamW.norm``, whose
+        second value multiplies the gradients."""
+        at = None
+        if factor is not None:
+            at = self._check("factor", factor, torch.float32, 2).data_ptr() + 4
+        arc_muon_step(self.ctx, arc_muon_step_config(lr, momentum, nesterov, 0),
+                      self._pointers("param", params, self._param),
+                      self._pointers("grad", grads, self._grad),
+                      None if copies is None else self._pointers("copy", copies, self._copy),
+                      at, *self._state_pointers())
+        if self._elsewhere():
+            self._keep(params, grads, copies, factor)
+
+    def close(self):
+        if getattr(self, "ctx", None):
+            arc_muon_destroy(self.ctx)
             self.ctx = None
