@@ -6,7 +6,10 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
-#include <new>
+#include <cstdlib>
+#include <cstdio>
+#include <functional>
+#include <utility>
 #include <vector>
 
 #include "arc_context.h"
@@ -19,9 +22,11 @@ namespace arc {
 struct MuonGroup {
   int32_t first = 0, count = 0;
   int64_t first_run = 0, runs = 0;
-  int64_t split = 0, splits = 0;    // their tiles in the context's list
-  int64_t half = 0, halves = 0;     // of symmetric results
-  int64_t whole = 0, wholes = 0;
+  struct Range {
+    int64_t at = 0, count = 0;
+  };
+  Range split;        // their tiles in the context's list
+  Range products[3];  // by MuonProduct
 };
 
 }  // namespace arc
@@ -34,6 +39,7 @@ struct arc_muon {
   std::vector<float> coefficients;  // three a step
   int32_t side = 128;
   int64_t state_elems = 0, workspace_bytes = 0;
+  int64_t parts = 0;  // most of one launch
   hipStream_t stream = nullptr;
   int device = 0;
   arc::MuonMatrix* matrices_dev = nullptr;
@@ -41,12 +47,15 @@ struct arc_muon {
   int32_t* run_matrix_dev = nullptr;
   double *sums_dev = nullptr, *inverse_dev = nullptr;
   char* workspace = nullptr;
+  float* parts_dev = nullptr;
+  uint32_t* arrived_dev = nullptr;
 
   void release() {
     (void)hipStreamSynchronize(stream);
     for (void* p : {static_cast<void*>(matrices_dev), static_cast<void*>(tiles_dev),
                     static_cast<void*>(run_matrix_dev), static_cast<void*>(sums_dev),
-                    static_cast<void*>(inverse_dev), static_cast<void*>(workspace)})
+                    static_cast<void*>(inverse_dev), static_cast<void*>(workspace),
+                    static_cast<void*>(parts_dev), static_cast<void*>(arrived_dev)})
       if (p) (void)hipFree(p);
   }
 };
@@ -136,32 +145,136 @@ arc_status check_muon(const arc_muon_config* cfg) {
   return ARC_OK;
 }
 
-// Tiles of 128 where they fill the card, else of 64.
-int32_t side_of(const arc_muon_config* cfg) {
-  int64_t tiles = 0;
-  for (int32_t i = 0; i < cfg->num_matrices; ++i)
-    tiles += ((cfg->matrices[i].rows + 127) / 128) * ((cfg->matrices[i].cols + 127) / 128);
-  return tiles >= 256 ? 128 : 64;
+// Which element of a list each workgroup takes: they go to the eight XCDs in turn,
+// and runs of 32 neighbours to the same one, whose L2 then holds what they share.
+std::vector<int64_t> launch_order(int64_t count) {
+  constexpr int64_t kXcds = 8, kRun = 32;
+  std::vector<int64_t> order(static_cast<size_t>(count));
+  const int64_t even = count / (kXcds * kRun) * (kXcds * kRun);
+  for (int64_t b = 0; b < count; ++b) {
+    const int64_t x = b % kXcds, q = b / kXcds;
+    order[static_cast<size_t>(b)] = b < even ? (q / kRun * kXcds + x) * kRun + q % kRun : b;
+  }
+  return order;
 }
 
-// The tables of a checked configuration (may throw std::bad_alloc).
-void plan_muon(const arc_muon_config* cfg, arc_muon* c) {
-  c->side = side_of(cfg);
-  const int32_t side = c->side;
-  std::vector<arc::MuonTile> split, half, whole;
+// Tiles of a grid of rows x cols (only those on and below the diagonal), in blocks
+// of 4 x 8 neighbours.
+template <typename Add>
+void each_tile(int32_t rows, int32_t cols, bool half, const Add& add) {
+  for (int32_t i0 = 0; i0 < rows; i0 += 4)
+    for (int32_t j0 = 0; j0 < cols; j0 += 8)
+      for (int32_t i = i0; i < std::min(rows, i0 + 4); ++i)
+        for (int32_t j = j0; j < std::min(cols, j0 + 8); ++j)
+          if (!half || j <= i) add(i, j);
+}
+
+// What a launch is expected to take, in us, by which tiles' sums are split and the
+// tiles' side is chosen.  Measured: a line of a tile's sum on a compute unit that is
+// full, and in a workgroup that has it for itself; a result written; a part written
+// (and read once more by the workgroup that adds them); a launch.
+struct Rates {
+  int32_t side;
+  double line, alone, result, part;
+};
+constexpr Rates kRates[] = {{64, 0.24, 0.32, 1.6, 0.8},
+                            {128, 0.76, 0.90, 6.0, 3.2},
+                            {256, 2.75, 2.75, 22.0, 13.0}};
+constexpr double kLaunch = 5.0;
+constexpr int64_t kUnits = 256;
+
+// The parts of each of `lines`, which descend, from number `from` on `parts` of them;
+// and the time that the busiest compute unit then needs.
+double launch_time(const Rates& r, const std::vector<int32_t>& lines, size_t from, int32_t parts) {
+  std::vector<double> queue;  // a heap, the least busy first
+  queue.assign(static_cast<size_t>(kUnits), 0.0);
+  double longest = 0.0;
+  const auto add = [&](double time, double least) {
+    std::pop_heap(queue.begin(), queue.end(), std::greater<>());
+    queue.back() += time;
+    std::push_heap(queue.begin(), queue.end(), std::greater<>());
+    longest = std::max(longest, least);
+  };
+  for (size_t k = 0; k < lines.size(); ++k) {
+    const int32_t p = k < from ? 1 : std::min(parts, lines[k]);
+    const int32_t each = (lines[k] + p - 1) / p;
+    const double end = p == 1 ? r.result : r.part;
+    for (int32_t q = 0; q < p; ++q) add(each * r.line + end, each * r.alone + end);
+    if (p > 1) add(r.result + p * r.part, each * r.alone + r.result + (p + 1) * r.part);
+  }
+  return kLaunch + std::max(longest, *std::max_element(queue.begin(), queue.end()));
+}
+
+// Turns a product's tiles (their sums `lines` long, descending) into workgroups, and
+// adds the time that they are expected to take.  Sums are split where tiles are few,
+// or where the last ones would leave most of the card idle.
+double plan_product(const Rates& r, std::vector<arc::MuonTile>* tiles, int64_t* parts_of_launch) {
+  constexpr size_t kMany = 4096;  // a split gains little then
+  double work = 0.0;
+  std::vector<int32_t> lines;
+  for (const arc::MuonTile& t : *tiles) {
+    lines.push_back(t.lines);
+    work += t.lines * r.line + r.result;
+  }
+  if (tiles->size() > kMany) return kLaunch + work / kUnits;
+  double best = launch_time(r, lines, lines.size(), 1);
+  size_t from = lines.size();
+  int32_t parts = 1;
+  const size_t rounds = lines.size() / kUnits * kUnits;
+  for (const int32_t p : {2, 3, 4, 6, 8, 12, 16})
+    for (const size_t f : {size_t{0}, rounds}) {
+      if (f == lines.size()) continue;
+      const double t = launch_time(r, lines, f, p);
+      if (t < 0.95 * best) best = t, from = f, parts = p;
+    }
+  std::vector<arc::MuonTile> out;
+  int32_t place = 0;
+  for (size_t k = 0; k < tiles->size(); ++k) {
+    arc::MuonTile t = (*tiles)[k];
+    const int32_t p = k < from ? 1 : std::min(parts, t.lines);
+    const int32_t each = (t.lines + p - 1) / p, all = t.lines;
+    t.parts = (all + each - 1) / each;
+    t.place = place;
+    if (t.parts > 1) place += t.parts;
+    for (t.part = 0; t.part < t.parts; ++t.part) {
+      t.first = t.part * each;
+      t.lines = std::min(each, all - t.first);
+      out.push_back(t);
+    }
+  }
+  *parts_of_launch = std::max<int64_t>(*parts_of_launch, place);
+  tiles->swap(out);
+  return best;
+}
+
+// The tables of a checked configuration for tiles of a side, and the time that its
+// products are expected to take (may throw std::bad_alloc).
+double plan_muon(const arc_muon_config* cfg, const Rates& rates, arc_muon* c) {
+  const int32_t side = rates.side;
+  c->side = side;
+  double time = 0.0;
+  std::vector<arc::MuonTile> split, products[3];
   arc::MuonGroup g;
   int64_t bytes = 0, runs = 0;
   const auto finish = [&] {
     if (g.count == 0) return;
-    const auto take = [&](std::vector<arc::MuonTile>& from, int64_t* at, int64_t* count) {
-      *at = static_cast<int64_t>(c->tiles.size());
-      *count = static_cast<int64_t>(from.size());
-      c->tiles.insert(c->tiles.end(), from.begin(), from.end());
+    const auto take = [&](std::vector<arc::MuonTile>& from, arc::MuonGroup::Range* range) {
+      range->at = static_cast<int64_t>(c->tiles.size());
+      range->count = static_cast<int64_t>(from.size());
+      for (const int64_t k : launch_order(range->count))
+        c->tiles.push_back(from[static_cast<size_t>(k)]);
       from.clear();
     };
-    take(split, &g.split, &g.splits);
-    take(half, &g.half, &g.halves);
-    take(whole, &g.whole, &g.wholes);
+    take(split, &g.split);
+    for (int k = 0; k < 3; ++k) {
+      // the longest sums first, so that short ones fill the end
+      std::stable_sort(products[k].begin(), products[k].end(),
+                       [](const arc::MuonTile& x, const arc::MuonTile& y) {
+                         return x.lines > y.lines;
+                       });
+      time += plan_product(rates, &products[k], &c->parts);
+      take(products[k], &g.products[k]);
+    }
     g.runs = runs - g.first_run;
     c->groups.push_back(g);
     c->workspace_bytes = std::max(c->workspace_bytes, bytes);
@@ -205,15 +318,35 @@ void plan_muon(const arc_muon_config* cfg, arc_muon* c) {
     bytes += need;
     c->matrices.push_back(t);
     if (count == 0) continue;
-    const int32_t s = arc::kSplitTile;
-    for (int32_t a = 0; a < t.mp / s; ++a)
-      for (int32_t b = 0; b < t.np / s; ++b) split.push_back({i, a, b});
-    for (int32_t a = 0; a < t.mp / side; ++a) {
-      for (int32_t b = 0; b <= a; ++b) half.push_back({i, a, b});
-      for (int32_t b = 0; b < t.np / side; ++b) whole.push_back({i, a, b});
-    }
+    const auto to = [&](std::vector<arc::MuonTile>* list, int32_t sum) {
+      return [=](int32_t a, int32_t b) {
+        list->push_back({i, a, b, 0, sum / arc::kPairLine, 0, 1, 0});
+      };
+    };
+    each_tile(t.mp / arc::kSplitTile, t.np / arc::kSplitTile, false, to(&split, 0));
+    each_tile(t.mp / side, t.mp / side, true, to(&products[arc::kMuonGram], t.np));
+    each_tile(t.mp / side, t.mp / side, true, to(&products[arc::kMuonPoly], t.mp));
+    each_tile(t.mp / side, t.np / side, false, to(&products[arc::kMuonApply], t.mp));
   }
   finish();
+  return time;
+}
+
+// The side whose products are expected to take the least time.
+arc_muon plan_best(const arc_muon_config* cfg) {
+  arc_muon best;
+  double least = INFINITY;
+  for (const Rates& r : kRates) {
+    if (const char* v = getenv("ARC_SIDE")) if (atoi(v) && r.side != atoi(v)) continue;
+    arc_muon c;
+    const double time = plan_muon(cfg, r, &c);
+    if (getenv("ARC_SAY")) fprintf(stderr, "side %d: %.1f us a step, parts %ld\n", r.side, time, (long)c.parts);
+    if (time < least) {
+      least = time;
+      best = std::move(c);
+    }
+  }
+  return best;
 }
 
 arc_status check_pointers(const arc_muon* c, const void* const* p, const char* what) {
@@ -231,9 +364,11 @@ arc_status enqueue(const arc_muon* c, arc::MuonArgs a, void* const* params,
   a.workspace = c->workspace;
   a.sums = c->sums_dev;
   a.inverse = c->inverse_dev;
+  a.parts = c->parts_dev;
+  a.arrived = c->arrived_dev;
   const OnDevice here(c->device);
   for (const arc::MuonGroup& g : c->groups) {
-    if (g.wholes == 0) continue;
+    if (g.split.count == 0) continue;
     a.first = g.first;
     arc::MuonPointers p;
     for (int32_t i = 0; i < g.count; ++i) {
@@ -244,22 +379,19 @@ arc_status enqueue(const arc_muon* c, arc::MuonArgs a, void* const* params,
     ARC_HIP(arc::launch_muon_momentum(a, p, c->run_matrix_dev, g.first_run, g.runs, c->stream),
             "momentum launch");
     ARC_HIP(arc::launch_muon_norms(a, g.count, c->stream), "norm launch");
-    ARC_HIP(arc::launch_muon_split(a, p, c->tiles_dev + g.split, g.splits, c->stream),
+    ARC_HIP(arc::launch_muon_split(a, p, c->tiles_dev + g.split.at, g.split.count, c->stream),
             "split launch");
     const size_t steps = c->coefficients.size() / 3;
     for (size_t k = 0; k < steps; ++k) {
       const float* q = &c->coefficients[3 * k];
       const arc::MuonStep s{q[0], q[1], q[2], static_cast<int32_t>(k % 2)};
-      const arc::MuonTile *half = c->tiles_dev + g.half, *whole = c->tiles_dev + g.whole;
-      ARC_HIP(arc::launch_muon_product(arc::kMuonGram, c->side, a, nullptr, s, half, g.halves,
-                                       c->stream),
-              "product launch");
-      ARC_HIP(arc::launch_muon_product(arc::kMuonPoly, c->side, a, nullptr, s, half, g.halves,
-                                       c->stream),
-              "product launch");
-      ARC_HIP(arc::launch_muon_product(k + 1 < steps ? arc::kMuonApply : arc::kMuonLast, c->side,
-                                       a, &p, s, whole, g.wholes, c->stream),
-              "product launch");
+      for (const auto what : {arc::kMuonGram, arc::kMuonPoly, arc::kMuonApply}) {
+        const auto last = what == arc::kMuonApply && k + 1 == steps ? arc::kMuonLast : what;
+        const auto& range = g.products[what];
+        ARC_HIP(arc::launch_muon_product(last, c->side, a, &p, s, c->tiles_dev + range.at,
+                                         range.count, c->stream),
+                "product launch");
+      }
     }
   }
   return ARC_OK;
@@ -274,18 +406,17 @@ arc_status arc_muon_create(const arc_muon_config* cfg, void* hip_stream, arc_muo
   *out = nullptr;
   arc_status st = check_muon(cfg);
   if (st != ARC_OK) return st;
-  arc_muon* c = new (std::nothrow) arc_muon();
-  if (c == nullptr) return fail(ARC_ERR_NOMEM, "host allocation failed");
+  arc_muon* c = nullptr;
   try {
+    std::vector<float> coefficients;
     for (int32_t k = 0; k < 3 * cfg->steps; ++k)
-      c->coefficients.push_back(cfg->coefficients ? cfg->coefficients[k] : kQuintic[k % 3]);
-    if (!in_range(c->coefficients)) {
-      delete c;
+      coefficients.push_back(cfg->coefficients ? cfg->coefficients[k] : kQuintic[k % 3]);
+    if (!in_range(coefficients))
       return fail(ARC_ERR_INVALID,
                   "coefficients: singular values in 0..1 have to stay below 2.7, and the "
                   "polynomials below 7.7");
-    }
-    plan_muon(cfg, c);
+    c = new arc_muon(plan_best(cfg));
+    c->coefficients = std::move(coefficients);
   } catch (const std::exception&) {
     delete c;
     return fail(ARC_ERR_NOMEM, "host allocation failed");
@@ -310,6 +441,10 @@ arc_status arc_muon_create(const arc_muon_config* cfg, void* hip_stream, arc_muo
   room(&c->sums_dev, c->run_matrix.size() * sizeof(double));
   room(&c->inverse_dev, c->matrices.size() * sizeof(double));
   room(&c->workspace, static_cast<size_t>(c->workspace_bytes));
+  room(&c->parts_dev, static_cast<size_t>(c->parts * c->side * c->side) * sizeof(float));
+  room(&c->arrived_dev, static_cast<size_t>(c->parts) * sizeof(uint32_t));
+  if (e == hipSuccess && c->parts > 0)
+    e = hipMemset(c->arrived_dev, 0, static_cast<size_t>(c->parts) * sizeof(uint32_t));
   if (e == hipSuccess) e = arc::prepare_muon_products();
   if (e == hipSuccess) e = hipDeviceSynchronize();
   if (e != hipSuccess) {

@@ -31,10 +31,14 @@ struct MuonMatrix {
   int32_t runs;
 };
 
-// One workgroup's part of a launch.
+// One workgroup's part of a launch: a tile, or with parts > 1 the terms of its sum
+// in `lines` lines from `first` on, which the last workgroup of the tile to arrive
+// adds to those of the others, at `place` and after it in the list of parts.
 struct MuonTile {
   int32_t matrix;
   int32_t i, j;
+  int32_t first, lines;
+  int32_t part, parts, place;
 };
 
 struct MuonPointers {
@@ -51,6 +55,8 @@ struct MuonArgs {
   float momentum, lr;
   int32_t nesterov, update;    // update: parameters; otherwise they are overwritten
   char* workspace;
+  float* parts;                // of tiles whose sums are split, side * side each
+  uint32_t* arrived;           // of each place, 0 between launches
   double* sums;                // of the runs' squares
   double* inverse;             // kPairScale / the norm, of each matrix
 };

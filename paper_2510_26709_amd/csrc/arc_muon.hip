@@ -16,6 +16,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "arc_device.h"
@@ -39,10 +40,57 @@ __device__ __forceinline__ float load_one(const void* p, int32_t bf16, int64_t a
               : static_cast<const float*>(p)[at];
 }
 
-__device__ __forceinline__ uint32_t bf16_bits(float x) {
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   uint32_t w;
-  asm("v_cvt_pk_bf16_f32 %0, %1, %1" : "=v"(w) : "v"(x));
-  return w & 0xFFFFu;
+  asm("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(w) : "v"(lo), "v"(hi));
+  return w;
+}
+
+typedef uint32_t loose_u32x4_t __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t loose_u32x2_t __attribute__((ext_vector_type(2), aligned(2)));
+
+// Four numbers from element `at` on, at any element alignment, of which `left` are
+// there (FULL: all of them).
+template <bool FULL>
+__device__ __forceinline__ void load_four(const void* p, int32_t bf16, int64_t at, int32_t left,
+                                          float (&x)[4]) {
+  if (FULL || left >= 4) {
+    if (bf16) {
+      const u32x2_t w =
+          *reinterpret_cast<const loose_u32x2_t*>(static_cast<const uint16_t*>(p) + at);
+      x[0] = bf16_lo(w.x), x[1] = bf16_hi(w.x), x[2] = bf16_lo(w.y), x[3] = bf16_hi(w.y);
+    } else {
+      const u32x4_t w = *reinterpret_cast<const loose_u32x4_t*>(static_cast<const float*>(p) + at);
+      x[0] = __uint_as_float(w.x), x[1] = __uint_as_float(w.y);
+      x[2] = __uint_as_float(w.z), x[3] = __uint_as_float(w.w);
+    }
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) x[k] = k < left ? load_one(p, bf16, at + k) : 0.f;
+}
+
+template <bool FULL>
+__device__ __forceinline__ void store_four(void* p, int32_t bf16, int64_t at, int32_t left,
+                                           const float (&x)[4]) {
+  const u32x2_t h = {bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
+  if (FULL || left >= 4) {
+    if (bf16)
+      *reinterpret_cast<loose_u32x2_t*>(static_cast<uint16_t*>(p) + at) = h;
+    else
+      *reinterpret_cast<loose_u32x4_t*>(static_cast<float*>(p) + at) =
+          u32x4_t{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
+                  __float_as_uint(x[3])};
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (k >= left) break;
+    if (bf16)
+      static_cast<uint16_t*>(p)[at + k] = (uint16_t)((k < 2 ? h.x : h.y) >> (k % 2 * 16));
+    else
+      static_cast<float*>(p)[at + k] = x[k];
+  }
 }
 
 // hi in the low half, lo in the high one, of a number times kPairScale.
@@ -204,18 +252,95 @@ template <>
 struct Shape<128> {
   static constexpr int kWavesI = 2, kWavesJ = 2, kStages = 2, kGroups = 2;
 };
+template <>
+struct Shape<256> {
+  static constexpr int kWavesI = 2, kWavesJ = 4, kStages = 2, kGroups = 2;
+};
 template <int SIDE>
 constexpr int kProductThreads = Shape<SIDE>::kWavesI * Shape<SIDE>::kWavesJ* kWave;
+// Results go through LDS a slab of rows at a time, two words apart from each other:
+// 32 columns of two runs of 16 rows then lie in 64 different banks.
 template <int SIDE>
-constexpr int kProductLds = Shape<SIDE>::kStages * 2 * SIDE* kLineBytes;
+constexpr int kSlabRows = SIDE <= 128 ? SIDE : 64;
+template <int SIDE>
+constexpr int kSlabPitch = SIDE + 2;
+template <int SIDE>
+constexpr int kProductLds =
+    std::max(Shape<SIDE>::kStages * 2 * SIDE * kLineBytes, kSlabRows<SIDE>* kSlabPitch<SIDE> * 4);
+
+// The numbers of 16 pairs of a row, in units of 1 / kPairScale.
+__device__ __forceinline__ void load_16(const char* row, int32_t at, float (&x)[16]) {
+  const char* line = row + (int64_t)(at / kPairLine) * kLineBytes + at % kPairLine * 2;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const half8_t hi = *reinterpret_cast<const half8_t*>(line + 16 * h);
+    const half8_t lo = *reinterpret_cast<const half8_t*>(line + 2 * kPairLine + 16 * h);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[8 * h + k] = (float)hi[k] + (float)lo[k];
+  }
+}
+
+// Adds a tile's parts in their order, in the last workgroup to arrive; false: this is
+// not the last.  Parts are written through to where every compute unit sees them,
+// and read from there.
+template <int SIDE, int TI, int TJ>
+__device__ __forceinline__ bool join_parts(const MuonArgs& a, const MuonTile& at,
+                                           f32x16_t (&acc)[TI][TJ]) {
+  __shared__ bool last;
+  constexpr int kThread = kProductThreads<SIDE>;
+  constexpr int kDevice = 16;  // the sc1 bit
+  constexpr uint32_t kBytes = SIDE * SIDE * 4u;
+  float* first = a.parts + (int64_t)at.place * SIDE * SIDE;
+  const buffer_rsrc mine = make_buffer(first + (int64_t)at.part * SIDE * SIDE, kBytes);
+#pragma unroll
+  for (int i = 0; i < TI; ++i)
+#pragma unroll
+    for (int j = 0; j < TJ; ++j)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const u32x4_t v = {
+            __float_as_uint(acc[i][j][4 * k]), __float_as_uint(acc[i][j][4 * k + 1]),
+            __float_as_uint(acc[i][j][4 * k + 2]), __float_as_uint(acc[i][j][4 * k + 3])};
+        __builtin_amdgcn_raw_buffer_store_b128(v, mine, (int)threadIdx.x * 16,
+                                               ((i * TJ + j) * 4 + k) * kThread * 16, kDevice);
+      }
+  wave_vmem_fence();  // written before it counts
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    last = __hip_atomic_fetch_add(&a.arrived[at.place], 1u, __ATOMIC_RELAXED,
+                                  __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(at.parts - 1);
+    if (last)
+      __hip_atomic_store(&a.arrived[at.place], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  if (!last) return false;
+  for (int32_t q = 0; q < at.parts; ++q) {
+    const buffer_rsrc of = make_buffer(first + (int64_t)q * SIDE * SIDE, kBytes);
+#pragma unroll
+    for (int i = 0; i < TI; ++i)
+#pragma unroll
+      for (int j = 0; j < TJ; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(
+              of, (int)threadIdx.x * 16, ((i * TJ + j) * 4 + k) * kThread * 16, kDevice);
+          const float x[4] = {__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z),
+                              __uint_as_float(v.w)};
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            acc[i][j][4 * k + e] = q == 0 ? x[e] : acc[i][j][4 * k + e] + x[e];
+        }
+  }
+  return true;
+}
 
 struct NoPointers {};
 template <MuonProduct WHAT>
 using PointersOf = std::conditional_t<WHAT == kMuonLast, MuonPointers, NoPointers>;
 
 // A tile of L R', both [rows][sum] in pairs.  The sum is taken a line (32 numbers)
-// at a time, staged in LDS: row r's 16-byte pieces lie at piece ^ (r % 8), so that
-// the eight rows that are read together lie in different banks.
+// at a time, staged in LDS: row r's 16-byte pieces lie at piece ^ (r / 2 % 8), so
+// that 16 rows' pieces, which are read together, lie in different banks.
 template <int SIDE, MuonProduct WHAT>
 __global__ void __launch_bounds__(kProductThreads<SIDE>, Shape<SIDE>::kGroups)
 muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonStep s,
@@ -225,7 +350,7 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonStep s,
   constexpr int TI = SIDE / Sh::kWavesI / 32, TJ = SIDE / Sh::kWavesJ / 32;
   constexpr int kStage = 2 * SIDE * kLineBytes;
   constexpr int kLoads = kStage / 1024 / kWaves;  // of a wave and stage
-  extern __shared__ char lds[];
+  extern __shared__ __attribute__((aligned(256))) char lds[];
   if (skipped(a)) return;
   const MuonTile at = tiles[blockIdx.x];
   const MuonMatrix& t = a.matrices[at.matrix];
@@ -253,15 +378,20 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonStep s,
   left += (int64_t)ti * SIDE * pitch;
   right += (int64_t)tj * SIDE * pitch;
   const buffer_rsrc from[2] = {make_buffer(left, SIDE * pitch), make_buffer(right, SIDE * pitch)};
-  const uint32_t lane_at = (uint32_t)(lane / 8) * pitch + (uint32_t)((lane % 8) ^ (lane / 8)) * 16u;
+  uint32_t lane_at[2];  // in even and odd pieces of 8 rows
+#pragma unroll
+  for (int q = 0; q < 2; ++q)
+    lane_at[q] = (uint32_t)(lane / 8) * pitch + (uint32_t)((lane % 8) ^ (4 * q + lane / 16)) * 16u;
+  static_assert(kLoads % 2 == 0, "a wave's first piece is an even one");
   const auto stage = [&](int32_t line) {
     char* to = lds + line % kStages * kStage;
 #pragma unroll
     for (int q = 0; q < kLoads; ++q) {
       const int piece = wave * kLoads + q;  // of 8 rows; the first half are left's
       const int rows = piece % (SIDE / 8) * 8;
-      load_lds(from[piece / (SIDE / 8)], lane_at,
-               (uint32_t)rows * pitch + (uint32_t)line * kLineBytes, to + piece * 1024);
+      load_lds(from[piece / (SIDE / 8)], lane_at[q % 2],
+               (uint32_t)rows * pitch + (uint32_t)(at.first + line) * kLineBytes,
+               to + piece * 1024);
     }
   };
   f32x16_t acc[TI][TJ];
@@ -271,7 +401,7 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonStep s,
     for (int j = 0; j < TJ; ++j)
 #pragma unroll
       for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.f;
-  const int32_t lines = sum / kPairLine;
+  const int32_t lines = at.lines;
 #pragma unroll
   for (int q = 0; q < kStages - 1; ++q)
     if (q < lines) stage(q);
@@ -288,7 +418,8 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonStep s,
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       half8_t lh[TI], ll[TI], rh[TJ], rl[TJ];
-      const int hi = ((2 * k + half) ^ (row % 8)) * 16, lo = ((4 + 2 * k + half) ^ (row % 8)) * 16;
+      const int turn = row / 2 % 8;
+      const int hi = ((2 * k + half) ^ turn) * 16, lo = ((4 + 2 * k + half) ^ turn) * 16;
 #pragma unroll
       for (int i = 0; i < TI; ++i) {
         lh[i] = *reinterpret_cast<const half8_t*>(l + i * 32 * kLineBytes + hi);
@@ -316,38 +447,71 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonStep s,
           acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh[i], rh[j], acc[i][j], 0, 0, 0);
     }
   }
+  if (at.parts > 1 && !join_parts<SIDE>(a, at, acc)) return;
   // Lane l holds column l % 32 of a 32 x 32 tile, element k in row 8 (k / 4) +
   // 4 (l / 32) + k % 4; all in units of kPairScale^-2.
+  constexpr int kThread = kWaves * kWave, kSlab = kSlabRows<SIDE>, kPitch = kSlabPitch<SIDE>;
+  float* slab = reinterpret_cast<float*>(lds);
+  const int32_t r0 = ti * SIDE, c0 = tj * SIDE;
+  const auto to_slab = [&](int first) {
+    __syncthreads();  // the stages are read, or the slab before
+#pragma unroll
+    for (int i = 0; i < TI; ++i) {
+      const int32_t down = (wi * TI + i) * 32 - first;
+      if (down >= 0 && down < kSlab)
+#pragma unroll
+        for (int j = 0; j < TJ; ++j)
+#pragma unroll
+          for (int k = 0; k < 16; ++k)
+            slab[(down + 8 * (k / 4) + 4 * half + k % 4) * kPitch + (wj * TJ + j) * 32 + row] =
+                acc[i][j][k];
+    }
+  };
   if constexpr (WHAT == kMuonLast) {
+    // A thread has all its loads in flight together, and whole lines are read and
+    // written.
+    constexpr int kAcross = SIDE / 4, kDown = kThread / kAcross, kPasses = kSlab / kDown;
     const int32_t q = at.matrix - a.first;
     const float step = a.lr * t.lr_scale;
     const float keep = 1.f - step * t.weight_decay;
     void* param = p.param[q];
     uint16_t* copy = p.copy[q];
+    const int32_t down = (int)threadIdx.x / kAcross, across = (int)threadIdx.x % kAcross * 4;
+    const int32_t left = t.cols - c0 - across;
+    const auto passes = [&](auto whole) {
+      constexpr bool FULL = decltype(whole)::value;
 #pragma unroll
-    for (int i = 0; i < TI; ++i)
+      for (int first = 0; first < SIDE; first += kSlab) {
+        const int32_t r = r0 + first + down;
+        const int64_t e0 = (int64_t)r * t.cols + c0 + across;
+        float x[kPasses][4];
 #pragma unroll
-      for (int j = 0; j < TJ; ++j)
+        for (int q = 0; q < kPasses; ++q)
+          if (a.update && r + q * kDown < t.rows)
+            load_four<FULL>(param, t.param_bf16, e0 + (int64_t)q * kDown * t.cols, left, x[q]);
+        to_slab(first);
+        __syncthreads();
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          const int32_t r = ti * SIDE + (wi * TI + i) * 32 + 8 * (k / 4) + 4 * half + k % 4;
-          const int32_t c = tj * SIDE + (wj * TJ + j) * 32 + row;
-          if (r >= t.rows || c >= t.cols) continue;
-          const int64_t e = (int64_t)r * t.cols + c;
-          float v = acc[i][j][k] * (1.f / (kPairScale * kPairScale));
-          if (a.update) v = fmaf(-step, v, load_one(param, t.param_bf16, e) * keep);
-          const uint32_t b = bf16_bits(v);
-          if (t.param_bf16)
-            static_cast<uint16_t*>(param)[e] = (uint16_t)b;
-          else
-            static_cast<float*>(param)[e] = v;
-          if (copy) copy[e] = (uint16_t)b;
+        for (int q = 0; q < kPasses; ++q) {
+          if (r + q * kDown >= t.rows) continue;
+          const float* of = slab + (q * kDown + down) * kPitch + across;
+          float v[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            v[k] = of[k] * (1.f / (kPairScale * kPairScale));
+            if (a.update) v[k] = fmaf(-step, v[k], x[q][k] * keep);
+          }
+          const int64_t e = e0 + (int64_t)q * kDown * t.cols;
+          store_four<FULL>(param, t.param_bf16, e, left, v);
+          if (copy) store_four<FULL>(copy, 1, e, left, v);
         }
+      }
+    };
+    if (c0 + SIDE <= t.cols)
+      passes(std::true_type());
+    else
+      passes(std::false_type());
   } else {
-    __syncthreads();  // the stages are read; each wave takes a part of them for itself
-    constexpr int kPitch = 33;
-    static_assert(kWaves * 32 * kPitch * 4 <= kProductLds<SIDE>, "room to turn a tile");
-    uint32_t* turn = reinterpret_cast<uint32_t*>(lds) + wave * 32 * kPitch;
     char* to = a.workspace + (WHAT == kMuonGram ? t.gram : WHAT == kMuonPoly ? t.poly : t.x);
     char* turned = a.workspace + (WHAT == kMuonGram   ? t.gram
                                   : WHAT == kMuonPoly ? t.poly
@@ -356,48 +520,50 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonStep s,
     const int64_t turned_pitch = (int64_t)t.mp * 4;
     const bool mirror = WHAT == kMuonApply || ti != tj;
 #pragma unroll
-    for (int i = 0; i < TI; ++i)
-#pragma unroll
-      for (int j = 0; j < TJ; ++j) {
-        const int32_t r0 = ti * SIDE + (wi * TI + i) * 32, c0 = tj * SIDE + (wj * TJ + j) * 32;
+    for (int first = 0; first < SIDE; first += kSlab) {
+      to_slab(first);
+      __syncthreads();
+      // Rows as they are, 16 numbers a thread and pass; the pairs take the numbers'
+      // places.
+      constexpr int kRuns = SIDE / 16;
+#pragma unroll 2
+      for (int u = threadIdx.x; u < kSlab * kRuns; u += kThread) {
+        const int r = u / kRuns, c = u % kRuns * 16;
+        float* of = slab + r * kPitch + c;
+        char* line = to + (r0 + first + r) * to_pitch;
         uint32_t v[16];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          float x = acc[i][j][k] * (1.f / kPairScale);
-          const int32_t r = r0 + 8 * (k / 4) + 4 * half + k % 4;
-          if constexpr (WHAT == kMuonPoly) {
-            const char* g = a.workspace + t.gram + (int64_t)r * to_pitch +
-                            (int64_t)(c0 / kPairLine) * kLineBytes + row * 2;
-            const float gram = (float)*reinterpret_cast<const _Float16*>(g) +
-                               (float)*reinterpret_cast<const _Float16*>(g + 2 * kPairLine);
-            x = fmaf(s.c, x, s.b * gram) + (r == c0 + row ? s.a * kPairScale : 0.f);
-          }
-          v[k] = pair_of(x);
-        }
-        // rows as they are: turned in LDS, 16 numbers a lane
+        for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(of[k] * (1.f / kPairScale));
+        if constexpr (WHAT == kMuonPoly) {
+          float gram[16];
+          load_16(a.workspace + t.gram + (r0 + first + r) * to_pitch, c0 + c, gram);
 #pragma unroll
-        for (int k = 0; k < 16; ++k) turn[(8 * (k / 4) + 4 * half + k % 4) * kPitch + row] = v[k];
-        wave_lds_fence();
-        uint32_t w[16];
-#pragma unroll
-        for (int k = 0; k < 16; ++k) w[k] = turn[lane / 2 * kPitch + lane % 2 * 16 + k];
-        store_16(to + (r0 + lane / 2) * to_pitch, c0 + lane % 2 * 16, w);
-        wave_lds_fence();
-        // and transposed: four numbers of a lane follow one another
-        if (mirror) {
-          char* line = turned + (int64_t)(c0 + row) * turned_pitch +
-                       (int64_t)(r0 / kPairLine) * kLineBytes;
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const u32x2_t hi = {(v[4 * q] & 0xFFFFu) | (v[4 * q + 1] << 16),
-                                (v[4 * q + 2] & 0xFFFFu) | (v[4 * q + 3] << 16)};
-            const u32x2_t lo = {(v[4 * q] >> 16) | (v[4 * q + 1] & 0xFFFF0000u),
-                                (v[4 * q + 2] >> 16) | (v[4 * q + 3] & 0xFFFF0000u)};
-            *reinterpret_cast<u32x2_t*>(line + (8 * q + 4 * half) * 2) = hi;
-            *reinterpret_cast<u32x2_t*>(line + 2 * kPairLine + (8 * q + 4 * half) * 2) = lo;
+          for (int k = 0; k < 16; ++k) {
+            const float x = fmaf(s.c, __uint_as_float(v[k]), s.b * gram[k]);
+            v[k] = __float_as_uint(
+                r0 + first + r == c0 + c + k ? x + s.a * kPairScale : x);
           }
         }
+#pragma unroll
+        for (int k = 0; k < 16; ++k) v[k] = pair_of(__uint_as_float(v[k]));
+        store_16(line, c0 + c, v);
+        if (mirror)
+#pragma unroll
+          for (int k = 0; k < 16; ++k) of[k] = __uint_as_float(v[k]);
       }
+      if (!mirror) continue;
+      __syncthreads();
+      // And transposed, two threads to a line.
+      constexpr int kLines = kSlab / 32;
+#pragma unroll 2
+      for (int u = threadIdx.x; u < 2 * kLines * SIDE; u += kThread) {
+        const int c = u / 2 % SIDE, r = u / (2 * SIDE) * 32 + u % 2 * 16;
+        uint32_t v[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(slab[(r + k) * kPitch + c]);
+        store_16(turned + (c0 + c) * turned_pitch, r0 + first + r, v);
+      }
+    }
   }
 }
 
@@ -439,8 +605,10 @@ hipError_t reserve_lds() {
 }  // namespace
 
 hipError_t prepare_muon_products() {
-  const hipError_t e = reserve_lds<64>();
-  return e != hipSuccess ? e : reserve_lds<128>();
+  hipError_t e = reserve_lds<64>();
+  if (e == hipSuccess) e = reserve_lds<128>();
+  if (e == hipSuccess) e = reserve_lds<256>();
+  return e;
 }
 
 hipError_t launch_muon_momentum(const MuonArgs& a, const MuonPointers& p, const int32_t* run_matrix,
@@ -465,8 +633,9 @@ hipError_t launch_muon_split(const MuonArgs& a, const MuonPointers& p, const Muo
 hipError_t launch_muon_product(MuonProduct what, int32_t side, const MuonArgs& a,
                                const MuonPointers* p, const MuonStep& s, const MuonTile* tiles,
                                int64_t count, hipStream_t stream) {
-  return side == 64 ? launch_product<64>(what, a, p, s, tiles, count, stream)
-                    : launch_product<128>(what, a, p, s, tiles, count, stream);
+  return side == 64    ? launch_product<64>(what, a, p, s, tiles, count, stream)
+         : side == 128 ? launch_product<128>(what, a, p, s, tiles, count, stream)
+                       : launch_product<256>(what, a, p, s, tiles, count, stream);
 }
 
 }  // namespace arc
