@@ -26,7 +26,12 @@ struct MuonGroup {
     int64_t at = 0, count = 0;
   };
   Range split;        // their tiles in the context's list
-  Range products[3];  // by MuonProduct
+  Range gram, half, whole;
+};
+
+struct MuonLaunch {
+  MuonKind kind;
+  MuonProduct product;
 };
 
 }  // namespace arc
@@ -36,7 +41,11 @@ struct arc_muon {
   std::vector<arc::MuonGroup> groups;
   std::vector<arc::MuonTile> tiles;
   std::vector<int32_t> run_matrix;
-  std::vector<float> coefficients;  // three a step
+  // The products of a pass, for each way to make it: step by step, or the steps'
+  // polynomials multiplied first.
+  std::vector<arc::MuonLaunch> plain, grouped;
+  bool group = false;     // the second one takes less time
+  bool any_f32 = false;   // a parameter is binary32
   int32_t side = 128;
   int64_t state_elems = 0, workspace_bytes = 0;
   int64_t parts = 0;  // most of one launch
@@ -74,6 +83,8 @@ constexpr int32_t kMaxSteps = 64;
 constexpr float kQuintic[3] = {3.4445f, -4.7750f, 2.0315f};
 // What a group's pairs may take: enough matrices to fill the card many times over.
 constexpr int64_t kGroupBytes = int64_t{4} << 30;
+// Steps whose polynomials are multiplied before X is.
+constexpr int32_t kTogether = 3;
 
 int64_t up_to(int64_t v, int64_t of) { return (v + of - 1) / of * of; }
 
@@ -101,17 +112,71 @@ double largest(double a, double b, double c, double top, bool odd) {
   return most;
 }
 
-// Whether no entry of X, X X' and the polynomial leaves the pairs' range: entries
-// are at most the largest singular value, which starts at 1.
-bool in_range(const std::vector<float>& coefficients) {
+// The largest entries of each step's polynomial; empty where an entry of X, X X' or
+// of one of those leaves the pairs' range.  Entries are at most the largest singular
+// value, which starts at 1.
+std::vector<double> polynomial_bounds(const std::vector<float>& coefficients) {
   constexpr double kMost = 7.75;  // 2^13 times it is below binary16's end
   double top = 1.001;             // rounding
+  std::vector<double> bounds;
   for (size_t k = 0; k < coefficients.size(); k += 3) {
     const double a = coefficients[k], b = coefficients[k + 1], c = coefficients[k + 2];
-    if (top * top > kMost || largest(a, b, c, top * top, false) > kMost) return false;
+    bounds.push_back(largest(a, b, c, top * top, false));
+    if (top * top > kMost || bounds.back() > kMost) return {};
     top = largest(a, b, c, top * top, true) * 1.001;
   }
-  return true;  // the last X is not held in pairs
+  return bounds;  // the last X is not held in pairs
+}
+
+// The launches of a pass in which runs of at most `together` steps (the longer ones
+// first) have their polynomials multiplied before X is.
+std::vector<arc::MuonLaunch> sequence(const std::vector<float>& coefficients,
+                                      const std::vector<double>& bounds, int32_t together) {
+  using namespace arc;
+  constexpr float kUnit = 1.f / kPairScale;
+  std::vector<MuonLaunch> out;
+  const auto steps = static_cast<int32_t>(bounds.size());
+  const int32_t runs = (steps + together - 1) / together;
+  int32_t xt = kMuonXt, k = 0;
+  for (int32_t run = 0; run < runs; ++run) {
+    const int32_t count = (steps - k + runs - run - 1) / (runs - run);
+    out.push_back({kMuonGram, {kMuonX, kMuonX, kMuonSquare, kMuonSquare, kUnit, 0, 0, 0}});
+    int32_t all = kMuonPoly;
+    float all_scale = kPairScale;
+    double bound = 1.0;
+    for (int32_t q = 0; q < count; ++q, ++k) {
+      const float a = coefficients[3 * k], b = coefficients[3 * k + 1],
+                  c = coefficients[3 * k + 2];
+      bound *= bounds[k];
+      out.push_back({kMuonStep, {kMuonSquare, kMuonSquare, kMuonPoly, kMuonPoly, kUnit, a, b, c}});
+      if (count > 1 && q == 0) {
+        out.back().product.out = out.back().product.turned = kMuonAll;
+        all = kMuonAll;
+      }
+      const int32_t poly = out.back().product.out;
+      if (q > 0) {
+        float scale = kPairScale;
+        while (scale * bound > 6e4) scale *= 0.5f;
+        const int32_t next = all == kMuonAll ? kMuonAll2 : kMuonAll;
+        // sums are in units of 1 / (kPairScale all_scale)
+        out.push_back({kMuonHalf,
+                       {poly, all, next, next, scale / (kPairScale * all_scale), 0, 0, 0}});
+        all = next;
+        all_scale = scale;
+      }
+      if (q + 1 < count) {
+        out.push_back({kMuonHalf, {poly, kMuonSquare, kMuonWay, kMuonWay, kUnit, 0, 0, 0}});
+        out.push_back({kMuonHalf, {poly, kMuonWay, kMuonSquare, kMuonSquare, kUnit, 0, 0, 0}});
+      }
+    }
+    const int32_t next = xt == kMuonXt ? kMuonXt2 : kMuonXt;
+    if (run + 1 < runs)
+      out.push_back({kMuonApply, {all, xt, kMuonX, next, 1.f / all_scale, 0, 0, 0}});
+    else
+      out.push_back({kMuonLast, {all, xt, kMuonX, next, 1.f / (kPairScale * all_scale), 0, 0, 0}});
+    xt = next;
+  }
+  return out;
 }
 
 arc_status check_muon(const arc_muon_config* cfg) {
@@ -178,8 +243,7 @@ struct Rates {
   double line, alone, result, part;
 };
 constexpr Rates kRates[] = {{64, 0.24, 0.32, 1.6, 0.8},
-                            {128, 0.76, 0.90, 6.0, 3.2},
-                            {256, 2.75, 2.75, 22.0, 13.0}};
+                            {128, 0.76, 0.90, 6.0, 3.2}};
 constexpr double kLaunch = 5.0;
 constexpr int64_t kUnits = 256;
 
@@ -218,6 +282,7 @@ double plan_product(const Rates& r, std::vector<arc::MuonTile>* tiles, int64_t* 
   }
   if (tiles->size() > kMany) return kLaunch + work / kUnits;
   double best = launch_time(r, lines, lines.size(), 1);
+  if (best < 1.1 * (kLaunch + work / kUnits)) return best;  // nearly even as it is
   size_t from = lines.size();
   int32_t parts = 1;
   const size_t rounds = lines.size() / kUnits * kUnits;
@@ -247,13 +312,26 @@ double plan_product(const Rates& r, std::vector<arc::MuonTile>* tiles, int64_t* 
   return best;
 }
 
-// The tables of a checked configuration for tiles of a side, and the time that its
-// products are expected to take (may throw std::bad_alloc).
-double plan_muon(const arc_muon_config* cfg, const Rates& rates, arc_muon* c) {
+// What the products of a context's matrices are expected to take, once each.
+struct Times {
+  double gram = 0.0, half = 0.0, whole = 0.0;
+  double of(const std::vector<arc::MuonLaunch>& launches) const {
+    double t = 0.0;
+    for (const arc::MuonLaunch& l : launches)
+      t += l.kind == arc::kMuonGram ? gram
+           : l.kind == arc::kMuonStep || l.kind == arc::kMuonHalf ? half
+                                                                  : whole;
+    return t;
+  }
+};
+
+// The tables of a checked configuration for tiles of a side (may throw
+// std::bad_alloc).
+Times plan_muon(const arc_muon_config* cfg, const Rates& rates, arc_muon* c) {
   const int32_t side = rates.side;
   c->side = side;
-  double time = 0.0;
-  std::vector<arc::MuonTile> split, products[3];
+  Times times;
+  std::vector<arc::MuonTile> split, gram, half, whole;
   arc::MuonGroup g;
   int64_t bytes = 0, runs = 0;
   const auto finish = [&] {
@@ -266,15 +344,19 @@ double plan_muon(const arc_muon_config* cfg, const Rates& rates, arc_muon* c) {
       from.clear();
     };
     take(split, &g.split);
-    for (int k = 0; k < 3; ++k) {
+    const auto product = [&](std::vector<arc::MuonTile>& tiles, arc::MuonGroup::Range* range) {
       // the longest sums first, so that short ones fill the end
-      std::stable_sort(products[k].begin(), products[k].end(),
+      std::stable_sort(tiles.begin(), tiles.end(),
                        [](const arc::MuonTile& x, const arc::MuonTile& y) {
                          return x.lines > y.lines;
                        });
-      time += plan_product(rates, &products[k], &c->parts);
-      take(products[k], &g.products[k]);
-    }
+      const double t = plan_product(rates, &tiles, &c->parts);
+      take(tiles, range);
+      return t;
+    };
+    times.gram += product(gram, &g.gram);
+    times.half += product(half, &g.half);
+    times.whole += product(whole, &g.whole);
     g.runs = runs - g.first_run;
     c->groups.push_back(g);
     c->workspace_bytes = std::max(c->workspace_bytes, bytes);
@@ -297,7 +379,7 @@ double plan_muon(const arc_muon_config* cfg, const Rates& rates, arc_muon* c) {
     t.state = c->state_elems;
     c->state_elems += up_to(count, ARC_STATE_BLOCK);
     const int64_t long_bytes = int64_t{4} * t.mp * t.np, short_bytes = int64_t{4} * t.mp * t.mp;
-    const int64_t need = count > 0 ? 3 * long_bytes + 2 * short_bytes : 0;
+    const int64_t need = count > 0 ? 3 * long_bytes + 5 * short_bytes : 0;
     if (g.count == arc::kMuonBatch || (g.count > 0 && bytes + need > kGroupBytes)) {
       finish();
       g = arc::MuonGroup{};
@@ -310,12 +392,12 @@ double plan_muon(const arc_muon_config* cfg, const Rates& rates, arc_muon* c) {
     t.runs = static_cast<int32_t>((count + arc::kMuonRun - 1) / arc::kMuonRun);
     runs += t.runs;
     c->run_matrix.insert(c->run_matrix.end(), static_cast<size_t>(t.runs), i);
-    t.x = bytes;
-    t.xt[0] = t.x + long_bytes;
-    t.xt[1] = t.xt[0] + long_bytes;
-    t.gram = t.xt[1] + long_bytes;
-    t.poly = t.gram + short_bytes;
+    for (int32_t k = 0, at = 0; k < 8; ++k) {
+      t.at[k] = bytes + at * short_bytes + std::min(k, 3) * long_bytes;
+      at += k >= 3;
+    }
     bytes += need;
+    if (count > 0 && !t.param_bf16) c->any_f32 = true;
     c->matrices.push_back(t);
     if (count == 0) continue;
     const auto to = [&](std::vector<arc::MuonTile>* list, int32_t sum) {
@@ -324,28 +406,37 @@ double plan_muon(const arc_muon_config* cfg, const Rates& rates, arc_muon* c) {
       };
     };
     each_tile(t.mp / arc::kSplitTile, t.np / arc::kSplitTile, false, to(&split, 0));
-    each_tile(t.mp / side, t.mp / side, true, to(&products[arc::kMuonGram], t.np));
-    each_tile(t.mp / side, t.mp / side, true, to(&products[arc::kMuonPoly], t.mp));
-    each_tile(t.mp / side, t.np / side, false, to(&products[arc::kMuonApply], t.mp));
+    each_tile(t.mp / side, t.mp / side, true, to(&gram, t.np));
+    each_tile(t.mp / side, t.mp / side, true, to(&half, t.mp));
+    each_tile(t.mp / side, t.np / side, false, to(&whole, t.mp));
   }
   finish();
-  return time;
+  return times;
 }
 
-// The side whose products are expected to take the least time.
-arc_muon plan_best(const arc_muon_config* cfg) {
+// The side, and the way to go through the steps, whose products are expected to take
+// the least time.
+arc_muon plan_best(const arc_muon_config* cfg, const std::vector<float>& coefficients,
+                   const std::vector<double>& bounds) {
+  const auto plain = sequence(coefficients, bounds, 1);
+  const auto grouped = sequence(coefficients, bounds, kTogether);
   arc_muon best;
   double least = INFINITY;
   for (const Rates& r : kRates) {
     if (const char* v = getenv("ARC_SIDE")) if (atoi(v) && r.side != atoi(v)) continue;
     arc_muon c;
-    const double time = plan_muon(cfg, r, &c);
-    if (getenv("ARC_SAY")) fprintf(stderr, "side %d: %.1f us a step, parts %ld\n", r.side, time, (long)c.parts);
-    if (time < least) {
-      least = time;
+    const Times times = plan_muon(cfg, r, &c);
+    const double one = times.of(plain), other = times.of(grouped);
+    if (getenv("ARC_SAY")) fprintf(stderr, "side %d: %.1f %.1f us a step, parts %ld\n", r.side, one, other, (long)c.parts);
+    c.group = other < 0.97 * one;
+    if (const char* v = getenv("ARC_GROUP")) c.group = atoi(v);
+    if (std::min(one, other) < least) {
+      least = std::min(one, other);
       best = std::move(c);
     }
   }
+  best.plain = plain;
+  best.grouped = grouped;
   return best;
 }
 
@@ -367,6 +458,7 @@ arc_status enqueue(const arc_muon* c, arc::MuonArgs a, void* const* params,
   a.parts = c->parts_dev;
   a.arrived = c->arrived_dev;
   const OnDevice here(c->device);
+  const auto& launches = c->group && (a.update || !c->any_f32) ? c->grouped : c->plain;
   for (const arc::MuonGroup& g : c->groups) {
     if (g.split.count == 0) continue;
     a.first = g.first;
@@ -381,17 +473,13 @@ arc_status enqueue(const arc_muon* c, arc::MuonArgs a, void* const* params,
     ARC_HIP(arc::launch_muon_norms(a, g.count, c->stream), "norm launch");
     ARC_HIP(arc::launch_muon_split(a, p, c->tiles_dev + g.split.at, g.split.count, c->stream),
             "split launch");
-    const size_t steps = c->coefficients.size() / 3;
-    for (size_t k = 0; k < steps; ++k) {
-      const float* q = &c->coefficients[3 * k];
-      const arc::MuonStep s{q[0], q[1], q[2], static_cast<int32_t>(k % 2)};
-      for (const auto what : {arc::kMuonGram, arc::kMuonPoly, arc::kMuonApply}) {
-        const auto last = what == arc::kMuonApply && k + 1 == steps ? arc::kMuonLast : what;
-        const auto& range = g.products[what];
-        ARC_HIP(arc::launch_muon_product(last, c->side, a, &p, s, c->tiles_dev + range.at,
-                                         range.count, c->stream),
-                "product launch");
-      }
+    for (const arc::MuonLaunch& l : launches) {
+      const auto& range = l.kind == arc::kMuonGram ? g.gram
+                          : l.kind == arc::kMuonStep || l.kind == arc::kMuonHalf ? g.half
+                                                                                 : g.whole;
+      ARC_HIP(arc::launch_muon_product(l.kind, c->side, a, p, l.product, c->tiles_dev + range.at,
+                                       range.count, c->stream),
+              "product launch");
     }
   }
   return ARC_OK;
@@ -411,12 +499,12 @@ arc_status arc_muon_create(const arc_muon_config* cfg, void* hip_stream, arc_muo
     std::vector<float> coefficients;
     for (int32_t k = 0; k < 3 * cfg->steps; ++k)
       coefficients.push_back(cfg->coefficients ? cfg->coefficients[k] : kQuintic[k % 3]);
-    if (!in_range(coefficients))
+    const std::vector<double> bounds = polynomial_bounds(coefficients);
+    if (bounds.empty())
       return fail(ARC_ERR_INVALID,
                   "coefficients: singular values in 0..1 have to stay below 2.7, and the "
                   "polynomials below 7.7");
-    c = new arc_muon(plan_best(cfg));
-    c->coefficients = std::move(coefficients);
+    c = new arc_muon(plan_best(cfg, coefficients, bounds));
   } catch (const std::exception&) {
     delete c;
     return fail(ARC_ERR_NOMEM, "host allocation failed");

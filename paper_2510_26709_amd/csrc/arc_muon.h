@@ -18,10 +18,17 @@ constexpr int kMuonRun = 8192;  // elements of a matrix whose squares one workgr
 constexpr int kSplitTile = 64;  // sides of what one workgroup splits into pairs
 constexpr int kMuonBatch = 160; // matrices of a launch (their pointers are arguments)
 
+// What lies there: X, its transpose (in turn), X X' and what follows from it, all in
+// pairs: the polynomial of a step, the product of those of some steps (in turn) and
+// a product of two of these on the way.
+enum MuonArray {
+  kMuonX, kMuonXt, kMuonXt2, kMuonSquare, kMuonPoly, kMuonWay, kMuonAll, kMuonAll2
+};
+
 // A matrix, seen from its shorter side: X is m x n, m <= n, or its transpose.
 struct MuonMatrix {
   int64_t state;                        // first element of its momentum
-  int64_t x, xt[2], gram, poly;         // where its pairs lie in the workspace, bytes
+  int64_t at[8];                        // where its pairs lie in the workspace, bytes
   int64_t first_run;                    // its runs' sums
   int32_t rows, cols;                   // as the caller has it
   int32_t m, n, mp, np;                 // sides, and those of the workspace
@@ -61,11 +68,15 @@ struct MuonArgs {
   double* inverse;             // kPairScale / the norm, of each matrix
 };
 
-enum MuonProduct { kMuonGram, kMuonPoly, kMuonApply, kMuonLast };
+// kMuonGram: X X'.  kMuonStep: a + b A + c A A of A = X X'.  kMuonHalf: a product of
+// two such, which commute, so that it is symmetric too.  kMuonApply: one of them times
+// X, and kMuonLast the same with the parameters' update at its end.
+enum MuonKind { kMuonGram, kMuonStep, kMuonHalf, kMuonApply, kMuonLast };
 
-struct MuonStep {
-  float a, b, c;
-  int32_t from;  // which of xt holds the transpose
+struct MuonProduct {
+  int32_t left, right, out, turned;  // MuonArray; turned: the transpose's place
+  float scale;                       // of the result in pairs, from the sums of pairs
+  float a, b, c;                     // kMuonStep
 };
 
 // The momenta, and the squares of what is orthogonalised.
@@ -76,9 +87,9 @@ hipError_t launch_muon_norms(const MuonArgs& a, int32_t count, hipStream_t strea
 hipError_t launch_muon_split(const MuonArgs& a, const MuonPointers& p, const MuonTile* tiles,
                              int64_t count, hipStream_t stream);
 // Products of square tiles of `side`.
-hipError_t launch_muon_product(MuonProduct what, int32_t side, const MuonArgs& a,
-                               const MuonPointers* p, const MuonStep& s, const MuonTile* tiles,
-                               int64_t count, hipStream_t stream);
+hipError_t launch_muon_product(MuonKind kind, int32_t side, const MuonArgs& a,
+                               const MuonPointers& p, const MuonProduct& s,
+                               const MuonTile* tiles, int64_t count, hipStream_t stream);
 hipError_t prepare_muon_products();
 
 }  // namespace arc

@@ -136,19 +136,39 @@ muon_momentum_kernel(MuonArgs a, MuonPointers p, const int32_t* __restrict__ run
   const int64_t first = (run - t.first_run) * kMuonRun;
   float* m = a.m ? a.m + t.state : nullptr;
   double sum = 0.0;
-#pragma unroll 4
-  for (int u = threadIdx.x; u < kMuonRun; u += kThreads) {
-    const int64_t e = first + u;
-    if (e >= count) break;
-    const float g = load_one(grad, bf16, e) * factor;
-    float v = 0.f;
-    if (m) {
-      v = a.momentum * m[e] + g;
-      m[e] = v;
+  const auto passes = [&](auto whole) {
+    constexpr bool FULL = decltype(whole)::value;
+    constexpr int U = 4;  // passes whose loads are in flight together
+    for (int u = 0; u < kMuonRun; u += U * 4 * kThreads) {
+      if (!FULL && first + u >= count) break;
+      float g[U][4], v[U][4];
+#pragma unroll
+      for (int q = 0; q < U; ++q) {
+        const int64_t e = first + u + (q * kThreads + (int)threadIdx.x) * 4;
+        const int32_t left = FULL ? 4 : (int32_t)max(min(count - e, (int64_t)4), (int64_t)0);
+        load_four<FULL>(grad, bf16, e, left, g[q]);
+        if (m) load_four<FULL>(m, 0, e, left, v[q]);
+      }
+#pragma unroll
+      for (int q = 0; q < U; ++q) {
+        const int64_t e = first + u + (q * kThreads + (int)threadIdx.x) * 4;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          g[q][k] *= factor;
+          if (m) v[q][k] = a.momentum * v[q][k] + g[q][k];
+          const double d = direction(a, g[q][k], m ? v[q][k] : 0.f);
+          sum = fma(d, d, sum);  // (behind the end: zeros)
+        }
+        if (m)
+          store_four<FULL>(m, 0, e, FULL ? 4 : (int32_t)max(min(count - e, (int64_t)4), (int64_t)0),
+                           v[q]);
+      }
     }
-    const double d = direction(a, g, v);
-    sum = fma(d, d, sum);
-  }
+  };
+  if (first + kMuonRun <= count)
+    passes(std::true_type());
+  else
+    passes(std::false_type());
   sum = group_sum(sum);
   if (threadIdx.x == 0) a.sums[run] = sum;
 }
@@ -196,16 +216,27 @@ muon_split_kernel(MuonArgs a, MuonPointers p, const MuonTile* __restrict__ tiles
   const double inverse = a.inverse[at.matrix];
   const float* m = a.m ? a.m + t.state : nullptr;
   const int32_t r0 = (t.tall ? at.j : at.i) * S, c0 = (t.tall ? at.i : at.j) * S;
-#pragma unroll 4
-  for (int u = threadIdx.x; u < S * S; u += kThreads) {
-    const int32_t r = r0 + u / S, c = c0 + u % S;
-    uint32_t v = 0;
-    if (r < t.rows && c < t.cols) {
-      const int64_t e = (int64_t)r * t.cols + c;
-      const float d = direction(a, load_one(grad, bf16, e) * factor, m ? m[e] : 0.f);
-      v = pair_of((float)((double)d * inverse));
+  {
+    constexpr int U = S * S / 4 / kThreads;
+    const int32_t c = c0 + (int)threadIdx.x % (S / 4) * 4, left = t.cols - c;
+    const int32_t r = r0 + (int)threadIdx.x / (S / 4);
+    constexpr int kDown = kThreads / (S / 4);
+    float g[U][4], v[U][4];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) g[u][k] = v[u][k] = 0.f;
+      if (r + u * kDown >= t.rows) continue;
+      const int64_t e = (int64_t)(r + u * kDown) * t.cols + c;
+      load_four<false>(grad, bf16, e, left, g[u]);
+      if (m) load_four<false>(m, 0, e, left, v[u]);
     }
-    tile[u / S][u % S] = v;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        tile[r - r0 + u * kDown][c - c0 + k] =
+            pair_of((float)((double)direction(a, g[u][k] * factor, v[u][k]) * inverse));
   }
   __syncthreads();
   const int line = threadIdx.x / 4, part = threadIdx.x % 4 * 16;
@@ -215,8 +246,8 @@ muon_split_kernel(MuonArgs a, MuonPointers p, const MuonTile* __restrict__ tiles
     along[k] = tile[line][part + k];
     across[k] = tile[part + k][line];
   }
-  char* x = a.workspace + t.x + (int64_t)(at.i * S + line) * t.np * 4;
-  char* xt = a.workspace + t.xt[0] + (int64_t)(at.j * S + line) * t.mp * 4;
+  char* x = a.workspace + t.at[kMuonX] + (int64_t)(at.i * S + line) * t.np * 4;
+  char* xt = a.workspace + t.at[kMuonXt] + (int64_t)(at.j * S + line) * t.mp * 4;
   if (t.tall) {
     store_16(x, at.j * S + part, across);
     store_16(xt, at.i * S + part, along);
@@ -251,10 +282,6 @@ struct Shape<64> {
 template <>
 struct Shape<128> {
   static constexpr int kWavesI = 2, kWavesJ = 2, kStages = 2, kGroups = 2;
-};
-template <>
-struct Shape<256> {
-  static constexpr int kWavesI = 2, kWavesJ = 4, kStages = 2, kGroups = 2;
 };
 template <int SIDE>
 constexpr int kProductThreads = Shape<SIDE>::kWavesI * Shape<SIDE>::kWavesJ* kWave;
@@ -335,15 +362,15 @@ __device__ __forceinline__ bool join_parts(const MuonArgs& a, const MuonTile& at
 }
 
 struct NoPointers {};
-template <MuonProduct WHAT>
+template <MuonKind WHAT>
 using PointersOf = std::conditional_t<WHAT == kMuonLast, MuonPointers, NoPointers>;
 
 // A tile of L R', both [rows][sum] in pairs.  The sum is taken a line (32 numbers)
 // at a time, staged in LDS: row r's 16-byte pieces lie at piece ^ (r / 2 % 8), so
 // that 16 rows' pieces, which are read together, lie in different banks.
-template <int SIDE, MuonProduct WHAT>
+template <int SIDE, MuonKind WHAT>
 __global__ void __launch_bounds__(kProductThreads<SIDE>, Shape<SIDE>::kGroups)
-muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonStep s,
+muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,
                     const MuonTile* __restrict__ tiles) {
   using Sh = Shape<SIDE>;
   constexpr int kWaves = Sh::kWavesI * Sh::kWavesJ, kStages = Sh::kStages;
@@ -359,21 +386,9 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonStep s,
   const int wi = wave / Sh::kWavesJ, wj = wave % Sh::kWavesJ;
   const bool swap = WHAT == kMuonLast && t.tall;  // lanes go along the parameter's rows
   const int32_t ti = swap ? at.j : at.i, tj = swap ? at.i : at.j;
-  const char* xt = a.workspace + t.xt[s.from];
-  const char* poly = a.workspace + t.poly;
-  const char *left, *right;
-  int32_t sum;
-  if constexpr (WHAT == kMuonGram) {
-    left = right = a.workspace + t.x;
-    sum = t.np;
-  } else if constexpr (WHAT == kMuonPoly) {
-    left = right = a.workspace + t.gram;
-    sum = t.mp;
-  } else {
-    left = swap ? xt : poly;
-    right = swap ? poly : xt;
-    sum = t.mp;
-  }
+  const char* left = a.workspace + t.at[swap ? s.right : s.left];
+  const char* right = a.workspace + t.at[swap ? s.left : s.right];
+  const int32_t sum = WHAT == kMuonGram ? t.np : t.mp;
   const uint32_t pitch = (uint32_t)sum * 4u;
   left += (int64_t)ti * SIDE * pitch;
   right += (int64_t)tj * SIDE * pitch;
@@ -498,7 +513,7 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonStep s,
           float v[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            v[k] = of[k] * (1.f / (kPairScale * kPairScale));
+            v[k] = of[k] * s.scale;
             if (a.update) v[k] = fmaf(-step, v[k], x[q][k] * keep);
           }
           const int64_t e = e0 + (int64_t)q * kDown * t.cols;
@@ -512,10 +527,8 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonStep s,
     else
       passes(std::false_type());
   } else {
-    char* to = a.workspace + (WHAT == kMuonGram ? t.gram : WHAT == kMuonPoly ? t.poly : t.x);
-    char* turned = a.workspace + (WHAT == kMuonGram   ? t.gram
-                                  : WHAT == kMuonPoly ? t.poly
-                                                      : t.xt[1 - s.from]);
+    char* to = a.workspace + t.at[s.out];
+    char* turned = a.workspace + t.at[s.turned];
     const int64_t to_pitch = (int64_t)(WHAT == kMuonApply ? t.np : t.mp) * 4;
     const int64_t turned_pitch = (int64_t)t.mp * 4;
     const bool mirror = WHAT == kMuonApply || ti != tj;
@@ -533,10 +546,10 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonStep s,
         char* line = to + (r0 + first + r) * to_pitch;
         uint32_t v[16];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(of[k] * (1.f / kPairScale));
-        if constexpr (WHAT == kMuonPoly) {
+        for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(of[k] * s.scale);
+        if constexpr (WHAT == kMuonStep) {
           float gram[16];
-          load_16(a.workspace + t.gram + (r0 + first + r) * to_pitch, c0 + c, gram);
+          load_16(a.workspace + t.at[s.left] + (r0 + first + r) * to_pitch, c0 + c, gram);
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
             const float x = fmaf(s.c, __uint_as_float(v[k]), s.b * gram[k]);
@@ -567,32 +580,32 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonStep s,
   }
 }
 
-template <int SIDE, MuonProduct WHAT>
-void launch_tiles(const MuonArgs& a, const PointersOf<WHAT>& p, const MuonStep& s,
+template <int SIDE, MuonKind WHAT>
+void launch_tiles(const MuonArgs& a, const PointersOf<WHAT>& p, const MuonProduct& s,
                   const MuonTile* tiles, int64_t count, hipStream_t stream) {
   hipLaunchKernelGGL((muon_product_kernel<SIDE, WHAT>), dim3((unsigned)count),
                      dim3(kProductThreads<SIDE>), kProductLds<SIDE>, stream, a, p, s, tiles);
 }
 
 template <int SIDE>
-hipError_t launch_product(MuonProduct what, const MuonArgs& a, const MuonPointers* p,
-                          const MuonStep& s, const MuonTile* tiles, int64_t count,
+hipError_t launch_product(MuonKind kind, const MuonArgs& a, const MuonPointers& p,
+                          const MuonProduct& s, const MuonTile* tiles, int64_t count,
                           hipStream_t stream) {
-  if (what == kMuonGram)
-    launch_tiles<SIDE, kMuonGram>(a, {}, s, tiles, count, stream);
-  else if (what == kMuonPoly)
-    launch_tiles<SIDE, kMuonPoly>(a, {}, s, tiles, count, stream);
-  else if (what == kMuonApply)
-    launch_tiles<SIDE, kMuonApply>(a, {}, s, tiles, count, stream);
-  else
-    launch_tiles<SIDE, kMuonLast>(a, *p, s, tiles, count, stream);
+  switch (kind) {
+    case kMuonGram: launch_tiles<SIDE, kMuonGram>(a, {}, s, tiles, count, stream); break;
+    case kMuonStep: launch_tiles<SIDE, kMuonStep>(a, {}, s, tiles, count, stream); break;
+    case kMuonHalf: launch_tiles<SIDE, kMuonHalf>(a, {}, s, tiles, count, stream); break;
+    case kMuonApply: launch_tiles<SIDE, kMuonApply>(a, {}, s, tiles, count, stream); break;
+    case kMuonLast: launch_tiles<SIDE, kMuonLast>(a, p, s, tiles, count, stream); break;
+  }
   return hipGetLastError();
 }
 
 template <int SIDE>
 hipError_t reserve_lds() {
   for (const void* kernel : {reinterpret_cast<const void*>(muon_product_kernel<SIDE, kMuonGram>),
-                             reinterpret_cast<const void*>(muon_product_kernel<SIDE, kMuonPoly>),
+                             reinterpret_cast<const void*>(muon_product_kernel<SIDE, kMuonStep>),
+                             reinterpret_cast<const void*>(muon_product_kernel<SIDE, kMuonHalf>),
                              reinterpret_cast<const void*>(muon_product_kernel<SIDE, kMuonApply>),
                              reinterpret_cast<const void*>(muon_product_kernel<SIDE, kMuonLast>)}) {
     const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize,
@@ -607,7 +620,6 @@ hipError_t reserve_lds() {
 hipError_t prepare_muon_products() {
   hipError_t e = reserve_lds<64>();
   if (e == hipSuccess) e = reserve_lds<128>();
-  if (e == hipSuccess) e = reserve_lds<256>();
   return e;
 }
 
@@ -630,12 +642,11 @@ hipError_t launch_muon_split(const MuonArgs& a, const MuonPointers& p, const Muo
   return hipGetLastError();
 }
 
-hipError_t launch_muon_product(MuonProduct what, int32_t side, const MuonArgs& a,
-                               const MuonPointers* p, const MuonStep& s, const MuonTile* tiles,
-                               int64_t count, hipStream_t stream) {
-  return side == 64    ? launch_product<64>(what, a, p, s, tiles, count, stream)
-         : side == 128 ? launch_product<128>(what, a, p, s, tiles, count, stream)
-                       : launch_product<256>(what, a, p, s, tiles, count, stream);
+hipError_t launch_muon_product(MuonKind kind, int32_t side, const MuonArgs& a,
+                               const MuonPointers& p, const MuonProduct& s,
+                               const MuonTile* tiles, int64_t count, hipStream_t stream) {
+  return side == 64 ? launch_product<64>(kind, a, p, s, tiles, count, stream)
+                    : launch_product<128>(kind, a, p, s, tiles, count, stream);
 }
 
 }  // namespace arc
