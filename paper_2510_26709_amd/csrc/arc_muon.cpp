@@ -54,7 +54,7 @@ struct arc_muon {
   arc::MuonMatrix* matrices_dev = nullptr;
   arc::MuonTile* tiles_dev = nullptr;
   int32_t* run_matrix_dev = nullptr;
-  double *sums_dev = nullptr, *inverse_dev = nullptr;
+  double* sums_dev = nullptr;
   char* workspace = nullptr;
   float* parts_dev = nullptr;
   uint32_t* arrived_dev = nullptr;
@@ -63,7 +63,7 @@ struct arc_muon {
     (void)hipStreamSynchronize(stream);
     for (void* p : {static_cast<void*>(matrices_dev), static_cast<void*>(tiles_dev),
                     static_cast<void*>(run_matrix_dev), static_cast<void*>(sums_dev),
-                    static_cast<void*>(inverse_dev), static_cast<void*>(workspace),
+                    static_cast<void*>(workspace),
                     static_cast<void*>(parts_dev), static_cast<void*>(arrived_dev)})
       if (p) (void)hipFree(p);
   }
@@ -454,7 +454,6 @@ arc_status enqueue(const arc_muon* c, arc::MuonArgs a, void* const* params,
   a.matrices = c->matrices_dev;
   a.workspace = c->workspace;
   a.sums = c->sums_dev;
-  a.inverse = c->inverse_dev;
   a.parts = c->parts_dev;
   a.arrived = c->arrived_dev;
   const OnDevice here(c->device);
@@ -470,7 +469,6 @@ arc_status enqueue(const arc_muon* c, arc::MuonArgs a, void* const* params,
     }
     ARC_HIP(arc::launch_muon_momentum(a, p, c->run_matrix_dev, g.first_run, g.runs, c->stream),
             "momentum launch");
-    ARC_HIP(arc::launch_muon_norms(a, g.count, c->stream), "norm launch");
     ARC_HIP(arc::launch_muon_split(a, p, c->tiles_dev + g.split.at, g.split.count, c->stream),
             "split launch");
     for (const arc::MuonLaunch& l : launches) {
@@ -527,7 +525,6 @@ arc_status arc_muon_create(const arc_muon_config* cfg, void* hip_stream, arc_muo
     if (e != hipSuccess) *p = nullptr;
   };
   room(&c->sums_dev, c->run_matrix.size() * sizeof(double));
-  room(&c->inverse_dev, c->matrices.size() * sizeof(double));
   room(&c->workspace, static_cast<size_t>(c->workspace_bytes));
   room(&c->parts_dev, static_cast<size_t>(c->parts * c->side * c->side) * sizeof(float));
   room(&c->arrived_dev, static_cast<size_t>(c->parts) * sizeof(uint32_t));

@@ -65,7 +65,6 @@ struct MuonArgs {
   float* parts;                // of tiles whose sums are split, side * side each
   uint32_t* arrived;           // of each place, 0 between launches
   double* sums;                // of the runs' squares
-  double* inverse;             // kPairScale / the norm, of each matrix
 };
 
 // kMuonGram: X X'.  kMuonStep: a + b A + c A A of A = X X'.  kMuonHalf: a product of
@@ -82,7 +81,6 @@ struct MuonProduct {
 // The momenta, and the squares of what is orthogonalised.
 hipError_t launch_muon_momentum(const MuonArgs& a, const MuonPointers& p, const int32_t* run_matrix,
                                 int64_t first_run, int64_t runs, hipStream_t stream);
-hipError_t launch_muon_norms(const MuonArgs& a, int32_t count, hipStream_t stream);
 // X and its transpose in pairs, of norm 1.
 hipError_t launch_muon_split(const MuonArgs& a, const MuonPointers& p, const MuonTile* tiles,
                              int64_t count, hipStream_t stream);

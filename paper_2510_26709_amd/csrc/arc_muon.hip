@@ -1,3 +1,4 @@
+
 // Matrices orthogonalised by Newton-Schulz products, and the optimizer step made
 // of them (the formulas are in libarctopk.h).
 //
@@ -29,7 +30,6 @@ constexpr int kThreads = 256;
 constexpr int kLineBytes = 4 * kPairLine;
 
 typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
-typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 __device__ __forceinline__ bool skipped(const MuonArgs& a) {
   return a.factor && !(fabsf(*a.factor) < INFINITY);
@@ -173,16 +173,6 @@ muon_momentum_kernel(MuonArgs a, MuonPointers p, const int32_t* __restrict__ run
   if (threadIdx.x == 0) a.sums[run] = sum;
 }
 
-__global__ void __launch_bounds__(kThreads) muon_norm_kernel(MuonArgs a) {
-  const int32_t i = a.first + blockIdx.x;
-  const MuonMatrix& t = a.matrices[i];
-  double sum = 0.0;
-#pragma unroll 4
-  for (int32_t r = threadIdx.x; r < t.runs; r += kThreads) sum += a.sums[t.first_run + r];
-  sum = group_sum(sum);
-  if (threadIdx.x == 0) a.inverse[i] = sum == 0.0 ? 0.0 : (double)kPairScale / sqrt(sum);
-}
-
 // ---------------------------------------------------------------- pairs
 
 // 16 numbers of a row: `at` is their first one's place in the row.
@@ -213,7 +203,11 @@ muon_split_kernel(MuonArgs a, MuonPointers p, const MuonTile* __restrict__ tiles
   const void* grad = p.grad[at.matrix - a.first];
   const int32_t bf16 = t.grad_bf16;
   const float factor = a.factor ? *a.factor : 1.f;
-  const double inverse = a.inverse[at.matrix];
+  double squares = 0.0;  // every workgroup adds the runs' sums in the same order
+#pragma unroll 4
+  for (int32_t r = threadIdx.x; r < t.runs; r += kThreads) squares += a.sums[t.first_run + r];
+  squares = group_sum(squares);
+  const double inverse = squares == 0.0 ? 0.0 : (double)kPairScale / sqrt(squares);
   const float* m = a.m ? a.m + t.state : nullptr;
   const int32_t r0 = (t.tall ? at.j : at.i) * S, c0 = (t.tall ? at.i : at.j) * S;
   {
@@ -285,15 +279,13 @@ struct Shape<128> {
 };
 template <int SIDE>
 constexpr int kProductThreads = Shape<SIDE>::kWavesI * Shape<SIDE>::kWavesJ* kWave;
-// Results go through LDS a slab of rows at a time, two words apart from each other:
-// 32 columns of two runs of 16 rows then lie in 64 different banks.
-template <int SIDE>
-constexpr int kSlabRows = SIDE <= 128 ? SIDE : 64;
+// Results go through LDS, rows two words apart from each other: 32 columns of two
+// runs of 16 rows then lie in 64 different banks.
 template <int SIDE>
 constexpr int kSlabPitch = SIDE + 2;
 template <int SIDE>
 constexpr int kProductLds =
-    std::max(Shape<SIDE>::kStages * 2 * SIDE * kLineBytes, kSlabRows<SIDE>* kSlabPitch<SIDE> * 4);
+    std::max(Shape<SIDE>::kStages * 2 * SIDE * kLineBytes, SIDE* kSlabPitch<SIDE> * 4);
 
 // The numbers of 16 pairs of a row, in units of 1 / kPairScale.
 __device__ __forceinline__ void load_16(const char* row, int32_t at, float (&x)[16]) {
@@ -312,7 +304,7 @@ __device__ __forceinline__ void load_16(const char* row, int32_t at, float (&x)[
 // and read from there.
 template <int SIDE, int TI, int TJ>
 __device__ __forceinline__ bool join_parts(const MuonArgs& a, const MuonTile& at,
-                                           f32x16_t (&acc)[TI][TJ]) {
+                                           f32x4_t (&acc)[TI][TJ]) {
   __shared__ bool last;
   constexpr int kThread = kProductThreads<SIDE>;
   constexpr int kDevice = 16;  // the sc1 bit
@@ -323,14 +315,9 @@ __device__ __forceinline__ bool join_parts(const MuonArgs& a, const MuonTile& at
   for (int i = 0; i < TI; ++i)
 #pragma unroll
     for (int j = 0; j < TJ; ++j)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const u32x4_t v = {
-            __float_as_uint(acc[i][j][4 * k]), __float_as_uint(acc[i][j][4 * k + 1]),
-            __float_as_uint(acc[i][j][4 * k + 2]), __float_as_uint(acc[i][j][4 * k + 3])};
-        __builtin_amdgcn_raw_buffer_store_b128(v, mine, (int)threadIdx.x * 16,
-                                               ((i * TJ + j) * 4 + k) * kThread * 16, kDevice);
-      }
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, acc[i][j]), mine,
+                                             (int)threadIdx.x * 16, (i * TJ + j) * kThread * 16,
+                                             kDevice);
   wave_vmem_fence();  // written before it counts
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -347,15 +334,11 @@ __device__ __forceinline__ bool join_parts(const MuonArgs& a, const MuonTile& at
     for (int i = 0; i < TI; ++i)
 #pragma unroll
       for (int j = 0; j < TJ; ++j)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(
-              of, (int)threadIdx.x * 16, ((i * TJ + j) * 4 + k) * kThread * 16, kDevice);
-          const float x[4] = {__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z),
-                              __uint_as_float(v.w)};
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            acc[i][j][4 * k + e] = q == 0 ? x[e] : acc[i][j][4 * k + e] + x[e];
+{
+          const f32x4_t v = __builtin_bit_cast(
+              f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(
+                           of, (int)threadIdx.x * 16, (i * TJ + j) * kThread * 16, kDevice));
+          acc[i][j] = q == 0 ? v : acc[i][j] + v;
         }
   }
   return true;
@@ -374,11 +357,10 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,
                     const MuonTile* __restrict__ tiles) {
   using Sh = Shape<SIDE>;
   constexpr int kWaves = Sh::kWavesI * Sh::kWavesJ, kStages = Sh::kStages;
-  constexpr int TI = SIDE / Sh::kWavesI / 32, TJ = SIDE / Sh::kWavesJ / 32;
+  constexpr int TI = SIDE / Sh::kWavesI / 16, TJ = SIDE / Sh::kWavesJ / 16;
   constexpr int kStage = 2 * SIDE * kLineBytes;
   constexpr int kLoads = kStage / 1024 / kWaves;  // of a wave and stage
   extern __shared__ __attribute__((aligned(256))) char lds[];
-  if (skipped(a)) return;
   const MuonTile at = tiles[blockIdx.x];
   const MuonMatrix& t = a.matrices[at.matrix];
   const int lane = threadIdx.x % kWave;
@@ -409,18 +391,18 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,
                to + piece * 1024);
     }
   };
-  f32x16_t acc[TI][TJ];
+  f32x4_t acc[TI][TJ];
 #pragma unroll
   for (int i = 0; i < TI; ++i)
 #pragma unroll
     for (int j = 0; j < TJ; ++j)
 #pragma unroll
-      for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.f;
+      for (int k = 0; k < 4; ++k) acc[i][j][k] = 0.f;
   const int32_t lines = at.lines;
 #pragma unroll
   for (int q = 0; q < kStages - 1; ++q)
     if (q < lines) stage(q);
-  const int row = lane % 32, half = lane / 32;
+  const int row = lane % 16, quarter = lane / 16;
   for (int32_t line = 0; line < lines; ++line) {
     if (line + kStages - 2 < lines)
       arrived<(kStages - 2) * kLoads>();
@@ -428,64 +410,59 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,
       arrived<0>();
     if (line + kStages - 1 < lines) stage(line + kStages - 1);
     const char* base = lds + line % kStages * kStage;
-    const char* l = base + (wi * TI * 32 + row) * kLineBytes;
-    const char* r = base + (SIDE + wj * TJ * 32 + row) * kLineBytes;
+    const char* l = base + (wi * TI * 16 + row) * kLineBytes;
+    const char* r = base + (SIDE + wj * TJ * 16 + row) * kLineBytes;
+    constexpr int kRows = TI < 4 ? TI : 4;  // of tiles whose pairs are in registers
+    half8_t lh[kRows], ll[kRows], rh[TJ], rl[TJ];
+    const int hi = (quarter ^ (row / 2)) * 16, lo = hi ^ 64;
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      half8_t lh[TI], ll[TI], rh[TJ], rl[TJ];
-      const int turn = row / 2 % 8;
-      const int hi = ((2 * k + half) ^ turn) * 16, lo = ((4 + 2 * k + half) ^ turn) * 16;
+    for (int j = 0; j < TJ; ++j) {
+      rh[j] = *reinterpret_cast<const half8_t*>(r + j * 16 * kLineBytes + hi);
+      rl[j] = *reinterpret_cast<const half8_t*>(r + j * 16 * kLineBytes + lo);
+    }
 #pragma unroll
-      for (int i = 0; i < TI; ++i) {
-        lh[i] = *reinterpret_cast<const half8_t*>(l + i * 32 * kLineBytes + hi);
-        ll[i] = *reinterpret_cast<const half8_t*>(l + i * 32 * kLineBytes + lo);
+    for (int i0 = 0; i0 < TI; i0 += kRows) {
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        lh[i] = *reinterpret_cast<const half8_t*>(l + (i0 + i) * 16 * kLineBytes + hi);
+        ll[i] = *reinterpret_cast<const half8_t*>(l + (i0 + i) * 16 * kLineBytes + lo);
       }
+      __builtin_amdgcn_sched_barrier(0);  // all reads ahead of the products
+      const auto multiply = [&](const half8_t(&x)[kRows], const half8_t(&y)[TJ]) {
 #pragma unroll
-      for (int j = 0; j < TJ; ++j) {
-        rh[j] = *reinterpret_cast<const half8_t*>(r + j * 32 * kLineBytes + hi);
-        rl[j] = *reinterpret_cast<const half8_t*>(r + j * 32 * kLineBytes + lo);
-      }
+        for (int i = 0; i < kRows; ++i)
 #pragma unroll
-      for (int i = 0; i < TI; ++i)
-#pragma unroll
-        for (int j = 0; j < TJ; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh[i], rl[j], acc[i][j], 0, 0, 0);
-#pragma unroll
-      for (int i = 0; i < TI; ++i)
-#pragma unroll
-        for (int j = 0; j < TJ; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ll[i], rh[j], acc[i][j], 0, 0, 0);
-#pragma unroll
-      for (int i = 0; i < TI; ++i)
-#pragma unroll
-        for (int j = 0; j < TJ; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh[i], rh[j], acc[i][j], 0, 0, 0);
+          for (int j = 0; j < TJ; ++j)
+            acc[i0 + i][j] =
+                __builtin_amdgcn_mfma_f32_16x16x32_f16(x[i], y[j], acc[i0 + i][j], 0, 0, 0);
+      };
+      multiply(lh, rl);
+      multiply(lh, rh);
+      multiply(ll, rh);
     }
   }
   if (at.parts > 1 && !join_parts<SIDE>(a, at, acc)) return;
-  // Lane l holds column l % 32 of a 32 x 32 tile, element k in row 8 (k / 4) +
-  // 4 (l / 32) + k % 4; all in units of kPairScale^-2.
-  constexpr int kThread = kWaves * kWave, kSlab = kSlabRows<SIDE>, kPitch = kSlabPitch<SIDE>;
+  // Lane l holds column l % 16 of a 16 x 16 tile, element k in row 4 (l / 16) + k.
+  constexpr int kThread = kWaves * kWave, kPitch = kSlabPitch<SIDE>;
   float* slab = reinterpret_cast<float*>(lds);
   const int32_t r0 = ti * SIDE, c0 = tj * SIDE;
-  const auto to_slab = [&](int first) {
-    __syncthreads();  // the stages are read, or the slab before
+  const auto to_slab = [&] {
+    __syncthreads();  // the stages are read
 #pragma unroll
-    for (int i = 0; i < TI; ++i) {
-      const int32_t down = (wi * TI + i) * 32 - first;
-      if (down >= 0 && down < kSlab)
+    for (int i = 0; i < TI; ++i)
 #pragma unroll
-        for (int j = 0; j < TJ; ++j)
+      for (int j = 0; j < TJ; ++j)
 #pragma unroll
-          for (int k = 0; k < 16; ++k)
-            slab[(down + 8 * (k / 4) + 4 * half + k % 4) * kPitch + (wj * TJ + j) * 32 + row] =
-                acc[i][j][k];
-    }
+        for (int k = 0; k < 4; ++k)
+          slab[((wi * TI + i) * 16 + 4 * quarter + k) * kPitch + (wj * TJ + j) * 16 + row] =
+              acc[i][j][k];
+    __syncthreads();
   };
   if constexpr (WHAT == kMuonLast) {
     // A thread has all its loads in flight together, and whole lines are read and
     // written.
-    constexpr int kAcross = SIDE / 4, kDown = kThread / kAcross, kPasses = kSlab / kDown;
+    if (skipped(a)) return;
+    constexpr int kAcross = SIDE / 4, kDown = kThread / kAcross, kPasses = SIDE / kDown;
     const int32_t q = at.matrix - a.first;
     const float step = a.lr * t.lr_scale;
     const float keep = 1.f - step * t.weight_decay;
@@ -493,33 +470,29 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,
     uint16_t* copy = p.copy[q];
     const int32_t down = (int)threadIdx.x / kAcross, across = (int)threadIdx.x % kAcross * 4;
     const int32_t left = t.cols - c0 - across;
+    const int32_t r = r0 + down;
+    const int64_t e0 = (int64_t)r * t.cols + c0 + across;
     const auto passes = [&](auto whole) {
       constexpr bool FULL = decltype(whole)::value;
+      float x[kPasses][4];
 #pragma unroll
-      for (int first = 0; first < SIDE; first += kSlab) {
-        const int32_t r = r0 + first + down;
-        const int64_t e0 = (int64_t)r * t.cols + c0 + across;
-        float x[kPasses][4];
+      for (int q = 0; q < kPasses; ++q)
+        if (a.update && r + q * kDown < t.rows)
+          load_four<FULL>(param, t.param_bf16, e0 + (int64_t)q * kDown * t.cols, left, x[q]);
+      to_slab();
 #pragma unroll
-        for (int q = 0; q < kPasses; ++q)
-          if (a.update && r + q * kDown < t.rows)
-            load_four<FULL>(param, t.param_bf16, e0 + (int64_t)q * kDown * t.cols, left, x[q]);
-        to_slab(first);
-        __syncthreads();
+      for (int q = 0; q < kPasses; ++q) {
+        if (r + q * kDown >= t.rows) continue;
+        const float* of = slab + (q * kDown + down) * kPitch + across;
+        float v[4];
 #pragma unroll
-        for (int q = 0; q < kPasses; ++q) {
-          if (r + q * kDown >= t.rows) continue;
-          const float* of = slab + (q * kDown + down) * kPitch + across;
-          float v[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            v[k] = of[k] * s.scale;
-            if (a.update) v[k] = fmaf(-step, v[k], x[q][k] * keep);
-          }
-          const int64_t e = e0 + (int64_t)q * kDown * t.cols;
-          store_four<FULL>(param, t.param_bf16, e, left, v);
-          if (copy) store_four<FULL>(copy, 1, e, left, v);
+        for (int k = 0; k < 4; ++k) {
+          v[k] = of[k] * s.scale;
+          if (a.update) v[k] = fmaf(-step, v[k], x[q][k] * keep);
         }
+        const int64_t e = e0 + (int64_t)q * kDown * t.cols;
+        store_four<FULL>(param, t.param_bf16, e, left, v);
+        if (copy) store_four<FULL>(copy, 1, e, left, v);
       }
     };
     if (c0 + SIDE <= t.cols)
@@ -532,50 +505,43 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,
     const int64_t to_pitch = (int64_t)(WHAT == kMuonApply ? t.np : t.mp) * 4;
     const int64_t turned_pitch = (int64_t)t.mp * 4;
     const bool mirror = WHAT == kMuonApply || ti != tj;
-#pragma unroll
-    for (int first = 0; first < SIDE; first += kSlab) {
-      to_slab(first);
-      __syncthreads();
-      // Rows as they are, 16 numbers a thread and pass; the pairs take the numbers'
-      // places.
-      constexpr int kRuns = SIDE / 16;
+    to_slab();
+    // Rows as they are, 16 numbers a thread and pass; the pairs take the numbers'
+    // places.
+    constexpr int kRuns = SIDE / 16;
 #pragma unroll 2
-      for (int u = threadIdx.x; u < kSlab * kRuns; u += kThread) {
-        const int r = u / kRuns, c = u % kRuns * 16;
-        float* of = slab + r * kPitch + c;
-        char* line = to + (r0 + first + r) * to_pitch;
-        uint32_t v[16];
+    for (int u = threadIdx.x; u < SIDE * kRuns; u += kThread) {
+      const int r = u / kRuns, c = u % kRuns * 16;
+      float* of = slab + r * kPitch + c;
+      uint32_t v[16];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(of[k] * s.scale);
-        if constexpr (WHAT == kMuonStep) {
-          float gram[16];
-          load_16(a.workspace + t.at[s.left] + (r0 + first + r) * to_pitch, c0 + c, gram);
+      for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(of[k] * s.scale);
+      if constexpr (WHAT == kMuonStep) {
+        float square[16];
+        load_16(a.workspace + t.at[s.left] + (r0 + r) * to_pitch, c0 + c, square);
 #pragma unroll
-          for (int k = 0; k < 16; ++k) {
-            const float x = fmaf(s.c, __uint_as_float(v[k]), s.b * gram[k]);
-            v[k] = __float_as_uint(
-                r0 + first + r == c0 + c + k ? x + s.a * kPairScale : x);
-          }
+        for (int k = 0; k < 16; ++k) {
+          const float x = fmaf(s.c, __uint_as_float(v[k]), s.b * square[k]);
+          v[k] = __float_as_uint(r0 + r == c0 + c + k ? x + s.a * kPairScale : x);
         }
-#pragma unroll
-        for (int k = 0; k < 16; ++k) v[k] = pair_of(__uint_as_float(v[k]));
-        store_16(line, c0 + c, v);
-        if (mirror)
-#pragma unroll
-          for (int k = 0; k < 16; ++k) of[k] = __uint_as_float(v[k]);
       }
-      if (!mirror) continue;
-      __syncthreads();
-      // And transposed, two threads to a line.
-      constexpr int kLines = kSlab / 32;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) v[k] = pair_of(__uint_as_float(v[k]));
+      store_16(to + (r0 + r) * to_pitch, c0 + c, v);
+      if (mirror)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) of[k] = __uint_as_float(v[k]);
+    }
+    if (!mirror) return;
+    __syncthreads();
+    // And transposed, two threads to a line.
 #pragma unroll 2
-      for (int u = threadIdx.x; u < 2 * kLines * SIDE; u += kThread) {
-        const int c = u / 2 % SIDE, r = u / (2 * SIDE) * 32 + u % 2 * 16;
-        uint32_t v[16];
+    for (int u = threadIdx.x; u < SIDE * kRuns; u += kThread) {
+      const int c = u / 2 % SIDE, r = u / (2 * SIDE) * 32 + u % 2 * 16;
+      uint32_t v[16];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(slab[(r + k) * kPitch + c]);
-        store_16(turned + (c0 + c) * turned_pitch, r0 + first + r, v);
-      }
+      for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(slab[(r + k) * kPitch + c]);
+      store_16(turned + (c0 + c) * turned_pitch, r0 + r, v);
     }
   }
 }
@@ -627,11 +593,6 @@ hipError_t launch_muon_momentum(const MuonArgs& a, const MuonPointers& p, const 
                                 int64_t first_run, int64_t runs, hipStream_t stream) {
   hipLaunchKernelGGL(muon_momentum_kernel, dim3((unsigned)runs), dim3(kThreads), 0, stream, a, p,
                      run_matrix, first_run);
-  return hipGetLastError();
-}
-
-hipError_t launch_muon_norms(const MuonArgs& a, int32_t count, hipStream_t stream) {
-  hipLaunchKernelGGL(muon_norm_kernel, dim3((unsigned)count), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 
