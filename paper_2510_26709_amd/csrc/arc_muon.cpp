@@ -378,8 +378,8 @@ Times plan_muon(const arc_muon_config* cfg, const Rates& rates, arc_muon* c) {
     t.lr_scale = in.lr_scale;
     t.state = c->state_elems;
     c->state_elems += up_to(count, ARC_STATE_BLOCK);
-    const int64_t long_bytes = int64_t{4} * t.mp * t.np, short_bytes = int64_t{4} * t.mp * t.mp;
-    const int64_t need = count > 0 ? 3 * long_bytes + 5 * short_bytes : 0;
+    const int64_t need =
+        count > 0 ? arc::array_at(0, t.mp, t.np, arc::kMuonArrays) : 0;
     if (g.count == arc::kMuonBatch || (g.count > 0 && bytes + need > kGroupBytes)) {
       finish();
       g = arc::MuonGroup{};
@@ -392,17 +392,14 @@ Times plan_muon(const arc_muon_config* cfg, const Rates& rates, arc_muon* c) {
     t.runs = static_cast<int32_t>((count + arc::kMuonRun - 1) / arc::kMuonRun);
     runs += t.runs;
     c->run_matrix.insert(c->run_matrix.end(), static_cast<size_t>(t.runs), i);
-    for (int32_t k = 0, at = 0; k < 8; ++k) {
-      t.at[k] = bytes + at * short_bytes + std::min(k, 3) * long_bytes;
-      at += k >= 3;
-    }
+    t.base = bytes;
     bytes += need;
     if (count > 0 && !t.param_bf16) c->any_f32 = true;
     c->matrices.push_back(t);
     if (count == 0) continue;
     const auto to = [&](std::vector<arc::MuonTile>* list, int32_t sum) {
       return [=](int32_t a, int32_t b) {
-        list->push_back({i, a, b, 0, sum / arc::kPairLine, 0, 1, 0});
+        list->push_back({i, a, b, 0, sum / arc::kPairLine, 0, 1, 0, t.base, t.mp, t.np});
       };
     };
     each_tile(t.mp / arc::kSplitTile, t.np / arc::kSplitTile, false, to(&split, 0));

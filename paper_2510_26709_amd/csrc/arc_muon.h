@@ -28,7 +28,7 @@ enum MuonArray {
 // A matrix, seen from its shorter side: X is m x n, m <= n, or its transpose.
 struct MuonMatrix {
   int64_t state;                        // first element of its momentum
-  int64_t at[8];                        // where its pairs lie in the workspace, bytes
+  int64_t base;                         // of its pairs in the workspace, bytes
   int64_t first_run;                    // its runs' sums
   int32_t rows, cols;                   // as the caller has it
   int32_t m, n, mp, np;                 // sides, and those of the workspace
@@ -46,7 +46,17 @@ struct MuonTile {
   int32_t i, j;
   int32_t first, lines;
   int32_t part, parts, place;
+  int64_t base;    // its matrix's, here too: one load less ahead of the first product
+  int32_t mp, np;
 };
+
+// Where an array of a matrix lies.
+__host__ __device__ inline int64_t array_at(int64_t base, int32_t mp, int32_t np, int32_t array) {
+  const int64_t row = int64_t{4} * mp;  // X and its two transposes, then squares
+  return array < kMuonSquare ? base + array * row * np
+                             : base + kMuonSquare * row * np + (array - kMuonSquare) * row * mp;
+}
+constexpr int32_t kMuonArrays = kMuonAll2 + 1;
 
 struct MuonPointers {
   const void* grad[kMuonBatch];

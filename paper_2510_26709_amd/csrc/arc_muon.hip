@@ -240,8 +240,8 @@ muon_split_kernel(MuonArgs a, MuonPointers p, const MuonTile* __restrict__ tiles
     along[k] = tile[line][part + k];
     across[k] = tile[part + k][line];
   }
-  char* x = a.workspace + t.at[kMuonX] + (int64_t)(at.i * S + line) * t.np * 4;
-  char* xt = a.workspace + t.at[kMuonXt] + (int64_t)(at.j * S + line) * t.mp * 4;
+  char* x = a.workspace + array_at(at.base, at.mp, at.np, kMuonX) + (int64_t)(at.i * S + line) * at.np * 4;
+  char* xt = a.workspace + array_at(at.base, at.mp, at.np, kMuonXt) + (int64_t)(at.j * S + line) * at.mp * 4;
   if (t.tall) {
     store_16(x, at.j * S + part, across);
     store_16(xt, at.i * S + part, along);
@@ -362,15 +362,18 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,
   constexpr int kLoads = kStage / 1024 / kWaves;  // of a wave and stage
   extern __shared__ __attribute__((aligned(256))) char lds[];
   const MuonTile at = tiles[blockIdx.x];
-  const MuonMatrix& t = a.matrices[at.matrix];
+  const MuonMatrix& t = a.matrices[at.matrix];  // (read by kMuonLast alone)
+  const auto array = [&](int32_t which) {
+    return a.workspace + array_at(at.base, at.mp, at.np, which);
+  };
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int wi = wave / Sh::kWavesJ, wj = wave % Sh::kWavesJ;
   const bool swap = WHAT == kMuonLast && t.tall;  // lanes go along the parameter's rows
   const int32_t ti = swap ? at.j : at.i, tj = swap ? at.i : at.j;
-  const char* left = a.workspace + t.at[swap ? s.right : s.left];
-  const char* right = a.workspace + t.at[swap ? s.left : s.right];
-  const int32_t sum = WHAT == kMuonGram ? t.np : t.mp;
+  const char* left = array(swap ? s.right : s.left);
+  const char* right = array(swap ? s.left : s.right);
+  const int32_t sum = WHAT == kMuonGram ? at.np : at.mp;
   const uint32_t pitch = (uint32_t)sum * 4u;
   left += (int64_t)ti * SIDE * pitch;
   right += (int64_t)tj * SIDE * pitch;
@@ -500,10 +503,10 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,
     else
       passes(std::false_type());
   } else {
-    char* to = a.workspace + t.at[s.out];
-    char* turned = a.workspace + t.at[s.turned];
-    const int64_t to_pitch = (int64_t)(WHAT == kMuonApply ? t.np : t.mp) * 4;
-    const int64_t turned_pitch = (int64_t)t.mp * 4;
+    char* to = array(s.out);
+    char* turned = array(s.turned);
+    const int64_t to_pitch = (int64_t)(WHAT == kMuonApply ? at.np : at.mp) * 4;
+    const int64_t turned_pitch = (int64_t)at.mp * 4;
     const bool mirror = WHAT == kMuonApply || ti != tj;
     to_slab();
     // Rows as they are, 16 numbers a thread and pass; the pairs take the numbers'
@@ -518,7 +521,7 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,
       for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(of[k] * s.scale);
       if constexpr (WHAT == kMuonStep) {
         float square[16];
-        load_16(a.workspace + t.at[s.left] + (r0 + r) * to_pitch, c0 + c, square);
+        load_16(array(s.left) + (r0 + r) * to_pitch, c0 + c, square);
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
           const float x = fmaf(s.c, __uint_as_float(v[k]), s.b * square[k]);
