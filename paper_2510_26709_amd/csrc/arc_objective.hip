@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "arc_device.h"
 #include "arc_objective.h"
@@ -14,88 +15,88 @@ namespace {
 
 constexpr int kThreads = 256;
 
-__device__ __forceinline__ double wave_sum_f64(double v) {
-#pragma unroll
-  for (int off = kWave / 2; off > 0; off >>= 1) v += __shfl_xor(v, off);
-  return v;
-}
+typedef float loose_f4_t __attribute__((ext_vector_type(4), aligned(4)));
+typedef int64_t loose_i2_t __attribute__((ext_vector_type(2), aligned(8)));
 
-// Sums of K values over a workgroup, on every thread, in a fixed order.
-template <int K>
-__device__ __forceinline__ void group_sums(double (&v)[K]) {
-  __shared__ double part[K][kThreads / kWave];
+// Four numbers from i on, of which `left` are there (FULL: all); `none` for an array
+// that is not there.
+template <bool FULL>
+__device__ __forceinline__ void load_four(const float* p, int64_t i, int64_t left, float none,
+                                          float (&x)[4]) {
 #pragma unroll
-  for (int k = 0; k < K; ++k) v[k] = wave_sum_f64(v[k]);
-  __syncthreads();  // of an earlier sum
-  if (threadIdx.x % kWave == 0)
+  for (int k = 0; k < 4; ++k) x[k] = none;
+  if (!p) return;
+  if (FULL) {
+    const loose_f4_t v = __builtin_nontemporal_load(reinterpret_cast<const loose_f4_t*>(p + i));
 #pragma unroll
-    for (int k = 0; k < K; ++k) part[k][threadIdx.x / kWave] = v[k];
-  __syncthreads();
+    for (int k = 0; k < 4; ++k) x[k] = v[k];
+  } else {
 #pragma unroll
-  for (int k = 0; k < K; ++k) v[k] = (part[k][0] + part[k][1]) + (part[k][2] + part[k][3]);
-}
-
-// Every workgroup's sums to `totals`: alone at once, otherwise by the last one to
-// arrive, in the order of the workgroups.  Parts are written through to where
-// every compute unit sees them, and read from there.
-template <int K>
-__device__ __forceinline__ void add_groups(double (&v)[K], ObjectiveScratch* scratch,
-                                           float* totals) {
-  __shared__ bool last;
-  group_sums<K>(v);
-  const uint32_t groups = gridDim.x;
-  if (groups > 1) {
-    if (threadIdx.x == 0) {
-#pragma unroll
-      for (int k = 0; k < K; ++k)
-        __hip_atomic_store(&scratch->totals[blockIdx.x][k], v[k], __ATOMIC_RELAXED,
-                           __HIP_MEMORY_SCOPE_AGENT);
-      wave_vmem_fence();  // written before it counts
-      last = __hip_atomic_fetch_add(&scratch->arrived, 1u, __ATOMIC_RELAXED,
-                                    __HIP_MEMORY_SCOPE_AGENT) == groups - 1;
-      if (last)
-        __hip_atomic_store(&scratch->arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-    __syncthreads();
-    if (!last) return;
-#pragma unroll
-    for (int k = 0; k < K; ++k) v[k] = 0.0;
-    for (uint32_t g = threadIdx.x; g < groups; g += kThreads)
-#pragma unroll
-      for (int k = 0; k < K; ++k)
-        v[k] += __hip_atomic_load(&scratch->totals[g][k], __ATOMIC_RELAXED,
-                                  __HIP_MEMORY_SCOPE_AGENT);
-    group_sums<K>(v);
+    for (int k = 0; k < 4; ++k)
+      if (k < left) x[k] = p[i + k];
   }
-  if (threadIdx.x == 0)
-#pragma unroll
-    for (int k = 0; k < K; ++k) totals[k] = (float)v[k];
 }
 
-// One token a thread and pass: every array is read and written in whole lines.
+template <bool FULL>
+__device__ __forceinline__ void store_four(float* p, int64_t i, int64_t left,
+                                           const float (&x)[4]) {
+  if (!p) return;
+  if (FULL) {
+    const loose_f4_t v = {x[0], x[1], x[2], x[3]};
+    __builtin_nontemporal_store(v, reinterpret_cast<loose_f4_t*>(p + i));
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k < left) p[i + k] = x[k];
+  }
+}
+
+// Four tokens a thread and pass, every array in 16 bytes a lane.
 __global__ void __launch_bounds__(kThreads)
 policy_kernel(PolicyArgs p, PolicyRows r, PolicyOutputs out, ObjectiveScratch* scratch) {
   double sums[kPolicyTotals] = {};
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < r.rows;
-       i += (int64_t)gridDim.x * kThreads) {
-    const bool given = r.targets[i] >= 0;
-    const float H = r.entropy ? r.entropy[i] : 0.f;
-    const PolicyTerm t = policy_term(p, i, given, r.logp[i], H);
-    if (out.loss) out.loss[i] = t.loss;
-    if (out.ratio) out.ratio[i] = t.ratio;
-    if (out.kl) out.kl[i] = t.kl;
-    if (out.d_logp) out.d_logp[i] = t.d_logp;
-    if (out.d_entropy) out.d_entropy[i] = t.d_entropy;
-    if (t.weight != 0.f) {
-      const double w = t.weight;
-      sums[0] += w * t.loss;
-      sums[1] += w * t.ratio;
-      sums[2] += w * t.kl;
-      sums[3] += w * H;
-      sums[4] += t.clipped ? w : 0.0;
+  const auto four = [&](int64_t i, auto whole) {
+    constexpr bool FULL = decltype(whole)::value;
+    const int64_t left = r.rows - i;
+    float lp[4], H[4], old[4], ref[4], A[4], w[4];
+    bool given[4];
+    if constexpr (FULL) {
+      const auto* y = reinterpret_cast<const loose_i2_t*>(r.targets + i);
+      const loose_i2_t y0 = __builtin_nontemporal_load(y), y1 = __builtin_nontemporal_load(y + 1);
+      given[0] = y0[0] >= 0, given[1] = y0[1] >= 0, given[2] = y1[0] >= 0, given[3] = y1[1] >= 0;
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) given[k] = k < left && r.targets[i + k] >= 0;
     }
+    load_four<FULL>(r.logp, i, left, 0.f, lp);
+    load_four<FULL>(r.entropy, i, left, 0.f, H);
+    load_four<FULL>(p.old_logp, i, left, 0.f, old);
+    load_four<FULL>(p.ref_logp, i, left, 0.f, ref);
+    load_four<FULL>(p.advantages, i, left, 0.f, A);
+    load_four<FULL>(p.weights, i, left, 1.f, w);
+    float loss[4], ratio[4], kl[4], d_logp[4], d_entropy[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const PolicyTerm t = policy_term(p, {old[k], ref[k], A[k], w[k]}, given[k], lp[k], H[k]);
+      add_term(t, H[k], sums);
+      loss[k] = t.loss, ratio[k] = t.ratio, kl[k] = t.kl;
+      d_logp[k] = t.d_logp, d_entropy[k] = t.d_entropy;
+    }
+    store_four<FULL>(out.loss, i, left, loss);
+    store_four<FULL>(out.ratio, i, left, ratio);
+    store_four<FULL>(out.kl, i, left, kl);
+    store_four<FULL>(out.d_logp, i, left, d_logp);
+    store_four<FULL>(out.d_entropy, i, left, d_entropy);
+  };
+  for (int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 4; i < r.rows;
+       i += (int64_t)gridDim.x * kThreads * 4) {
+    if (i + 4 <= r.rows)
+      four(i, std::true_type());
+    else
+      four(i, std::false_type());
   }
-  add_groups<kPolicyTotals>(sums, scratch, out.totals);
+  group_sums<kThreads, kPolicyTotals>(sums);
+  add_groups<kThreads, kPolicyTotals>(sums, blockIdx.x, gridDim.x, scratch, out.totals);
 }
 
 // ---------------------------------------------------------------- preference
@@ -109,26 +110,36 @@ __device__ __forceinline__ Sequence sequence(const PreferenceArgs& a, int64_t s)
   return {first, min(max(a.offsets[s + 1], first), a.rows)};
 }
 
-// The sum of logp - ref of the given tokens among [first, last), and their count.
-__device__ __forceinline__ void sum_tokens(const PreferenceArgs& a, int64_t first, int64_t last,
-                                           double (&v)[2]) {
-  constexpr int U = 4;  // passes whose loads are in flight together
-  for (int64_t i = first + threadIdx.x; i < last; i += U * kThreads) {
-    int64_t y[U];
-    float lp[U], ref[U];
+// The sums of logp - ref of the given tokens of N runs, and their counts: v[2 n],
+// v[2 n + 1].  The loads of all runs' first passes are in flight together.
+template <int N>
+__device__ __forceinline__ void sum_tokens(const PreferenceArgs& a, const Sequence (&run)[N],
+                                           double (&v)[2 * N]) {
+  constexpr int U = 4;
+  int64_t longest = 0;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t at = i + u * kThreads;
-      y[u] = at < last ? a.targets[at] : -1;
-      lp[u] = at < last ? a.logp[at] : 0.f;
-      ref[u] = a.ref_logp && at < last ? a.ref_logp[at] : 0.f;
-    }
+  for (int n = 0; n < N; ++n) longest = max(longest, run[n].last - run[n].first);
+  for (int64_t i = threadIdx.x; i < longest; i += U * kThreads) {
+    int64_t y[N][U];
+    float lp[N][U], ref[N][U];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (y[u] >= 0) {
-        v[0] += (double)lp[u] - (double)ref[u];
-        v[1] += 1.0;
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t at = run[n].first + i + u * kThreads;
+        const bool there = at < run[n].last;
+        y[n][u] = there ? a.targets[at] : -1;
+        lp[n][u] = there ? a.logp[at] : 0.f;
+        ref[n][u] = there && a.ref_logp ? a.ref_logp[at] : 0.f;
       }
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (y[n][u] >= 0) {
+          v[2 * n] += (double)lp[n][u] - (double)ref[n][u];
+          v[2 * n + 1] += 1.0;
+        }
   }
 }
 
@@ -209,23 +220,19 @@ preference_kernel(PreferenceArgs a, PreferenceOutputs out, ObjectiveScratch* scr
   double totals[kPreferenceTotals] = {};
   for (int64_t pair = blockIdx.x; pair < a.pairs; pair += gridDim.x) {
     const Sequence seq[2] = {sequence(a, pair), sequence(a, a.pairs + pair)};
-    double v[2][2] = {};
-    sum_tokens(a, seq[0].first, seq[0].last, v[0]);
-    sum_tokens(a, seq[1].first, seq[1].last, v[1]);
-    double all[4] = {v[0][0], v[0][1], v[1][0], v[1][1]};
-    group_sums<4>(all);
-    const PairTerm t = pair_term(a, pair, {all[0], all[2]}, {all[1], all[3]});
-    if (threadIdx.x == 0) {
-      write_pair(a, out, pair, t);
-      add_pair(t, totals);
-    }
+    double v[4] = {};
+    sum_tokens(a, seq, v);
+    group_sums<kThreads, 4>(v);
+    const PairTerm t = pair_term(a, pair, {v[0], v[2]}, {v[1], v[3]});
+    if (threadIdx.x == 0) write_pair(a, out, pair, t);
+    add_pair(t, totals);
     if (out.d_logp) {
       write_tokens(a, out.d_logp, seq[0].first, seq[0].last, (float)t.d[0]);
       write_tokens(a, out.d_logp, seq[1].first, seq[1].last, (float)t.d[1]);
     }
   }
   if (out.d_logp) clear_outside(a, out.d_logp);
-  add_groups<kPreferenceTotals>(totals, scratch, out.totals);
+  add_groups<kThreads, kPreferenceTotals>(totals, blockIdx.x, gridDim.x, scratch, out.totals);
 }
 
 // Few pairs of long sequences: `parts` workgroups for each sequence, one launch
@@ -238,10 +245,10 @@ __device__ __forceinline__ Sequence part_of(const Sequence& s, int32_t part, int
 
 __global__ void __launch_bounds__(kThreads)
 sequence_sum_kernel(PreferenceArgs a, int32_t parts, ObjectiveScratch* scratch) {
-  const Sequence s = part_of(sequence(a, blockIdx.x / parts), blockIdx.x % parts, parts);
+  const Sequence run[1] = {part_of(sequence(a, blockIdx.x / parts), blockIdx.x % parts, parts)};
   double v[2] = {};
-  sum_tokens(a, s.first, s.last, v);
-  group_sums<2>(v);
+  sum_tokens(a, run, v);
+  group_sums<kThreads, 2>(v);
   if (threadIdx.x == 0) {
     scratch->sum[blockIdx.x] = v[0];
     scratch->count[blockIdx.x] = (int64_t)v[1];
@@ -262,19 +269,19 @@ pair_grad_kernel(PreferenceArgs a, int32_t parts, PreferenceOutputs out,
       v[2 * k] += scratch->sum[at];
       v[2 * k + 1] += (double)scratch->count[at];
     }
-  group_sums<4>(v);
+  group_sums<kThreads, 4>(v);
   const PairTerm t = pair_term(a, pair, {v[0], v[2]}, {v[1], v[3]});
-  double totals[kPreferenceTotals] = {};
-  if (part == 0 && number < a.pairs && threadIdx.x == 0) {
-    write_pair(a, out, pair, t);
-    add_pair(t, totals);
-  }
   if (out.d_logp) {
     const Sequence s = part_of(sequence(a, number), part, parts);
     write_tokens(a, out.d_logp, s.first, s.last, (float)(number < a.pairs ? t.d[0] : t.d[1]));
     clear_outside(a, out.d_logp);
   }
-  add_groups<kPreferenceTotals>(totals, scratch, out.totals);
+  if (part != 0 || number >= a.pairs) return;
+  if (threadIdx.x == 0) write_pair(a, out, pair, t);
+  double totals[kPreferenceTotals] = {};
+  add_pair(t, totals);
+  add_groups<kThreads, kPreferenceTotals>(totals, (uint32_t)pair, (uint32_t)a.pairs, scratch,
+                                          out.totals);
 }
 
 }  // namespace
@@ -282,7 +289,7 @@ pair_grad_kernel(PreferenceArgs a, int32_t parts, PreferenceOutputs out,
 hipError_t launch_policy_terms(const PolicyArgs& p, const PolicyRows& r, const PolicyOutputs& out,
                                ObjectiveScratch* scratch, hipStream_t stream) {
   const int64_t groups = std::max<int64_t>(
-      1, std::min<int64_t>(kTotalsGroups, (r.rows + kThreads - 1) / kThreads));
+      1, std::min<int64_t>(kTotalsGroups, (r.rows + 4 * kThreads - 1) / (4 * kThreads)));
   hipLaunchKernelGGL(policy_kernel, dim3((unsigned)groups), dim3(kThreads), 0, stream, p, r, out,
                      scratch);
   return hipGetLastError();

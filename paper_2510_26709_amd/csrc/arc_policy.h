@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "arc_device.h"
 #include "arc_objective.h"
 
 namespace arc {
@@ -32,16 +33,26 @@ __device__ __forceinline__ float exp_beyond_line(float x, float exp_minus_1) {
   return s * x * x;
 }
 
-// Token i's terms; `given`: it has a token of its own.  What a token without one
+// What a token's terms are made of.
+struct PolicyToken {
+  float old_logp, ref_logp, advantage, weight;
+};
+
+__device__ __forceinline__ PolicyToken policy_token(const PolicyArgs& p, int64_t i) {
+  return {p.old_logp ? p.old_logp[i] : 0.f, p.ref_logp ? p.ref_logp[i] : 0.f, p.advantages[i],
+          p.weights ? p.weights[i] : 1.f};
+}
+
+// A token's terms; `given`: it has a token of its own.  What a token without one
 // holds, and what one of weight 0 does to sums and gradients, is left out by
 // selection, not by a product, so that no infinity or NaN there gets through.
-__device__ __forceinline__ PolicyTerm policy_term(const PolicyArgs& p, int64_t i, bool given,
-                                                  float logp, float H) {
+__device__ __forceinline__ PolicyTerm policy_term(const PolicyArgs& p, const PolicyToken& of,
+                                                  bool given, float logp, float H) {
   PolicyTerm t{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, false};
   if (!given) return t;
-  const float A = p.advantages[i];
-  t.weight = p.weights ? p.weights[i] * p.scale : p.scale;
-  t.ratio = p.old_logp ? expf(logp - p.old_logp[i]) : logp != logp ? logp : 1.f;
+  const float A = of.advantage;
+  t.weight = of.weight * p.scale;
+  t.ratio = p.old_logp ? expf(logp - of.old_logp) : logp != logp ? logp : 1.f;
   const float held = fminf(fmaxf(t.ratio, p.low), p.high) * A;
   float gain = t.ratio * A;
   t.clipped = gain > held;  // (a ratio that is NaN is not, and stays one)
@@ -53,7 +64,7 @@ __device__ __forceinline__ PolicyTerm policy_term(const PolicyArgs& p, int64_t i
   float d = t.clipped ? 0.f : -t.ratio * A;
   t.loss = -gain;
   if (p.ref_logp) {
-    const float away = p.ref_logp[i] - logp;
+    const float away = of.ref_logp - logp;
     const float grown = expm1f(away);
     t.kl = exp_beyond_line(away, grown);
     if (p.kl != 0.f) {
@@ -67,6 +78,76 @@ __device__ __forceinline__ PolicyTerm policy_term(const PolicyArgs& p, int64_t i
     t.d_entropy = -p.entropy * t.weight;
   }
   return t;
+}
+
+// A token's part of the totals.
+__device__ __forceinline__ void add_term(const PolicyTerm& t, float H,
+                                         double (&sums)[kPolicyTotals]) {
+  if (t.weight == 0.f) return;
+  const double w = t.weight;
+  sums[0] += w * t.loss;
+  sums[1] += w * t.ratio;
+  sums[2] += w * t.kl;
+  sums[3] += w * H;
+  sums[4] += t.clipped ? w : 0.0;
+}
+
+// Sums of K values over a workgroup of W threads, on every thread, in a fixed order.
+template <int W, int K>
+__device__ __forceinline__ void group_sums(double (&v)[K]) {
+  __shared__ double part[K][W / kWave];
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+#pragma unroll
+    for (int off = kWave / 2; off > 0; off >>= 1) v[k] += __shfl_xor(v[k], off);
+  __syncthreads();  // of an earlier sum
+  if (threadIdx.x % kWave == 0)
+#pragma unroll
+    for (int k = 0; k < K; ++k) part[k][threadIdx.x / kWave] = v[k];
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    v[k] = part[k][0];
+#pragma unroll
+    for (int w = 1; w < W / kWave; ++w) v[k] += part[k][w];
+  }
+}
+
+// The values of workgroup `group` of `groups`, the same on all its threads, to
+// `totals`: alone at once, otherwise by the last one to arrive, in the order of the
+// groups.  They are written through to where every compute unit sees them, and
+// read from there.
+template <int W, int K>
+__device__ __forceinline__ void add_groups(double (&v)[K], uint32_t group, uint32_t groups,
+                                           ObjectiveScratch* scratch, float* totals) {
+  __shared__ bool last;
+  if (groups > 1) {
+    if (threadIdx.x == 0) {
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+        __hip_atomic_store(&scratch->totals[group][k], v[k], __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
+      wave_vmem_fence();  // written before it counts
+      last = __hip_atomic_fetch_add(&scratch->arrived, 1u, __ATOMIC_RELAXED,
+                                    __HIP_MEMORY_SCOPE_AGENT) == groups - 1;
+      if (last)
+        __hip_atomic_store(&scratch->arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (!last) return;
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] = 0.0;
+#pragma unroll 4
+    for (uint32_t g = threadIdx.x; g < groups; g += W)
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+        v[k] += __hip_atomic_load(&scratch->totals[g][k], __ATOMIC_RELAXED,
+                                  __HIP_MEMORY_SCOPE_AGENT);
+    group_sums<W, K>(v);
+  }
+  if (threadIdx.x == 0)
+#pragma unroll
+    for (int k = 0; k < K; ++k) totals[k] = (float)v[k];
 }
 
 }  // namespace arc

@@ -896,7 +896,7 @@ token_loss_kernel(TokenArgs a, TokenScores out, TokenGrad g, PolicyArgs p) {
   GradRow r;
   if constexpr (POLICY) {
     const float logp = y >= a.vocab ? NAN : res.logp(given);
-    const PolicyTerm t = policy_term(p, i, y >= 0, logp, H);
+    const PolicyTerm t = policy_term(p, policy_token(p, i), y >= 0, logp, H);
     r = grad_row(a, y, t.d_logp, t.d_entropy, 0.f, H, res.empty);
   } else {
     r = grad_row(a, g, i, H, res.empty);
