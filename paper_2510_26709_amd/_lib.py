@@ -318,9 +318,7 @@ def _check(status: int, where: str) -> None:
 
 def _addr(x):
     """Device/host address of a tensor, numpy array or integer (None -> NULL)."""
-    if x is None:
-        return None
-    if isinstance(x, int):
+    if x is None or isinstance(x, int):
         return x
     if hasattr(x, "data_ptr"):
         return x.data_ptr()

@@ -164,11 +164,15 @@ class TokenLogProbs(_Bound):
             self._keep(logits, targets, d_logp, d_entropy, d_lse, out)
         return Loss(*row.split(T) if T else (row,) * 3, out)
 
+    def _at(self, name, x, count, dtype=torch.float32):
+        """The address of a checked tensor; None for None."""
+        return None if x is None else self._check(name, x, dtype, count).data_ptr()
+
     def _policy_inputs(self, T, targets, advantages, old_logp, ref_logp, weights):
-        each = self._each
-        return (each("targets", targets, T, torch.int64), each("old_logp", old_logp, T),
-                each("ref_logp", ref_logp, T), each("advantages", advantages, T),
-                each("weights", weights, T))
+        at = self._at
+        return (at("targets", targets, T, torch.int64), at("old_logp", old_logp, T),
+                at("ref_logp", ref_logp, T), at("advantages", advantages, T),
+                at("weights", weights, T))
 
     def policy_loss(self, logits, targets, advantages, *, old_logp=None, ref_logp=None,
                     weights=None, clip_low=0.2, clip_high=0.2, dual=0.0, kl_coef=0.0,
@@ -187,7 +191,8 @@ class TokenLogProbs(_Bound):
         at = [row.data_ptr() + 4 * k * T for k in range(7)]
         arc_tokens_policy(self.ctx, arc_policy_config(clip_low, clip_high, dual, kl_coef,
                                                       entropy_coef, scale),
-                          T, logits, stride, y, old, ref, A, w, *at, out, out_stride)
+                          T, logits.data_ptr(), stride, y, old, ref, A, w, *at, out.data_ptr(),
+                          out_stride)
         if self._elsewhere():
             self._keep(logits, targets, old_logp, ref_logp, advantages, weights, out)
         *rows, totals = row.split_with_sizes((T,) * 6 + (ARC_POLICY_TOTALS,))
@@ -201,15 +206,14 @@ class TokenLogProbs(_Bound):
         T = targets.numel()
         y, old, ref, A, w = self._policy_inputs(T, targets, advantages, old_logp, ref_logp,
                                                 weights)
-        self._each("logp", logp, T)
-        self._each("entropy", entropy, T)
+        scored, H = self._at("logp", logp, T), self._at("entropy", entropy, T)
         n = 5 if entropy_coef else 4
         row = self._empty(n * T + ARC_POLICY_TOTALS)
         at = [row.data_ptr() + 4 * k * T for k in range(n + 1)]
         loss, ratio, kl, d_logp, *d_entropy, totals = at
         arc_tokens_policy_terms(self.ctx, arc_policy_config(clip_low, clip_high, dual, kl_coef,
                                                             entropy_coef, scale),
-                                T, logp, entropy, y, old, ref, A, w, loss, ratio, kl, totals,
+                                T, scored, H, y, old, ref, A, w, loss, ratio, kl, totals,
                                 d_logp, d_entropy[0] if d_entropy else None)
         if self._elsewhere():
             self._keep(logp, entropy, targets, old_logp, ref_logp, advantages, weights)
@@ -220,11 +224,10 @@ class TokenLogProbs(_Bound):
         P = (offsets.numel() - 1) // 2
         if offsets.numel() != 2 * P + 1:
             raise ValueError(f"offsets: need 2 * pairs + 1 elements, got {offsets.numel()}")
-        self._each("targets", targets, T, torch.int64)
-        self._each("offsets", offsets, 2 * P + 1, torch.int64)
-        self._each("ref_logp", ref_logp, T)
-        self._each("weights", weights, P)
-        return P
+        at = self._at
+        return (P, at("targets", targets, T, torch.int64),
+                at("offsets", offsets, 2 * P + 1, torch.int64), at("ref_logp", ref_logp, T),
+                at("weights", weights, P))
 
     def preference_loss(self, logits, targets, offsets, *, ref_logp=None, weights=None,
                         kind="sigmoid", beta=0.1, margin=0.0, smoothing=0.0, average=False,
@@ -238,15 +241,15 @@ class TokenLogProbs(_Bound):
         ``scale`` is each pair's part.  ``out``: where to write the gradient (the
         logits themselves allowed)."""
         T, stride = self._rows(logits)
-        P = self._pairs(T, targets, offsets, ref_logp, weights)
+        P, y, o, ref, w = self._pairs(T, targets, offsets, ref_logp, weights)
         out, out_stride = self._out(out, T)
         row = self._empty(3 * T + 3 * P + ARC_PREFERENCE_TOTALS)
         at = row.data_ptr()
         arc_tokens_preference(
             self.ctx, arc_preference_config(PREFERENCES[kind], average, beta, margin, smoothing,
                                             scale),
-            T, logits, stride, targets, P, offsets, ref_logp, weights, at, at + 4 * T, at + 8 * T,
-            at + 12 * T, at + 4 * (3 * T + P), at + 12 * (T + P), out, out_stride)
+            T, logits.data_ptr(), stride, y, P, o, ref, w, at, at + 4 * T, at + 8 * T,
+            at + 12 * T, at + 4 * (3 * T + P), at + 12 * (T + P), out.data_ptr(), out_stride)
         if self._elsewhere():
             self._keep(logits, targets, offsets, ref_logp, weights, out)
         *rows, totals = row.split_with_sizes((T, T, T, P, 2 * P, ARC_PREFERENCE_TOTALS))
@@ -257,15 +260,14 @@ class TokenLogProbs(_Bound):
         """The same from scored rows: (totals [3], loss [P], rewards [2 P], d_logp
         [T]); d_logp is for ``grad``."""
         T = targets.numel()
-        P = self._pairs(T, targets, offsets, ref_logp, weights)
-        self._each("logp", logp, T)
+        P, y, o, ref, w = self._pairs(T, targets, offsets, ref_logp, weights)
+        scored = self._at("logp", logp, T)
         row = self._empty(T + 3 * P + ARC_PREFERENCE_TOTALS)
         at = row.data_ptr()
         arc_tokens_preference_terms(
             self.ctx, arc_preference_config(PREFERENCES[kind], average, beta, margin, smoothing,
                                             scale),
-            T, logp, targets, P, offsets, ref_logp, weights, at + 4 * T, at + 4 * (T + P),
-            at + 4 * (T + 3 * P), at)
+            T, scored, y, P, o, ref, w, at + 4 * T, at + 4 * (T + P), at + 4 * (T + 3 * P), at)
         if self._elsewhere():
             self._keep(logp, targets, offsets, ref_logp, weights)
         d_logp, loss, rewards, totals = row.split_with_sizes(
