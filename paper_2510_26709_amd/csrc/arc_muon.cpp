@@ -242,8 +242,8 @@ struct Rates {
   int32_t side;
   double line, alone, result, part;
 };
-constexpr Rates kRates[] = {{64, 0.24, 0.32, 1.6, 0.8},
-                            {128, 0.76, 0.90, 6.0, 3.2}};
+constexpr Rates kRates[] = {{64, 0.24, 0.32, 1.7, 0.8},
+                            {128, 0.66, 0.90, 6.7, 3.2}};
 constexpr double kLaunch = 5.0;
 constexpr int64_t kUnits = 256;
 

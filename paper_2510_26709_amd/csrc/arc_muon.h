@@ -50,11 +50,15 @@ struct MuonTile {
   int32_t mp, np;
 };
 
+// Bytes from one row of n numbers to the next.
+__host__ __device__ inline int64_t pair_pitch(int32_t n) { return int64_t{4} * n; }
+
 // Where an array of a matrix lies.
 __host__ __device__ inline int64_t array_at(int64_t base, int32_t mp, int32_t np, int32_t array) {
-  const int64_t row = int64_t{4} * mp;  // X and its two transposes, then squares
-  return array < kMuonSquare ? base + array * row * np
-                             : base + kMuonSquare * row * np + (array - kMuonSquare) * row * mp;
+  const int64_t x = pair_pitch(np) * mp, xt = pair_pitch(mp) * np, square = pair_pitch(mp) * mp;
+  if (array == kMuonX) return base;
+  if (array < kMuonSquare) return base + x + (array - kMuonXt) * xt;
+  return base + x + 2 * xt + (array - kMuonSquare) * square;
 }
 constexpr int32_t kMuonArrays = kMuonAll2 + 1;
 

@@ -35,9 +35,20 @@ __device__ __forceinline__ bool skipped(const MuonArgs& a) {
   return a.factor && !(fabsf(*a.factor) < INFINITY);
 }
 
-__device__ __forceinline__ float load_one(const void* p, int32_t bf16, int64_t at) {
-  return bf16 ? __uint_as_float((uint32_t) static_cast<const uint16_t*>(p)[at] << 16)
-              : static_cast<const float*>(p)[at];
+template <bool BF16>
+__device__ __forceinline__ float load_one(const void* p, int64_t at) {
+  if constexpr (BF16)
+    return __uint_as_float((uint32_t) static_cast<const uint16_t*>(p)[at] << 16);
+  return static_cast<const float*>(p)[at];
+}
+
+// Calls f(std::true_type()) or f(std::false_type()).
+template <typename F>
+__device__ __forceinline__ void choose(bool which, const F& f) {
+  if (which)
+    f(std::true_type());
+  else
+    f(std::false_type());
 }
 
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
@@ -50,12 +61,13 @@ typedef uint32_t loose_u32x4_t __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t loose_u32x2_t __attribute__((ext_vector_type(2), aligned(2)));
 
 // Four numbers from element `at` on, at any element alignment, of which `left` are
-// there (FULL: all of them).
-template <bool FULL>
-__device__ __forceinline__ void load_four(const void* p, int32_t bf16, int64_t at, int32_t left,
+// there (FULL: all of them).  The type is a template's argument: a branch around each
+// load would wait for it before the next.
+template <bool BF16, bool FULL>
+__device__ __forceinline__ void load_four(const void* p, int64_t at, int32_t left,
                                           float (&x)[4]) {
   if (FULL || left >= 4) {
-    if (bf16) {
+    if constexpr (BF16) {
       const u32x2_t w =
           *reinterpret_cast<const loose_u32x2_t*>(static_cast<const uint16_t*>(p) + at);
       x[0] = bf16_lo(w.x), x[1] = bf16_hi(w.x), x[2] = bf16_lo(w.y), x[3] = bf16_hi(w.y);
@@ -67,15 +79,15 @@ __device__ __forceinline__ void load_four(const void* p, int32_t bf16, int64_t a
     return;
   }
 #pragma unroll
-  for (int k = 0; k < 4; ++k) x[k] = k < left ? load_one(p, bf16, at + k) : 0.f;
+  for (int k = 0; k < 4; ++k) x[k] = k < left ? load_one<BF16>(p, at + k) : 0.f;
 }
 
-template <bool FULL>
-__device__ __forceinline__ void store_four(void* p, int32_t bf16, int64_t at, int32_t left,
+template <bool BF16, bool FULL>
+__device__ __forceinline__ void store_four(void* p, int64_t at, int32_t left,
                                            const float (&x)[4]) {
   const u32x2_t h = {bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
   if (FULL || left >= 4) {
-    if (bf16)
+    if constexpr (BF16)
       *reinterpret_cast<loose_u32x2_t*>(static_cast<uint16_t*>(p) + at) = h;
     else
       *reinterpret_cast<loose_u32x4_t*>(static_cast<float*>(p) + at) =
@@ -86,7 +98,7 @@ __device__ __forceinline__ void store_four(void* p, int32_t bf16, int64_t at, in
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     if (k >= left) break;
-    if (bf16)
+    if constexpr (BF16)
       static_cast<uint16_t*>(p)[at + k] = (uint16_t)((k < 2 ? h.x : h.y) >> (k % 2 * 16));
     else
       static_cast<float*>(p)[at + k] = x[k];
@@ -130,14 +142,14 @@ muon_momentum_kernel(MuonArgs a, MuonPointers p, const int32_t* __restrict__ run
   const int32_t i = run_matrix[run];
   const MuonMatrix& t = a.matrices[i];
   const void* grad = p.grad[i - a.first];
-  const int32_t bf16 = t.grad_bf16;
   const float factor = a.factor ? *a.factor : 1.f;
   const int64_t count = (int64_t)t.rows * t.cols;
   const int64_t first = (run - t.first_run) * kMuonRun;
   float* m = a.m ? a.m + t.state : nullptr;
   double sum = 0.0;
-  const auto passes = [&](auto whole) {
-    constexpr bool FULL = decltype(whole)::value;
+  const auto passes = [&](auto bf16, auto whole, auto kept) {
+    constexpr bool BF16 = decltype(bf16)::value, FULL = decltype(whole)::value;
+    constexpr bool KEPT = decltype(kept)::value;
     constexpr int U = 4;  // passes whose loads are in flight together
     for (int u = 0; u < kMuonRun; u += U * 4 * kThreads) {
       if (!FULL && first + u >= count) break;
@@ -146,8 +158,8 @@ muon_momentum_kernel(MuonArgs a, MuonPointers p, const int32_t* __restrict__ run
       for (int q = 0; q < U; ++q) {
         const int64_t e = first + u + (q * kThreads + (int)threadIdx.x) * 4;
         const int32_t left = FULL ? 4 : (int32_t)max(min(count - e, (int64_t)4), (int64_t)0);
-        load_four<FULL>(grad, bf16, e, left, g[q]);
-        if (m) load_four<FULL>(m, 0, e, left, v[q]);
+        load_four<BF16, FULL>(grad, e, left, g[q]);
+        if constexpr (KEPT) load_four<false, FULL>(m, e, left, v[q]);
       }
 #pragma unroll
       for (int q = 0; q < U; ++q) {
@@ -155,53 +167,50 @@ muon_momentum_kernel(MuonArgs a, MuonPointers p, const int32_t* __restrict__ run
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           g[q][k] *= factor;
-          if (m) v[q][k] = a.momentum * v[q][k] + g[q][k];
-          const double d = direction(a, g[q][k], m ? v[q][k] : 0.f);
+          if constexpr (KEPT) v[q][k] = a.momentum * v[q][k] + g[q][k];
+          const double d = direction(a, g[q][k], KEPT ? v[q][k] : 0.f);
           sum = fma(d, d, sum);  // (behind the end: zeros)
         }
-        if (m)
-          store_four<FULL>(m, 0, e, FULL ? 4 : (int32_t)max(min(count - e, (int64_t)4), (int64_t)0),
-                           v[q]);
+        if constexpr (KEPT)
+          store_four<false, FULL>(
+              m, e, FULL ? 4 : (int32_t)max(min(count - e, (int64_t)4), (int64_t)0), v[q]);
       }
     }
   };
-  if (first + kMuonRun <= count)
-    passes(std::true_type());
-  else
-    passes(std::false_type());
+  choose(t.grad_bf16, [&](auto bf16) {
+    choose(first + kMuonRun <= count, [&](auto whole) {
+      choose(m != nullptr, [&](auto kept) { passes(bf16, whole, kept); });
+    });
+  });
   sum = group_sum(sum);
   if (threadIdx.x == 0) a.sums[run] = sum;
 }
 
 // ---------------------------------------------------------------- pairs
 
-// 16 numbers of a row: `at` is their first one's place in the row.
-__device__ __forceinline__ void store_16(char* row, int32_t at, const uint32_t (&v)[16]) {
+// Eight numbers of a row, `at` the first one's place in it: four threads that follow
+// one another write 64 bytes together, twice.  (16 numbers a thread take twice the
+// requests, which the L2 has to take beside those of the tiles that are read.)
+__device__ __forceinline__ void store_8(char* row, int32_t at, const uint32_t (&v)[8]) {
   char* line = row + (int64_t)(at / kPairLine) * kLineBytes + at % kPairLine * 2;
-  uint32_t hi[8], lo[8];
+  uint32_t hi[4], lo[4];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
+  for (int k = 0; k < 4; ++k) {
     hi[k] = (v[2 * k] & 0xFFFFu) | (v[2 * k + 1] << 16);
     lo[k] = (v[2 * k] >> 16) | (v[2 * k + 1] & 0xFFFF0000u);
   }
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    *reinterpret_cast<u32x4_t*>(line + 16 * h) =
-        u32x4_t{hi[4 * h], hi[4 * h + 1], hi[4 * h + 2], hi[4 * h + 3]};
-    *reinterpret_cast<u32x4_t*>(line + 2 * kPairLine + 16 * h) =
-        u32x4_t{lo[4 * h], lo[4 * h + 1], lo[4 * h + 2], lo[4 * h + 3]};
-  }
+  *reinterpret_cast<u32x4_t*>(line) = u32x4_t{hi[0], hi[1], hi[2], hi[3]};
+  *reinterpret_cast<u32x4_t*>(line + 2 * kPairLine) = u32x4_t{lo[0], lo[1], lo[2], lo[3]};
 }
 
 __global__ void __launch_bounds__(kThreads)
 muon_split_kernel(MuonArgs a, MuonPointers p, const MuonTile* __restrict__ tiles) {
   constexpr int S = kSplitTile;
-  __shared__ uint32_t tile[S][S + 1];  // as the caller's matrix lies
+  __shared__ uint32_t tile[S][S + 2];  // as the caller's matrix lies
   if (skipped(a)) return;
   const MuonTile at = tiles[blockIdx.x];
   const MuonMatrix& t = a.matrices[at.matrix];
   const void* grad = p.grad[at.matrix - a.first];
-  const int32_t bf16 = t.grad_bf16;
   const float factor = a.factor ? *a.factor : 1.f;
   double squares = 0.0;  // every workgroup adds the runs' sums in the same order
 #pragma unroll 4
@@ -210,20 +219,21 @@ muon_split_kernel(MuonArgs a, MuonPointers p, const MuonTile* __restrict__ tiles
   const double inverse = squares == 0.0 ? 0.0 : (double)kPairScale / sqrt(squares);
   const float* m = a.m ? a.m + t.state : nullptr;
   const int32_t r0 = (t.tall ? at.j : at.i) * S, c0 = (t.tall ? at.i : at.j) * S;
-  {
-    constexpr int U = S * S / 4 / kThreads;
+  const auto fill = [&](auto bf16, auto kept, auto whole) {
+    constexpr bool BF16 = decltype(bf16)::value, KEPT = decltype(kept)::value;
+    constexpr bool FULL = decltype(whole)::value;
+    constexpr int U = S * S / 4 / kThreads, kDown = kThreads / (S / 4);
     const int32_t c = c0 + (int)threadIdx.x % (S / 4) * 4, left = t.cols - c;
     const int32_t r = r0 + (int)threadIdx.x / (S / 4);
-    constexpr int kDown = kThreads / (S / 4);
     float g[U][4], v[U][4];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) g[u][k] = v[u][k] = 0.f;
-      if (r + u * kDown >= t.rows) continue;
+      if (!FULL && r + u * kDown >= t.rows) continue;
       const int64_t e = (int64_t)(r + u * kDown) * t.cols + c;
-      load_four<false>(grad, bf16, e, left, g[u]);
-      if (m) load_four<false>(m, 0, e, left, v[u]);
+      load_four<BF16, FULL>(grad, e, left, g[u]);
+      if constexpr (KEPT) load_four<false, FULL>(m, e, left, v[u]);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -231,23 +241,29 @@ muon_split_kernel(MuonArgs a, MuonPointers p, const MuonTile* __restrict__ tiles
       for (int k = 0; k < 4; ++k)
         tile[r - r0 + u * kDown][c - c0 + k] =
             pair_of((float)((double)direction(a, g[u][k] * factor, v[u][k]) * inverse));
-  }
+  };
+  choose(t.grad_bf16, [&](auto bf16) {
+    choose(m != nullptr, [&](auto kept) {
+      choose(r0 + S <= t.rows && c0 + S <= t.cols, [&](auto whole) { fill(bf16, kept, whole); });
+    });
+  });
   __syncthreads();
-  const int line = threadIdx.x / 4, part = threadIdx.x % 4 * 16;
-  uint32_t along[16], across[16];
+  char* x = a.workspace + array_at(at.base, at.mp, at.np, kMuonX) + at.i * S * pair_pitch(at.np);
+  char* xt = a.workspace + array_at(at.base, at.mp, at.np, kMuonXt) + at.j * S * pair_pitch(at.mp);
+  char *along = t.tall ? xt : x, *across = t.tall ? x : xt;
+  const int64_t along_pitch = pair_pitch(t.tall ? at.mp : at.np);
+  const int64_t across_pitch = pair_pitch(t.tall ? at.np : at.mp);
 #pragma unroll
-  for (int k = 0; k < 16; ++k) {
-    along[k] = tile[line][part + k];
-    across[k] = tile[part + k][line];
-  }
-  char* x = a.workspace + array_at(at.base, at.mp, at.np, kMuonX) + (int64_t)(at.i * S + line) * at.np * 4;
-  char* xt = a.workspace + array_at(at.base, at.mp, at.np, kMuonXt) + (int64_t)(at.j * S + line) * at.mp * 4;
-  if (t.tall) {
-    store_16(x, at.j * S + part, across);
-    store_16(xt, at.i * S + part, along);
-  } else {
-    store_16(x, at.j * S + part, along);
-    store_16(xt, at.i * S + part, across);
+  for (int u = threadIdx.x; u < S * S / 8; u += kThreads) {
+    uint32_t v[8];
+    const int line = u / (S / 8), part = u % (S / 8) * 8;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = tile[line][part + k];
+    store_8(along + line * along_pitch, c0 + part, v);
+    const int column = u / 4 % S, run = u / (4 * S) * 32 + u % 4 * 8;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = tile[run + k][column];
+    store_8(across + column * across_pitch, r0 + run, v);
   }
 }
 
@@ -279,24 +295,21 @@ struct Shape<128> {
 };
 template <int SIDE>
 constexpr int kProductThreads = Shape<SIDE>::kWavesI * Shape<SIDE>::kWavesJ* kWave;
-// Results go through LDS, rows two words apart from each other: 32 columns of two
-// runs of 16 rows then lie in 64 different banks.
+// Results go through LDS, rows two words apart from each other: 16 columns of four
+// runs of eight rows then lie in 64 different banks.
 template <int SIDE>
 constexpr int kSlabPitch = SIDE + 2;
 template <int SIDE>
 constexpr int kProductLds =
     std::max(Shape<SIDE>::kStages * 2 * SIDE * kLineBytes, SIDE* kSlabPitch<SIDE> * 4);
 
-// The numbers of 16 pairs of a row, in units of 1 / kPairScale.
-__device__ __forceinline__ void load_16(const char* row, int32_t at, float (&x)[16]) {
+// The numbers of eight pairs of a row, in units of 1 / kPairScale.
+__device__ __forceinline__ void load_8(const char* row, int32_t at, float (&x)[8]) {
   const char* line = row + (int64_t)(at / kPairLine) * kLineBytes + at % kPairLine * 2;
+  const half8_t hi = *reinterpret_cast<const half8_t*>(line);
+  const half8_t lo = *reinterpret_cast<const half8_t*>(line + 2 * kPairLine);
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const half8_t hi = *reinterpret_cast<const half8_t*>(line + 16 * h);
-    const half8_t lo = *reinterpret_cast<const half8_t*>(line + 2 * kPairLine + 16 * h);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) x[8 * h + k] = (float)hi[k] + (float)lo[k];
-  }
+  for (int k = 0; k < 8; ++k) x[k] = (float)hi[k] + (float)lo[k];
 }
 
 // Adds a tile's parts in their order, in the last workgroup to arrive; false: this is
@@ -374,7 +387,7 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,
   const char* left = array(swap ? s.right : s.left);
   const char* right = array(swap ? s.left : s.right);
   const int32_t sum = WHAT == kMuonGram ? at.np : at.mp;
-  const uint32_t pitch = (uint32_t)sum * 4u;
+  const uint32_t pitch = (uint32_t)pair_pitch(sum);
   left += (int64_t)ti * SIDE * pitch;
   right += (int64_t)tj * SIDE * pitch;
   const buffer_rsrc from[2] = {make_buffer(left, SIDE * pitch), make_buffer(right, SIDE * pitch)};
@@ -439,9 +452,11 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,
             acc[i0 + i][j] =
                 __builtin_amdgcn_mfma_f32_16x16x32_f16(x[i], y[j], acc[i0 + i][j], 0, 0, 0);
       };
+      __builtin_amdgcn_s_setprio(1);
       multiply(lh, rl);
       multiply(lh, rh);
       multiply(ll, rh);
+      __builtin_amdgcn_s_setprio(0);
     }
   }
   if (at.parts > 1 && !join_parts<SIDE>(a, at, acc)) return;
@@ -475,17 +490,18 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,
     const int32_t left = t.cols - c0 - across;
     const int32_t r = r0 + down;
     const int64_t e0 = (int64_t)r * t.cols + c0 + across;
-    const auto passes = [&](auto whole) {
-      constexpr bool FULL = decltype(whole)::value;
+    const auto passes = [&](auto bf16, auto whole) {
+      constexpr bool BF16 = decltype(bf16)::value, FULL = decltype(whole)::value;
       float x[kPasses][4];
+      if (a.update)
 #pragma unroll
-      for (int q = 0; q < kPasses; ++q)
-        if (a.update && r + q * kDown < t.rows)
-          load_four<FULL>(param, t.param_bf16, e0 + (int64_t)q * kDown * t.cols, left, x[q]);
+        for (int q = 0; q < kPasses; ++q)
+          if (FULL || r + q * kDown < t.rows)
+            load_four<BF16, FULL>(param, e0 + (int64_t)q * kDown * t.cols, left, x[q]);
       to_slab();
 #pragma unroll
       for (int q = 0; q < kPasses; ++q) {
-        if (r + q * kDown >= t.rows) continue;
+        if (!FULL && r + q * kDown >= t.rows) continue;
         const float* of = slab + (q * kDown + down) * kPitch + across;
         float v[4];
 #pragma unroll
@@ -494,57 +510,58 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,
           if (a.update) v[k] = fmaf(-step, v[k], x[q][k] * keep);
         }
         const int64_t e = e0 + (int64_t)q * kDown * t.cols;
-        store_four<FULL>(param, t.param_bf16, e, left, v);
-        if (copy) store_four<FULL>(copy, 1, e, left, v);
+        store_four<BF16, FULL>(param, e, left, v);
+        if (copy) store_four<true, FULL>(copy, e, left, v);
       }
     };
-    if (c0 + SIDE <= t.cols)
-      passes(std::true_type());
-    else
-      passes(std::false_type());
+    choose(t.param_bf16, [&](auto bf16) {
+      choose(r0 + SIDE <= t.rows && c0 + SIDE <= t.cols,
+             [&](auto whole) { passes(bf16, whole); });
+    });
   } else {
     char* to = array(s.out);
     char* turned = array(s.turned);
-    const int64_t to_pitch = (int64_t)(WHAT == kMuonApply ? at.np : at.mp) * 4;
-    const int64_t turned_pitch = (int64_t)at.mp * 4;
+    const int64_t to_pitch = pair_pitch(WHAT == kMuonApply ? at.np : at.mp);
+    const int64_t turned_pitch = pair_pitch(at.mp);
     const bool mirror = WHAT == kMuonApply || ti != tj;
     to_slab();
-    // Rows as they are, 16 numbers a thread and pass; the pairs take the numbers'
+    // Rows as they are, eight numbers a thread and pass; the pairs take the numbers'
     // places.
-    constexpr int kRuns = SIDE / 16;
-#pragma unroll 2
+    constexpr int kRuns = SIDE / 8;
+#pragma unroll 4
     for (int u = threadIdx.x; u < SIDE * kRuns; u += kThread) {
-      const int r = u / kRuns, c = u % kRuns * 16;
+      const int r = u / kRuns, c = u % kRuns * 8;
       float* of = slab + r * kPitch + c;
-      uint32_t v[16];
+      float x[8];
 #pragma unroll
-      for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(of[k] * s.scale);
+      for (int k = 0; k < 8; ++k) x[k] = of[k] * s.scale;
       if constexpr (WHAT == kMuonStep) {
-        float square[16];
-        load_16(array(s.left) + (r0 + r) * to_pitch, c0 + c, square);
+        float square[8];
+        load_8(array(s.left) + (r0 + r) * to_pitch, c0 + c, square);
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          const float x = fmaf(s.c, __uint_as_float(v[k]), s.b * square[k]);
-          v[k] = __float_as_uint(r0 + r == c0 + c + k ? x + s.a * kPairScale : x);
+        for (int k = 0; k < 8; ++k) {
+          x[k] = fmaf(s.c, x[k], s.b * square[k]);
+          if (r0 + r == c0 + c + k) x[k] += s.a * kPairScale;
         }
       }
+      uint32_t v[8];
 #pragma unroll
-      for (int k = 0; k < 16; ++k) v[k] = pair_of(__uint_as_float(v[k]));
-      store_16(to + (r0 + r) * to_pitch, c0 + c, v);
+      for (int k = 0; k < 8; ++k) v[k] = pair_of(x[k]);
+      store_8(to + (r0 + r) * to_pitch, c0 + c, v);
       if (mirror)
 #pragma unroll
-        for (int k = 0; k < 16; ++k) of[k] = __uint_as_float(v[k]);
+        for (int k = 0; k < 8; ++k) of[k] = __uint_as_float(v[k]);
     }
     if (!mirror) return;
     __syncthreads();
-    // And transposed, two threads to a line.
-#pragma unroll 2
+    // And transposed, four threads to a line.
+#pragma unroll 4
     for (int u = threadIdx.x; u < SIDE * kRuns; u += kThread) {
-      const int c = u / 2 % SIDE, r = u / (2 * SIDE) * 32 + u % 2 * 16;
-      uint32_t v[16];
+      const int c = u / 4 % SIDE, r = u / (4 * SIDE) * 32 + u % 4 * 8;
+      uint32_t v[8];
 #pragma unroll
-      for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(slab[(r + k) * kPitch + c]);
-      store_16(turned + (c0 + c) * turned_pitch, r0 + r, v);
+      for (int k = 0; k < 8; ++k) v[k] = __float_as_uint(slab[(r + k) * kPitch + c]);
+      store_8(turned + (c0 + c) * turned_pitch, r0 + r, v);
     }
   }
 }
