@@ -673,9 +673,12 @@ arc_status arc_optim_destroy(arc_optim *ctx);
  *   x <- (1 - lr' weight_decay) x - lr' O(U)
  *
  * X and A are held in 22 bits (two binary16 numbers each), products are summed in
- * binary32 in a fixed order, norms in binary64, all else is binary32: O is as exact
- * as binary32 products make it, and a call repeats its bits.  A matrix with a NaN
- * or infinity in U gets NaN everywhere, the others none of it.
+ * binary32 in a fixed order, norms in binary64, all else is binary32, and a call
+ * repeats its bits.  O in binary32 is as exact as binary32 products make it (off by
+ * 2e-6 of its norm for matrices of some hundreds of rows).  In optimizer steps, and
+ * where all parameters are bfloat16, it may be off by a few times that: products of
+ * several steps' polynomials are taken first where that is less work.  A matrix with a
+ * NaN or infinity in U gets NaN everywhere, the others none of it.
  *
  * Momenta lie in one array of arc_muon_state_elems binary32 elements, matrix i's from
  * arc_muon_state_offset(i), a multiple of ARC_STATE_BLOCK, on, row after row.
@@ -716,9 +719,11 @@ typedef struct {
 } arc_muon_step_config;
 
 /* Validate cfg, allocate the tables and the workspace (12 bytes for each element and
- * 8 for each of a square of the shorter side, of as many matrices as fit into 4 GiB,
- * or of the largest) on the current HIP device and bind the context to `hip_stream`,
- * as arc_create does.  On failure *out is NULL. */
+ * 20 for each of a square of the shorter side, sides rounded up to 64 or 128, of as many
+ * matrices as fit into 4 GiB, or of the largest) on the current HIP device and bind
+ * the context to `hip_stream`, as arc_create does.  Graphs captured from one context
+ * share its workspace: replays of them must not overlap in time.  On failure *out is
+ * NULL. */
 arc_status arc_muon_create(const arc_muon_config *cfg, void *hip_stream, arc_muon **out);
 
 /* Elements of the momenta; -1 for NULL. */

@@ -6,8 +6,6 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
-#include <cstdlib>
-#include <cstdio>
 #include <functional>
 #include <utility>
 #include <vector>
@@ -83,7 +81,14 @@ constexpr int32_t kMaxSteps = 64;
 constexpr float kQuintic[3] = {3.4445f, -4.7750f, 2.0315f};
 // What a group's pairs may take: enough matrices to fill the card many times over.
 constexpr int64_t kGroupBytes = int64_t{4} << 30;
-// Steps whose polynomials are multiplied before X is.
+// Steps whose polynomials are multiplied before X is: then X X' and P X, the products
+// that grow with the longer side, are made once for three steps and not three times, for
+// six more products of the shorter side (five steps of m x n numbers: 15 m^2 n + 5 m^3
+// multiplications with all steps apart, 6 m^2 n + 14 m^3 in runs of three and two).  An
+// error of A is taken from step to step within a run, 12 times larger each in the
+// directions of small singular values: O is off by 3e-6 to 5e-6 where it is by 2e-6
+// step by step, and with all five in one run by 1e-4.  Step by step where O itself is
+// asked for in binary32.
 constexpr int32_t kTogether = 3;
 
 int64_t up_to(int64_t v, int64_t of) { return (v + of - 1) / of * of; }
@@ -235,9 +240,16 @@ void each_tile(int32_t rows, int32_t cols, bool half, const Add& add) {
 }
 
 // What a launch is expected to take, in us, by which tiles' sums are split and the
-// tiles' side is chosen.  Measured: a line of a tile's sum on a compute unit that is
-// full, and in a workgroup that has it for itself; a result written; a part written
-// (and read once more by the workgroup that adds them); a launch.
+// tiles' side and the way through the steps are chosen.  Measured: a line of a tile's
+// sum on a compute unit that is full, and in a workgroup that has it for itself; a
+// result written; a part written (and read once more by the workgroup that adds them);
+// a launch.  us with tiles of 64 and of 128, step by step / in runs: 257 x 1001 126 /
+// 126 and 268 / 268, 24 matrices of a decoder of width 384 455 / 389 and 495 / 459, 32 of
+// width 576 1702 / 1164 and 1668 / 1223, a ResNet-18's convolutions 489 / 363 and 531 /
+// 478, 48 of width 640 3498 / 2455 and 2818 / 2144, a 4096 x 4096 4497 / 4759 and 3526 /
+// 3673.  What is chosen was within 2% of the best of the four in 28 of 30 cases, and
+// within 11% in all.  Split sums: X X' of a ResNet-18's convolutions (sums of 4608 in
+// few tiles) 40 us against 103.
 struct Rates {
   int32_t side;
   double line, alone, result, part;
@@ -246,6 +258,8 @@ constexpr Rates kRates[] = {{64, 0.24, 0.32, 1.7, 0.8},
                             {128, 0.66, 0.90, 6.7, 3.2}};
 constexpr double kLaunch = 5.0;
 constexpr int64_t kUnits = 256;
+// Tiles of 128 that fill the card so often that smaller ones are not looked at.
+constexpr int64_t kPlenty = 16 * 2 * kUnits;
 
 // The parts of each of `lines`, which descend, from number `from` on `parts` of them;
 // and the time that the busiest compute unit then needs.
@@ -419,14 +433,15 @@ arc_muon plan_best(const arc_muon_config* cfg, const std::vector<float>& coeffic
   const auto grouped = sequence(coefficients, bounds, kTogether);
   arc_muon best;
   double least = INFINITY;
+  int64_t tiles = 0;  // of 128
+  for (int32_t i = 0; i < cfg->num_matrices; ++i)
+    tiles += (cfg->matrices[i].rows + 127) / 128 * ((cfg->matrices[i].cols + 127) / 128);
   for (const Rates& r : kRates) {
-    if (const char* v = getenv("ARC_SIDE")) if (atoi(v) && r.side != atoi(v)) continue;
+    if (r.side < 128 && tiles > kPlenty) continue;
     arc_muon c;
     const Times times = plan_muon(cfg, r, &c);
     const double one = times.of(plain), other = times.of(grouped);
-    if (getenv("ARC_SAY")) fprintf(stderr, "side %d: %.1f %.1f us a step, parts %ld\n", r.side, one, other, (long)c.parts);
     c.group = other < 0.97 * one;
-    if (const char* v = getenv("ARC_GROUP")) c.group = atoi(v);
     if (std::min(one, other) < least) {
       least = std::min(one, other);
       best = std::move(c);

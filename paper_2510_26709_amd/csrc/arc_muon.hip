@@ -4,9 +4,9 @@
 //
 // X is held as pairs of binary16 numbers (arc_muon.h), 22 bits in all, and a
 // product of two takes three matrix instructions, hi hi + hi lo + lo hi, summed in
-// binary32: what is left out (lo lo) is 2^-22 of a term, so that the result is as
-// exact as a binary32 product's, at a third of binary16's rate, which is four
-// times binary32's.  Rounded once to binary16 or bfloat16 instead, X is off by 1e-3
+// binary32: what is left out (lo lo) is 2^-24 of a term, so that the result is as
+// exact as a binary32 product's, at a third of binary16's rate, which is three
+// times what binary32 matrix instructions reach (132 to 153 TFLOP/s).  Rounded once to binary16 or bfloat16 instead, X is off by 1e-3
 // and 1e-2 after five steps, since small singular values grow 3.4 times in each
 // and errors in their directions with them.
 //
@@ -346,13 +346,12 @@ __device__ __forceinline__ bool join_parts(const MuonArgs& a, const MuonTile& at
 #pragma unroll
     for (int i = 0; i < TI; ++i)
 #pragma unroll
-      for (int j = 0; j < TJ; ++j)
-{
-          const f32x4_t v = __builtin_bit_cast(
-              f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(
-                           of, (int)threadIdx.x * 16, (i * TJ + j) * kThread * 16, kDevice));
-          acc[i][j] = q == 0 ? v : acc[i][j] + v;
-        }
+      for (int j = 0; j < TJ; ++j) {
+        const f32x4_t v = __builtin_bit_cast(
+            f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(
+                         of, (int)threadIdx.x * 16, (i * TJ + j) * kThread * 16, kDevice));
+        acc[i][j] = q == 0 ? v : acc[i][j] + v;
+      }
   }
   return true;
 }
@@ -364,6 +363,19 @@ using PointersOf = std::conditional_t<WHAT == kMuonLast, MuonPointers, NoPointer
 // A tile of L R', both [rows][sum] in pairs.  The sum is taken a line (32 numbers)
 // at a time, staged in LDS: row r's 16-byte pieces lie at piece ^ (r / 2 % 8), so
 // that 16 rows' pieces, which are read together, lie in different banks.
+//
+// Bound by the matrix units at the clock that the card's power leaves them (1.7 GHz of
+// 2.4; of a matrix of zeros the same products take 0.7 of the time): 4096^3 in 323 to
+// 354 us, 1160 to 1280 TFLOP/s of binary16 products, where the library's plain binary16
+// product runs at 1390; 64 x 64 tiles of few lines are bound by latency, 6 to 8 us a
+// launch.  Hence 16 x 16 x 32 instructions, which read and write each binary32 sum
+// once for 32 terms: with 32 x 32 x 16 (16 terms) all of it took 9% longer.  Waves that
+// multiply go ahead of those that read: 5%.  What made no difference: reading the next
+// half line's pairs while one is multiplied, tiles of 256 x 256 by eight waves (half
+// the reads; but nothing hides a workgroup's ends then), rows an odd number of lines
+// apart.  Lines of 16 numbers, three workgroups a compute unit: 13% longer.  A tile's
+// end (results through LDS, 64 bytes of a line together) is 13% of the time with sums of
+// 2048, a third with 640.
 template <int SIDE, MuonKind WHAT>
 __global__ void __launch_bounds__(kProductThreads<SIDE>, Shape<SIDE>::kGroups)
 muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,
@@ -428,8 +440,7 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,
     const char* base = lds + line % kStages * kStage;
     const char* l = base + (wi * TI * 16 + row) * kLineBytes;
     const char* r = base + (SIDE + wj * TJ * 16 + row) * kLineBytes;
-    constexpr int kRows = TI < 4 ? TI : 4;  // of tiles whose pairs are in registers
-    half8_t lh[kRows], ll[kRows], rh[TJ], rl[TJ];
+    half8_t lh[TI], ll[TI], rh[TJ], rl[TJ];
     const int hi = (quarter ^ (row / 2)) * 16, lo = hi ^ 64;
 #pragma unroll
     for (int j = 0; j < TJ; ++j) {
@@ -437,27 +448,23 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,
       rl[j] = *reinterpret_cast<const half8_t*>(r + j * 16 * kLineBytes + lo);
     }
 #pragma unroll
-    for (int i0 = 0; i0 < TI; i0 += kRows) {
-#pragma unroll
-      for (int i = 0; i < kRows; ++i) {
-        lh[i] = *reinterpret_cast<const half8_t*>(l + (i0 + i) * 16 * kLineBytes + hi);
-        ll[i] = *reinterpret_cast<const half8_t*>(l + (i0 + i) * 16 * kLineBytes + lo);
-      }
-      __builtin_amdgcn_sched_barrier(0);  // all reads ahead of the products
-      const auto multiply = [&](const half8_t(&x)[kRows], const half8_t(&y)[TJ]) {
-#pragma unroll
-        for (int i = 0; i < kRows; ++i)
-#pragma unroll
-          for (int j = 0; j < TJ; ++j)
-            acc[i0 + i][j] =
-                __builtin_amdgcn_mfma_f32_16x16x32_f16(x[i], y[j], acc[i0 + i][j], 0, 0, 0);
-      };
-      __builtin_amdgcn_s_setprio(1);
-      multiply(lh, rl);
-      multiply(lh, rh);
-      multiply(ll, rh);
-      __builtin_amdgcn_s_setprio(0);
+    for (int i = 0; i < TI; ++i) {
+      lh[i] = *reinterpret_cast<const half8_t*>(l + i * 16 * kLineBytes + hi);
+      ll[i] = *reinterpret_cast<const half8_t*>(l + i * 16 * kLineBytes + lo);
     }
+    __builtin_amdgcn_sched_barrier(0);  // all reads ahead of the products
+    const auto multiply = [&](const half8_t(&x)[TI], const half8_t(&y)[TJ]) {
+#pragma unroll
+      for (int i = 0; i < TI; ++i)
+#pragma unroll
+        for (int j = 0; j < TJ; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[i], y[j], acc[i][j], 0, 0, 0);
+    };
+    __builtin_amdgcn_s_setprio(1);
+    multiply(lh, rl);
+    multiply(lh, rh);
+    multiply(ll, rh);
+    __builtin_amdgcn_s_setprio(0);
   }
   if (at.parts > 1 && !join_parts<SIDE>(a, at, acc)) return;
   // Lane l holds column l % 16 of a 16 x 16 tile, element k in row 4 (l / 16) + k.
