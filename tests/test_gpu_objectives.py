@@ -552,6 +552,24 @@ def test_preference_gradient_against_differences(o):
             assert abs(float(got[i, j]) - want) < 1e-7 + 2e-6 * (1 + abs(want))
 
 
+def test_no_rows():
+    """Nothing to do gives totals of 0 and gradients without rows."""
+    head = arc.TokenLogProbs(V=10, rows=4, dtype="bf16")
+    x = torch.zeros(0, 10, dtype=torch.bfloat16).cuda()
+    y, v = torch.zeros(0, dtype=torch.int64).cuda(), torch.zeros(0).cuda()
+    out = head.policy_loss(x, y, v, old_logp=v, ref_logp=v, kl_coef=0.1, entropy_coef=0.1)
+    assert out.totals.tolist() == [0.0] * 5 and out.grad.shape == (0, 10)
+    assert head.policy(v, y, v).totals.tolist() == [0.0] * 5
+    for P in (0, 3):  # no pair, and pairs without tokens
+        o = torch.zeros(2 * P + 1, dtype=torch.int64).cuda()
+        out = head.preference_loss(x, y, o)
+        want = [P * math.log(2.0), 0.0, 0.0]
+        for got in (out, head.preference(v, y, o)):
+            near("totals", got.totals, torch.tensor(want), 4 * EPS * P)
+            assert got.rewards.tolist() == [0.0] * (2 * P)
+        assert out.grad.shape == (0, 10)
+
+
 # ---------------------------------------------------------------- streams, graphs, refusals
 
 def test_on_another_stream_and_in_a_graph():
