@@ -128,7 +128,7 @@ inline TokenArgs token_args(const arc_tokens* c, int64_t rows, const void* logit
 
 inline arc_status check_score(const arc_tokens* c, int64_t rows, const void* logits, int64_t stride,
                        const int64_t* targets, const TokenScores& out) {
-  if (out.logp != nullptr && targets == nullptr)
+  if (rows > 0 && out.logp != nullptr && targets == nullptr)
     return fail(ARC_ERR_INVALID, "logp needs targets");
   if ((out.top_ids == nullptr) != (out.top_logp == nullptr))
     return fail(ARC_ERR_INVALID, "top_ids and top_logp are given together");
@@ -146,7 +146,7 @@ inline arc_status check_grad(const arc_tokens* c, int64_t rows, const void* logi
   if (g.stride < c->vocab) return fail(ARC_ERR_INVALID, "grad_stride must be at least vocab");
   if (g.stride > INT64_MAX / 8 / std::max<int64_t>(rows, 1))
     return fail(ARC_ERR_INVALID, "rows * grad_stride overflows");
-  if (g.d_logp != nullptr && targets == nullptr)
+  if (rows > 0 && g.d_logp != nullptr && targets == nullptr)
     return fail(ARC_ERR_INVALID, "d_logp needs targets");
   const int64_t v = rows * 4;
   const bool in_place = g.grad == logits && g.stride == stride;
