@@ -77,7 +77,8 @@ class Model:
         dh = (dlogits @ U) * (1 - h * h)
         torch.mm(e.t(), dh, out=gW)
         gb.copy_(dh.sum(0, keepdim=True))
-        gE.zero_().index_add_(0, tokens, dh @ W.t())
+        # (sorted sums: their order, and with it a run's every bit, is the same each time)
+        gE.zero_().index_put_((tokens,), dh @ W.t(), accumulate=True)
 
 
 def train(*, steps=300, workers=4, vocab=501, hidden=128, rows=32, length=16, keep=0.2, lr=1e-2,
