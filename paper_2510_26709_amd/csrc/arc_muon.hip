@@ -366,16 +366,16 @@ using PointersOf = std::conditional_t<WHAT == kMuonLast, MuonPointers, NoPointer
 //
 // Bound by the matrix units at the clock that the card's power leaves them (1.7 GHz of
 // 2.4; of a matrix of zeros the same products take 0.7 of the time): 4096^3 in 323 to
-// 354 us, 1160 to 1280 TFLOP/s of binary16 products, where the library's plain binary16
-// product runs at 1390; 64 x 64 tiles of few lines are bound by latency, 6 to 8 us a
-// launch.  Hence 16 x 16 x 32 instructions, which read and write each binary32 sum
-// once for 32 terms: with 32 x 32 x 16 (16 terms) all of it took 9% longer.  Waves that
-// multiply go ahead of those that read: 5%.  What made no difference: reading the next
-// half line's pairs while one is multiplied, tiles of 256 x 256 by eight waves (half
-// the reads; but nothing hides a workgroup's ends then), rows an odd number of lines
-// apart.  Lines of 16 numbers, three workgroups a compute unit: 13% longer.  A tile's
-// end (results through LDS, 64 bytes of a line together) is 13% of the time with sums of
-// 2048, a third with 640.
+// 360 us, 1140 to 1280 TFLOP/s of binary16 products, where the library's plain binary16
+// product runs at 1390; tiles of 64 with few lines are bound by latency, 6 to 8 us a
+// launch.  Hence 16 x 16 x 32 instructions, which read and write each binary32 sum once
+// for 32 terms: with 32 x 32 x 16 (16 terms) a 4096 x 4096 took 3.96 ms against 3.61.
+// Within 1% either way, timed in turn: the next line's pairs read while one is
+// multiplied, wave priorities, rows an odd number of lines apart; 1 to 4% slower: no
+// products above the diagonal of symmetric tiles; tiles of 256 x 256 by eight waves
+// were even at sums of 4096 and slower at others, as nothing hides a workgroup's ends.
+// A tile's end (results through LDS, 64 bytes of a line together) is 13% of the time
+// with sums of 2048, a third with 640.
 template <int SIDE, MuonKind WHAT>
 __global__ void __launch_bounds__(kProductThreads<SIDE>, Shape<SIDE>::kGroups)
 muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,
@@ -460,11 +460,9 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,
         for (int j = 0; j < TJ; ++j)
           acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[i], y[j], acc[i][j], 0, 0, 0);
     };
-    __builtin_amdgcn_s_setprio(1);
     multiply(lh, rl);
     multiply(lh, rh);
     multiply(ll, rh);
-    __builtin_amdgcn_s_setprio(0);
   }
   if (at.parts > 1 && !join_parts<SIDE>(a, at, acc)) return;
   // Lane l holds column l % 16 of a 16 x 16 tile, element k in row 4 (l / 16) + k.
