@@ -243,18 +243,21 @@ void each_tile(int32_t rows, int32_t cols, bool half, const Add& add) {
 // tiles' side and the way through the steps are chosen.  Measured: a line of a tile's
 // sum on a compute unit that is full, and in a workgroup that has it for itself; a
 // result written; a part written (and read once more by the workgroup that adds them);
-// a launch.  us with tiles of 64 and of 128, step by step / in runs: 257 x 1001 126 /
-// 126 and 268 / 268, 24 matrices of a decoder of width 384 455 / 389 and 495 / 459, 32 of
-// width 576 1702 / 1164 and 1668 / 1223, a ResNet-18's convolutions 489 / 363 and 531 /
-// 478, 48 of width 640 3498 / 2455 and 2818 / 2144, a 4096 x 4096 4497 / 4759 and 3526 /
-// 3673.  What is chosen was within 2% of the best of the four in 28 of 30 cases, and
-// within 11% in all.  Split sums: X X' of a ResNet-18's convolutions (sums of 4608 in
-// few tiles) 40 us against 103.
+// a launch.  us with tiles of 32, 64 and 128, the better of step by step and in runs:
+// 24 vectors and small matrices 66, 66 and 126, 257 x 1001 101, 123 and 265, a
+// ResNet-18's convolutions 390, 362 and 482, three layers of width 384 272, 243 and 342,
+// of width 576 622, 481 and 657, 48 matrices of width 640 3460, 2450 and 2140, a 4096 x
+// 4096 7870, 4500 and 3600.  Step by step and in runs: 257 x 1001 123 and 123, the
+// convolutions 489 and 363, width 640 2860 and 2140, 4096 x 4096 3597 and 3765.  What is
+// chosen was within 3% of the best of the six in 48 of 51 drawn cases, and within 16% in
+// all.  Split sums: X X' of a ResNet-18's convolutions (sums of 4608 in few tiles) 40 us
+// against 103.
 struct Rates {
   int32_t side;
   double line, alone, result, part;
 };
-constexpr Rates kRates[] = {{64, 0.24, 0.32, 1.7, 0.8},
+constexpr Rates kRates[] = {{32, 0.10, 0.16, 0.5, 0.3},
+                            {64, 0.24, 0.32, 1.7, 0.8},
                             {128, 0.66, 0.90, 6.7, 3.2}};
 constexpr double kLaunch = 5.0;
 constexpr int64_t kUnits = 256;
@@ -384,8 +387,9 @@ Times plan_muon(const arc_muon_config* cfg, const Rates& rates, arc_muon* c) {
     t.tall = in.rows > in.cols;
     t.m = std::min(t.rows, t.cols);
     t.n = std::max(t.rows, t.cols);
-    t.mp = static_cast<int32_t>(up_to(t.m, side));
-    t.np = static_cast<int32_t>(count > 0 ? up_to(t.n, side) : 0);
+    const int32_t whole_of = std::max(side, arc::kSplitTile);
+    t.mp = static_cast<int32_t>(up_to(t.m, whole_of));
+    t.np = static_cast<int32_t>(count > 0 ? up_to(t.n, whole_of) : 0);
     t.param_bf16 = in.param_dtype == ARC_DTYPE_BF16;
     t.grad_bf16 = in.grad_dtype == ARC_DTYPE_BF16;
     t.weight_decay = in.weight_decay;

@@ -6,9 +6,10 @@
 // product of two takes three matrix instructions, hi hi + hi lo + lo hi, summed in
 // binary32: what is left out (lo lo) is 2^-24 of a term, so that the result is as
 // exact as a binary32 product's, at a third of binary16's rate, which is three
-// times what binary32 matrix instructions reach (132 to 153 TFLOP/s).  Rounded once to binary16 or bfloat16 instead, X is off by 1e-3
-// and 1e-2 after five steps, since small singular values grow 3.4 times in each
-// and errors in their directions with them.
+// times what binary32 matrix instructions reach (132 to 153 TFLOP/s).  Rounded once
+// to binary16 or bfloat16 instead, X is off by 1e-3 and 1e-2 after five steps, since
+// small singular values grow 3.4 times in each and errors in their directions with
+// them.
 //
 // All three products of a step have rows on both sides that lie along the sum:
 // X X' from X, A A' (A is symmetric), and P X from P and the transpose of X.  So X
@@ -283,8 +284,16 @@ __device__ __forceinline__ void arrived() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
+// Waves of a tile, lines of its sum in LDS (one is multiplied while the others
+// arrive; as many as leave kGroups workgroups room on a compute unit), workgroups that
+// the registers are shared by.  Four waves in all: each then holds 64 x 64, 32 x 32 or
+// 16 x 16 of a result.
 template <int SIDE>
 struct Shape;
+template <>
+struct Shape<32> {
+  static constexpr int kWavesI = 2, kWavesJ = 2, kStages = 4, kGroups = 4;
+};
 template <>
 struct Shape<64> {
   static constexpr int kWavesI = 2, kWavesJ = 2, kStages = 3, kGroups = 3;
@@ -367,8 +376,8 @@ using PointersOf = std::conditional_t<WHAT == kMuonLast, MuonPointers, NoPointer
 // Bound by the matrix units at the clock that the card's power leaves them (1.7 GHz of
 // 2.4; of a matrix of zeros the same products take 0.7 of the time): 4096^3 in 323 to
 // 360 us, 1140 to 1280 TFLOP/s of binary16 products, where the library's plain binary16
-// product runs at 1390; tiles of 64 with few lines are bound by latency, 6 to 8 us a
-// launch.  Hence 16 x 16 x 32 instructions, which read and write each binary32 sum once
+// product runs at 1390; small contexts are bound by latency, 4 us a launch with tiles
+// of 32 and 5 to 6 with tiles of 64 (five steps of a few vectors 63 and 73 us).  Hence 16 x 16 x 32 instructions, which read and write each binary32 sum once
 // for 32 terms: with 32 x 32 x 16 (16 terms) a 4096 x 4096 took 3.96 ms against 3.61.
 // Within 1% either way, timed in turn: the next line's pairs read while one is
 // multiplied, wave priorities, rows an odd number of lines apart; 1 to 4% slower: no
@@ -609,7 +618,8 @@ hipError_t reserve_lds() {
 }  // namespace
 
 hipError_t prepare_muon_products() {
-  hipError_t e = reserve_lds<64>();
+  hipError_t e = reserve_lds<32>();
+  if (e == hipSuccess) e = reserve_lds<64>();
   if (e == hipSuccess) e = reserve_lds<128>();
   return e;
 }
@@ -631,8 +641,9 @@ hipError_t launch_muon_split(const MuonArgs& a, const MuonPointers& p, const Muo
 hipError_t launch_muon_product(MuonKind kind, int32_t side, const MuonArgs& a,
                                const MuonPointers& p, const MuonProduct& s,
                                const MuonTile* tiles, int64_t count, hipStream_t stream) {
-  return side == 64 ? launch_product<64>(kind, a, p, s, tiles, count, stream)
-                    : launch_product<128>(kind, a, p, s, tiles, count, stream);
+  return side == 32   ? launch_product<32>(kind, a, p, s, tiles, count, stream)
+         : side == 64 ? launch_product<64>(kind, a, p, s, tiles, count, stream)
+                      : launch_product<128>(kind, a, p, s, tiles, count, stream);
 }
 
 }  // namespace arc

@@ -214,14 +214,10 @@ def placed(x, dtype, shift):
     return buf, view
 
 
-@pytest.mark.parametrize("nesterov", [True, False])
-@pytest.mark.parametrize("param,grad,copy", [("f32", "f32", True), ("f32", "bf16", True),
-                                             ("bf16", "bf16", False), ("bf16", "f32", False)])
-@pytest.mark.parametrize("shift", [0, 1, 3])
-def test_steps(param, grad, copy, nesterov, shift):
-    shapes = [(100, 260), (260, 100), (7, 3), (0, 5), (129, 129), (1, 1)]
-    num, lr, mu, wd = len(shapes), 0.03, 0.9, [0.1, 0.0, 0.2, 0.0, 0.1, 0.0]
-    scales = [1.0, 2.0, 0.5, 1.0, -1.0, 1.0]
+def run_steps(shapes, param, grad, copy, nesterov, shift):
+    num, lr, mu = len(shapes), 0.03, 0.9
+    wd = [(0.1, 0.0, 0.2, 0.0, 0.1, 0.0)[k % 6] for k in range(num)]
+    scales = [(1.0, 2.0, 0.5, 1.0, -1.0, 1.0)[k % 6] for k in range(num)]
     pd = torch.float32 if param == "f32" else torch.bfloat16
     gd = torch.float32 if grad == "f32" else torch.bfloat16
     opt = arc.Muon(shapes, param_dtype=param, grad_dtype=grad, weight_decay=wd, lr_scale=scales)
@@ -270,6 +266,37 @@ def test_steps(param, grad, copy, nesterov, shift):
     assert bool((opt.m[~inside] == 0).all())
     if copy:
         assert torch.equal(copies[2][1], x0[2].bfloat16())
+
+
+@pytest.mark.parametrize("nesterov", [True, False])
+@pytest.mark.parametrize("param,grad,copy", [("f32", "f32", True), ("f32", "bf16", True),
+                                             ("bf16", "bf16", False), ("bf16", "f32", False)])
+@pytest.mark.parametrize("shift", [0, 1, 3])
+def test_steps(param, grad, copy, nesterov, shift):
+    run_steps([(100, 260), (260, 100), (7, 3), (0, 5), (129, 129), (1, 1)], param, grad, copy,
+              nesterov, shift)
+
+
+# Contexts of more work, whose products have larger tiles, step by step and in runs.
+LARGER = [[(641, 643)] * 4 + [(643, 130)],
+          [(1500, 2100), (2101, 1501), (7, 3), (129, 129)],
+          [(1001, 1003)] * 4 + [(1003, 1001)] * 4 + [(9, 70)],
+          [(897, 3588)] * 6 + [(3588, 897)] * 6 + [(65, 3)]]
+
+
+@pytest.mark.parametrize("param,grad,copy,shift", [("f32", "f32", True, 1),
+                                                   ("bf16", "bf16", False, 3)])
+@pytest.mark.parametrize("shapes", LARGER, ids=["640", "1500", "1000", "four"])
+def test_larger_contexts(shapes, param, grad, copy, shift):
+    u = matrices(shapes, 13, torch.float32 if grad == "f32" else torch.bfloat16)
+    opt = arc.Muon(shapes, param_dtype=param, grad_dtype=grad)
+    got = opt.orthogonalize(u)
+    again = opt.orthogonalize(u)
+    for k, (shape, x) in enumerate(zip(shapes, u)):
+        assert torch.equal(got[k], again[k]), "a call repeats its bits"
+        if k < 2 or k > len(shapes) - 3:
+            close_to(got[k], x, (k, shape))
+    run_steps(shapes, param, grad, copy, True, shift)
 
 
 def test_factors_that_are_not_finite_leave_everything():
