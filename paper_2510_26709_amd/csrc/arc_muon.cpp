@@ -261,7 +261,8 @@ constexpr Rates kRates[] = {{32, 0.10, 0.16, 0.5, 0.3},
                             {128, 0.66, 0.90, 6.7, 3.2}};
 constexpr double kLaunch = 5.0;
 constexpr int64_t kUnits = 256;
-// Tiles of 128 that fill the card so often that smaller ones are not looked at.
+// Tiles of 128, most of them full, that fill the card so often that smaller ones are not
+// looked at.
 constexpr int64_t kPlenty = 16 * 2 * kUnits;
 
 // The parts of each of `lines`, which descend, from number `from` on `parts` of them;
@@ -437,11 +438,15 @@ arc_muon plan_best(const arc_muon_config* cfg, const std::vector<float>& coeffic
   const auto grouped = sequence(coefficients, bounds, kTogether);
   arc_muon best;
   double least = INFINITY;
-  int64_t tiles = 0;  // of 128
-  for (int32_t i = 0; i < cfg->num_matrices; ++i)
-    tiles += (cfg->matrices[i].rows + 127) / 128 * ((cfg->matrices[i].cols + 127) / 128);
+  int64_t tiles = 0, full = 0;  // of 128
+  for (int32_t i = 0; i < cfg->num_matrices; ++i) {
+    const arc_muon_matrix& t = cfg->matrices[i];
+    tiles += up_to(t.rows, 128) / 128 * (up_to(t.cols, 128) / 128);
+    full += t.rows * t.cols / (128 * 128);
+  }
+  const bool plenty = full > kPlenty && full > tiles / 4 * 3;
   for (const Rates& r : kRates) {
-    if (r.side < 128 && tiles > kPlenty) continue;
+    if (r.side < 128 && plenty) continue;
     arc_muon c;
     const Times times = plan_muon(cfg, r, &c);
     const double one = times.of(plain), other = times.of(grouped);

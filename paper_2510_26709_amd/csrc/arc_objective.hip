@@ -310,7 +310,9 @@ hipError_t launch_preference(const PreferenceArgs& a, const PreferenceOutputs& o
                        scratch);
     return hipGetLastError();
   }
-  const int64_t groups = std::max<int64_t>(1, std::min<int64_t>(kTotalsGroups, a.pairs));
+  // (Without pairs there are rows to clear.)
+  const int64_t groups = std::max<int64_t>(
+      1, std::min<int64_t>(kTotalsGroups, a.pairs > 0 ? a.pairs : a.rows / kPartTokens));
   hipLaunchKernelGGL(preference_kernel, dim3((unsigned)groups), dim3(kThreads), 0, stream, a, out,
                      scratch);
   return hipGetLastError();

@@ -139,8 +139,9 @@ MANY = [(512, 2048), (2048, 512), (300, 1100), (1024, 1024), (1, 5), (0, 9), (12
 
 @pytest.mark.parametrize("param", ["f32", "bf16"])
 @pytest.mark.parametrize("shapes", [MANY, SHAPES[:-1], [(33, 65)] * 170 + [(70, 20)],
-                                    [(2048, 2048)], [(1100, 2500), (2500, 1100)]],
-                         ids=["many", "all", "batches", "square", "wide"])
+                                    [(2048, 2048)], [(1100, 2500), (2500, 1100)],
+                                    [(5, 3)] * 1000],
+                         ids=["many", "all", "batches", "square", "wide", "tiny"])
 def test_many_matrices(shapes, param):
     u = matrices(shapes, 5)
     opt = arc.Muon(shapes, param_dtype=param)

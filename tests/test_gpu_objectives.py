@@ -432,6 +432,19 @@ def test_preference_terms(lengths, o, outside):
     assert bool((d[:outside[0]] == 0).all()) and bool((d[T - outside[1]:] == 0).all())
 
 
+@pytest.mark.parametrize("lengths", [[], [1, 1]])
+def test_many_rows_outside_all_sequences(lengths):
+    s = pair_inputs(lengths, 2, 50, 100_003)
+    T = s["y"].numel()
+    head = arc.TokenLogProbs(V=10, rows=T, dtype="f32")
+    got = head.preference(s["logp"], s["y"], s["offsets"])
+    want = pair_formulas(s["logp"], s["y"], s["offsets"])
+    for name, x in got._asdict().items():
+        near(name, x, *want[name])
+    d = got.d_logp
+    assert bool((d[:50] == 0).all()) and bool((d[50 + sum(lengths):] == 0).all())
+
+
 def test_preference_leaves_out_what_has_no_part():
     s = pair_inputs([100, 50, 0, 2000, 30, 4], 8, 5, 9)
     head = arc.TokenLogProbs(V=10, rows=3000, dtype="f32")
