@@ -106,6 +106,35 @@ __device__ __forceinline__ void store_four(void* p, int64_t at, int32_t left,
   }
 }
 
+// The same for the N numbers that a lane holds of a row.
+template <bool BF16, bool FULL, int N>
+__device__ __forceinline__ void load_some(const void* p, int64_t at, int32_t left,
+                                          float (&x)[N]) {
+  if constexpr (N == 4) {
+    load_four<BF16, FULL>(p, at, left, x);
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] = FULL || k < left ? load_one<BF16>(p, at + k) : 0.f;
+  }
+}
+
+template <bool BF16, bool FULL, int N>
+__device__ __forceinline__ void store_some(void* p, int64_t at, int32_t left,
+                                           const float (&x)[N]) {
+  if constexpr (N == 4) {
+    store_four<BF16, FULL>(p, at, left, x);
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      if (!FULL && k >= left) break;
+      if constexpr (BF16)
+        static_cast<uint16_t*>(p)[at + k] = (uint16_t)bf16_pair(x[k], 0.f);
+      else
+        static_cast<float*>(p)[at + k] = x[k];
+    }
+  }
+}
+
 // hi in the low half, lo in the high one, of a number times kPairScale.
 __device__ __forceinline__ uint32_t pair_of(float scaled) {
   const _Float16 hi = (_Float16)scaled;
@@ -304,22 +333,58 @@ struct Shape<128> {
 };
 template <int SIDE>
 constexpr int kProductThreads = Shape<SIDE>::kWavesI * Shape<SIDE>::kWavesJ* kWave;
-// Results go through LDS, rows two words apart from each other: 16 columns of four
-// runs of eight rows then lie in 64 different banks.
 template <int SIDE>
-constexpr int kSlabPitch = SIDE + 2;
-template <int SIDE>
-constexpr int kProductLds =
-    std::max(Shape<SIDE>::kStages * 2 * SIDE * kLineBytes, SIDE* kSlabPitch<SIDE> * 4);
+constexpr int kProductLds = std::max(Shape<SIDE>::kStages * 2 * SIDE * kLineBytes, SIDE* SIDE * 4);
 
-// The numbers of eight pairs of a row, in units of 1 / kPairScale.
-__device__ __forceinline__ void load_8(const char* row, int32_t at, float (&x)[8]) {
-  const char* line = row + (int64_t)(at / kPairLine) * kLineBytes + at % kPairLine * 2;
-  const half8_t hi = *reinterpret_cast<const half8_t*>(line);
-  const half8_t lo = *reinterpret_cast<const half8_t*>(line + 2 * kPairLine);
-#pragma unroll
-  for (int k = 0; k < 8; ++k) x[k] = (float)hi[k] + (float)lo[k];
-}
+// N numbers that lie side by side in a row, `at` the first one's place: the hi and lo
+// halves of their pairs.
+template <int N>
+struct Halves {
+  static_assert(N == 1 || N == 2 || N == 4, "a lane's columns");
+  using Word = std::conditional_t<N == 1, uint16_t, std::conditional_t<N == 2, uint32_t, u32x2_t>>;
+  Word hi, lo;
+  static __device__ __forceinline__ int64_t place(int32_t at) {
+    return (int64_t)(at / kPairLine) * kLineBytes + at % kPairLine * 2;
+  }
+  __device__ __forceinline__ void load(const char* row, int32_t at) {
+    hi = *reinterpret_cast<const Word*>(row + place(at));
+    lo = *reinterpret_cast<const Word*>(row + place(at) + 2 * kPairLine);
+  }
+  __device__ __forceinline__ void store(char* row, int32_t at) const {
+    *reinterpret_cast<Word*>(row + place(at)) = hi;
+    *reinterpret_cast<Word*>(row + place(at) + 2 * kPairLine) = lo;
+  }
+  // In units of 1 / kPairScale.
+  __device__ __forceinline__ float number(int k) const {
+    return (float)half(hi, k) + (float)half(lo, k);
+  }
+  __device__ __forceinline__ void set(const uint32_t (&pair)[N]) {
+    if constexpr (N == 1) {
+      hi = (uint16_t)pair[0], lo = (uint16_t)(pair[0] >> 16);
+    } else if constexpr (N == 2) {
+      hi = low(pair[0], pair[1]), lo = high(pair[0], pair[1]);
+    } else {
+      hi = Word{low(pair[0], pair[1]), low(pair[2], pair[3])};
+      lo = Word{high(pair[0], pair[1]), high(pair[2], pair[3])};
+    }
+  }
+
+ private:
+  static __device__ __forceinline__ _Float16 half(const Word& w, int k) {
+    uint32_t v;
+    if constexpr (N == 4)
+      v = k < 2 ? w.x : w.y;
+    else
+      v = w;
+    return __builtin_bit_cast(_Float16, (uint16_t)(v >> (k % 2 * 16)));
+  }
+  static __device__ __forceinline__ uint32_t low(uint32_t a, uint32_t b) {
+    return (a & 0xFFFFu) | (b << 16);
+  }
+  static __device__ __forceinline__ uint32_t high(uint32_t a, uint32_t b) {
+    return (a >> 16) | (b & 0xFFFF0000u);
+  }
+};
 
 // Adds a tile's parts in their order, in the last workgroup to arrive; false: this is
 // not the last.  Parts are written through to where every compute unit sees them,
@@ -383,8 +448,9 @@ using PointersOf = std::conditional_t<WHAT == kMuonLast, MuonPointers, NoPointer
 // multiplied, wave priorities, rows an odd number of lines apart; 1 to 4% slower: no
 // products above the diagonal of symmetric tiles; tiles of 256 x 256 by eight waves
 // were even at sums of 4096 and slower at others, as nothing hides a workgroup's ends.
-// A tile's end (results through LDS, 64 bytes of a line together) is 13% of the time
-// with sums of 2048, a third with 640.
+// A tile's end is 13% of the time with sums of 2048, a third with 640.  Results go from
+// registers to their rows, 64 bytes of a line together, and only the transposed copy
+// through LDS: a 4096 x 4096 3470 us against 3540 with both through it.
 template <int SIDE, MuonKind WHAT>
 __global__ void __launch_bounds__(kProductThreads<SIDE>, Shape<SIDE>::kGroups)
 muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,
@@ -411,21 +477,25 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,
   const uint32_t pitch = (uint32_t)pair_pitch(sum);
   left += (int64_t)ti * SIDE * pitch;
   right += (int64_t)tj * SIDE * pitch;
-  const buffer_rsrc from[2] = {make_buffer(left, SIDE * pitch), make_buffer(right, SIDE * pitch)};
+  // The right side's rows are staged in the order 0, TJ, 2 TJ, .. 15 TJ, 1, TJ + 1, .. of
+  // each 16 TJ, so that a lane's columns of the result follow one another.
+  static_assert(kWaves % 2 == 0 && kLoads % 2 == 0, "a wave has one side, an even piece first");
+  const bool of_right = wave >= kWaves / 2;
+  const uint32_t apart = pitch * (of_right ? TJ : 1);
   uint32_t lane_at[2];  // in even and odd pieces of 8 rows
 #pragma unroll
   for (int q = 0; q < 2; ++q)
-    lane_at[q] = (uint32_t)(lane / 8) * pitch + (uint32_t)((lane % 8) ^ (4 * q + lane / 16)) * 16u;
-  static_assert(kLoads % 2 == 0, "a wave's first piece is an even one");
+    lane_at[q] = (uint32_t)(lane / 8) * apart + (uint32_t)((lane % 8) ^ (4 * q + lane / 16)) * 16u;
+  const buffer_rsrc from = make_buffer(of_right ? right : left, SIDE * pitch);
   const auto stage = [&](int32_t line) {
-    char* to = lds + line % kStages * kStage;
+    char* to = lds + line % kStages * kStage + wave * kLoads * 1024;
 #pragma unroll
     for (int q = 0; q < kLoads; ++q) {
-      const int piece = wave * kLoads + q;  // of 8 rows; the first half are left's
-      const int rows = piece % (SIDE / 8) * 8;
-      load_lds(from[piece / (SIDE / 8)], lane_at[q % 2],
-               (uint32_t)rows * pitch + (uint32_t)(at.first + line) * kLineBytes,
-               to + piece * 1024);
+      const int piece = (of_right ? wave - kWaves / 2 : wave) * kLoads + q;
+      const int first = of_right ? piece / (2 * TJ) * 16 * TJ + piece % 2 * 8 * TJ + piece / 2 % TJ
+                                 : piece * 8;
+      load_lds(from, lane_at[q % 2],
+               (uint32_t)first * pitch + (uint32_t)(at.first + line) * kLineBytes, to + q * 1024);
     }
   };
   f32x4_t acc[TI][TJ];
@@ -474,108 +544,103 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,
     multiply(ll, rh);
   }
   if (at.parts > 1 && !join_parts<SIDE>(a, at, acc)) return;
-  // Lane l holds column l % 16 of a 16 x 16 tile, element k in row 4 (l / 16) + k.
-  constexpr int kThread = kWaves * kWave, kPitch = kSlabPitch<SIDE>;
-  float* slab = reinterpret_cast<float*>(lds);
-  const int32_t r0 = ti * SIDE, c0 = tj * SIDE;
-  const auto to_slab = [&] {
-    __syncthreads();  // the stages are read
-#pragma unroll
-    for (int i = 0; i < TI; ++i)
-#pragma unroll
-      for (int j = 0; j < TJ; ++j)
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          slab[((wi * TI + i) * 16 + 4 * quarter + k) * kPitch + (wj * TJ + j) * 16 + row] =
-              acc[i][j][k];
-    __syncthreads();
-  };
+  // Lane l holds columns TJ (l % 16) + j of its wave's result and rows 16 i + 4 (l / 16)
+  // + k: TJ numbers that follow one another in a row, 16 lanes' together whole lines.
+  const int32_t r0 = ti * SIDE + wi * TI * 16 + 4 * quarter;
+  const int32_t c0 = tj * SIDE + wj * TJ * 16 + row * TJ;
   if constexpr (WHAT == kMuonLast) {
-    // A thread has all its loads in flight together, and whole lines are read and
-    // written.
     if (skipped(a)) return;
-    constexpr int kAcross = SIDE / 4, kDown = kThread / kAcross, kPasses = SIDE / kDown;
     const int32_t q = at.matrix - a.first;
     const float step = a.lr * t.lr_scale;
     const float keep = 1.f - step * t.weight_decay;
     void* param = p.param[q];
     uint16_t* copy = p.copy[q];
-    const int32_t down = (int)threadIdx.x / kAcross, across = (int)threadIdx.x % kAcross * 4;
-    const int32_t left = t.cols - c0 - across;
-    const int32_t r = r0 + down;
-    const int64_t e0 = (int64_t)r * t.cols + c0 + across;
-    const auto passes = [&](auto bf16, auto whole) {
+    const int32_t left = t.cols - c0;
+    const auto rows = [&](auto bf16, auto whole) {
       constexpr bool BF16 = decltype(bf16)::value, FULL = decltype(whole)::value;
-      float x[kPasses][4];
+      float x[TI][4][TJ];  // all loads are in flight together
       if (a.update)
 #pragma unroll
-        for (int q = 0; q < kPasses; ++q)
-          if (FULL || r + q * kDown < t.rows)
-            load_four<BF16, FULL>(param, e0 + (int64_t)q * kDown * t.cols, left, x[q]);
-      to_slab();
+        for (int i = 0; i < TI; ++i)
 #pragma unroll
-      for (int q = 0; q < kPasses; ++q) {
-        if (!FULL && r + q * kDown >= t.rows) continue;
-        const float* of = slab + (q * kDown + down) * kPitch + across;
-        float v[4];
+          for (int k = 0; k < 4; ++k)
+            if (FULL || r0 + 16 * i + k < t.rows)
+              load_some<BF16, FULL>(param, (int64_t)(r0 + 16 * i + k) * t.cols + c0, left, x[i][k]);
+#pragma unroll
+      for (int i = 0; i < TI; ++i)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          v[k] = of[k] * s.scale;
-          if (a.update) v[k] = fmaf(-step, v[k], x[q][k] * keep);
+          if (!FULL && r0 + 16 * i + k >= t.rows) continue;
+          float v[TJ];
+#pragma unroll
+          for (int j = 0; j < TJ; ++j) {
+            v[j] = acc[i][j][k] * s.scale;
+            if (a.update) v[j] = fmaf(-step, v[j], x[i][k][j] * keep);
+          }
+          const int64_t e = (int64_t)(r0 + 16 * i + k) * t.cols + c0;
+          store_some<BF16, FULL>(param, e, left, v);
+          if (copy) store_some<true, FULL>(copy, e, left, v);
         }
-        const int64_t e = e0 + (int64_t)q * kDown * t.cols;
-        store_four<BF16, FULL>(param, e, left, v);
-        if (copy) store_four<true, FULL>(copy, e, left, v);
-      }
     };
     choose(t.param_bf16, [&](auto bf16) {
-      choose(r0 + SIDE <= t.rows && c0 + SIDE <= t.cols,
-             [&](auto whole) { passes(bf16, whole); });
+      choose((ti + 1) * SIDE <= t.rows && (tj + 1) * SIDE <= t.cols,
+             [&](auto whole) { rows(bf16, whole); });
     });
   } else {
-    char* to = array(s.out);
-    char* turned = array(s.turned);
-    const int64_t to_pitch = pair_pitch(WHAT == kMuonApply ? at.np : at.mp);
-    const int64_t turned_pitch = pair_pitch(at.mp);
-    const bool mirror = WHAT == kMuonApply || ti != tj;
-    to_slab();
-    // Rows as they are, eight numbers a thread and pass; the pairs take the numbers'
-    // places.
-    constexpr int kRuns = SIDE / 8;
-#pragma unroll 4
-    for (int u = threadIdx.x; u < SIDE * kRuns; u += kThread) {
-      const int r = u / kRuns, c = u % kRuns * 8;
-      float* of = slab + r * kPitch + c;
-      float x[8];
+    const int64_t out_pitch = pair_pitch(WHAT == kMuonApply ? at.np : at.mp);
+    char* out = array(s.out) + r0 * out_pitch;
+    uint32_t pair[TI][TJ][4];
+    Halves<TJ> square[TI][4];  // of X X', for a step's polynomial of it
+    if constexpr (WHAT == kMuonStep)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = of[k] * s.scale;
-      if constexpr (WHAT == kMuonStep) {
-        float square[8];
-        load_8(array(s.left) + (r0 + r) * to_pitch, c0 + c, square);
+      for (int i = 0; i < TI; ++i)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          x[k] = fmaf(s.c, x[k], s.b * square[k]);
-          if (r0 + r == c0 + c + k) x[k] += s.a * kPairScale;
+        for (int k = 0; k < 4; ++k)
+          square[i][k].load(array(s.left) + (r0 + 16 * i + k) * out_pitch, c0);
+#pragma unroll
+    for (int i = 0; i < TI; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint32_t side_by_side[TJ];
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) {
+          float x = acc[i][j][k] * s.scale;
+          if constexpr (WHAT == kMuonStep) {
+            x = fmaf(s.c, x, s.b * square[i][k].number(j));
+            if (r0 + 16 * i + k == c0 + j) x += s.a * kPairScale;
+          }
+          side_by_side[j] = pair[i][j][k] = pair_of(x);
         }
+        Halves<TJ> h;
+        h.set(side_by_side);
+        h.store(out + (16 * i + k) * out_pitch, c0);
       }
-      uint32_t v[8];
+    if (WHAT != kMuonApply && ti == tj) return;
+    // And transposed, through LDS: a column's rows follow one another there, in pieces of
+    // four, which 16 lanes write and read from different banks.
+    u32x4_t* slab = reinterpret_cast<u32x4_t*>(lds);
+    constexpr int kPieces = SIDE / 4, kTurn = TJ > 2 ? TJ : 2, kTurns = kPieces < 16 ? kPieces : 16;
+    const auto place = [=](int32_t column, int32_t piece) {
+      return column * kPieces + (piece ^ (column / kTurn % kTurns));
+    };
+    __syncthreads();  // the stages are read
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = pair_of(x[k]);
-      store_8(to + (r0 + r) * to_pitch, c0 + c, v);
-      if (mirror)
+    for (int i = 0; i < TI; ++i)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) of[k] = __uint_as_float(v[k]);
-    }
-    if (!mirror) return;
+      for (int j = 0; j < TJ; ++j)
+        slab[place((wj * 16 + row) * TJ + j, (wi * TI + i) * 4 + quarter)] =
+            u32x4_t{pair[i][j][0], pair[i][j][1], pair[i][j][2], pair[i][j][3]};
     __syncthreads();
-    // And transposed, four threads to a line.
+    const int64_t turned_pitch = pair_pitch(at.mp);
+    char* turned = array(s.turned) + tj * SIDE * turned_pitch;
+    constexpr int kThread = kWaves * kWave;
 #pragma unroll 4
-    for (int u = threadIdx.x; u < SIDE * kRuns; u += kThread) {
-      const int c = u / 4 % SIDE, r = u / (4 * SIDE) * 32 + u % 4 * 8;
-      uint32_t v[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = __float_as_uint(slab[(r + k) * kPitch + c]);
-      store_8(turned + (c0 + c) * turned_pitch, r0 + r, v);
+    for (int u = threadIdx.x; u < SIDE * SIDE / 8; u += kThread) {  // four threads to a line
+      const int n = u / 4 % SIDE, r = u / (4 * SIDE) * 32 + u % 4 * 8;
+      const int column = n % 32 * TJ + n / 32;
+      const u32x4_t x = slab[place(column, r / 4)], y = slab[place(column, r / 4 + 1)];
+      const uint32_t v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+      store_8(turned + column * turned_pitch, ti * SIDE + r, v);
     }
   }
 }
