@@ -20,11 +20,11 @@ namespace arc {
 struct MuonGroup {
   int32_t first = 0, count = 0;
   int64_t first_run = 0, runs = 0;
-  struct Range {
+  struct Range {  // their tiles in the context's list, and those tiles' sides
     int64_t at = 0, count = 0;
+    int32_t side = kSplitTile;
   };
-  Range split;        // their tiles in the context's list
-  Range gram, half, whole;
+  Range split, gram, half, whole;
 };
 
 struct MuonLaunch {
@@ -44,9 +44,8 @@ struct arc_muon {
   std::vector<arc::MuonLaunch> plain, grouped;
   bool group = false;     // the second one takes less time
   bool any_f32 = false;   // a parameter is binary32
-  int32_t side = 128;
   int64_t state_elems = 0, workspace_bytes = 0;
-  int64_t parts = 0;  // most of one launch
+  int64_t parts = 0, part_elems = 0;  // most of one launch
   hipStream_t stream = nullptr;
   int device = 0;
   arc::MuonMatrix* matrices_dev = nullptr;
@@ -250,15 +249,16 @@ void each_tile(int32_t rows, int32_t cols, bool half, const Add& add) {
 // 4096 7870, 4500 and 3600.  Step by step and in runs: 257 x 1001 123 and 123, the
 // convolutions 489 and 363, width 640 2860 and 2140, 4096 x 4096 3597 and 3765.  What is
 // chosen was within 3% of the best of the six in 48 of 51 drawn cases, and within 16% in
-// all.  Split sums: X X' of a ResNet-18's convolutions (sums of 4608 in few tiles) 40 us
-// against 103.
+// all.  Each product has a side of its own: of 40 drawn cases 14 take 2 to 13% less than
+// with one side for all (a ResNet-18's 344 against 360), the others the same to 2%.  Split
+// sums: X X' of a ResNet-18's convolutions (sums of 4608 in few tiles) 40 us against 103.
 struct Rates {
   int32_t side;
   double line, alone, result, part;
 };
-constexpr Rates kRates[] = {{32, 0.10, 0.16, 0.5, 0.3},
+constexpr Rates kRates[] = {{128, 0.66, 0.90, 6.7, 3.2},
                             {64, 0.24, 0.32, 1.7, 0.8},
-                            {128, 0.66, 0.90, 6.7, 3.2}};
+                            {32, 0.10, 0.16, 0.5, 0.3}};
 constexpr double kLaunch = 5.0;
 constexpr int64_t kUnits = 256;
 // Tiles of 128, most of them full, that fill the card so often that smaller ones are not
@@ -343,38 +343,68 @@ struct Times {
   }
 };
 
-// The tables of a checked configuration for tiles of a side (may throw
-// std::bad_alloc).
-Times plan_muon(const arc_muon_config* cfg, const Rates& rates, arc_muon* c) {
-  const int32_t side = rates.side;
-  c->side = side;
+// The tables of a checked configuration whose matrices' sides are rounded up to
+// multiples of `whole_of` (may throw std::bad_alloc).
+Times plan_muon(const arc_muon_config* cfg, int32_t whole_of, arc_muon* c) {
   Times times;
-  std::vector<arc::MuonTile> split, gram, half, whole;
   arc::MuonGroup g;
   int64_t bytes = 0, runs = 0;
-  const auto finish = [&] {
-    if (g.count == 0) return;
-    const auto take = [&](std::vector<arc::MuonTile>& from, arc::MuonGroup::Range* range) {
-      range->at = static_cast<int64_t>(c->tiles.size());
-      range->count = static_cast<int64_t>(from.size());
-      for (const int64_t k : launch_order(range->count))
-        c->tiles.push_back(from[static_cast<size_t>(k)]);
-      from.clear();
-    };
-    take(split, &g.split);
-    const auto product = [&](std::vector<arc::MuonTile>& tiles, arc::MuonGroup::Range* range) {
+  // A product's tiles of a side: of m x n or m x m (half of them) results.
+  const auto tiles_of = [&](int32_t side, bool whole, bool long_sum) {
+    std::vector<arc::MuonTile> list;
+    for (int32_t i = g.first; i < g.first + g.count; ++i) {
+      const arc::MuonMatrix& t = c->matrices[static_cast<size_t>(i)];
+      if (t.m == 0) continue;
+      const int32_t lines = (long_sum ? t.np : t.mp) / arc::kPairLine;
+      each_tile(t.mp / side, (whole ? t.np : t.mp) / side, !whole, [&](int32_t a, int32_t b) {
+        list.push_back({i, a, b, 0, lines, 0, 1, 0, t.base, t.mp, t.np});
+      });
+    }
+    return list;
+  };
+  const auto take = [&](const std::vector<arc::MuonTile>& from, arc::MuonGroup::Range* range) {
+    range->at = static_cast<int64_t>(c->tiles.size());
+    range->count = static_cast<int64_t>(from.size());
+    for (const int64_t k : launch_order(range->count))
+      c->tiles.push_back(from[static_cast<size_t>(k)]);
+  };
+  // The tiles that are expected to take the least time.
+  const auto product = [&](bool whole, bool long_sum, arc::MuonGroup::Range* range) {
+    std::vector<arc::MuonTile> best;
+    double least = INFINITY;
+    int64_t parts = 0;
+    for (const Rates& r : kRates) {
+      if (r.side > whole_of) continue;
+      std::vector<arc::MuonTile> tiles = tiles_of(r.side, whole, long_sum);
+      const auto count = static_cast<int64_t>(tiles.size());
       // the longest sums first, so that short ones fill the end
       std::stable_sort(tiles.begin(), tiles.end(),
                        [](const arc::MuonTile& x, const arc::MuonTile& y) {
                          return x.lines > y.lines;
                        });
-      const double t = plan_product(rates, &tiles, &c->parts);
-      take(tiles, range);
-      return t;
-    };
-    times.gram += product(gram, &g.gram);
-    times.half += product(half, &g.half);
-    times.whole += product(whole, &g.whole);
+      int64_t places = 0;
+      const double t = plan_product(r, &tiles, &places);
+      if (t < least) {
+        least = t;
+        parts = places;
+        range->side = r.side;
+        best.swap(tiles);
+      }
+      if (count > kPlenty) break;
+    }
+    c->parts = std::max(c->parts, parts);
+    c->part_elems = std::max(c->part_elems, parts * range->side * range->side);
+    take(best, range);
+    return least;
+  };
+  const auto finish = [&] {
+    if (g.count == 0) return;
+    std::vector<arc::MuonTile> split = tiles_of(arc::kSplitTile, true, false);
+    for (arc::MuonTile& t : split) t.lines = 0;
+    take(split, &g.split);
+    times.gram += product(false, true, &g.gram);
+    times.half += product(false, false, &g.half);
+    times.whole += product(true, false, &g.whole);
     g.runs = runs - g.first_run;
     c->groups.push_back(g);
     c->workspace_bytes = std::max(c->workspace_bytes, bytes);
@@ -388,7 +418,6 @@ Times plan_muon(const arc_muon_config* cfg, const Rates& rates, arc_muon* c) {
     t.tall = in.rows > in.cols;
     t.m = std::min(t.rows, t.cols);
     t.n = std::max(t.rows, t.cols);
-    const int32_t whole_of = std::max(side, arc::kSplitTile);
     t.mp = static_cast<int32_t>(up_to(t.m, whole_of));
     t.np = static_cast<int32_t>(count > 0 ? up_to(t.n, whole_of) : 0);
     t.param_bf16 = in.param_dtype == ARC_DTYPE_BF16;
@@ -415,22 +444,12 @@ Times plan_muon(const arc_muon_config* cfg, const Rates& rates, arc_muon* c) {
     bytes += need;
     if (count > 0 && !t.param_bf16) c->any_f32 = true;
     c->matrices.push_back(t);
-    if (count == 0) continue;
-    const auto to = [&](std::vector<arc::MuonTile>* list, int32_t sum) {
-      return [=](int32_t a, int32_t b) {
-        list->push_back({i, a, b, 0, sum / arc::kPairLine, 0, 1, 0, t.base, t.mp, t.np});
-      };
-    };
-    each_tile(t.mp / arc::kSplitTile, t.np / arc::kSplitTile, false, to(&split, 0));
-    each_tile(t.mp / side, t.mp / side, true, to(&gram, t.np));
-    each_tile(t.mp / side, t.mp / side, true, to(&half, t.mp));
-    each_tile(t.mp / side, t.np / side, false, to(&whole, t.mp));
   }
   finish();
   return times;
 }
 
-// The side, and the way to go through the steps, whose products are expected to take
+// The plan, and the way to go through the steps, whose products are expected to take
 // the least time.
 arc_muon plan_best(const arc_muon_config* cfg, const std::vector<float>& coefficients,
                    const std::vector<double>& bounds) {
@@ -445,10 +464,10 @@ arc_muon plan_best(const arc_muon_config* cfg, const std::vector<float>& coeffic
     full += t.rows * t.cols / (128 * 128);
   }
   const bool plenty = full > kPlenty && full > tiles / 4 * 3;
-  for (const Rates& r : kRates) {
-    if (r.side < 128 && plenty) continue;
+  for (const int32_t whole_of : {128, arc::kSplitTile}) {
+    if (whole_of < 128 && plenty) continue;
     arc_muon c;
-    const Times times = plan_muon(cfg, r, &c);
+    const Times times = plan_muon(cfg, whole_of, &c);
     const double one = times.of(plain), other = times.of(grouped);
     c.group = other < 0.97 * one;
     if (std::min(one, other) < least) {
@@ -496,7 +515,7 @@ arc_status enqueue(const arc_muon* c, arc::MuonArgs a, void* const* params,
       const auto& range = l.kind == arc::kMuonGram ? g.gram
                           : l.kind == arc::kMuonStep || l.kind == arc::kMuonHalf ? g.half
                                                                                  : g.whole;
-      ARC_HIP(arc::launch_muon_product(l.kind, c->side, a, p, l.product, c->tiles_dev + range.at,
+      ARC_HIP(arc::launch_muon_product(l.kind, range.side, a, p, l.product, c->tiles_dev + range.at,
                                        range.count, c->stream),
               "product launch");
     }
@@ -547,7 +566,7 @@ arc_status arc_muon_create(const arc_muon_config* cfg, void* hip_stream, arc_muo
   };
   room(&c->sums_dev, c->run_matrix.size() * sizeof(double));
   room(&c->workspace, static_cast<size_t>(c->workspace_bytes));
-  room(&c->parts_dev, static_cast<size_t>(c->parts * c->side * c->side) * sizeof(float));
+  room(&c->parts_dev, static_cast<size_t>(c->part_elems) * sizeof(float));
   room(&c->arrived_dev, static_cast<size_t>(c->parts) * sizeof(uint32_t));
   if (e == hipSuccess && c->parts > 0)
     e = hipMemset(c->arrived_dev, 0, static_cast<size_t>(c->parts) * sizeof(uint32_t));

@@ -42,7 +42,10 @@ static bool refused(arc_status s) { return s == ARC_ERR_INVALID && !arc::why.emp
 // ---------------------------------------------------------------- plans
 
 static void check_list(const arc_muon& c, const arc::MuonGroup& g,
-                       const arc::MuonGroup::Range& range, int32_t side, int what) {
+                       const arc::MuonGroup::Range& range, int32_t whole_of, int what) {
+  const int32_t side = range.side;
+  CHECK((what == 0 ? side == arc::kSplitTile : side == 32 || side == 64 || side == 128) &&
+        side <= whole_of);
   std::map<std::tuple<int32_t, int32_t, int32_t>, std::vector<arc::MuonTile>> seen;
   CHECK(range.at >= 0 && range.at + range.count <= static_cast<int64_t>(c.tiles.size()));
   for (int64_t k = range.at; k < range.at + range.count; ++k) {
@@ -79,6 +82,7 @@ static void check_list(const arc_muon& c, const arc::MuonGroup& g,
           }
           if (t.parts > 1) {
             CHECK(t.place + t.part < c.parts && places.insert(t.place + t.part).second);
+            CHECK(int64_t{t.place + t.part + 1} * side * side <= c.part_elems);
           }
         }
         for (const bool x : taken) CHECK(x);
@@ -90,9 +94,9 @@ static void check_list(const arc_muon& c, const arc::MuonGroup& g,
 static void check_plan(const std::vector<arc_muon_matrix>& list) {
   const arc_muon_config cfg{list.data(), nullptr, static_cast<int32_t>(list.size()), 5, 0};
   CHECK(check_muon(&cfg) == ARC_OK);
-  for (const Rates& r : kRates) {
+  for (const int32_t whole_of : {64, 128}) {
     arc_muon c;
-    const Times times = plan_muon(&cfg, r, &c);
+    const Times times = plan_muon(&cfg, whole_of, &c);
     CHECK(std::isfinite(times.gram + times.half + times.whole));
     CHECK(c.matrices.size() == list.size());
     int64_t state = 0, runs = 0;
@@ -110,7 +114,7 @@ static void check_plan(const std::vector<arc_muon_matrix>& list) {
         runs += m.runs;
         CHECK(int64_t{m.runs} * arc::kMuonRun >= count);
         if (count == 0) continue;
-        CHECK(m.mp % r.side == 0 && m.np % r.side == 0 && m.mp >= m.m && m.np >= m.n);
+        CHECK(m.mp % whole_of == 0 && m.np % whole_of == 0 && m.mp >= m.m && m.np >= m.n);
         CHECK(m.base >= end && m.base % 256 == 0);
         // the arrays of a matrix, one after the other
         for (int32_t k = 0; k < arc::kMuonArrays; ++k) {
@@ -124,10 +128,10 @@ static void check_plan(const std::vector<arc_muon_matrix>& list) {
         CHECK(end <= c.workspace_bytes);
       }
       CHECK(g.runs == runs - g.first_run);
-      check_list(c, g, g.split, arc::kSplitTile, 0);
-      check_list(c, g, g.gram, r.side, 1);
-      check_list(c, g, g.half, r.side, 2);
-      check_list(c, g, g.whole, r.side, 3);
+      check_list(c, g, g.split, whole_of, 0);
+      check_list(c, g, g.gram, whole_of, 1);
+      check_list(c, g, g.half, whole_of, 2);
+      check_list(c, g, g.whole, whole_of, 3);
     }
     CHECK(next == static_cast<int32_t>(list.size()) && c.state_elems == state);
     CHECK(static_cast<int64_t>(c.run_matrix.size()) == runs);
