@@ -17,12 +17,21 @@ struct PolicyTerm {
   bool clipped;
 };
 
-// e^x - x - 1 without the difference that cancels it near 0: its series up to
-// |x| = 1/2 (what is left out is 2^-28 of the value), where the plain difference
-// of binary32 numbers would lose two bits and, further in, all.
-__device__ __forceinline__ float exp_beyond_line(float x, float exp_minus_1) {
-  if (!(fabsf(x) < 0.5f)) return exp_minus_1 == INFINITY ? INFINITY : exp_minus_1 - x;
-  float s = 1.f / 362880.f;
+struct ExpBeyond {
+  float one, line;  // e^x - 1, e^x - 1 - x
+};
+
+// Without the differences that cancel them near 0: up to |x| = 1 by e^x's series (what is
+// left out is 2^-27 of the value), where the plain difference of binary32 numbers would
+// lose two bits and, further in, all.
+__device__ __forceinline__ ExpBeyond exp_beyond(float x) {
+  if (!(fabsf(x) < 1.f)) {
+    const float e = expf(x);
+    return {e - 1.f, e == INFINITY ? INFINITY : e - 1.f - x};
+  }
+  float s = 1.f / 39916800.f;
+  s = fmaf(s, x, 1.f / 3628800.f);
+  s = fmaf(s, x, 1.f / 362880.f);
   s = fmaf(s, x, 1.f / 40320.f);
   s = fmaf(s, x, 1.f / 5040.f);
   s = fmaf(s, x, 1.f / 720.f);
@@ -30,7 +39,8 @@ __device__ __forceinline__ float exp_beyond_line(float x, float exp_minus_1) {
   s = fmaf(s, x, 1.f / 24.f);
   s = fmaf(s, x, 1.f / 6.f);
   s = fmaf(s, x, 0.5f);
-  return s * x * x;
+  s = s * x * x;
+  return {x + s, s};
 }
 
 // What a token's terms are made of.
@@ -64,12 +74,11 @@ __device__ __forceinline__ PolicyTerm policy_term(const PolicyArgs& p, const Pol
   float d = t.clipped ? 0.f : -t.ratio * A;
   t.loss = -gain;
   if (p.ref_logp) {
-    const float away = of.ref_logp - logp;
-    const float grown = expm1f(away);
-    t.kl = exp_beyond_line(away, grown);
+    const ExpBeyond grown = exp_beyond(of.ref_logp - logp);
+    t.kl = grown.line;
     if (p.kl != 0.f) {
       t.loss = fmaf(p.kl, t.kl, t.loss);
-      d = fmaf(-p.kl, grown, d);
+      d = fmaf(-p.kl, grown.one, d);
     }
   }
   if (p.entropy != 0.f) t.loss = fmaf(-p.entropy, H, t.loss);
