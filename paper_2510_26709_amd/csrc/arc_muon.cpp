@@ -215,15 +215,17 @@ arc_status check_muon(const arc_muon_config* cfg) {
 }
 
 // Which element of a list each workgroup takes: they go to the eight XCDs in turn,
-// and runs of 32 neighbours to the same one, whose L2 then holds what they share.
+// and runs of neighbours to the same one, whose L2 then holds what they share: runs of
+// 32, and shorter ones towards the end, so that every XCD gets as many.
 std::vector<int64_t> launch_order(int64_t count) {
-  constexpr int64_t kXcds = 8, kRun = 32;
+  constexpr int64_t kXcds = 8;
   std::vector<int64_t> order(static_cast<size_t>(count));
-  const int64_t even = count / (kXcds * kRun) * (kXcds * kRun);
-  for (int64_t b = 0; b < count; ++b) {
-    const int64_t x = b % kXcds, q = b / kXcds;
-    order[static_cast<size_t>(b)] = b < even ? (q / kRun * kXcds + x) * kRun + q % kRun : b;
-  }
+  int64_t from = 0;
+  for (int64_t run = 32; run > 0; run /= 2)
+    for (; count - from >= kXcds * run; from += kXcds * run)
+      for (int64_t b = 0; b < kXcds * run; ++b)
+        order[static_cast<size_t>(from + b)] = from + b % kXcds * run + b / kXcds;
+  for (; from < count; ++from) order[static_cast<size_t>(from)] = from;
   return order;
 }
 
