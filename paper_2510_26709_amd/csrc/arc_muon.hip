@@ -164,6 +164,9 @@ __device__ __forceinline__ double group_sum(double v) {
   return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
+// The new momenta and the squares of U, a workgroup for each 8192 elements of a matrix
+// (their sums are added in order by whoever needs the norm).  HBM: 1.76e8 elements with
+// bf16 gradients (10 bytes) 299 us, 5.9 TB/s; 5.9e7 in binary32 (12) 119, 6.0.
 __global__ void __launch_bounds__(kThreads)
 muon_momentum_kernel(MuonArgs a, MuonPointers p, const int32_t* __restrict__ run_matrix,
                      int64_t first_run) {
@@ -233,6 +236,10 @@ __device__ __forceinline__ void store_8(char* row, int32_t at, const uint32_t (&
   *reinterpret_cast<u32x4_t*>(line + 2 * kPairLine) = u32x4_t{lo[0], lo[1], lo[2], lo[3]};
 }
 
+// X and its transpose in pairs, a workgroup for each 64 x 64 of a matrix.  The norm has to
+// be known first, so that U is read, and made of the momentum, a second time.  HBM, more
+// than half of it writes: 1.76e8 elements with bf16 gradients (6 bytes read, 8 written)
+// 494 us, 5.0 TB/s; 5.9e7 in binary32 (8, 8) 183, 5.2.
 __global__ void __launch_bounds__(kThreads)
 muon_split_kernel(MuonArgs a, MuonPointers p, const MuonTile* __restrict__ tiles) {
   constexpr int S = kSplitTile;
@@ -438,19 +445,24 @@ using PointersOf = std::conditional_t<WHAT == kMuonLast, MuonPointers, NoPointer
 // at a time, staged in LDS: row r's 16-byte pieces lie at piece ^ (r / 2 % 8), so
 // that 16 rows' pieces, which are read together, lie in different banks.
 //
-// Bound by the matrix units at the clock that the card's power leaves them (1.7 GHz of
-// 2.4; of a matrix of zeros the same products take 0.7 of the time): 4096^3 in 323 to
-// 360 us, 1140 to 1280 TFLOP/s of binary16 products, where the library's plain binary16
-// product runs at 1390; small contexts are bound by latency, 4 us a launch with tiles
-// of 32 and 5 to 6 with tiles of 64 (five steps of a few vectors 63 and 73 us).  Hence 16 x 16 x 32 instructions, which read and write each binary32 sum once
-// for 32 terms: with 32 x 32 x 16 (16 terms) a 4096 x 4096 took 3.96 ms against 3.61.
-// Within 1% either way, timed in turn: the next line's pairs read while one is
-// multiplied, wave priorities, rows an odd number of lines apart; 1 to 4% slower: no
-// products above the diagonal of symmetric tiles; tiles of 256 x 256 by eight waves
-// were even at sums of 4096 and slower at others, as nothing hides a workgroup's ends.
-// A tile's end is 13% of the time with sums of 2048, a third with 640.  Results go from
-// registers to their rows, 64 bytes of a line together, and only the transposed copy
-// through LDS: a 4096 x 4096 3470 us against 3540 with both through it.
+// Large sums are bound by the matrix units at the clock that the card's power leaves them
+// (1.6 GHz of 2.4; of zeros the same products take 0.8 of the time): P X of 4096^3 in 320
+// us, 1260 TFLOP/s of binary16 products, where the library's plain binary16 product runs
+// at 1390.  With short sums the ends count: 48 matrices of width 640 take P X in 282 us,
+// of which 179 are the sums (1260 TFLOP/s again) and 90 the writing of X both ways (472
+// MB, 5.2 TB/s), one after the other though two workgroups share a compute unit; starting
+// them apart, priorities and fewer stores in flight made no difference.  Small contexts
+// are bound by latency, 4 us a launch with tiles of 32 and 5 to 6 with tiles of 64 (five
+// steps of a few vectors 63 and 73 us).
+//
+// Hence 16 x 16 x 32 instructions, which read and write each binary32 sum once for 32
+// terms: with 32 x 32 x 16 (16 terms) a 4096 x 4096 took 3.96 ms against 3.61.  Within 1%
+// either way, timed in turn: the next line's pairs read while one is multiplied, wave
+// priorities, rows an odd number of lines apart; 1 to 4% slower: no products above the
+// diagonal of symmetric tiles; tiles of 256 x 256 by eight waves were even at sums of 4096
+// and slower at others, as nothing hides a workgroup's ends.  Results go from registers to
+// their rows, 64 bytes of a line together, and only the transposed copy through LDS: a
+// 4096 x 4096 3470 us against 3540 with both through it.
 template <int SIDE, MuonKind WHAT>
 __global__ void __launch_bounds__(kProductThreads<SIDE>, Shape<SIDE>::kGroups)
 muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,

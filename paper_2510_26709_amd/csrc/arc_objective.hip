@@ -51,7 +51,11 @@ __device__ __forceinline__ void store_four(float* p, int64_t i, int64_t left,
   }
 }
 
-// Four tokens a thread and pass, every array in 16 bytes a lane.
+// Four tokens a thread and pass, every array in 16 bytes a lane.  With a reference, old
+// log probabilities and weights 28 bytes of a token are read and 16 written: 4,000,003
+// take 38.5 us, 4.6 TB/s, as much as a copy of 256 MB reaches (4.7).  Single words a lane
+// took 62 us; twice as many workgroups 46, for the totals of each; the next pass's loads
+// ahead 41.  Up to some thousand tokens it is a launch's latency, 4 us.
 __global__ void __launch_bounds__(kThreads)
 policy_kernel(PolicyArgs p, PolicyRows r, PolicyOutputs out, ObjectiveScratch* scratch) {
   double sums[kPolicyTotals] = {};
@@ -214,7 +218,10 @@ __device__ __forceinline__ void clear_outside(const PreferenceArgs& a, float* d_
   for (int64_t i = tail + at; i < a.rows; i += step) d_logp[i] = 0.f;
 }
 
-// A workgroup takes whole pairs: both sums, then both gradients.
+// A workgroup takes whole pairs: both sums, then both gradients (16 bytes of a token read,
+// 4 written).  Bound by latency: the offsets, the tokens of both sequences at once, the
+// sums over the workgroup, and the targets once more take 5 us, 16 pairs of up to 700
+// tokens 7.7.
 __global__ void __launch_bounds__(kThreads)
 preference_kernel(PreferenceArgs a, PreferenceOutputs out, ObjectiveScratch* scratch) {
   double totals[kPreferenceTotals] = {};
@@ -236,7 +243,8 @@ preference_kernel(PreferenceArgs a, PreferenceOutputs out, ObjectiveScratch* scr
 }
 
 // Few pairs of long sequences: `parts` workgroups for each sequence, one launch
-// for the sums and one for the gradients.
+// for the sums and one for the gradients, as a gradient needs both sequences' sums: 3 us
+// each, 600,002 tokens 11.5 (1390 by one workgroup).
 __device__ __forceinline__ Sequence part_of(const Sequence& s, int32_t part, int32_t parts) {
   const int64_t run = ((s.last - s.first + parts - 1) / parts + kThreads - 1) / kThreads * kThreads;
   const int64_t first = min(s.first + part * run, s.last);
@@ -297,11 +305,16 @@ hipError_t launch_policy_terms(const PolicyArgs& p, const PolicyRows& r, const P
 
 hipError_t launch_preference(const PreferenceArgs& a, const PreferenceOutputs& out,
                              ObjectiveScratch* scratch, hipStream_t stream) {
-  // Parts of a sequence of at least 2048 tokens on average, where there are few.
-  constexpr int64_t kPartTokens = 2048;
-  const int64_t most = a.pairs > 0 ? kTotalsGroups / (2 * a.pairs) : 0;
-  const int64_t parts =
-      a.pairs > 0 ? std::min<int64_t>(most, a.rows / (2 * a.pairs) / kPartTokens) : 0;
+  // Sequences of more than 1280 tokens on average are taken in parts of 256 or more, by two
+  // launches.  us in one launch and in two, pairs x tokens of a sequence: 1 x 600 5.5 / 7.1,
+  // 16 x 700 7.7 / 9.1, 1 x 1500 7.8 / 7.4, 64 x 3000 13.8 / 11.7, 1 x 6000 18.5 / 7.6, 16 x
+  // 6000 21.2 / 10.8, 200 x 6000 35.8 / 22.2; two launches with parts of 1024 or more, 1 x
+  // 6000 8.7, of 2048 11.2.
+  constexpr int64_t kLong = 1280, kPartTokens = 256;
+  const int64_t average = a.pairs > 0 ? a.rows / (2 * a.pairs) : 0;
+  const int64_t parts = average > kLong
+                            ? std::min(kTotalsGroups / (2 * a.pairs), average / kPartTokens)
+                            : 1;
   if (parts > 1) {
     const auto grid = dim3((unsigned)(2 * a.pairs * parts));
     hipLaunchKernelGGL(sequence_sum_kernel, grid, dim3(kThreads), 0, stream, a, (int32_t)parts,
@@ -310,9 +323,9 @@ hipError_t launch_preference(const PreferenceArgs& a, const PreferenceOutputs& o
                        scratch);
     return hipGetLastError();
   }
-  // (Without pairs there are rows to clear.)
+  // (Without pairs there are rows to clear, 8 a thread.)
   const int64_t groups = std::max<int64_t>(
-      1, std::min<int64_t>(kTotalsGroups, a.pairs > 0 ? a.pairs : a.rows / kPartTokens));
+      1, std::min<int64_t>(kTotalsGroups, a.pairs > 0 ? a.pairs : a.rows / (8 * kThreads)));
   hipLaunchKernelGGL(preference_kernel, dim3((unsigned)groups), dim3(kThreads), 0, stream, a, out,
                      scratch);
   return hipGetLastError();

@@ -809,7 +809,10 @@ token_grad_kernel(TokenArgs a, TokenGrad g, int32_t tiles) {
 // 32,000 binary32 361 us (5.8 TB/s): HBM.  4096 of 50,257 bf16 159 us (5.2 TB/s): two
 // workgroups a compute unit that read, add and write more or less in step (three
 // of its 19 instructions an element left out made no difference).  POLICY: the
-// upstream gradients come from the row's own logp and entropy (policy_term()).
+// upstream gradients come from the row's own logp and entropy (policy_term()): 8192 x
+// 32,000 358 us, 512 x 50,257 bf16 24 (23 without).  The totals are a launch of their own
+// behind it, 4 us: added by the last row of this one, they wait for its gradient to be
+// written, 30.8 us for those 512 rows against 27.9.
 template <bool BF16, int W, int N, bool POLICY>
 __global__ void __launch_bounds__(W, N <= 8 ? 8 : 4)
 token_loss_kernel(TokenArgs a, TokenScores out, TokenGrad g, PolicyArgs p) {
