@@ -243,8 +243,8 @@ preference_kernel(PreferenceArgs a, PreferenceOutputs out, ObjectiveScratch* scr
 }
 
 // Few pairs of long sequences: `parts` workgroups for each sequence, one launch
-// for the sums and one for the gradients, as a gradient needs both sequences' sums: 3 us
-// each, 600,002 tokens 11.5 (1390 by one workgroup).
+// for the sums and one for the gradients, as a gradient needs both sequences' sums: 4 us
+// each at least, 504,741 tokens 4.5 and 6.2 (600,000 by one workgroup 1390).
 __device__ __forceinline__ Sequence part_of(const Sequence& s, int32_t part, int32_t parts) {
   const int64_t run = ((s.last - s.first + parts - 1) / parts + kThreads - 1) / kThreads * kThreads;
   const int64_t first = min(s.first + part * run, s.last);
@@ -309,11 +309,14 @@ hipError_t launch_preference(const PreferenceArgs& a, const PreferenceOutputs& o
   // launches.  us in one launch and in two, pairs x tokens of a sequence: 1 x 600 5.5 / 7.1,
   // 16 x 700 7.7 / 9.1, 1 x 1500 7.8 / 7.4, 64 x 3000 13.8 / 11.7, 1 x 6000 18.5 / 7.6, 16 x
   // 6000 21.2 / 10.8, 200 x 6000 35.8 / 22.2; two launches with parts of 1024 or more, 1 x
-  // 6000 8.7, of 2048 11.2.
-  constexpr int64_t kLong = 1280, kPartTokens = 256;
+  // 6000 8.7, of 2048 11.2.  Every workgroup of the second one reads the sums of all its
+  // pair's parts: 1 x 100,000 in 128 parts 8.5, in 390 10.3; 1 x 300,000 in 128 11.1, 256
+  // 10.3, 512 11.9; 1 x 1,000,000 33, 21 and 17.7.
+  constexpr int64_t kLong = 1280, kPartTokens = 256, kParts = 128, kManyTokens = 1024;
   const int64_t average = a.pairs > 0 ? a.rows / (2 * a.pairs) : 0;
   const int64_t parts = average > kLong
-                            ? std::min(kTotalsGroups / (2 * a.pairs), average / kPartTokens)
+                            ? std::min({kTotalsGroups / (2 * a.pairs), average / kPartTokens,
+                                        std::max(kParts, average / kManyTokens)})
                             : 1;
   if (parts > 1) {
     const auto grid = dim3((unsigned)(2 * a.pairs * parts));
