@@ -718,12 +718,12 @@ typedef struct {
   int32_t reserved; /* must be 0 */
 } arc_muon_step_config;
 
-/* Validate cfg, allocate the tables and the workspace (12 bytes for each element and
- * 20 for each of a square of the shorter side, sides rounded up to a multiple of 64 or
- * 128, of as many matrices as fit into 4 GiB, or of the largest) on the current HIP
- * device and bind the context to `hip_stream`, as arc_create does.  Graphs captured
- * from one context share its workspace: replays of them must not overlap in time.  On
- * failure *out is NULL. */
+/* Validate cfg, allocate the tables, the workspace (12 bytes for each element and 20
+ * for each of a square of the shorter side, sides rounded up to a multiple of 64 or
+ * 128, of as many matrices as fit into 4 GiB, or of the largest) and room for sums
+ * taken in parts on the current HIP device and bind the context to `hip_stream`, as
+ * arc_create does.  Graphs captured from one context share its workspace: replays of
+ * them must not overlap in time.  On failure *out is NULL. */
 arc_status arc_muon_create(const arc_muon_config *cfg, void *hip_stream, arc_muon **out);
 
 /* Elements of the momenta; -1 for NULL. */

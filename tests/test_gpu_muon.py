@@ -164,6 +164,32 @@ def test_other_polynomials(steps, coefficients):
         close_to(got[k], u[k], (steps, shapes[k]), steps=steps, coefficients=coefficients)
 
 
+@pytest.mark.parametrize("tall", [False, True])
+def test_offsets_beyond_32_bits(tall):
+    """4096 x 2^20 with one number in each row (or column), at the far end: their singular
+    values are those numbers over the norm, and every product is theirs alone."""
+    m, n = 4096, 1 << 20
+    u = torch.zeros((n, m) if tall else (m, n), dtype=torch.bfloat16, device="cuda")
+    values = torch.linspace(0.5, 4.0, m, device="cuda").bfloat16()
+    short = torch.arange(m, device="cuda")
+    long = n - 1 - 3 * short.flip(0)
+    at = (long, short) if tall else (short, long)
+    u[at] = values
+    opt = arc.Muon([tuple(u.shape)], param_dtype="bf16", grad_dtype="bf16")
+    got, = opt.orthogonalize([u])
+    x = values.double() / values.double().norm()
+    for a, b, c in [QUINTIC] * 5:
+        x = f32(a) * x + f32(b) * x ** 3 + f32(c) * x ** 5
+    # pairs are off by 2^-23, a product's one term by 2^-24 and its sum by 2^-24; a singular
+    # value's error grows 3.4445 times in a step, with three roundings of pairs and four of
+    # products in each: less than 12 EPS, 5 times, and the result's half step
+    grown = sum(3.4445 ** k for k in range(6)) * 12 * EPS
+    off = (got[at].double() - x).abs()
+    assert bool((off <= (grown + 2.0 ** -8) * x.abs() + grown * 1e-3).all())
+    got[at] = 0
+    assert not bool(got.any()), "zeros elsewhere"
+
+
 def test_singular_values_come_together():
     gen = torch.Generator(device="cuda").manual_seed(1)
     u = torch.randn(200, 500, device="cuda", generator=gen)

@@ -583,6 +583,42 @@ def test_no_rows():
         assert out.grad.shape == (0, 10)
 
 
+# ---------------------------------------------------------------- large calls
+
+@pytest.mark.parametrize("T,V,dtype", [(1_100_003, 9, "f32"), (45_000, 50_257, "bf16")])
+def test_rows_and_offsets_of_large_calls(T, V, dtype):
+    """More rows than one launch takes, and elements beyond 32 bits: each row's results
+    are those of a smaller call (its kernel is the same one)."""
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    kind = torch.float32 if dtype == "f32" else torch.bfloat16
+    x = torch.randn(T, V, generator=gen, device="cuda", dtype=kind)
+    y = torch.randint(-1, V, (T,), generator=gen, device="cuda")
+    old, ref, A = (torch.randn(T, generator=gen, device="cuda") for _ in range(3))
+    old, ref = old - math.log(V), ref - math.log(V)
+    w = torch.rand(T, generator=gen, device="cuda")
+    kw = dict(kl_coef=0.05, entropy_coef=0.01, dual=3.0)
+    head = arc.TokenLogProbs(V=V, rows=T, dtype=dtype)
+    got = head.policy_loss(x, y, A, old_logp=old, ref_logp=ref, weights=w, **kw)
+    # a pair of two halves, and rows behind it
+    o = torch.tensor([0, T // 2, T - 9]).cuda()
+    pairs = head.preference_loss(x, y, o, ref_logp=ref, beta=1e-4)
+    terms = head.preference(pairs.logp, y, o, ref_logp=ref, beta=1e-4)
+    assert torch.equal(terms.totals, pairs.totals) and torch.equal(terms.loss, pairs.loss)
+    for rows in (slice(0, 300), slice(1 << 20, (1 << 20) + 300), slice(T - 300, T)):
+        if rows.start >= T:
+            continue
+        part = head.policy_loss(x[rows], y[rows], A[rows], old_logp=old[rows],
+                                ref_logp=ref[rows], weights=w[rows], **kw)
+        for name in ("logp", "entropy", "lse", "loss", "ratio", "kl", "grad"):
+            assert torch.equal(getattr(got, name)[rows], getattr(part, name)), name
+        want = formulas(x[rows], y[rows], 1.0, 0)
+        near("logp", pairs.logp[rows], want["logp"],
+             slack(x[rows], 1.0) + 4 * EPS * want["logp"].abs())
+        d = terms.d_logp[rows]
+        check_policy_grad(x[rows], y[rows].cpu(), 1.0, dtype, want, (d, torch.zeros(300).cuda()),
+                          {"d_logp": (d, EPS * d.double().abs().cpu())}, pairs.grad[rows])
+
+
 # ---------------------------------------------------------------- streams, graphs, refusals
 
 def test_on_another_stream_and_in_a_graph():
