@@ -53,6 +53,14 @@ arc_status check_policy(const arc_policy_config* cfg, int64_t rows, const int64_
   return ARC_OK;
 }
 
+// So many rows have their terms and totals from the kernel that holds them, which costs a
+// count of arrivals in one place, 16 ns a row, and saves a launch.  us, a launch of
+// its own / inside: 8 rows of 1001 bf16 8.3 / 6.6, 64 of 50,257 bf16 14.7 / 12.1, 128 of
+// 1001 8.5 / 8.2, 128 of 32,000 binary32 13.1 / 11.4, 200 of 1001 8.6 / 9.6, 512 of 50,257
+// 25.0 / 28.1; called from Python one after the other 18.8 / 16.1.
+constexpr int64_t kRowsInside = 128;
+static_assert(kRowsInside <= arc::kTotalsGroups, "a place for each row");
+
 arc::PolicyArgs policy_args(const arc_policy_config* cfg, const float* old_logp,
                             const float* ref_logp, const float* advantages,
                             const float* weights) {
@@ -158,8 +166,12 @@ arc_status arc_tokens_policy(arc_tokens* c, const arc_policy_config* cfg, int64_
   const arc::PolicyRows r{out.logp, out.entropy, targets, rows};
   arc::PolicyOutputs terms{loss, ratio, kl, nullptr, nullptr, totals};
   hipError_t e;
-  if (arc::launch_token_loss(a, out, g, c->stream, &e, &p)) {
+  arc::PolicyRowTerms inside;
+  if (rows <= kRowsInside)
+    inside = {loss, ratio, kl, totals, c->scratch, static_cast<uint32_t>(rows)};
+  if (arc::launch_token_loss(a, out, g, c->stream, &e, &p, &inside)) {
     ARC_HIP(e, "policy loss launch");
+    if (inside.rows > 0) return ARC_OK;
     ARC_HIP(arc::launch_policy_terms(p, r, terms, c->scratch, c->stream), "policy terms launch");
     return ARC_OK;
   }

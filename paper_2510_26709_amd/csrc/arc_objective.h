@@ -35,6 +35,17 @@ struct PolicyOutputs {
 };
 constexpr int kPolicyTotals = 5;
 
+struct ObjectiveScratch;
+
+// For the kernel that holds rows of logits, a workgroup each: where it puts its rows'
+// terms and, the last of `rows` workgroups, their totals.  rows 0: nowhere.
+struct PolicyRowTerms {
+  float *loss = nullptr, *ratio = nullptr, *kl = nullptr;
+  float* totals = nullptr;
+  ObjectiveScratch* scratch = nullptr;
+  uint32_t rows = 0;
+};
+
 // ---------------------------------------------------------------- preference
 
 struct PreferenceArgs {

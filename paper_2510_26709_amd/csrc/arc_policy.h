@@ -159,4 +159,44 @@ __device__ __forceinline__ void add_groups(double (&v)[K], uint32_t group, uint3
     for (int k = 0; k < K; ++k) totals[k] = (float)v[k];
 }
 
+// One row's terms; true on the whole first wave of the last row to come, whose turn
+// it is to add_rows().  For that wave alone.
+__device__ __forceinline__ bool write_row(const PolicyRowTerms& out, int64_t i,
+                                          const PolicyTerm& t, float H) {
+  uint32_t before = 0;
+  if (threadIdx.x == 0) {
+    double v[kPolicyTotals] = {};
+    add_term(t, H, v);
+#pragma unroll
+    for (int k = 0; k < kPolicyTotals; ++k)
+      __hip_atomic_store(&out.scratch->totals[i][k], v[k], __ATOMIC_RELAXED,
+                         __HIP_MEMORY_SCOPE_AGENT);
+    wave_vmem_fence();  // written before it counts
+    before = __hip_atomic_fetch_add(&out.scratch->arrived, 1u, __ATOMIC_RELAXED,
+                                    __HIP_MEMORY_SCOPE_AGENT);
+    if (before == out.rows - 1)
+      __hip_atomic_store(&out.scratch->arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (out.loss) out.loss[i] = t.loss;
+    if (out.ratio) out.ratio[i] = t.ratio;
+    if (out.kl) out.kl[i] = t.kl;
+  }
+  return (uint32_t)__builtin_amdgcn_readfirstlane((int)before) == out.rows - 1;
+}
+
+__device__ __forceinline__ void add_rows(const PolicyRowTerms& out) {
+  double v[kPolicyTotals] = {};
+#pragma unroll 2
+  for (uint32_t i = threadIdx.x; i < out.rows; i += kWave)
+#pragma unroll
+    for (int k = 0; k < kPolicyTotals; ++k)
+      v[k] += __hip_atomic_load(&out.scratch->totals[i][k], __ATOMIC_RELAXED,
+                                __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+  for (int k = 0; k < kPolicyTotals; ++k) {
+#pragma unroll
+    for (int off = kWave / 2; off > 0; off >>= 1) v[k] += __shfl_xor(v[k], off);
+    if (threadIdx.x == 0) out.totals[k] = (float)v[k];
+  }
+}
+
 }  // namespace arc

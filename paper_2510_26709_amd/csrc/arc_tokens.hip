@@ -808,14 +808,15 @@ token_grad_kernel(TokenArgs a, TokenGrad g, int32_t tiles) {
 // relative to the row's reference, A' and B' divided by the row's sum.  8192 rows of
 // 32,000 binary32 361 us (5.8 TB/s): HBM.  4096 of 50,257 bf16 159 us (5.2 TB/s): two
 // workgroups a compute unit that read, add and write more or less in step (three
-// of its 19 instructions an element left out made no difference).  POLICY: the
+// of its 19 instructions an element left out made no difference).  kPolicy: the
 // upstream gradients come from the row's own logp and entropy (policy_term()): 8192 x
-// 32,000 358 us, 512 x 50,257 bf16 24 (23 without).  The totals are a launch of their own
-// behind it, 4 us: added by the last row of this one, they wait for its gradient to be
-// written, 30.8 us for those 512 rows against 27.9.
-template <bool BF16, int W, int N, bool POLICY>
+// 32,000 358 us, 512 x 50,257 bf16 24 (23 without), and a launch of 4 us behind it for the
+// terms and totals.  kPolicyWithTerms makes those as well, for few rows.
+enum LossKind { kGivenGradients, kPolicy, kPolicyWithTerms };
+
+template <bool BF16, int W, int N, LossKind KIND>
 __global__ void __launch_bounds__(W, N <= 8 ? 8 : 4)
-token_loss_kernel(TokenArgs a, TokenScores out, TokenGrad g, PolicyArgs p) {
+token_loss_kernel(TokenArgs a, TokenScores out, TokenGrad g, PolicyArgs p, PolicyRowTerms rows) {
   using S = Scorer<BF16, W>;
   constexpr int C = S::C;
   __shared__ float part_most[S::kWaves];
@@ -897,10 +898,13 @@ token_loss_kernel(TokenArgs a, TokenScores out, TokenGrad g, PolicyArgs p) {
   const RowResult res = finish_row(a, out, i, s, y, given);
   const float H = res.empty ? 0.f : res.log_total - s.spread * kLn2 / s.total;
   GradRow r;
-  if constexpr (POLICY) {
+  bool last = false;
+  if constexpr (KIND != kGivenGradients) {
     const float logp = y >= a.vocab ? NAN : res.logp(given);
     const PolicyTerm t = policy_term(p, policy_token(p, i), y >= 0, logp, H);
     r = grad_row(a, y, t.d_logp, t.d_entropy, 0.f, H, res.empty);
+    if constexpr (KIND == kPolicyWithTerms)
+      if (threadIdx.x < kWave) last = write_row(rows, i, t, H);
   } else {
     r = grad_row(a, g, i, H, res.empty);
   }
@@ -945,6 +949,8 @@ token_loss_kernel(TokenArgs a, TokenScores out, TokenGrad g, PolicyArgs p) {
       return __builtin_amdgcn_exp2f(t) * fmaf(B, fmaxf(t, kFarBelow), A);
     });
   }
+  if constexpr (KIND == kPolicyWithTerms)
+    if (last) add_rows(rows);
 }
 
 }  // namespace
@@ -1040,8 +1046,12 @@ hipError_t launch_token_grad(const TokenArgs& a, const TokenGrad& g, hipStream_t
   return hipGetLastError();
 }
 
+template <LossKind KIND>
+using Kind = std::integral_constant<LossKind, KIND>;
+
 bool launch_token_loss(const TokenArgs& a, const TokenScores& out, const TokenGrad& g,
-                       hipStream_t stream, hipError_t* e, const PolicyArgs* policy) {
+                       hipStream_t stream, hipError_t* e, const PolicyArgs* policy,
+                       const PolicyRowTerms* terms) {
   *e = hipSuccess;
   if (a.rows <= 0) return true;
   const int64_t chunks = a.vocab / (a.bf16 ? 8 : 4);
@@ -1052,6 +1062,7 @@ bool launch_token_loss(const TokenArgs& a, const TokenScores& out, const TokenGr
   if (chunks > 5000 && a.rows <= (chunks > 12288 && a.bf16 ? 128 : 32)) return false;
   bool found = true;
   PolicyArgs p = policy ? *policy : PolicyArgs{};
+  const PolicyRowTerms t = terms ? *terms : PolicyRowTerms{};
   each_rows(a, out, g, kRowsPerLaunch, [&](const TokenArgs& b, const TokenScores& o,
                                            const TokenGrad& h) {
   // The smallest that holds the row.  us with a variant and with the next larger, 2.5e8
@@ -1063,11 +1074,14 @@ bool launch_token_loss(const TokenArgs& a, const TokenScores& out, const TokenGr
   // three would be 3 to 6% faster in the next; the rule is the same for both types.
 #define ARC_LOSS(WW, NN)                                                                        \
   if (chunks <= (WW) * (NN)) {                                                                  \
-    hipLaunchKernelGGL(policy ? (a.bf16 ? (token_loss_kernel<true, WW, NN, true>)               \
-                                        : (token_loss_kernel<false, WW, NN, true>))             \
-                              : (a.bf16 ? (token_loss_kernel<true, WW, NN, false>)              \
-                                        : (token_loss_kernel<false, WW, NN, false>)),           \
-                       dim3((unsigned)b.rows), dim3(WW), 0, stream, b, o, h, p);                \
+    const auto kernel = [&](auto kind) {                                                        \
+      return a.bf16 ? token_loss_kernel<true, WW, NN, decltype(kind)::value>                    \
+                    : token_loss_kernel<false, WW, NN, decltype(kind)::value>;                  \
+    };                                                                                          \
+    hipLaunchKernelGGL(t.rows > 0 ? kernel(Kind<kPolicyWithTerms>())                            \
+                       : policy   ? kernel(Kind<kPolicy>())                                     \
+                                  : kernel(Kind<kGivenGradients>()),                            \
+                       dim3((unsigned)b.rows), dim3(WW), 0, stream, b, o, h, p, t);             \
   } else
     ARC_LOSS(64, 8)
     ARC_LOSS(256, 5)

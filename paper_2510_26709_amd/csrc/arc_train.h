@@ -43,8 +43,10 @@ hipError_t launch_token_score(const TokenArgs& a, const TokenScores& out, void* 
 // nothing was launched); g's lse and entropy are not read.  With `policy` the
 // upstream gradients are the policy loss's, and g's are not read.
 struct PolicyArgs;
+struct PolicyRowTerms;
 bool launch_token_loss(const TokenArgs& a, const TokenScores& out, const TokenGrad& g,
-                       hipStream_t stream, hipError_t* e, const PolicyArgs* policy = nullptr);
+                       hipStream_t stream, hipError_t* e, const PolicyArgs* policy = nullptr,
+                       const PolicyRowTerms* terms = nullptr);
 hipError_t launch_token_grad(const TokenArgs& a, const TokenGrad& g, hipStream_t stream);
 
 // ---------------------------------------------------------------- optimizer

@@ -221,7 +221,7 @@ LOGITS = [  # rows, V, dtype, pad: a row in registers of each kernel, and rows r
     (64, 5000, "f32", 0), (70, 9001, "bf16", 0), (33, 12_001, "f32", 1), (60, 32_000, "bf16", 0),
     (40, 40_000, "f32", 0), (40, 50_257, "bf16", 47), (3, 50_257, "bf16", 0),
     (140, 100_003, "bf16", 0), (36, 98_000, "f32", 0), (2, 131_077, "f32", 5),
-    (9, 200_003, "bf16", 0)]
+    (9, 200_003, "bf16", 0), (128, 700, "bf16", 1), (129, 701, "f32", 0), (300, 12_001, "bf16", 0)]
 
 
 @pytest.mark.parametrize("o", [OPTIONS[0], OPTIONS[2], OPTIONS[5]])
@@ -621,17 +621,18 @@ def test_rows_and_offsets_of_large_calls(T, V, dtype):
 
 # ---------------------------------------------------------------- streams, graphs, refusals
 
-def test_on_another_stream_and_in_a_graph():
+@pytest.mark.parametrize("T,lengths", [(200, [60, 40, 55, 45]), (90, [27, 18, 25, 20])])
+def test_on_another_stream_and_in_a_graph(T, lengths):
     """Captured calls repeat on new contents, with eager calls of the same context
     between the replays."""
-    T, V = 200, 5001
+    V = 5001
     stream = torch.cuda.Stream()
     gen = torch.Generator().manual_seed(1)
     x = place(torch.randn(T, V, generator=gen), "bf16")
     fresh = [torch.randn(T, V, generator=gen).bfloat16().cuda() for _ in range(3)]
     y = tokens(T, V - 10, 3)
     s = policy_inputs(T, 1)
-    p = pair_inputs([60, 40, 55, 45], 1)
+    p = pair_inputs(lengths, 1)
     head = arc.TokenLogProbs(V=V, rows=T, dtype="bf16", stream=stream)
     torch.cuda.synchronize()
 
