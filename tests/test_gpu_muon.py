@@ -164,6 +164,23 @@ def test_other_polynomials(steps, coefficients):
         close_to(got[k], u[k], (steps, shapes[k]), steps=steps, coefficients=coefficients)
 
 
+@pytest.mark.parametrize("rank", [1, 4, 64])
+@pytest.mark.parametrize("shape,count", [((300, 1100), 1), ((1100, 300), 3), ((897, 3588), 12)])
+def test_few_directions(shape, count, rank):
+    """All other directions hold roundings alone, which grow 485 times in five steps: by
+    as much as with binary32 products, step by step and in runs of steps."""
+    gen = torch.Generator(device="cuda").manual_seed(rank)
+    u = [torch.randn(shape[0], rank, device="cuda", generator=gen)
+         @ torch.randn(rank, shape[1], device="cuda", generator=gen) for _ in range(count)]
+    opt = arc.Muon([shape] * count, lr_scale=1.0)
+    got = opt.orthogonalize(u)
+    x = [torch.zeros_like(v) for v in u]
+    opt.step(x, u, lr=1.0, momentum=0.0, nesterov=False)
+    for k in {0, count - 1}:
+        close_to(got[k], u[k], (k, "alone"))
+        close_to(-x[k], u[k], (k, "a step"))
+
+
 @pytest.mark.parametrize("tall", [False, True])
 def test_offsets_beyond_32_bits(tall):
     """4096 x 2^20 with one number in each row (or column), at the far end: their singular
