@@ -476,6 +476,7 @@ arc_status arc_tokens_policy_terms(arc_tokens *ctx, const arc_policy_config *cfg
  *   h_s = sum (l - f), or with `average` its mean (0 for a sequence without tokens)
  *   reward_s = beta h_s        z = reward_p - reward_(P+p) - margin
  *   sigmoid:  loss = -(1 - smoothing) log sigmoid(z) - smoothing log sigmoid(-z)
+ *             (the first term alone where smoothing is 0, for an infinite z too)
  *   hinge:    loss = max(0, 1 - z)
  *   squared:  loss = ((z - 1/2) / beta)^2
  * totals are the sums over pairs of w' = scale * w times loss, reward_p -

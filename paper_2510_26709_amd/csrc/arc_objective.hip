@@ -167,7 +167,10 @@ __device__ __forceinline__ PairTerm pair_term(const PreferenceArgs& a, int64_t p
   if (a.kind == 0) {
     const double e = a.smoothing, s = exp(-fabs(z));  // sigmoid(-|z|) = s / (1 + s)
     const double soft = log1p(s), under = s / (1.0 + s), over = 1.0 / (1.0 + s);
-    t.loss = soft + (1.0 - e) * fmax(-z, 0.0) + e * fmax(z, 0.0);
+    // -log sigmoid(-|z|) is |z| more than that of |z|.  Without smoothing the loss at z =
+    // infinity (a rejected answer with a masked token) is 0, and not 0 times infinity.
+    const double far = z >= 0.0 ? e : 1.0 - e;
+    t.loss = far != 0.0 ? soft + far * fabs(z) : soft;
     if (z != z) t.loss = z;
     dz = e * (z >= 0.0 ? over : under) - (1.0 - e) * (z >= 0.0 ? under : over);
     if (z != z) dz = z;
