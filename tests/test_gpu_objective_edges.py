@@ -1,10 +1,13 @@
-"""Far losses of preferences, whose other test compares them only in part."""
+"""Far losses, and rows outside all sequences: what the preferences' other tests
+compare only in part."""
 import math
 
 import pytest
 import torch
 
 import paper_2510_26709_amd as arc
+from test_gpu_objectives import pair_formulas
+from test_gpu_tokens import near
 
 pytestmark = pytest.mark.gpu
 INF = math.inf
@@ -29,3 +32,33 @@ def test_far_losses():
     keep = [0, 1, 2, 4, 5, 6]
     got = head.preference(l[keep], y[:6], torch.arange(7).cuda(), beta=1.0)
     assert got.loss.tolist() == [0.0, 200.0, 0.0] and got.totals.tolist() == [200.0, 300.0, 2.0]
+
+
+# of 60 rows, and a hundred times that, where sequences are taken in parts: each row's
+# sequence, -1 for none
+@pytest.mark.parametrize("times", [1, 100])
+@pytest.mark.parametrize("offsets,runs", [
+    ([20, 20, 30, 30, 40], [(20, 30), (30, 40)]), ([70, 80, 90, 100, 110], []),
+    ([-9, -8, -7, -6, -5], []), ([60, 60, 60, 60, 60], []), ([0, 0, 0, 0, 0], []),
+    ([10, 2**40, 2**41, 2**42, 2**43], [(10, 60)]), ([-2**40, 7, 8, 9, 50], [(0, 50)])])
+def test_rows_outside_all_sequences_have_no_gradient(offsets, runs, times):
+    T = 60 * times
+    gen = torch.Generator().manual_seed(3)
+    l = -torch.rand(T, generator=gen).cuda()
+    y = torch.zeros(T, dtype=torch.int64).cuda()
+    o = torch.tensor([v * times if abs(v) < 2**30 else v for v in offsets]).cuda()
+    buf = torch.full((T + 200,), 7.0, device="cuda")
+    head = arc.TokenLogProbs(V=10, rows=T, dtype="f32")
+    cfg = arc.arc_preference_config(0, 0, 0.1, 0.0, 0.0, 1.0)
+    totals = torch.zeros(3).cuda()
+    arc.arc_tokens_preference_terms(head.ctx, cfg, T, l, y, 2, o, None, None, None, None, totals,
+                                    buf[100:100 + T])
+    got = buf.cpu()
+    assert bool((got[:100] == 7.0).all()) and bool((got[100 + T:] == 7.0).all())
+    inside = torch.zeros(T, dtype=torch.bool)
+    for first, last in runs:
+        inside[first * times:last * times] = True
+    d = got[100:100 + T]
+    assert bool((d[~inside] == 0).all())
+    want = pair_formulas(l, y, torch.tensor(offsets).mul(times).clamp(0, T))["d_logp"]
+    near("d_logp", d, *want)
