@@ -419,7 +419,9 @@ arc_status arc_tokens_loss(arc_tokens *ctx, int64_t rows, const void *logits, in
  * is not looked at.  A token with w' = 0 has its loss, ratio and KL, and adds
  * nothing to sums and gradients, whatever they are.  Elsewhere infinities and NaN
  * go the way of the formulas (y >= V has l = NaN; a given token that is masked has
- * l = -infinity, ratio = 0 and, with a KL term, an infinite gradient).
+ * l = -infinity, ratio = 0 (1 without old_logp) and a finite gradient, but with a KL
+ * term d loss / d l = -infinity, whose row of logits has an infinite gradient where p
+ * is not 0 and NaN where it is).
  *
  * Terms are binary32; totals are summed in binary64 in a fixed order and rounded
  * once.
