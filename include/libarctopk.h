@@ -357,8 +357,11 @@ typedef struct {
   int32_t reserved; /* must be 0 */
 } arc_tokens_config;
 
-/* Validate cfg, allocate the workspace on the current HIP device and bind the
- * context to `hip_stream`, as arc_create does.  On failure *out is NULL. */
+/* Validate cfg, allocate the workspace (24 bytes for each of max_rows, and less than 400 KB)
+ * on the current HIP device and bind the context to `hip_stream`, as arc_create does.
+ * All calls of a context share its workspace, the losses made in one launch too: graphs
+ * captured from it must not be replayed so that they overlap in time with one another
+ * or with calls on its stream.  On failure *out is NULL. */
 arc_status arc_tokens_create(const arc_tokens_config *cfg, void *hip_stream, arc_tokens **out);
 
 /*

@@ -67,13 +67,16 @@ struct PreferenceOutputs {
 constexpr int kPreferenceTotals = 3;
 
 // Scratch of both in a token context: the totals of workgroups, the sums of
-// parts of sequences (one a workgroup), and a count of workgroups that is 0 between launches.
+// parts of sequences (one a workgroup), and counts of workgroups, one for launches of
+// each number of them.  A count goes round, 0 after as many arrivals as its number, so
+// that it is 0 between launches whatever came before: replays that overlap in time, which
+// they must not, spoil their own totals and those of no later call.
 constexpr int kTotalsGroups = 1024;
 struct ObjectiveScratch {
   double totals[kTotalsGroups][kPolicyTotals];
   double sum[kTotalsGroups];
   int64_t count[kTotalsGroups];
-  uint32_t arrived;
+  uint32_t arrived[kTotalsGroups + 1];
 };
 
 hipError_t launch_policy_terms(const PolicyArgs& p, const PolicyRows& r, const PolicyOutputs& out,

@@ -137,10 +137,7 @@ __device__ __forceinline__ void add_groups(double (&v)[K], uint32_t group, uint3
         __hip_atomic_store(&scratch->totals[group][k], v[k], __ATOMIC_RELAXED,
                            __HIP_MEMORY_SCOPE_AGENT);
       wave_vmem_fence();  // written before it counts
-      last = __hip_atomic_fetch_add(&scratch->arrived, 1u, __ATOMIC_RELAXED,
-                                    __HIP_MEMORY_SCOPE_AGENT) == groups - 1;
-      if (last)
-        __hip_atomic_store(&scratch->arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      last = atomicInc(&scratch->arrived[groups], groups - 1) == groups - 1;
     }
     __syncthreads();
     if (!last) return;
@@ -172,10 +169,7 @@ __device__ __forceinline__ bool write_row(const PolicyRowTerms& out, int64_t i,
       __hip_atomic_store(&out.scratch->totals[i][k], v[k], __ATOMIC_RELAXED,
                          __HIP_MEMORY_SCOPE_AGENT);
     wave_vmem_fence();  // written before it counts
-    before = __hip_atomic_fetch_add(&out.scratch->arrived, 1u, __ATOMIC_RELAXED,
-                                    __HIP_MEMORY_SCOPE_AGENT);
-    if (before == out.rows - 1)
-      __hip_atomic_store(&out.scratch->arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    before = atomicInc(&out.scratch->arrived[out.rows], out.rows - 1);
     if (out.loss) out.loss[i] = t.loss;
     if (out.ratio) out.ratio[i] = t.ratio;
     if (out.kl) out.kl[i] = t.kl;

@@ -4,8 +4,9 @@ and ``AdamW`` (gradient norms and the AdamW step over many tensors).
 
 Both own one context of the C library, bound to a torch stream: inputs must be
 ready on that stream, and outputs are.  Where it is not the current stream,
-making them so (an event, a synchronization) is the caller's part.  Tensors may
-be dropped after a call all the same: the allocator keeps inputs until the
+making them so (an event, a synchronization) is the caller's part.  A context has
+one workspace: graphs captured from it, and calls, must not overlap in time.  Tensors
+may be dropped after a call all the same: the allocator keeps inputs until the
 context's stream is done with them, and outputs until the stream is that was
 current at the call.  Tensors are checked here for what the library cannot see
 in a pointer (type, device, shape, strides).
