@@ -625,10 +625,8 @@ token_score_kernel(TokenArgs a, TokenScores out, int32_t pieces, int32_t piece_c
   wave_vmem_fence();
   __syncthreads();
   if (threadIdx.x == 0) {
-    const uint32_t before = __hip_atomic_fetch_add(&arrived[i], 1u, __ATOMIC_RELAXED,
-                                                   __HIP_MEMORY_SCOPE_AGENT);
-    last = before == (uint32_t)(pieces - 1);
-    if (last) share_store(&arrived[i], 0u);  // for the next call
+    const auto most_before = (uint32_t)(pieces - 1);
+    last = atomicInc(&arrived[i], most_before) == most_before;  // and 0 for the next call
   }
   __syncthreads();
   if (!last) return;
@@ -955,8 +953,14 @@ token_loss_kernel(TokenArgs a, TokenScores out, TokenGrad g, PolicyArgs p, Polic
 
 }  // namespace
 
+// Rows in two pieces or more, at most.
+constexpr int64_t kSplitRows = kSplitParts / 2;
+
+// Parts, and for each number of pieces the rows' counts of those that have arrived, which go
+// round at that number: 0 between launches, whatever launches overlapped before.
 size_t token_workspace_bytes() {
-  return (size_t)kSplitParts * (sizeof(TokenPart) + sizeof(uint32_t));
+  return (size_t)kSplitParts * sizeof(TokenPart) +
+         (size_t)(kMostPieces + 1) * kSplitRows * sizeof(uint32_t);
 }
 
 // Pieces of a row of that many chunks, for few rows.
@@ -998,7 +1002,7 @@ static void launch_score(const TokenArgs& a, const TokenScores& o, int32_t piece
                          void* workspace, hipStream_t stream) {
   const auto piece_chunks = static_cast<int32_t>((chunks + pieces - 1) / pieces);
   auto* parts = static_cast<TokenPart*>(workspace);
-  auto* arrived = reinterpret_cast<uint32_t*>(parts + kSplitParts);
+  auto* arrived = reinterpret_cast<uint32_t*>(parts + kSplitParts) + pieces * kSplitRows;
   const auto kernel =
       o.top_ids && a.top > 0
           ? (a.bf16 ? token_score_kernel<true, W, true> : token_score_kernel<false, W, true>)
