@@ -611,8 +611,9 @@ typedef struct {
 } arc_adamw_config;
 
 /* Validate cfg, allocate the tables and the norms' workspace on the current
- * HIP device and bind the context to `hip_stream`, as arc_create does.  On
- * failure *out is NULL. */
+ * HIP device and bind the context to `hip_stream`, as arc_create does.  Graphs
+ * captured from one context share its workspace: replays of norms must not overlap
+ * in time with one another or with calls on its stream.  On failure *out is NULL. */
 arc_status arc_optim_create(const arc_optim_config *cfg, void *hip_stream, arc_optim **out);
 
 /* Elements of each state array; -1 for NULL.  The scales have one for each

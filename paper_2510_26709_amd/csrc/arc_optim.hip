@@ -411,9 +411,8 @@ norm_tensor_kernel(const OptimTensor* __restrict__ tensors, int32_t num, int32_t
     if (norms) norms[blockIdx.x] = (float)((double)scale * sqrt(sum));
     __hip_atomic_store(&squares[blockIdx.x], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     wave_vmem_fence();  // written before it counts
-    last = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
-           (uint32_t)(num - 1);
-    if (last) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    // (goes round at the number of tensors: 0 after a launch, whatever overlapped before)
+    last = atomicInc(arrived, (uint32_t)(num - 1)) == (uint32_t)(num - 1);
   }
   __syncthreads();
   if (!last) return;
