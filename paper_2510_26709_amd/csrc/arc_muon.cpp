@@ -23,6 +23,7 @@ struct MuonGroup {
   struct Range {  // their tiles in the context's list, and those tiles' sides
     int64_t at = 0, count = 0;
     int32_t side = kSplitTile;
+    int64_t counts = 0;  // where their counts of parts begin
   };
   Range split, gram, half, whole;
 };
@@ -46,6 +47,7 @@ struct arc_muon {
   bool any_f32 = false;   // a parameter is binary32
   int64_t state_elems = 0, workspace_bytes = 0;
   int64_t parts = 0, part_elems = 0;  // most of one launch
+  int64_t counts = 0;                 // of all ranges
   hipStream_t stream = nullptr;
   int device = 0;
   arc::MuonMatrix* matrices_dev = nullptr;
@@ -394,6 +396,9 @@ Times plan_muon(const arc_muon_config* cfg, int32_t whole_of, arc_muon* c) {
       }
       if (count > kPlenty) break;
     }
+    // (A count is of the same number of parts in every launch, and goes round at it.)
+    range->counts = c->counts;
+    c->counts += parts;
     c->parts = std::max(c->parts, parts);
     c->part_elems = std::max(c->part_elems, parts * range->side * range->side);
     take(best, range);
@@ -497,7 +502,6 @@ arc_status enqueue(const arc_muon* c, arc::MuonArgs a, void* const* params,
   a.workspace = c->workspace;
   a.sums = c->sums_dev;
   a.parts = c->parts_dev;
-  a.arrived = c->arrived_dev;
   const OnDevice here(c->device);
   const auto& launches = c->group && (a.update || !c->any_f32) ? c->grouped : c->plain;
   for (const arc::MuonGroup& g : c->groups) {
@@ -517,6 +521,7 @@ arc_status enqueue(const arc_muon* c, arc::MuonArgs a, void* const* params,
       const auto& range = l.kind == arc::kMuonGram ? g.gram
                           : l.kind == arc::kMuonStep || l.kind == arc::kMuonHalf ? g.half
                                                                                  : g.whole;
+      a.arrived = c->arrived_dev + range.counts;
       ARC_HIP(arc::launch_muon_product(l.kind, range.side, a, p, l.product, c->tiles_dev + range.at,
                                        range.count, c->stream),
               "product launch");
@@ -569,9 +574,9 @@ arc_status arc_muon_create(const arc_muon_config* cfg, void* hip_stream, arc_muo
   room(&c->sums_dev, c->run_matrix.size() * sizeof(double));
   room(&c->workspace, static_cast<size_t>(c->workspace_bytes));
   room(&c->parts_dev, static_cast<size_t>(c->part_elems) * sizeof(float));
-  room(&c->arrived_dev, static_cast<size_t>(c->parts) * sizeof(uint32_t));
-  if (e == hipSuccess && c->parts > 0)
-    e = hipMemset(c->arrived_dev, 0, static_cast<size_t>(c->parts) * sizeof(uint32_t));
+  room(&c->arrived_dev, static_cast<size_t>(c->counts) * sizeof(uint32_t));
+  if (e == hipSuccess && c->counts > 0)
+    e = hipMemset(c->arrived_dev, 0, static_cast<size_t>(c->counts) * sizeof(uint32_t));
   if (e == hipSuccess) e = arc::prepare_muon_products();
   if (e == hipSuccess) e = hipDeviceSynchronize();
   if (e != hipSuccess) {

@@ -77,7 +77,7 @@ struct MuonArgs {
   int32_t nesterov, update;    // update: parameters; otherwise they are overwritten
   char* workspace;
   float* parts;                // of tiles whose sums are split, side * side each
-  uint32_t* arrived;           // of each place, 0 between launches
+  uint32_t* arrived;           // of each place, which go round at its number of parts
   double* sums;                // of the runs' squares
 };
 

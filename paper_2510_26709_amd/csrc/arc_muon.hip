@@ -415,10 +415,8 @@ __device__ __forceinline__ bool join_parts(const MuonArgs& a, const MuonTile& at
   wave_vmem_fence();  // written before it counts
   __syncthreads();
   if (threadIdx.x == 0) {
-    last = __hip_atomic_fetch_add(&a.arrived[at.place], 1u, __ATOMIC_RELAXED,
-                                  __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(at.parts - 1);
-    if (last)
-      __hip_atomic_store(&a.arrived[at.place], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const auto most_before = (uint32_t)(at.parts - 1);
+    last = atomicInc(&a.arrived[at.place], most_before) == most_before;
   }
   __syncthreads();
   if (!last) return false;
