@@ -680,12 +680,13 @@ arc_status arc_optim_destroy(arc_optim *ctx);
  *   x <- (1 - lr' weight_decay) x - lr' O(U)
  *
  * X and A are held in 22 bits (two binary16 numbers each), products are summed in
- * binary32 in a fixed order, norms in binary64, all else is binary32, and a call
- * repeats its bits.  O in binary32 is as exact as binary32 products make it (off by
- * 2e-6 of its norm for matrices of some hundreds of rows).  In optimizer steps, and
- * where all parameters are bfloat16, it may be off by a few times that: products of
- * several steps' polynomials are taken first where that is less work.  A matrix with a
- * NaN or infinity in U gets NaN everywhere, the others none of it.
+ * binary32 in a fixed order, those of the longer side in blocks, norms in binary64, all
+ * else is binary32, and a call repeats its bits.  O in binary32 is as exact as binary32
+ * products make it (off by 2e-6 of its norm for matrices of some hundreds of rows).  In
+ * optimizer steps it may be off by up to five times that: products of two steps'
+ * polynomials are taken first where that is less work.  Where all parameters are
+ * bfloat16, those of three are, and O may be off by 1e-4 before it is rounded to 2^-9.  A
+ * matrix with a NaN or infinity in U gets NaN everywhere, the others none of it.
  *
  * Momenta lie in one array of arc_muon_state_elems binary32 elements, matrix i's from
  * arc_muon_state_offset(i), a multiple of ARC_STATE_BLOCK, on, row after row.

@@ -83,14 +83,24 @@ constexpr float kQuintic[3] = {3.4445f, -4.7750f, 2.0315f};
 // What a group's pairs may take: enough matrices to fill the card many times over.
 constexpr int64_t kGroupBytes = int64_t{4} << 30;
 // Steps whose polynomials are multiplied before X is: then X X' and P X, the products
-// that grow with the longer side, are made once for three steps and not three times, for
-// six more products of the shorter side (five steps of m x n numbers: 15 m^2 n + 5 m^3
-// multiplications with all steps apart, 6 m^2 n + 14 m^3 in runs of three and two).  An
-// error of A is taken from step to step within a run, 12 times larger each in the
-// directions of small singular values: O is off by 3e-6 to 5e-6 where it is by 2e-6
-// step by step, and with all five in one run by 1e-4.  Step by step where O itself is
-// asked for in binary32.
-constexpr int32_t kTogether = 3;
+// that grow with the longer side, are made once for a run of steps and not in each, for
+// three more products of the shorter side with each step that joins one (five steps of m x n
+// numbers: 15 m^2 n + 5 m^3 multiplications step by step, 9 m^2 n + 11 m^3 in runs of two,
+// one and two, 6 m^2 n + 14 m^3 in runs of two and three).
+//
+// An error of A = X X' is taken from step to step within a run, and in the directions of
+// small singular values it grows as A does there, with the square of the polynomial (12
+// times for the usual one), where step by step A is made anew from X.  What O is off by, of
+// its norm, and how many times step by step or binary32 products, the larger: matrices of
+// 4 to 640 rows, one to half of whose singular values are the strong ones, runs of three and
+// two 4e-5 to 2e-4, up to 90 times; of two and three 7e-5, 14 times; of two, one and two
+// 1e-5, 1.7 times (step by step 1e-5 too, of matrices whose others are 0.003).  So runs of
+// two where a parameter is binary32, and runs of two and three where all are bfloat16,
+// whose rounding is off by 1.7e-3.  O itself in binary32 is made step by step.
+constexpr int32_t kTogetherF32 = 2, kTogetherBf16 = 3;
+// What errors may grow in a run, and in a last run of three, before which as small singular
+// values have grown as much.
+constexpr double kRunGrows = 12.0, kLastRunGrows = 144.0;
 
 int64_t up_to(int64_t v, int64_t of) { return (v + of - 1) / of * of; }
 
@@ -134,18 +144,41 @@ std::vector<double> polynomial_bounds(const std::vector<float>& coefficients) {
   return bounds;  // the last X is not held in pairs
 }
 
-// The launches of a pass in which runs of at most `together` steps (the longer ones
-// first) have their polynomials multiplied before X is.
+// How many steps each run takes, at most `together` (1 to 3).  Of an odd number in pairs the
+// lone one comes second (in a model of the roundings, of five steps at most 3.3 times what
+// step by step or binary32 is off by; with it last 3.5, and first 7.3).
+std::vector<int32_t> runs_of(const std::vector<double>& bounds, int32_t together) {
+  std::vector<int32_t> runs;
+  const size_t steps = bounds.size();
+  const auto grown = [&](size_t from, size_t to) {  // what errors of A grow in these steps
+    double most = 1.0;
+    for (size_t k = from; k < to; ++k) most *= bounds[k] * bounds[k];
+    return most;
+  };
+  size_t end = steps;
+  if (together > 2 && steps > 4 && grown(steps - 3, steps - 1) <= kLastRunGrows &&
+      grown(steps - 3, steps - 1) <= grown(0, steps - 3))
+    end -= 3;
+  for (size_t k = 0; k < end;) {
+    const bool alone = k + 1 == end || (end % 2 == 1 && runs.size() == 1);
+    const bool pair = together > 1 && !alone && grown(k, k + 1) <= kRunGrows;
+    runs.push_back(pair ? 2 : 1);
+    k += pair ? 2 : 1;
+  }
+  if (end < steps) runs.push_back(3);
+  return runs;
+}
+
+// The launches of a pass in which runs of at most `together` steps have their polynomials
+// multiplied before X is.
 std::vector<arc::MuonLaunch> sequence(const std::vector<float>& coefficients,
                                       const std::vector<double>& bounds, int32_t together) {
   using namespace arc;
   constexpr float kUnit = 1.f / kPairScale;
   std::vector<MuonLaunch> out;
   const auto steps = static_cast<int32_t>(bounds.size());
-  const int32_t runs = (steps + together - 1) / together;
   int32_t xt = kMuonXt, k = 0;
-  for (int32_t run = 0; run < runs; ++run) {
-    const int32_t count = (steps - k + runs - run - 1) / (runs - run);
+  for (const int32_t count : runs_of(bounds, together)) {
     out.push_back({kMuonGram, {kMuonX, kMuonX, kMuonSquare, kMuonSquare, kUnit, 0, 0, 0}});
     int32_t all = kMuonPoly;
     float all_scale = kPairScale;
@@ -176,7 +209,7 @@ std::vector<arc::MuonLaunch> sequence(const std::vector<float>& coefficients,
       }
     }
     const int32_t next = xt == kMuonXt ? kMuonXt2 : kMuonXt;
-    if (run + 1 < runs)
+    if (k < steps)
       out.push_back({kMuonApply, {all, xt, kMuonX, next, 1.f / all_scale, 0, 0, 0}});
     else
       out.push_back({kMuonLast, {all, xt, kMuonX, next, 1.f / (kPairScale * all_scale), 0, 0, 0}});
@@ -461,7 +494,10 @@ Times plan_muon(const arc_muon_config* cfg, int32_t whole_of, arc_muon* c) {
 arc_muon plan_best(const arc_muon_config* cfg, const std::vector<float>& coefficients,
                    const std::vector<double>& bounds) {
   const auto plain = sequence(coefficients, bounds, 1);
-  const auto grouped = sequence(coefficients, bounds, kTogether);
+  bool any_f32 = false;
+  for (int32_t i = 0; i < cfg->num_matrices; ++i)
+    any_f32 = any_f32 || cfg->matrices[i].param_dtype == ARC_DTYPE_F32;
+  const auto grouped = sequence(coefficients, bounds, any_f32 ? kTogetherF32 : kTogetherBf16);
   arc_muon best;
   double least = INFINITY;
   int64_t tiles = 0, full = 0;  // of 128

@@ -443,6 +443,11 @@ using PointersOf = std::conditional_t<WHAT == kMuonLast, MuonPointers, NoPointer
 // at a time, staged in LDS: row r's 16-byte pieces lie at piece ^ (r / 2 % 8), so
 // that 16 rows' pieces, which are read together, lie in different banks.
 //
+// X X' is summed in blocks of as many lines as there are blocks, or nearly, each added to
+// those before it: what a chain of additions is off by grows with its length, and steps in
+// runs let the error of X X' grow (runs_of()).  Its diagonal is off by 1.6 * 2^-24, of 2048
+// numbers to 65,536, where one chain had 2.3 to 5.8; X X' of 4096^3 takes 2% longer.
+//
 // Large sums are bound by the matrix units at the clock that the card's power leaves them
 // (1.6 GHz of 2.4; of zeros the same products take 0.8 of the time): P X of 4096^3 in 320
 // us, 1260 TFLOP/s of binary16 products, where the library's plain binary16 product runs
@@ -508,14 +513,17 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,
                (uint32_t)first * pitch + (uint32_t)(at.first + line) * kLineBytes, to + q * 1024);
     }
   };
-  f32x4_t acc[TI][TJ];
+  f32x4_t acc[TI][TJ], sums[TI][TJ];  // sums: kMuonGram's, of blocks that are done
+  const auto each = [&](const auto& f) {
 #pragma unroll
-  for (int i = 0; i < TI; ++i)
+    for (int i = 0; i < TI; ++i)
 #pragma unroll
-    for (int j = 0; j < TJ; ++j)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) acc[i][j][k] = 0.f;
+      for (int j = 0; j < TJ; ++j) f(acc[i][j], sums[i][j]);
+  };
+  each([](f32x4_t& x, f32x4_t& done) { x = done = f32x4_t{0.f, 0.f, 0.f, 0.f}; });
   const int32_t lines = at.lines;
+  int32_t block = 8;  // lines, a power of two
+  while (block * block < lines) block *= 2;
 #pragma unroll
   for (int q = 0; q < kStages - 1; ++q)
     if (q < lines) stage(q);
@@ -552,7 +560,11 @@ muon_product_kernel(MuonArgs a, PointersOf<WHAT> p, MuonProduct s,
     multiply(lh, rl);
     multiply(lh, rh);
     multiply(ll, rh);
+    if constexpr (WHAT == kMuonGram)
+      if ((line & (block - 1)) == block - 1)
+        each([](f32x4_t& x, f32x4_t& done) { done += x, x = f32x4_t{0.f, 0.f, 0.f, 0.f}; });
   }
+  if constexpr (WHAT == kMuonGram) each([](f32x4_t& x, f32x4_t& done) { x += done; });
   if (at.parts > 1 && !join_parts<SIDE>(a, at, acc)) return;
   // Lane l holds columns TJ (l % 16) + j of its wave's result and rows 16 i + 4 (l / 16)
   // + k: TJ numbers that follow one another in a row, 16 lanes' together whole lines.
