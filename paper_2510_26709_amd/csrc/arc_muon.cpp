@@ -280,15 +280,16 @@ void each_tile(int32_t rows, int32_t cols, bool half, const Add& add) {
 // sum on a compute unit that is full, and in a workgroup that has it for itself; a
 // result written; a part written (and read once more by the workgroup that adds them);
 // a launch.  us with tiles of 32, 64 and 128, the better of step by step and in runs:
-// 24 vectors and small matrices 66, 66 and 126, 257 x 1001 101, 123 and 265, a
-// ResNet-18's convolutions 390, 362 and 482, three layers of width 384 272, 243 and 342,
-// of width 576 622, 481 and 657, 48 matrices of width 640 3460, 2450 and 2140, a 4096 x
-// 4096 7870, 4500 and 3600.  Step by step and in runs: 257 x 1001 123 and 123, the
-// convolutions 489 and 363, width 640 2860 and 2140, 4096 x 4096 3597 and 3765.  What is
-// chosen was within 3% of the best of the six in 48 of 51 drawn cases, and within 16% in
-// all.  Each product has a side of its own: of 40 drawn cases 14 take 2 to 13% less than
-// with one side for all (a ResNet-18's 344 against 360), the others the same to 2%.  Split
+// 24 vectors and small matrices 82, 81 and 138, 257 x 1001 100, 127 and 259, a ResNet-18's
+// convolutions 485, 411 and 502, three layers of width 384 280, 243 and 324, of width 576
+// 717, 539 and 681, 48 matrices of width 640 4023, 2772 and 2376, a 4096 x 4096 in bfloat16
+// 7752, 4437 and 3524.  Step by step and in runs: the convolutions 495 and 411, width 576
+// 633 and 539, width 640 2911 and 2376, 4096 x 4096 3524 and 3713.  Each product has a side
+// of its own: the convolutions then take 398.  Of 51 drawn cases (in runs of three and two)
+// what is chosen was within 3% of the best of the six in 48, and within 16% in all.  Split
 // sums: X X' of a ResNet-18's convolutions (sums of 4608 in few tiles) 40 us against 103.
+// The plan takes the host 1.4 ms for 257 x 1001, 15 for a 4096 x 4096, 3 to 5 for the
+// convolutions and the 48 matrices, 91 for 224 of an 8-billion-weight model.
 struct Rates {
   int32_t side;
   double line, alone, result, part;

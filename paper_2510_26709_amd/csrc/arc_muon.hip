@@ -237,7 +237,9 @@ __device__ __forceinline__ void store_8(char* row, int32_t at, const uint32_t (&
 }
 
 // X and its transpose in pairs, a workgroup for each 64 x 64 of a matrix.  The norm has to
-// be known first, so that U is read, and made of the momentum, a second time.  HBM, more
+// be known first, so that U is read, and made of the momentum, a second time; every
+// workgroup adds all the runs' sums of its matrix, which grows with the square of the size
+// (4096 x 4096 31 us, 128,256 x 4096 4.4 ms, of which 3.3 for that).  Else HBM, more
 // than half of it writes: 1.76e8 elements with bf16 gradients (6 bytes read, 8 written)
 // 494 us, 5.0 TB/s; 5.9e7 in binary32 (8, 8) 183, 5.2.
 __global__ void __launch_bounds__(kThreads)
@@ -446,13 +448,13 @@ using PointersOf = std::conditional_t<WHAT == kMuonLast, MuonPointers, NoPointer
 // X X' is summed in blocks of as many lines as there are blocks, or nearly, each added to
 // those before it: what a chain of additions is off by grows with its length, and steps in
 // runs let the error of X X' grow (runs_of()).  Its diagonal is off by 1.6 * 2^-24, of 2048
-// numbers to 65,536, where one chain had 2.3 to 5.8; X X' of 4096^3 takes 2% longer.
+// numbers to 65,536, where one chain had 2.3 to 5.8; X X' of 4096^3 takes 190 us, not 185.
 //
 // Large sums are bound by the matrix units at the clock that the card's power leaves them
-// (1.6 GHz of 2.4; of zeros the same products take 0.8 of the time): P X of 4096^3 in 320
-// us, 1260 TFLOP/s of binary16 products, where the library's plain binary16 product runs
+// (1.6 GHz of 2.4; of zeros the same products take 0.8 of the time): P X of 4096^3 in 317
+// us, 1300 TFLOP/s of binary16 products, where the library's plain binary16 product runs
 // at 1390.  With short sums the ends count: 48 matrices of width 640 take P X in 282 us,
-// of which 179 are the sums (1260 TFLOP/s again) and 90 the writing of X both ways (472
+// of which 179 are the sums (1260 TFLOP/s) and 90 the writing of X both ways (472
 // MB, 5.2 TB/s), one after the other though two workgroups share a compute unit; starting
 // them apart, priorities and fewer stores in flight made no difference.  Small contexts
 // are bound by latency, 4 us a launch with tiles of 32 and 5 to 6 with tiles of 64 (five

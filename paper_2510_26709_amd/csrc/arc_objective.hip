@@ -314,7 +314,8 @@ hipError_t launch_preference(const PreferenceArgs& a, const PreferenceOutputs& o
   // 6000 21.2 / 10.8, 200 x 6000 35.8 / 22.2; two launches with parts of 1024 or more, 1 x
   // 6000 8.7, of 2048 11.2.  Every workgroup of the second one reads the sums of all its
   // pair's parts: 1 x 100,000 in 128 parts 8.5, in 390 10.3; 1 x 300,000 in 128 11.1, 256
-  // 10.3, 512 11.9; 1 x 1,000,000 33, 21 and 17.7.
+  // 10.3, 512 11.9; 1 x 1,000,000 33, 21 and 17.7.  A batch whose average is short is taken
+  // in pairs, however long one is: 300,000 tokens among 300 pairs of 100 511 us.
   constexpr int64_t kLong = 1280, kPartTokens = 256, kParts = 128, kManyTokens = 1024;
   const int64_t average = a.pairs > 0 ? a.rows / (2 * a.pairs) : 0;
   const int64_t parts = average > kLong

@@ -1,8 +1,10 @@
 """The two ends of a training step over libarctopk: ``TokenLogProbs`` (log
-probabilities of given tokens, entropy, top alternatives and their gradient)
-and ``AdamW`` (gradient norms and the AdamW step over many tensors).
+probabilities of given tokens, entropy, top alternatives and their gradient,
+and the policy and preference losses made of them), ``AdamW`` (gradient norms
+and the AdamW step over many tensors) and ``Muon`` (orthogonalised steps of
+matrices).
 
-Both own one context of the C library, bound to a torch stream: inputs must be
+Each owns one context of the C library, bound to a torch stream: inputs must be
 ready on that stream, and outputs are.  Where it is not the current stream,
 making them so (an event, a synchronization) is the caller's part.  A context has
 one workspace: graphs captured from it, and calls, must not overlap in time.  Tensors
@@ -453,6 +455,10 @@ class Muon(_Optimizer):
     ``coefficients``: a, b, c of one Newton-Schulz step, or of each of ``steps``.
     ``states``: a dict with existing momenta, used in place; else they start at
     zero.
+
+    Steps are as exact as binary32 products make them where a parameter is "f32";
+    where all are "bf16", O may be off by 1e-4 of its norm before it is rounded.
+    Making one takes the host some milliseconds, which serve all later calls.
     """
 
     _names = ("m",)
