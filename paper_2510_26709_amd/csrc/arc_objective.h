@@ -70,7 +70,7 @@ constexpr int kPreferenceTotals = 3;
 // parts of sequences (one a workgroup), and counts of workgroups, one for launches of
 // each number of them.  A count goes round, 0 after as many arrivals as its number, so
 // that it is 0 between launches whatever came before: replays that overlap in time, which
-// they must not, spoil their own totals and those of no later call.
+// they must not, spoil their own totals, but no later call's.
 constexpr int kTotalsGroups = 1024;
 struct ObjectiveScratch {
   double totals[kTotalsGroups][kPolicyTotals];
